@@ -492,6 +492,151 @@ int cdadam_compress_topk(const float *x, int64_t d, int64_t k, uint32_t *idx, fl
 int cdadam_compress_sign_static(const float *x, int64_t d, uint32_t *bits, float *scale,
                                 void *stream);
 
+/*
+ * Operators of a worker around its loss.
+ *
+ * Algorithm 1 starts from the n stochastic gradients, which the caller computes.  For a
+ * worker that trains a language model, the three operators below are the parts of that
+ * computation between the activations and the gradients that are no matrix products: the
+ * layer norm in front of a product, the log probabilities of given tokens (the teacher's pass
+ * of a distillation, the evaluation, a policy's gradient) and the distillation loss.  They
+ * use no context: all memory is the caller's, nothing is allocated inside, every call only
+ * queues work on `stream` (stream capture is allowed) and calls on different streams do not
+ * touch each other.  Results do not depend on scheduling: repeated calls give the same bits.
+ *
+ * Matrices are row-major on the device current at the call, elements of a row adjacent, rows
+ * `stride` elements apart (any stride >= the row's length, and any stride >= 0 for inputs, so
+ * that a broadcast row is given with stride 0).  Pointers need the alignment of their element
+ * only; rows whose address is a multiple of 16 bytes are read and written fastest.  `type` is
+ * the element type of activations and logits; all arithmetic is binary32 or wider and every
+ * output is rounded once.  rows = 0 is allowed and queues only what an empty sum defines.
+ */
+
+/* element types */
+enum { CDADAM_F32 = 0, CDADAM_BF16 = 1, CDADAM_F16 = 2 };
+/* types of token indexes */
+enum { CDADAM_I32 = 0, CDADAM_I64 = 1 };
+
+#define CDADAM_MAX_LIST 128              /* longest list of alternatives / of a teacher */
+#define CDADAM_MAX_VOCAB 393216          /* longest row of logits */
+#define CDADAM_MAX_NORM_COLS 1048576     /* longest row of a layer norm */
+
+/*
+ * Layer norm of every row: with mu = mean(x), v = mean((x - mu)^2), s = 1 / sqrt(v + eps),
+ *     y_j = (x_j - mu) s w_j + b_j.
+ *   x, y     rows x cols of `type`; y may be x itself (same address and stride)
+ *   weight, bias   cols elements of `weight_type` (any of the three types: the optimizer's
+ *            own binary32 parameters or a copy in `type`); NULL means 1 and 0
+ *   mean, rstd     device, rows floats: mu and s, which the backward pass needs; may be NULL
+ *   eps >= 0, 1 <= cols <= CDADAM_MAX_NORM_COLS, rows < 2^31
+ */
+int cdadam_layer_norm(const void *x, int64_t x_stride, const void *weight, const void *bias,
+                      int64_t rows, int64_t cols, float eps, int type, int weight_type,
+                      void *y, int64_t y_stride, float *mean, float *rstd, void *stream);
+
+/*
+ * Its gradient.  With xh_j = (x_j - mu) s and h_j = dy_j w_j, for every row
+ *     dx_j = s (h_j - mean(h) - xh_j mean(h xh)),
+ * and summed over the rows of a group
+ *     dweight_j = sum dy_j xh_j,   dbias_j = sum dy_j.
+ * The rows form `groups` groups of rows / groups consecutive rows (rows must be a multiple of
+ * groups, 1 <= groups <= 65535), one for each worker whose batch is in x: group i writes its sums at dweight + i *
+ * dweight_stride and dbias + i * dbias_stride, elements of `grad_type`, so that both can be
+ * slices of the n x d gradients that cdadam_step (CDADAM_F32) or cdadam_step_bf16
+ * (CDADAM_BF16) takes.  accumulate != 0 adds to what is there (in binary32, rounded once).
+ *   dx       may be dy or x itself (same address and stride); any of dx, dweight, dbias may
+ *            be NULL: not computed
+ *   workspace   device, 16-byte aligned, at least cdadam_layer_norm_workspace(rows, cols,
+ *            groups) bytes (0 without dweight and dbias), for partial sums; its contents are
+ *            scratch, and two calls that may run at the same time need one each
+ * The sums over rows are added in an order that depends on the sizes alone (no atomics).
+ */
+int cdadam_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride,
+                               const void *weight, const float *mean, const float *rstd,
+                               int64_t rows, int64_t cols, int64_t groups,
+                               int type, int weight_type, int grad_type,
+                               void *dx, int64_t dx_stride,
+                               void *dweight, int64_t dweight_stride,
+                               void *dbias, int64_t dbias_stride, int accumulate,
+                               void *workspace, int64_t workspace_bytes, void *stream);
+int64_t cdadam_layer_norm_workspace(int64_t rows, int64_t cols, int64_t groups);
+
+/*
+ * Log probabilities of given tokens, entropy, and the k most probable tokens of every row of
+ * logits z.  With y_i = z_i / temperature, lse = log sum_i exp(y_i), p_i = exp(y_i - lse):
+ *     logprob = y_token - lse,   entropy = - sum_i p_i log p_i,
+ *     top_ids = the k largest z_i in descending order (ties: the lower index first; -0 = +0),
+ *     top_logprobs = y_i - lse of those.
+ *   logits   rows x vocab of `type`, 1 <= vocab <= CDADAM_MAX_VOCAB
+ *   tokens   rows indexes of `index_type`; NULL where logprob is NULL.  A negative token is
+ *            "none": its logprob is 0, whatever the logits.  A token >= vocab gives NaN
+ *   k        0 .. min(vocab, CDADAM_MAX_LIST); top_ids (of `index_type`) and top_logprobs are
+ *            rows x k
+ *   logprob, entropy, lse   rows floats; every output may be NULL (top_ids and top_logprobs
+ *            both or neither)
+ *   temperature   in [1e-4, 1e4]
+ * A logit of -inf is masked: probability 0, no term of the entropy, never an alternative;
+ * where fewer than k tokens are not masked the list ends with index -1 and -inf.  A row with
+ * everything masked has lse = logprob = -inf and entropy 0.  A row that holds a NaN or +inf has
+ * no distribution: NaN everywhere and indexes -1.
+ */
+int cdadam_token_logprobs(const void *logits, int64_t logits_stride, const void *tokens,
+                          int64_t rows, int64_t vocab, int type, int index_type,
+                          float temperature, int k,
+                          float *logprob, float *entropy, float *lse,
+                          void *top_ids, float *top_logprobs, void *stream);
+
+/*
+ * Gradient of logprob and entropy with respect to the logits, from what the forward pass gave:
+ *     dz_i = (dlogprob ([i = token] - p_i) - dentropy p_i (log p_i + entropy)) / temperature.
+ *   lse, and entropy where dentropy is given: rows floats, the forward pass's outputs for the
+ *            same logits and temperature
+ *   dlogprob, dentropy   rows floats, the gradients of the two outputs; either may be NULL: 0
+ *   tokens   NULL only where dlogprob is.  A token that is negative or >= vocab has no gradient
+ *   dlogits  rows x vocab of `type`; may be logits itself (same address and stride)
+ * A masked logit (-inf) gets gradient 0.  A row without any gradient coming in (no token or
+ * dlogprob 0, and dentropy 0) gets 0 whatever its logits are, so that padding may hold anything,
+ * and so does a row with |lse| >= 2^24 (every token masked by the type's lowest value, for
+ * instance): a binary32 lse of that size says nothing about the probabilities.
+ */
+int cdadam_token_logprobs_backward(const void *logits, int64_t logits_stride, const void *tokens,
+                                   int64_t rows, int64_t vocab, int type, int index_type,
+                                   float temperature, const float *lse, const float *entropy,
+                                   const float *dlogprob, const float *dentropy,
+                                   void *dlogits, int64_t dlogits_stride, void *stream);
+
+/*
+ * Distillation from a teacher's most probable tokens: per row, with S the listed tokens, q_j
+ * the teacher's probability of j and p the student's softmax(z / temperature),
+ *   rest != 0   q_j = exp(teacher_logprobs_j), r = max(0, 1 - sum q_j); everything outside S is
+ *               one further outcome with r for the teacher and R = sum over i not in S of p_i
+ *               for the student:
+ *       loss = sum_j q_j (log q_j - log p_j) + r (log r - log R)
+ *       dz_j = p_j - q_j (j in S),   dz_i = p_i (1 - r / R) (i not in S)
+ *   rest == 0   q = softmax of the listed teacher_logprobs (so the teacher's logits divided by
+ *               the temperature do as well):
+ *       loss = sum_j q_j (log q_j - log p_j),   dz_i = p_i - q_i (q_i = 0 outside S)
+ * and dlogits = dz dloss / temperature.  (A factor temperature^2, where wanted, goes into dloss.)
+ *   logits   rows x vocab of `type` (the student's), 1 <= vocab <= CDADAM_MAX_VOCAB
+ *   teacher_ids, teacher_logprobs   rows x k, indexes of `index_type` and floats, as
+ *            cdadam_token_logprobs gives them for the teacher at the same temperature;
+ *            1 <= k <= CDADAM_MAX_LIST.  An index outside [0, vocab) is an unused entry; an
+ *            index listed twice is one token with the sum of its probabilities
+ *   loss     rows floats, or NULL
+ *   dloss    rows floats, the gradient of every row's loss; needed where dlogits is given
+ *   dlogits  rows x vocab of `type`, or NULL (loss alone); may be logits itself
+ * Terms with q_j = 0 (or r = 0) are 0, and r is 0 where S is the whole vocabulary.  A logit of
+ * -inf is masked: probability 0 and gradient 0 (and loss = +inf where the teacher gives it a
+ * probability).  A list without a used entry (with rest == 0: without one of probability above
+ * 0) gives loss 0 and gradient 0.  A row that holds a NaN or +inf gives NaN.  A row whose dloss
+ * is 0 gets gradient 0 whatever its logits are.
+ */
+int cdadam_distill(const void *logits, int64_t logits_stride,
+                   const void *teacher_ids, const float *teacher_logprobs,
+                   int64_t rows, int64_t vocab, int k, int type, int index_type,
+                   float temperature, int rest, const float *dloss,
+                   float *loss, void *dlogits, int64_t dlogits_stride, void *stream);
+
 /* Message of the calling thread's most recent failure ("" if none).  Never NULL. */
 const char *cdadam_last_error(void);
 
