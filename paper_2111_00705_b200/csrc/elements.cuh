@@ -64,4 +64,147 @@ __device__ __forceinline__ float block_max_all(float v, float *sh)
     return warp_max(lane < NT / 32 ? sh[lane] : kNegInf);
 }
 
+
+// 2^x, relative error below 2^-22; results below 2^-126 are 0.
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// Two binary32 operations in one instruction, each rounded to nearest.
+__device__ __forceinline__ uint64_t bits64(float2 v)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
+    return r;
+}
+__device__ __forceinline__ float2 floats(uint64_t b)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(b));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits64(a)), "l"(bits64(b)));
+    return floats(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits64(a)), "l"(bits64(b)));
+    return floats(r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits64(a)), "l"(bits64(b)), "l"(bits64(c)));
+    return floats(r);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// A 16-byte vector of T: n elements, widened to n / 2 pairs and narrowed back; `running` is the
+// type in which a maximum is carried along (the 16-bit types keep it packed).
+template <typename T> struct Vec;
+
+template <> struct Vec<float> {
+    static constexpr int n = 4;
+    typedef float running;
+    static __device__ __forceinline__ running lowest() { return kNegInf; }
+    static __device__ __forceinline__ void wide(const uint4 &u, float2 (&f)[2])
+    {
+        f[0] = make_float2(__uint_as_float(u.x), __uint_as_float(u.y));
+        f[1] = make_float2(__uint_as_float(u.z), __uint_as_float(u.w));
+    }
+    static __device__ __forceinline__ uint4 pack(const float2 (&f)[2])
+    {
+        return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
+    }
+    static __device__ __forceinline__ running top(const uint4 &u)
+    {
+        return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
+    }
+    static __device__ __forceinline__ running max(running a, running b) { return fmaxf(a, b); }
+    static __device__ __forceinline__ float value(running a) { return a; }
+    static __device__ __forceinline__ running all(float v) { return v; }
+    static __device__ __forceinline__ bool reaches(running a, running t) { return a >= t; }
+};
+
+template <> struct Vec<bf16> {
+    static constexpr int n = 8;
+    typedef __nv_bfloat162 running;
+    static __device__ __forceinline__ __nv_bfloat162 two(uint32_t w) { return *reinterpret_cast<__nv_bfloat162 *>(&w); }
+    static __device__ __forceinline__ running lowest() { return two(0xFF80FF80u); }
+    static __device__ __forceinline__ float2 up(uint32_t w)
+    {
+        return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+    }
+    static __device__ __forceinline__ void wide(const uint4 &u, float2 (&f)[4])
+    {
+        f[0] = up(u.x); f[1] = up(u.y); f[2] = up(u.z); f[3] = up(u.w);
+    }
+    static __device__ __forceinline__ uint32_t down(float2 f)
+    {
+        __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+        return *reinterpret_cast<uint32_t *>(&h);
+    }
+    static __device__ __forceinline__ uint4 pack(const float2 (&f)[4])
+    {
+        return make_uint4(down(f[0]), down(f[1]), down(f[2]), down(f[3]));
+    }
+    static __device__ __forceinline__ running max(running a, running b) { return __hmax2(a, b); }
+    static __device__ __forceinline__ running top(const uint4 &u)
+    {
+        return __hmax2(__hmax2(two(u.x), two(u.y)), __hmax2(two(u.z), two(u.w)));
+    }
+    static __device__ __forceinline__ float value(running a) { return fmaxf(__low2float(a), __high2float(a)); }
+    static __device__ __forceinline__ running all(float v) { return __float2bfloat162_rn(v); }
+    static __device__ __forceinline__ bool reaches(running a, running t) { return !__hblt2(a, t) ; }
+};
+
+template <> struct Vec<f16> {
+    static constexpr int n = 8;
+    typedef __half2 running;
+    static __device__ __forceinline__ __half2 two(uint32_t w) { return *reinterpret_cast<__half2 *>(&w); }
+    static __device__ __forceinline__ running lowest() { return two(0xFC00FC00u); }
+    static __device__ __forceinline__ void wide(const uint4 &u, float2 (&f)[4])
+    {
+        f[0] = __half22float2(two(u.x)); f[1] = __half22float2(two(u.y));
+        f[2] = __half22float2(two(u.z)); f[3] = __half22float2(two(u.w));
+    }
+    static __device__ __forceinline__ uint32_t down(float2 f)
+    {
+        __half2 h = __floats2half2_rn(f.x, f.y);
+        return *reinterpret_cast<uint32_t *>(&h);
+    }
+    static __device__ __forceinline__ uint4 pack(const float2 (&f)[4])
+    {
+        return make_uint4(down(f[0]), down(f[1]), down(f[2]), down(f[3]));
+    }
+    static __device__ __forceinline__ running max(running a, running b) { return __hmax2(a, b); }
+    static __device__ __forceinline__ running top(const uint4 &u)
+    {
+        return __hmax2(__hmax2(two(u.x), two(u.y)), __hmax2(two(u.z), two(u.w)));
+    }
+    static __device__ __forceinline__ float value(running a) { return fmaxf(__low2float(a), __high2float(a)); }
+    static __device__ __forceinline__ running all(float v) { return __float2half2_rn(v); }
+    static __device__ __forceinline__ bool reaches(running a, running t) { return !__hblt2(a, t); }
+};
+
+template <typename T> __device__ __forceinline__ T minus_inf() { return narrow<T>(kNegInf); }
+
+// 16 bytes global -> shared without passing through registers; complete for the issuing thread
+// after copies_done().
+__device__ __forceinline__ void copy16(void *dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_done()
+{
+    asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
+}
+
 }  // namespace cdadam
