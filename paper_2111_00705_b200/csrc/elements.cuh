@@ -106,8 +106,17 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
 }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
+// The larger of two; NaN if either is NaN.
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
 // A 16-byte vector of T: n elements, widened to n / 2 pairs and narrowed back; `running` is the
-// type in which a maximum is carried along (the 16-bit types keep it packed).
+// type in which a maximum is carried along (the 16-bit types keep it packed), `below` the largest
+// value of T that is not above v, `at_least` raises every element to a bound (NaN stays NaN).
 template <typename T> struct Vec;
 
 template <> struct Vec<float> {
@@ -129,7 +138,12 @@ template <> struct Vec<float> {
     }
     static __device__ __forceinline__ running max(running a, running b) { return fmaxf(a, b); }
     static __device__ __forceinline__ float value(running a) { return a; }
-    static __device__ __forceinline__ running all(float v) { return v; }
+    static __device__ __forceinline__ running below(float v) { return v; }
+    static __device__ __forceinline__ uint4 at_least(const uint4 &u, running t)
+    {
+        return make_uint4(__float_as_uint(max_nan(__uint_as_float(u.x), t)), __float_as_uint(max_nan(__uint_as_float(u.y), t)),
+                          __float_as_uint(max_nan(__uint_as_float(u.z), t)), __float_as_uint(max_nan(__uint_as_float(u.w), t)));
+    }
     static __device__ __forceinline__ bool reaches(running a, running t) { return a >= t; }
 };
 
@@ -161,8 +175,14 @@ template <> struct Vec<bf16> {
         return __hmax2(__hmax2(two(u.x), two(u.y)), __hmax2(two(u.z), two(u.w)));
     }
     static __device__ __forceinline__ float value(running a) { return fmaxf(__low2float(a), __high2float(a)); }
-    static __device__ __forceinline__ running all(float v) { return __float2bfloat162_rn(v); }
-    static __device__ __forceinline__ bool reaches(running a, running t) { return !__hblt2(a, t) ; }
+    static __device__ __forceinline__ running below(float v) { return __bfloat162bfloat162(__float2bfloat16_rd(v)); }
+    static __device__ __forceinline__ uint32_t word(__nv_bfloat162 h) { return *reinterpret_cast<uint32_t *>(&h); }
+    static __device__ __forceinline__ uint4 at_least(const uint4 &u, running t)
+    {
+        return make_uint4(word(__hmax2_nan(two(u.x), t)), word(__hmax2_nan(two(u.y), t)), word(__hmax2_nan(two(u.z), t)),
+                          word(__hmax2_nan(two(u.w), t)));
+    }
+    static __device__ __forceinline__ bool reaches(running a, running t) { return !__hblt2(a, t); }
 };
 
 template <> struct Vec<f16> {
@@ -190,7 +210,13 @@ template <> struct Vec<f16> {
         return __hmax2(__hmax2(two(u.x), two(u.y)), __hmax2(two(u.z), two(u.w)));
     }
     static __device__ __forceinline__ float value(running a) { return fmaxf(__low2float(a), __high2float(a)); }
-    static __device__ __forceinline__ running all(float v) { return __float2half2_rn(v); }
+    static __device__ __forceinline__ running below(float v) { return __half2half2(__float2half_rd(v)); }
+    static __device__ __forceinline__ uint32_t word(__half2 h) { return *reinterpret_cast<uint32_t *>(&h); }
+    static __device__ __forceinline__ uint4 at_least(const uint4 &u, running t)
+    {
+        return make_uint4(word(__hmax2_nan(two(u.x), t)), word(__hmax2_nan(two(u.y), t)), word(__hmax2_nan(two(u.z), t)),
+                          word(__hmax2_nan(two(u.w), t)));
+    }
     static __device__ __forceinline__ bool reaches(running a, running t) { return !__hblt2(a, t); }
 };
 

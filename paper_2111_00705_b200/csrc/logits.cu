@@ -81,19 +81,35 @@ struct Slice {
     }
 };
 
+// Thread 0 starts the copies of the whole vectors, in order; the (at most two) vectors that reach
+// beyond the row are filled by threads.  The copies of a block are bulk copies because these are
+// served one after the other: of several blocks on an SM one has its slice early and computes
+// while the next one's is on its way.  (Copies issued by all threads share the bandwidth evenly,
+// all blocks then wait together and compute together.)
+// A copy that does not arrive within the limit of a wait (seconds) makes the row one without a
+// distribution: its maximum counts as +inf, its outputs are NaN.
+constexpr float kLate = __builtin_huge_valf();
+constexpr uint32_t kCopyBytes = 16 * 1024;
+
 template <typename T, int NT>
-__device__ __forceinline__ void load_slice(const Slice<T> &s, uint4 *buf)
+__device__ __forceinline__ void start_slice(const Slice<T> &s, uint4 *buf, uint64_t *bar)
 {
     constexpr int V = Vec<T>::n;
-    for (int v = threadIdx.x; v < s.nv; v += NT) {
-        const int c = s.start + v * V;
-        if (s.whole(v)) {
-            copy16(buf + v, s.row + c);
-        } else {
-            T *e = reinterpret_cast<T *>(buf + v);
-#pragma unroll
-            for (int i = 0; i < V; ++i) e[i] = c + i >= 0 && c + i < s.vocab ? s.row[c + i] : minus_inf<T>();
-        }
+    const int v0 = s.nv > 0 && !s.whole(0) ? 1 : 0, v1 = s.nv > v0 && !s.whole(s.nv - 1) ? s.nv - 1 : max(s.nv, v0);
+    if (threadIdx.x == 0) {
+        mbar_init(bar, 1);
+        mbar_fence_init();
+        const uint32_t bytes = (uint32_t)(v1 - v0) * 16;
+        mbar_arrive_expect_tx(bar, bytes);
+        const char *from = reinterpret_cast<const char *>(s.row + s.start + v0 * V);
+        char *to = reinterpret_cast<char *>(buf + v0);
+        for (uint32_t at = 0; at < bytes; at += kCopyBytes)
+            bulk_copy_g2s(to + at, from + at, min(kCopyBytes, bytes - at), bar);
+    }
+    if (threadIdx.x >= NT - 2 * V) {
+        const int i = threadIdx.x - (NT - 2 * V), v = i < V ? 0 : s.nv - 1, c = s.start + v * V + i % V;
+        if (i < V ? v0 == 1 : v1 < s.nv && v >= v0)
+            reinterpret_cast<T *>(buf)[v * V + i % V] = c >= 0 && c < s.vocab ? s.row[c] : minus_inf<T>();
     }
 }
 
@@ -114,7 +130,37 @@ __device__ __forceinline__ float slice_max(const uint4 *buf, int nv)
     return Vec<T>::value(m);
 }
 
-// Sums of a slice: e = sum 2^t, h = sum 2^t t with t = (z - mu) s.
+// Exponentials are taken relative to a slice's maximum m: t = z s - c with c = m s rounded to
+// binary32, one fused operation; the same c is used wherever sums of slices are joined, so its
+// rounding cancels.  Where c does not exist (nothing but masked logits: m is -inf or the type's
+// lowest value) t = (z - m) s.
+struct Origin {
+    float m, c;
+    bool far;               // no c
+    __device__ __forceinline__ Origin(float top, float s)
+    {
+        far = !(fabsf(top) < 1e30f);
+        m = top == kNegInf ? 0.0f : top;
+        c = m * s;
+    }
+};
+template <bool FAR>
+__device__ __forceinline__ float2 exponents(float2 z, const Origin &o, float s)
+{
+    return FAR ? mul2(add2(z, both(-o.m)), both(s)) : fma2(z, both(s), both(-o.c));
+}
+// Exponent of slice p's origin relative to the row's, at least -1e4.
+__device__ __forceinline__ float shift(const Origin &p, const Origin &row, float s)
+{
+    return row.far ? fmaxf((p.m - row.m) * s, -1e4f) : p.far ? -1e4f : fmaxf(p.c - row.c, -1e4f);
+}
+// z relative to the row's origin, in 64 bits.
+__device__ __forceinline__ double exponent64(float z, const Origin &row, float s)
+{
+    return row.far ? ((double)z - (double)row.m) * (double)s : (double)z * (double)s - (double)row.c;
+}
+
+// Sums of a slice: m its maximum, e = sum 2^t, h = sum 2^t t.
 struct Sums {
     float m, e, h;
     int n;                  // entries of the slice's list of alternatives
@@ -124,31 +170,31 @@ struct Sums {
 // Alternatives.  Every slice gives its k first tokens in descending order, the cluster's first
 // block merges them.  Within a slice: 128 groups of threads have each met a largest value; the
 // k-th largest of these 128 is a value that at least k elements reach, and in a row without
-// structure hardly more (128 ln(128 / (128 - k)) are expected: 89 for k = 64).  The pass that
-// adds up the exponentials collects the elements that reach it, and counting for each how many
-// are greater sorts them.  Only where more than kCap are collected (thousands of equal values, or
-// the largest all in a few threads' vectors) the slice is walked again in order, the best k so
-// far always kept.
+// structure hardly more (128 ln(128 / (128 - k)) are expected: 89 for k = 64).  It is found bit by
+// bit in the upper 16 bits of the values' order (a bound a little too low only lets a few more
+// in).  The pass that adds up the exponentials notes the vectors that reach it; their elements
+// that do are collected, and counting for each how many are greater sorts them.  Only where more
+// than kCap are noted or collected (thousands of equal values, or the largest all in a few
+// threads' vectors) the slice is walked again in order, the best k so far always kept.
 // ---------------------------------------------------------------------------------------------
 constexpr int kCap = 512;
 constexpr int kGroups = 128;
 
-template <typename T>
-__device__ __forceinline__ void collect(const uint4 &u, int c, float reach, uint64_t *cand, int *count, uint64_t above)
+// A lower bound of the k-th largest of the 4 x 32 values of a warp (1 <= k <= 128).
+__device__ __forceinline__ float kth_of_groups(const float (&g)[kGroups / 32], int k)
 {
-    float2 f[Vec<T>::n / 2];
-    Vec<T>::wide(u, f);
+    uint32_t o[kGroups / 32], t = 0;
 #pragma unroll
-    for (int i = 0; i < Vec<T>::n; ++i) {
-        const float v = i & 1 ? f[i / 2].y : f[i / 2].x;
-        if (v >= reach && v > kNegInf) {
-            const uint64_t key = order_key(v, c + i);
-            if (key > above) {
-                const int at = atomicAdd(count, 1);
-                if (at < kCap) cand[at] = key;
-            }
-        }
+    for (int i = 0; i < kGroups / 32; ++i) o[i] = (uint32_t)(order_key(g[i], 0) >> 48);
+#pragma unroll
+    for (int b = 15; b >= 0; --b) {
+        const uint32_t next = t | (1u << b);
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kGroups / 32; ++i) n += o[i] >= next;
+        if (__reduce_add_sync(0xffffffffu, n) >= k) t = next;
     }
+    return t <= 0x7Fu ? kNegInf : key_value((uint64_t)t << 48);     // 0x7F: the order of -inf
 }
 
 __device__ __forceinline__ int rank_of(uint64_t key, const uint64_t *keys, int n)
@@ -171,7 +217,16 @@ __device__ __noinline__ int collect_in_order(const uint4 *buf, int nv, int start
         if (threadIdx.x == 0) *count = kept;
         __syncthreads();
         const int v = base + (int)threadIdx.x;
-        if (threadIdx.x < step && v < nv) collect<T>(buf[v], start + v * V, kNegInf, cand, count, above);
+        if (threadIdx.x < step && v < nv) {
+            float2 f[V / 2];
+            Vec<T>::wide(buf[v], f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float z = i & 1 ? f[i / 2].y : f[i / 2].x;
+                const uint64_t key = order_key(z, start + v * V + i);
+                if (z > kNegInf && key > above) cand[atomicAdd(count, 1)] = key;
+            }
+        }
         __syncthreads();
         kept = *count;
         if (kept > kMaxList) {
@@ -195,76 +250,114 @@ __device__ __noinline__ int collect_in_order(const uint4 *buf, int nv, int start
     return kept;
 }
 
+// One pass over a slice: e = sum 2^t, h = sum 2^t t; with TOP the vectors that hold an element
+// >= reach are noted.  FAR: see Origin.  LOW: `low` is a value of T whose t is finite and below
+// -150; raising what is lower (masked logits) to it keeps 0 times -inf out of h, and 2^t is 0 for
+// both.  Without LOW (no such value of T) t itself is bounded, an operation for each element
+// instead of one for two.
+template <typename T, int NT, bool TOP, bool FAR, bool LOW>
+__device__ __forceinline__ void add_up(const uint4 *buf, int nv, const Origin &o, float s, float low, float reach, int *hits,
+                                       int *count, float &e, float &h)
+{
+    constexpr int V = Vec<T>::n;
+    const typename Vec<T>::running low2 = Vec<T>::below(low), reach2 = Vec<T>::below(reach);
+    float2 e2 = both(0.0f), h2 = both(0.0f);
+#pragma unroll 2
+    for (int v = threadIdx.x; v < nv; v += NT) {
+        const uint4 u = buf[v];
+        float2 f[V / 2];
+        Vec<T>::wide(LOW ? Vec<T>::at_least(u, low2) : u, f);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            float2 t = exponents<FAR>(f[i], o, s);
+            const float2 p = make_float2(exp2_fast(t.x), exp2_fast(t.y));
+            e2 = add2(e2, p);
+            if (!LOW) t = make_float2(fmaxf(t.x, -1e4f), fmaxf(t.y, -1e4f));
+            h2 = fma2(p, t, h2);
+        }
+        if (TOP && Vec<T>::reaches(Vec<T>::top(u), reach2)) {
+            const int at = atomicAdd(count, 1);
+            if (at < kCap) hits[at] = v;
+        }
+    }
+    e = e2.x + e2.y;
+    h = h2.x + h2.y;
+}
+
 template <typename T, int NT, bool TOP>
 __global__ void __launch_bounds__(NT) k_logprobs(Logprobs a, int parts, int slice)
 {
     constexpr int V = Vec<T>::n;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float sh[3][NT / 32], reach_sh;
-    __shared__ __align__(16) float group[kGroups];
     __shared__ Sums sums[kMaxParts];
-    __shared__ int count;
+    __shared__ int count[2];
+    __shared__ uint64_t bar;
     uint4 *buf = reinterpret_cast<uint4 *>(smem);
     uint64_t *cand = reinterpret_cast<uint64_t *>(smem + slice);    // kCap keys; before that every thread's maximum
-    uint64_t *lists = cand + kCap;                                  // first block: parts x k keys
+    int *hits = reinterpret_cast<int *>(cand + kCap);               // kCap vectors
+    uint64_t *lists = reinterpret_cast<uint64_t *>(hits + kCap);    // first block: parts x k keys
     const int part = (int)(blockIdx.x % (unsigned)parts);
     const int64_t row = blockIdx.x / (unsigned)parts;
     cg::cluster_group cluster = cg::this_cluster();
-    if (parts > 1) cluster_arrive();        // the first block runs before anything is written to it
+    if (parts > 1) cluster_arrive();                // the first block runs before anything is written to it
 
     const Slice<T> sl(a.z, a.stride, row, a.vocab, part, parts);
-    load_slice<T, NT>(sl, buf);
-    copies_done();
-    float m = slice_max<T, NT>(buf, sl.nv);
+    start_slice<T, NT>(sl, buf, &bar);
+    __syncthreads();
+    const bool late = !mbar_wait_bounded(&bar, 0);
+    float m = late ? kLate : slice_max<T, NT>(buf, sl.nv);
     if (TOP) reinterpret_cast<float *>(cand)[threadIdx.x] = m;
     m = block_max_all<NT>(m, sh[0]);
     float reach = 0.0f;
     if (TOP) {
-        if (threadIdx.x < kGroups) {
+        if (threadIdx.x < 32) {
             const float *all = reinterpret_cast<const float *>(cand);
-            float g = all[threadIdx.x];
+            float g[kGroups / 32];
 #pragma unroll
-            for (int i = kGroups; i < NT; i += kGroups) g = fmaxf(g, all[threadIdx.x + i]);
-            group[threadIdx.x] = g;
-            asm volatile("bar.sync 1, %0;" ::"n"(kGroups) : "memory");
-            int gt = 0, ge = 0;
-#pragma unroll 8
-            for (int i = 0; i < kGroups; i += 4) {
-                const float4 q = *reinterpret_cast<const float4 *>(group + i);
-                gt += (q.x > g) + (q.y > g) + (q.z > g) + (q.w > g);
-                ge += (q.x >= g) + (q.y >= g) + (q.z >= g) + (q.w >= g);
+            for (int i = 0; i < kGroups / 32; ++i) {
+                g[i] = all[threadIdx.x + 32 * i];
+#pragma unroll
+                for (int o = kGroups; o < NT; o += kGroups) g[i] = fmaxf(g[i], all[threadIdx.x + 32 * i + o]);
             }
-            if (gt < a.k && a.k <= ge) reach_sh = g;
-            if (threadIdx.x == 0) count = 0;
+            const float r = kth_of_groups(g, a.k);
+            if (threadIdx.x == 0) { reach_sh = r; count[0] = count[1] = 0; }
         }
         __syncthreads();
         reach = reach_sh;
     }
 
-    const float s = (float)a.scale2, mu = m == kNegInf ? 0.0f : m;
-    const typename Vec<T>::running reach2 = Vec<T>::all(reach);
-    float2 e2 = both(0.0f), h2 = both(0.0f);
-#pragma unroll 2
-    for (int v = threadIdx.x; v < sl.nv; v += NT) {
-        const uint4 u = buf[v];
-        float2 f[V / 2];
-        Vec<T>::wide(u, f);
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i) {
-            const float2 t = mul2(add2(f[i], both(-mu)), both(s));
-            const float2 p = make_float2(exp2_fast(t.x), exp2_fast(t.y));
-            e2 = add2(e2, p);
-            h2 = fma2(p, make_float2(fmaxf(t.x, -1e4f), fmaxf(t.y, -1e4f)), h2);   // 0 times -inf is 0 here
-        }
-        if (TOP && Vec<T>::reaches(Vec<T>::top(u), reach2)) collect<T>(u, sl.start + v * V, reach, cand, &count, 0);
-    }
-    float e = warp_sum(e2.x + e2.y), h = warp_sum(h2.x + h2.y);
+    const float s = (float)a.scale2;
+    const Origin own(m, s);
+    const float low = widen(narrow<T>(own.m - fmaxf(200.0f / s, 0.015625f * fabsf(own.m))));
+    float e, h;
+    if (own.far)
+        add_up<T, NT, TOP, true, false>(buf, sl.nv, own, s, 0.0f, reach, hits, &count[0], e, h);
+    else if (!(low > kNegInf) || (own.m - low) * s < 150.0f)
+        add_up<T, NT, TOP, false, false>(buf, sl.nv, own, s, 0.0f, reach, hits, &count[0], e, h);
+    else
+        add_up<T, NT, TOP, false, true>(buf, sl.nv, own, s, low, reach, hits, &count[0], e, h);
+    e = warp_sum(e);
+    h = warp_sum(h);
     if ((threadIdx.x & 31) == 0) { sh[1][threadIdx.x >> 5] = e; sh[2][threadIdx.x >> 5] = h; }
     __syncthreads();
     int n = 0;
     if (TOP) {
-        n = count;
-        if (n > kCap) n = collect_in_order<T, NT>(buf, sl.nv, sl.start, a.k, cand, &count);
+        const int noted = count[0];
+        if (noted <= kCap) {
+            const T *elem = reinterpret_cast<const T *>(smem);
+            for (int i = threadIdx.x; i < noted * V; i += NT) {
+                const int c = hits[i / V] * V + i % V;
+                const float z = widen(elem[c]);
+                if (z >= reach && z > kNegInf) {
+                    const int at = atomicAdd(&count[1], 1);
+                    if (at < kCap) cand[at] = order_key(z, sl.start + c);
+                }
+            }
+            __syncthreads();
+            n = count[1];
+        }
+        if (noted > kCap || n > kCap) n = collect_in_order<T, NT>(buf, sl.nv, sl.start, a.k, cand, &count[1]);
         __syncthreads();
     }
     if (parts > 1) cluster_wait();
@@ -283,6 +376,7 @@ __global__ void __launch_bounds__(NT) k_logprobs(Logprobs a, int parts, int slic
             to[part] = Sums{m, e, h, min(n, a.k)};
         }
     }
+    if (late) mbar_wait_bounded(&bar, 0);            // no block leaves with copies in flight
     if (parts > 1) {
         cluster_arrive();
         if (part != 0) return;                       // nothing reads this block's shared memory
@@ -297,11 +391,11 @@ __global__ void __launch_bounds__(NT) k_logprobs(Logprobs a, int parts, int slic
     float M = kNegInf, E = 0.0f, H = 0.0f;
     int total = 0;
     for (int i = 0; i < parts; ++i) { M = fmaxf(M, sums[i].m); total += sums[i].n; }
-    const float Mu = M == kNegInf ? 0.0f : M;
+    const Origin all(M, s);
     for (int i = 0; i < parts; ++i) {
         const Sums p = sums[i];
         if (p.e == 0.0f) continue;                   // all masked
-        const float d = fmaxf((p.m - Mu) * s, -1e4f), f = p.m == kNegInf ? 1.0f : exp2_fast(d);
+        const float d = shift(Origin(p.m, s), all, s), f = p.e != p.e ? 1.0f : exp2_fast(d);
         E = fmaf(f, p.e, E);
         H += f * fmaf(d, p.e, p.h);
     }
@@ -311,10 +405,11 @@ __global__ void __launch_bounds__(NT) k_logprobs(Logprobs a, int parts, int slic
         if (a.logprob) {
             const int64_t t = index_at(a.tokens, row, a.index64);
             a.logprob[row] = t < 0 ? 0.0f : t >= a.vocab || none ? NAN : empty ? kNegInf
-                : (float)((((double)widen(sl.row[t]) - (double)Mu) * (double)s - l2) * kLn2);
+                : (float)((exponent64(widen(sl.row[t]), all, s) - l2) * kLn2);
         }
         if (a.entropy) a.entropy[row] = empty ? 0.0f : (float)((l2 - (double)H / (double)E) * kLn2);
-        if (a.lse) a.lse[row] = (float)((double)Mu * (a.scale2 * kLn2) + l2 * kLn2);
+        // z s - c - l2 is the log of p_i for s as rounded; the exact scale for the origin itself
+        if (a.lse) a.lse[row] = (float)(((all.far ? (double)all.m * a.scale2 : (double)all.c * (a.scale2 / (double)s)) + l2) * kLn2);
     }
     if (!TOP) return;
     for (int t = threadIdx.x; t < parts * a.k; t += NT) {
@@ -333,7 +428,7 @@ __global__ void __launch_bounds__(NT) k_logprobs(Logprobs a, int parts, int slic
         }
         if (at < a.k) {
             store_index(a.top_ids, row * a.k + at, a.index64, key_index(key));
-            a.top_logprobs[row * a.k + at] = (float)((((double)key_value(key) - (double)Mu) * (double)s - l2) * kLn2);
+            a.top_logprobs[row * a.k + at] = (float)((exponent64(key_value(key), all, s) - l2) * kLn2);
         }
     }
     for (int t = threadIdx.x; t < a.k; t += NT)
@@ -379,15 +474,60 @@ struct Rest {
     float m, e;
 };
 
+__device__ __forceinline__ double warp_sum64(double v)
+{
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+
+template <typename T, int NT, bool FAR>
+__device__ __forceinline__ float slice_sum(const uint4 *buf, int nv, const Origin &o, float s)
+{
+    constexpr int V = Vec<T>::n;
+    float2 e2 = both(0.0f);
+#pragma unroll 2
+    for (int v = threadIdx.x; v < nv; v += NT) {
+        float2 f[V / 2];
+        Vec<T>::wide(buf[v], f);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            const float2 t = exponents<FAR>(f[i], o, s);
+            e2 = add2(e2, make_float2(exp2_fast(t.x), exp2_fast(t.y)));
+        }
+    }
+    return e2.x + e2.y;
+}
+
+// The slice becomes scale 2^t.
+template <typename T, int NT, bool FAR>
+__device__ __forceinline__ void slice_gradient(uint4 *buf, int nv, const Origin &o, float s, float scale)
+{
+    constexpr int V = Vec<T>::n;
+#pragma unroll 2
+    for (int v = threadIdx.x; v < nv; v += NT) {
+        float2 f[V / 2];
+        Vec<T>::wide(buf[v], f);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            const float2 t = exponents<FAR>(f[i], o, s);
+            f[i] = mul2(make_float2(exp2_fast(t.x), exp2_fast(t.y)), both(scale));
+        }
+        buf[v] = Vec<T>::pack(f);
+    }
+}
+
 template <typename T, int NT>
 __global__ void __launch_bounds__(NT) k_distill(Distill a, int parts)
 {
     constexpr int V = Vec<T>::n, kWarps = kMaxList / 32;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float sh[2][NT / 32], shm[kWarps], she[kWarps];
-    __shared__ int32_t id[kMaxList];
-    __shared__ double lq[kMaxList], w[kMaxList], terms[kWarps], mass_sh;
+    __shared__ __align__(16) int32_t id[kMaxList];
+    __shared__ double w[kMaxList], sum64[kWarps];
+    __shared__ float top32[kWarps];
     __shared__ Rest rest_sh[kMaxParts];
+    __shared__ uint64_t bar;
     uint4 *buf = reinterpret_cast<uint4 *>(smem);
     T *elem = reinterpret_cast<T *>(smem);
     const int part = (int)(blockIdx.x % (unsigned)parts), j = threadIdx.x, k = a.k;
@@ -396,72 +536,73 @@ __global__ void __launch_bounds__(NT) k_distill(Distill a, int parts)
     if (parts > 1) cluster_arrive();
 
     const Slice<T> sl(a.z, a.stride, row, a.vocab, part, parts);
-    load_slice<T, NT>(sl, buf);
+    start_slice<T, NT>(sl, buf, &bar);
 
-    // while the slice is on its way, the teacher's distribution over the list: thread j < k has
-    // entry j, an index listed twice is taken together by its first entry
+    // While the slice is on its way, the teacher's distribution over the list.  Thread j < k has
+    // entry j; an index listed again is left to its first entry.  Unused: id -1, weight 0.
     int mine = -1;
+    float zj = kNegInf, lq = kNegInf;
     double q = 0.0;
-    float zj = kNegInf;
-    if (j < k) {
-        const int64_t i = index_at(a.ids, row * k + j, a.index64);
-        const float t = a.teacher[row * k + j];
-        mine = i >= 0 && i < a.vocab && (a.rest || t != kNegInf) ? (int)i : -1;
-        if (mine >= 0) zj = widen(sl.row[mine]);
-        id[j] = mine;
-        lq[j] = mine >= 0 ? (double)t : (double)kNegInf;
-    }
-    __syncthreads();
-    if (j < k) {
-        double top = 0.0;
-        if (!a.rest) {
-            top = (double)kNegInf;
-            for (int i = 0; i < k; ++i) top = fmax(top, lq[i]);
-            if (top == (double)kNegInf) top = 0.0;
+    if (j < kMaxList) {
+        if (j < k) {
+            const int64_t i = index_at(a.ids, row * k + j, a.index64);
+            lq = a.teacher[row * k + j];
+            mine = i >= 0 && i < a.vocab && (a.rest || lq != kNegInf) ? (int)i : -1;
+            if (mine >= 0) zj = widen(sl.row[mine]);
+            else lq = kNegInf;
         }
-        w[j] = exp(lq[j] - top);
+        id[j] = j < k ? mine : -1;
+        if (!a.rest) {
+            const float m = warp_max(lq);
+            if ((j & 31) == 0) top32[j >> 5] = m;
+        }
     }
     __syncthreads();
-    bool first = mine >= 0;
-    if (j < k) {
-        double sum = 0.0;
-        for (int i = 0; i < k; ++i) {
-            sum += w[i];
-            if (id[i] == mine) {
-                q += w[i];
-                if (i < j) first = false;
+    bool again = false;
+    if (j < kMaxList) {
+        float top = 0.0f;
+        if (!a.rest) {
+            top = fmaxf(fmaxf(top32[0], top32[1]), fmaxf(top32[2], top32[3]));
+            if (top == kNegInf) top = 0.0f;
+        }
+        if (mine >= 0) {
+            q = exp((double)lq - (double)top);
+#pragma unroll 4
+            for (int i = 0; i < j; i += 4) {
+                const int4 d = *reinterpret_cast<const int4 *>(id + i);
+                again |= (d.x == mine) | (d.y == mine && i + 1 < j) | (d.z == mine && i + 2 < j) | (d.w == mine && i + 3 < j);
             }
         }
-        if (!a.rest && sum != 0.0) q /= sum;
-        if (j == 0) mass_sh = sum;
-        if (!first) { q = 0.0; zj = kNegInf; }
+        w[j] = q;
+        const double sum = warp_sum64(q);
+        if ((j & 31) == 0) sum64[j >> 5] = sum;
     }
-    copies_done();
-    const int used = __syncthreads_count(first);
-    const double mass = mass_sh, r = !a.rest || used >= a.vocab ? 0.0 : mass != mass ? mass : fmax(0.0, 1.0 - mass);
+    const bool late = !mbar_wait_bounded(&bar, 0);
+    const int used = __syncthreads_count(mine >= 0 && !again);
+    if (__syncthreads_or(again) && mine >= 0) {          // some index is listed more than once
+        if (again) { q = 0.0; zj = kNegInf; }
+        else
+            for (int i = j + 1; i < k; ++i)
+                if (id[i] == mine) q += w[i];
+    }
+    const bool first = mine >= 0 && !again;
+    const double mass = (sum64[0] + sum64[1]) + (sum64[2] + sum64[3]);
+    if (!a.rest && mass != 0.0) q /= mass;
+    const double r = !a.rest || used >= a.vocab ? 0.0 : mass != mass ? mass : fmax(0.0, 1.0 - mass);
     const float s = (float)a.scale2;
-    if (first && mine >= sl.start && mine < sl.start + sl.nv * V) elem[mine - sl.start] = minus_inf<T>();
+    const bool here = first && mine >= sl.start && mine < sl.start + sl.nv * V;
+    if (here) elem[mine - sl.start] = minus_inf<T>();
     if (j < kMaxList) {
         const float m = warp_max(zj), p = zj == kNegInf ? 0.0f : exp2_fast((zj - m) * s);
-        const float e = warp_sum(zj != zj ? zj : p);
+        const float e = warp_sum(p);
         if ((j & 31) == 0) { shm[j >> 5] = m; she[j >> 5] = e; }
     }
     __syncthreads();
 
-    float m = block_max_all<NT>(slice_max<T, NT>(buf, sl.nv), sh[0]);
-    const float mu = m == kNegInf ? 0.0f : m;
-    float2 e2 = both(0.0f);
-#pragma unroll 4
-    for (int v = threadIdx.x; v < sl.nv; v += NT) {
-        float2 f[V / 2];
-        Vec<T>::wide(buf[v], f);
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i) {
-            const float2 t = mul2(add2(f[i], both(-mu)), both(s));
-            e2 = add2(e2, make_float2(exp2_fast(t.x), exp2_fast(t.y)));
-        }
-    }
-    float e = block_sum_all<NT>(e2.x + e2.y, sh[1]);
+    const float m = block_max_all<NT>(late ? kLate : slice_max<T, NT>(buf, sl.nv), sh[0]);
+    const Origin own(m, s);
+    float e = own.far ? slice_sum<T, NT, true>(buf, sl.nv, own, s) : slice_sum<T, NT, false>(buf, sl.nv, own, s);
+    e = block_sum_all<NT>(e, sh[1]);
     if (parts > 1) {
         cluster_wait();
         if (j < parts) cluster.map_shared_rank(rest_sh, j)[part] = Rest{m, e};
@@ -472,58 +613,62 @@ __global__ void __launch_bounds__(NT) k_distill(Distill a, int parts)
         __syncthreads();
     }
 
-    // rest and list, each relative to its own maximum; both relative to the larger of these
+    // rest and list, each relative to its own origin; then both relative to the larger
     float mr = kNegInf, er = 0.0f, ml = kNegInf, el = 0.0f;
     for (int i = 0; i < parts; ++i) mr = fmaxf(mr, rest_sh[i].m);
     for (int i = 0; i < kWarps; ++i) ml = fmaxf(ml, shm[i]);
-    const float mru = mr == kNegInf ? 0.0f : mr, mlu = ml == kNegInf ? 0.0f : ml;
+    const Origin rest(mr, s), top(fmaxf(mr, ml), s);
+    const float mlu = ml == kNegInf ? 0.0f : ml;
     for (int i = 0; i < parts; ++i) {
         const Rest p = rest_sh[i];
-        if (p.e != 0.0f) er = fmaf(p.m == kNegInf ? 1.0f : exp2_fast((p.m - mru) * s), p.e, er);
+        if (p.e != 0.0f) er = fmaf(p.e != p.e ? 1.0f : exp2_fast(shift(Origin(p.m, s), rest, s)), p.e, er);
     }
     for (int i = 0; i < kWarps; ++i)
-        if (she[i] != 0.0f) el = fmaf(shm[i] == kNegInf ? 1.0f : exp2_fast((shm[i] - mlu) * s), she[i], el);
-    const float top = fmaxf(mr, ml);
-    const bool bad = er != er || el != el || top > 3.402823466e38f, empty = !bad && top == kNegInf;
-    const float fr = er == 0.0f ? 0.0f : exp2_fast((mru - top) * s), fl = el == 0.0f ? 0.0f : exp2_fast((mlu - top) * s);
+        if (she[i] != 0.0f) el = fmaf(she[i] != she[i] ? 1.0f : exp2_fast((shm[i] - mlu) * s), she[i], el);
+    const bool bad = er != er || el != el || fmaxf(mr, ml) > 3.402823466e38f, empty = !bad && fmaxf(mr, ml) == kNegInf;
+    // the list's sum is relative to ml s, the origin's c is rounded: exponents of the difference
+    const float fr = er == 0.0f ? 0.0f : exp2_fast(shift(rest, top, s)), fl = el == 0.0f ? 0.0f
+        : exp2_fast(top.far ? (mlu - top.m) * s : fmaf(mlu, s, -top.c));
     const float E = fmaf(fr, er, fl * el);
 
     const bool loss = part == 0 && a.loss;
     if (loss && j < kMaxList) {
-        // relative to `top` and in 64 bits: the only rounding is that of the sums
+        // in 64 bits from here: the only roundings are those of the sums
         const double l2 = log2((double)E);
         double t = 0.0;
-        if (first && !(q == 0.0)) t = q * (log(q) - (((double)zj - (double)top) * (double)s - l2) * kLn2);
-        if (j == 0 && r > 0.0)
-            t += r * (log(r) - (((double)mru - (double)top) * (double)s + log2((double)er) - l2) * kLn2);
+        if (first && !(q == 0.0)) t = q * (log(q) - (exponent64(zj, top, s) - l2) * kLn2);
+        if (j == 0 && r > 0.0) {
+            const double at = top.far ? ((double)rest.m - (double)top.m) * (double)s
+                : (rest.far ? exponent64(rest.m, top, s) : (double)rest.c - (double)top.c);
+            t += r * (log(r) - (at + log2((double)er) - l2) * kLn2);
+        }
         if (j == 0 && r != r) t = r;
-#pragma unroll
-        for (int d = 16; d >= 1; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
-        if ((j & 31) == 0) terms[j >> 5] = t;
+        t = warp_sum64(t);
+        if ((j & 31) == 0) sum64[j >> 5] = t;
     }
 
     if (a.dz) {
         const float g = a.dloss[row] * a.inv_temperature;
         const bool zero = g == 0.0f || empty || (used == 0 && !bad);
         const float others = er == 0.0f ? 0.0f : g * (fr / E - (float)r / er);
-#pragma unroll 2
-        for (int v = threadIdx.x; v < sl.nv; v += NT) {
-            float2 f[V / 2];
-            Vec<T>::wide(buf[v], f);
+        if (zero || bad) {
+            for (int v = threadIdx.x; v < sl.nv; v += NT) {
+                float2 f[V / 2];
+                Vec<T>::wide(buf[v], f);
 #pragma unroll
-            for (int i = 0; i < V / 2; ++i) {
-                if (zero) f[i] = both(0.0f);
-                else if (bad) f[i] = make_float2(f[i].x == kNegInf ? 0.0f : NAN, f[i].y == kNegInf ? 0.0f : NAN);
-                else {
-                    const float2 t = mul2(add2(f[i], both(-mru)), both(s));
-                    f[i] = mul2(make_float2(exp2_fast(t.x), exp2_fast(t.y)), both(others));
-                }
+                for (int i = 0; i < V / 2; ++i)
+                    f[i] = zero ? both(0.0f) : make_float2(f[i].x == kNegInf ? 0.0f : NAN, f[i].y == kNegInf ? 0.0f : NAN);
+                buf[v] = Vec<T>::pack(f);
             }
-            buf[v] = Vec<T>::pack(f);
+        } else if (rest.far) {
+            slice_gradient<T, NT, true>(buf, sl.nv, rest, s, others);
+        } else {
+            slice_gradient<T, NT, false>(buf, sl.nv, rest, s, others);
         }
         __syncthreads();
-        if (first && mine >= sl.start && mine < sl.start + sl.nv * V) {
-            const float d = zero || zj == kNegInf ? 0.0f : bad ? NAN : g * (exp2_fast((zj - top) * s) / E - (float)q);
+        if (here) {
+            const float t = top.far ? (zj - top.m) * s : fmaf(zj, s, -top.c);
+            const float d = zero || zj == kNegInf ? 0.0f : bad ? NAN : g * (exp2_fast(t) / E - (float)q);
             elem[mine - sl.start] = narrow<T>(d);
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // the bulk copy reads what the threads wrote
@@ -547,11 +692,9 @@ __global__ void __launch_bounds__(NT) k_distill(Distill a, int parts)
     } else {
         __syncthreads();
     }
-    if (loss && j == 0) {
-        double t = 0.0;
-        for (int i = 0; i < kWarps; ++i) t += terms[i];
-        a.loss[row] = bad ? NAN : used == 0 ? 0.0f : empty ? INFINITY : (float)t;
-    }
+    if (loss && j == 0)
+        a.loss[row] = bad ? NAN : used == 0 ? 0.0f : empty ? INFINITY : (float)((sum64[0] + sum64[1]) + (sum64[2] + sum64[3]));
+    if (late) mbar_wait_bounded(&bar, 0);                               // no block leaves with copies in flight
     if (a.dz && threadIdx.x == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
 }
 
@@ -599,7 +742,7 @@ template <typename T>
 static void logprobs(const Logprobs &a, cudaStream_t st)
 {
     int parts = parts_for(a.vocab * (int64_t)sizeof(T)), slice = (int)slice_bytes<T>(a.vocab, parts);
-    const size_t smem = slice + (a.k ? kCap * 8 + (size_t)parts * a.k * 8 : 0);
+    const size_t smem = slice + (a.k ? kCap * 12 + (size_t)parts * a.k * 8 : 0);
     for_row_blocks(a.rows, parts, [&](int64_t at, int64_t n) {
         Logprobs b = a;
         b.z = static_cast<const T *>(a.z) + at * a.stride;
