@@ -121,6 +121,7 @@ template <typename T> struct Vec;
 
 template <> struct Vec<float> {
     static constexpr int n = 4;
+    static constexpr bool wide_range = true;
     typedef float running;
     static __device__ __forceinline__ running lowest() { return kNegInf; }
     static __device__ __forceinline__ void wide(const uint4 &u, float2 (&f)[2])
@@ -149,6 +150,7 @@ template <> struct Vec<float> {
 
 template <> struct Vec<bf16> {
     static constexpr int n = 8;
+    static constexpr bool wide_range = true;
     typedef __nv_bfloat162 running;
     static __device__ __forceinline__ __nv_bfloat162 two(uint32_t w) { return *reinterpret_cast<__nv_bfloat162 *>(&w); }
     static __device__ __forceinline__ running lowest() { return two(0xFF80FF80u); }
@@ -187,6 +189,7 @@ template <> struct Vec<bf16> {
 
 template <> struct Vec<f16> {
     static constexpr int n = 8;
+    static constexpr bool wide_range = false;   // -65504 is too near for "far below everything"
     typedef __half2 running;
     static __device__ __forceinline__ __half2 two(uint32_t w) { return *reinterpret_cast<__half2 *>(&w); }
     static __device__ __forceinline__ running lowest() { return two(0xFC00FC00u); }

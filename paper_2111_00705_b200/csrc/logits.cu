@@ -65,12 +65,13 @@ struct Slice {
     int off, vocab, nv;
     int start;              // column of the slice's first element (negative where off > 0)
 
-    __device__ __forceinline__ Slice(const void *z, int64_t stride, int64_t r, int64_t n, int part, int parts)
+    // parts = 2^log_parts
+    __device__ __forceinline__ Slice(const void *z, int64_t stride, int64_t r, int64_t n, int part, int log_parts)
     {
         row = static_cast<const T *>(z) + r * stride;
         vocab = (int)n;
         off = (int)(((uintptr_t)row & 15) / sizeof(T));
-        const int nvec = (off + vocab + V - 1) / V, per = (nvec + parts - 1) / parts, first = part * per;
+        const int nvec = (off + vocab + V - 1) / V, per = (nvec + (1 << log_parts) - 1) >> log_parts, first = part * per;
         nv = max(0, min(per, nvec - first));
         start = first * V - off;
     }
@@ -160,12 +161,6 @@ __device__ __forceinline__ double exponent64(float z, const Origin &row, float s
     return row.far ? ((double)z - (double)row.m) * (double)s : (double)z * (double)s - (double)row.c;
 }
 
-// Sums of a slice: m its maximum, e = sum 2^t, h = sum 2^t t.
-struct Sums {
-    float m, e, h;
-    int n;                  // entries of the slice's list of alternatives
-};
-
 // ---------------------------------------------------------------------------------------------
 // Alternatives.  Every slice gives its k first tokens in descending order, the cluster's first
 // block merges them.  Within a slice: 128 groups of threads have each met a largest value; the
@@ -180,8 +175,8 @@ struct Sums {
 constexpr int kCap = 512;
 constexpr int kGroups = 128;
 
-// A lower bound of the k-th largest of the 4 x 32 values of a warp (1 <= k <= 128).
-__device__ __forceinline__ float kth_of_groups(const float (&g)[kGroups / 32], int k)
+// The upper 16 bits of the order of the k-th largest of the 4 x 32 values of a warp (1 <= k <= 128).
+__device__ __forceinline__ int kth_of_groups(const float (&g)[kGroups / 32], int k)
 {
     uint32_t o[kGroups / 32], t = 0;
 #pragma unroll
@@ -194,7 +189,7 @@ __device__ __forceinline__ float kth_of_groups(const float (&g)[kGroups / 32], i
         for (int i = 0; i < kGroups / 32; ++i) n += o[i] >= next;
         if (__reduce_add_sync(0xffffffffu, n) >= k) t = next;
     }
-    return t <= 0x7Fu ? kNegInf : key_value((uint64_t)t << 48);     // 0x7F: the order of -inf
+    return (int)t;
 }
 
 __device__ __forceinline__ int rank_of(uint64_t key, const uint64_t *keys, int n)
@@ -206,26 +201,20 @@ __device__ __forceinline__ int rank_of(uint64_t key, const uint64_t *keys, int n
 }
 
 template <typename T, int NT>
-__device__ __noinline__ int collect_in_order(const uint4 *buf, int nv, int start, int k, uint64_t *cand, int *count)
+__device__ __noinline__ int collect_in_order(const Slice<T> &sl, float reach, int k, uint64_t *cand, int *count)
 {
-    constexpr int V = Vec<T>::n, step = (kCap - kMaxList) / V, per = (kCap + NT - 1) / NT;
-    static_assert(step <= NT, "one vector per thread and step");
+    constexpr int step = kCap - kMaxList, per = (kCap + NT - 1) / NT;
+    const int lo = max(0, sl.start), hi = min(sl.vocab, sl.start + sl.nv * Vec<T>::n);
     int kept = 0;
     uint64_t above = 0;
-    for (int base = 0; base < nv; base += step) {
+    for (int base = lo; base < hi; base += step) {
         __syncthreads();
         if (threadIdx.x == 0) *count = kept;
         __syncthreads();
-        const int v = base + (int)threadIdx.x;
-        if (threadIdx.x < step && v < nv) {
-            float2 f[V / 2];
-            Vec<T>::wide(buf[v], f);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float z = i & 1 ? f[i / 2].y : f[i / 2].x;
-                const uint64_t key = order_key(z, start + v * V + i);
-                if (z > kNegInf && key > above) cand[atomicAdd(count, 1)] = key;
-            }
+        for (int c = base + threadIdx.x; c < min(base + step, hi); c += NT) {
+            const float z = widen(sl.row[c]);
+            const uint64_t key = order_key(z, c);
+            if (z >= reach && z > kNegInf && key > above) cand[atomicAdd(count, 1)] = key;
         }
         __syncthreads();
         kept = *count;
@@ -250,67 +239,150 @@ __device__ __noinline__ int collect_in_order(const uint4 *buf, int nv, int start
     return kept;
 }
 
-// One pass over a slice: e = sum 2^t, h = sum 2^t t; with TOP the vectors that hold an element
-// >= reach are noted.  FAR: see Origin.  LOW: `low` is a value of T whose t is finite and below
-// -150; raising what is lower (masked logits) to it keeps 0 times -inf out of h, and 2^t is 0 for
-// both.  Without LOW (no such value of T) t itself is bounded, an operation for each element
-// instead of one for two.
-template <typename T, int NT, bool TOP, bool FAR, bool LOW>
-__device__ __forceinline__ void add_up(const uint4 *buf, int nv, const Origin &o, float s, float low, float reach, int *hits,
-                                       int *count, float &e, float &h)
+// ---------------------------------------------------------------------------------------------
+// The forward pass reads every logit once, in batches of kBatch vectors a thread, the next batch
+// on its way while one is worked on.  A thread's sums are relative to the largest value it has
+// met, c = max(m, -1e30) s, and are rescaled when a batch raises it (about ten operations for 32
+// logits): no barrier and no second look at a logit, so memory is never waited for together.
+//   e = sum 2^t, h = sum 2^t t, t = z s - c (one fused operation for two logits).
+// Masked logits must not make 0 times -inf in h.  LOW raises them (four packed operations for
+// eight) to a value whose t is finite and far below -150; binary16 has no such value next to its
+// lowest and bounds t itself.  Rows beyond +-1e30, and rows where all is masked by the type's
+// lowest value, give no sums this way (infinite c, or e = 0): they are added up again relative to
+// their maximum.
+// For the alternatives each batch leaves the upper 16 bits of its maximum's order in shared
+// memory; after the pass only batches that reach the threshold are looked at again (in L2).
+// ---------------------------------------------------------------------------------------------
+constexpr int kBatch = 4;
+constexpr float kFar = 1e30f;
+
+template <typename T>
+__device__ __noinline__ uint4 edge_vector(const Slice<T> sl, int v)
 {
     constexpr int V = Vec<T>::n;
-    const typename Vec<T>::running low2 = Vec<T>::below(low), reach2 = Vec<T>::below(reach);
-    float2 e2 = both(0.0f), h2 = both(0.0f);
-#pragma unroll 2
-    for (int v = threadIdx.x; v < nv; v += NT) {
-        const uint4 u = buf[v];
-        float2 f[V / 2];
-        Vec<T>::wide(LOW ? Vec<T>::at_least(u, low2) : u, f);
+    const int c = sl.start + v * V;
+    __align__(16) T e[V];
 #pragma unroll
-        for (int i = 0; i < V / 2; ++i) {
-            float2 t = exponents<FAR>(f[i], o, s);
-            const float2 p = make_float2(exp2_fast(t.x), exp2_fast(t.y));
-            e2 = add2(e2, p);
-            if (!LOW) t = make_float2(fmaxf(t.x, -1e4f), fmaxf(t.y, -1e4f));
-            h2 = fma2(p, t, h2);
-        }
-        if (TOP && Vec<T>::reaches(Vec<T>::top(u), reach2)) {
-            const int at = atomicAdd(count, 1);
-            if (at < kCap) hits[at] = v;
+    for (int i = 0; i < V; ++i) e[i] = v < sl.nv && c + i >= 0 && c + i < sl.vocab ? sl.row[c + i] : minus_inf<T>();
+    return *reinterpret_cast<uint4 *>(e);
+}
+
+__device__ __forceinline__ uint4 ld_stream(const void *p)
+{
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+template <typename T, int NT>
+__device__ __forceinline__ void load_batch(const Slice<T> &sl, int v, uint4 (&u)[kBatch])
+{
+    constexpr int V = Vec<T>::n;
+    const int first = v - (int)threadIdx.x;             // of the block's batch
+    const T *p = sl.row + (sl.start + v * V);
+    if (sl.start + first * V >= 0 && sl.start + (first + kBatch * NT) * V <= sl.vocab && first + kBatch * NT <= sl.nv) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) u[i] = ld_stream(p + i * NT * V);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int w = v + i * NT;
+            if (w < sl.nv && sl.whole(w)) u[i] = ld_stream(p + i * NT * V);
+            else u[i] = edge_vector(sl, w);
         }
     }
-    e = e2.x + e2.y;
-    h = h2.x + h2.y;
+}
+
+struct Running {
+    float m, c;
+    float2 e, h;
+};
+
+// Sums of a slice: m its maximum, c the origin of t, e = sum 2^t, h = sum 2^t t.
+struct Sums {
+    float m, c, e, h;
+    int n;                  // entries of the slice's list of alternatives
+};
+
+// The sums of a warp's lanes, each relative to its own c, relative to the largest c.  (An origin
+// infinitely far below belongs to sums of 0.)
+__device__ __forceinline__ void join_warp(float &c, float &e, float &h)
+{
+    const float n = warp_max(c), d = c - n, f = exp2_fast(d);
+    h = warp_sum(f == 0.0f && e == e ? 0.0f : f * fmaf(d, e, h));
+    e = warp_sum(f * e);
+    c = n;
 }
 
 template <typename T, int NT, bool TOP>
-__global__ void __launch_bounds__(NT) k_logprobs(Logprobs a, int parts, int slice)
+__global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_parts, int rounds)
 {
+    const int parts = 1 << log_parts;
     constexpr int V = Vec<T>::n;
+    constexpr bool LOW = Vec<T>::wide_range;
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ float sh[3][NT / 32], reach_sh;
+    __shared__ float sh[4][NT / 32];
     __shared__ Sums sums[kMaxParts];
-    __shared__ int count[2];
-    __shared__ uint64_t bar;
-    uint4 *buf = reinterpret_cast<uint4 *>(smem);
-    uint64_t *cand = reinterpret_cast<uint64_t *>(smem + slice);    // kCap keys; before that every thread's maximum
-    int *hits = reinterpret_cast<int *>(cand + kCap);               // kCap vectors
-    uint64_t *lists = reinterpret_cast<uint64_t *>(hits + kCap);    // first block: parts x k keys
-    const int part = (int)(blockIdx.x % (unsigned)parts);
-    const int64_t row = blockIdx.x / (unsigned)parts;
+    __shared__ int count[2], reach_sh;
+    uint64_t *cand = reinterpret_cast<uint64_t *>(smem);            // kCap keys; before that every thread's maximum
+    uint64_t *lists = cand + kCap;                                  // first block: parts x k keys
+    int *hits = reinterpret_cast<int *>(lists + parts * a.k);       // kCap batches
+    uint16_t *keys = reinterpret_cast<uint16_t *>(hits + kCap);     // one of every batch
+    const int part = (int)(blockIdx.x & (unsigned)(parts - 1));
+    const int64_t row = blockIdx.x >> log_parts;
     cg::cluster_group cluster = cg::this_cluster();
     if (parts > 1) cluster_arrive();                // the first block runs before anything is written to it
 
-    const Slice<T> sl(a.z, a.stride, row, a.vocab, part, parts);
-    start_slice<T, NT>(sl, buf, &bar);
-    __syncthreads();
-    const bool late = !mbar_wait_bounded(&bar, 0);
-    float m = late ? kLate : slice_max<T, NT>(buf, sl.nv);
-    if (TOP) reinterpret_cast<float *>(cand)[threadIdx.x] = m;
-    m = block_max_all<NT>(m, sh[0]);
-    float reach = 0.0f;
+    const Slice<T> sl(a.z, a.stride, row, a.vocab, part, log_parts);
+    const float s = (float)a.scale2, gap = 200.0f / s;
+    Running r = {kNegInf, -kFar * s, {0.0f, 0.0f}, {0.0f, 0.0f}};
+    uint4 u[kBatch], next[kBatch];
+    if (sl.nv > 0) load_batch<T, NT>(sl, threadIdx.x, u);
+#pragma unroll 2
+    for (int i = 0, v = threadIdx.x; i < rounds && i * (kBatch * NT) < sl.nv; ++i, v += kBatch * NT) {
+        if ((i + 1) * (kBatch * NT) < sl.nv) load_batch<T, NT>(sl, v + kBatch * NT, next);
+        typename Vec<T>::running mx = Vec<T>::top(u[0]);
+#pragma unroll
+        for (int b = 1; b < kBatch; ++b) mx = Vec<T>::max(mx, Vec<T>::top(u[b]));
+        const float top = Vec<T>::value(mx);
+        if (TOP) keys[i * NT + threadIdx.x] = (uint16_t)(order_key(top, 0) >> 48);
+        r.m = fmaxf(r.m, top);
+        const float m = fmaxf(r.m, -kFar), c = m * s, d = r.c - c, f = exp2_fast(d);
+        r.c = c;
+        r.h = mul2(fma2(both(d), r.e, r.h), both(f));
+        r.e = mul2(r.e, both(f));
+        const typename Vec<T>::running low = Vec<T>::below(m - fmaxf(gap, 0.015625f * fabsf(m)));
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            float2 z[V / 2];
+            Vec<T>::wide(LOW ? Vec<T>::at_least(u[b], low) : u[b], z);
+#pragma unroll
+            for (int j = 0; j < V / 2; ++j) {
+                float2 t = fma2(z[j], both(s), both(-c));
+                const float2 p = make_float2(exp2_fast(t.x), exp2_fast(t.y));
+                r.e = add2(r.e, p);
+                if (!LOW) t = make_float2(fmaxf(t.x, -1e4f), fmaxf(t.y, -1e4f));
+                r.h = fma2(p, t, r.h);
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) u[b] = next[b];
+    }
+
+    const int lane = threadIdx.x & 31;
+    // the block's sums, and the threshold of its alternatives
+    float c = r.c, e = r.e.x + r.e.y, h = r.h.x + r.h.y;
+    float m = warp_max(r.m);
+    join_warp(c, e, h);
+    if ((threadIdx.x & 31) == 0) {
+        const int w = threadIdx.x >> 5;
+        sh[0][w] = m; sh[1][w] = c; sh[2][w] = e; sh[3][w] = h;
+    }
+    int n = 0;
     if (TOP) {
+        reinterpret_cast<float *>(cand)[threadIdx.x] = r.m;
+        __syncthreads();
         if (threadIdx.x < 32) {
             const float *all = reinterpret_cast<const float *>(cand);
             float g[kGroups / 32];
@@ -320,63 +392,58 @@ __global__ void __launch_bounds__(NT) k_logprobs(Logprobs a, int parts, int slic
 #pragma unroll
                 for (int o = kGroups; o < NT; o += kGroups) g[i] = fmaxf(g[i], all[threadIdx.x + 32 * i + o]);
             }
-            const float r = kth_of_groups(g, a.k);
-            if (threadIdx.x == 0) { reach_sh = r; count[0] = count[1] = 0; }
+            const int t = kth_of_groups(g, a.k);
+            if (threadIdx.x == 0) { reach_sh = t; count[0] = count[1] = 0; }
         }
         __syncthreads();
-        reach = reach_sh;
-    }
-
-    const float s = (float)a.scale2;
-    const Origin own(m, s);
-    const float low = widen(narrow<T>(own.m - fmaxf(200.0f / s, 0.015625f * fabsf(own.m))));
-    float e, h;
-    if (own.far)
-        add_up<T, NT, TOP, true, false>(buf, sl.nv, own, s, 0.0f, reach, hits, &count[0], e, h);
-    else if (!(low > kNegInf) || (own.m - low) * s < 150.0f)
-        add_up<T, NT, TOP, false, false>(buf, sl.nv, own, s, 0.0f, reach, hits, &count[0], e, h);
-    else
-        add_up<T, NT, TOP, false, true>(buf, sl.nv, own, s, low, reach, hits, &count[0], e, h);
-    e = warp_sum(e);
-    h = warp_sum(h);
-    if ((threadIdx.x & 31) == 0) { sh[1][threadIdx.x >> 5] = e; sh[2][threadIdx.x >> 5] = h; }
-    __syncthreads();
-    int n = 0;
-    if (TOP) {
+        const int reach16 = max(reach_sh, 0x80);                    // 0x7F: the order of -inf
+        const float reach = key_value((uint64_t)reach16 << 48);
+        const int batches = min(rounds, (sl.nv + kBatch * NT - 1) / (kBatch * NT)) * NT;
+        for (int i = threadIdx.x; i < batches; i += NT)
+            if (keys[i] >= reach16) {
+                const int at = atomicAdd(&count[0], 1);
+                if (at < kCap) hits[at] = i;
+            }
+        __syncthreads();
         const int noted = count[0];
         if (noted <= kCap) {
-            const T *elem = reinterpret_cast<const T *>(smem);
-            for (int i = threadIdx.x; i < noted * V; i += NT) {
-                const int c = hits[i / V] * V + i % V;
-                const float z = widen(elem[c]);
-                if (z >= reach && z > kNegInf) {
-                    const int at = atomicAdd(&count[1], 1);
-                    if (at < kCap) cand[at] = order_key(z, sl.start + c);
+            for (int i = threadIdx.x >> 5; i < noted; i += NT / 32) {
+                const int b = hits[i], v = b / NT * (kBatch * NT) + b % NT + lane / V * NT, at = sl.start + v * V + lane % V;
+                if (lane < kBatch * V && v < sl.nv && at >= 0 && at < sl.vocab) {
+                    const float z = widen(sl.row[at]);
+                    if (z >= reach) {
+                        const int to = atomicAdd(&count[1], 1);
+                        if (to < kCap) cand[to] = order_key(z, at);
+                    }
                 }
             }
             __syncthreads();
             n = count[1];
         }
-        if (noted > kCap || n > kCap) n = collect_in_order<T, NT>(buf, sl.nv, sl.start, a.k, cand, &count[1]);
-        __syncthreads();
+        if (noted > kCap || n > kCap) n = collect_in_order<T, NT>(sl, reach, a.k, cand, &count[1]);
     }
+    __syncthreads();
     if (parts > 1) cluster_wait();
-    uint64_t *list = parts > 1 ? cluster.map_shared_rank(lists, 0) : lists;
-    if (TOP)
+    if (TOP) {
+        uint64_t *list = parts > 1 ? cluster.map_shared_rank(lists, 0) : lists;
         for (int i = threadIdx.x; i < n; i += NT) {
             const uint64_t key = cand[i];
-            const int r = rank_of(key, cand, n);
-            if (r < a.k) list[part * a.k + r] = key;
-        }
-    if (threadIdx.x < 32) {
-        e = warp_sum(threadIdx.x < NT / 32 ? sh[1][threadIdx.x] : 0.0f);
-        h = warp_sum(threadIdx.x < NT / 32 ? sh[2][threadIdx.x] : 0.0f);
-        if (threadIdx.x == 0) {
-            Sums *to = parts > 1 ? cluster.map_shared_rank(sums, 0) : sums;
-            to[part] = Sums{m, e, h, min(n, a.k)};
+            const int at = rank_of(key, cand, n);
+            if (at < a.k) list[part * a.k + at] = key;
         }
     }
-    if (late) mbar_wait_bounded(&bar, 0);            // no block leaves with copies in flight
+    if (threadIdx.x < 32) {
+        const bool is = threadIdx.x < NT / 32;
+        m = warp_max(is ? sh[0][threadIdx.x] : kNegInf);
+        c = is ? sh[1][threadIdx.x] : -kFar * s;
+        e = is ? sh[2][threadIdx.x] : 0.0f;
+        h = is ? sh[3][threadIdx.x] : 0.0f;
+        join_warp(c, e, h);
+        if (threadIdx.x == 0) {
+            Sums *to = parts > 1 ? cluster.map_shared_rank(sums, 0) : sums;
+            to[part] = Sums{m, c, e, h, min(n, a.k)};
+        }
+    }
     if (parts > 1) {
         cluster_arrive();
         if (part != 0) return;                       // nothing reads this block's shared memory
@@ -385,20 +452,27 @@ __global__ void __launch_bounds__(NT) k_logprobs(Logprobs a, int parts, int slic
         __syncthreads();
     }
 
-    // the row: slices relative to the row's maximum
-    const int todo = TOP ? max(1, parts * a.k) : 1;
-    if ((int)(threadIdx.x & ~31u) >= max(todo, a.k)) return;
-    float M = kNegInf, E = 0.0f, H = 0.0f;
-    int total = 0;
-    for (int i = 0; i < parts; ++i) { M = fmaxf(M, sums[i].m); total += sums[i].n; }
-    const Origin all(M, s);
-    for (int i = 0; i < parts; ++i) {
-        const Sums p = sums[i];
-        if (p.e == 0.0f) continue;                   // all masked
-        const float d = shift(Origin(p.m, s), all, s), f = p.e != p.e ? 1.0f : exp2_fast(d);
-        E = fmaf(f, p.e, E);
-        H += f * fmaf(d, p.e, p.h);
+    // the row
+    const bool is = lane < parts;
+    const Sums p = sums[is ? lane : 0];
+    float M = warp_max(p.m), C = p.c, E = is ? p.e : 0.0f, H = is ? p.h : 0.0f;
+    join_warp(C, E, H);
+    const int total = TOP ? (int)__reduce_add_sync(0xffffffffu, is ? p.n : 0) : 0;
+    Origin all(M, s);
+    all.c = C;
+    all.far = fabsf(M) >= kFar && M > kNegInf && M <= 3.402823466e38f;
+    if (all.far) {                                   // relative to the maximum, by this block alone
+        e = h = 0.0f;
+        for (int64_t i = threadIdx.x; i < a.vocab; i += NT) {
+            const float t = (widen(static_cast<const T *>(sl.row)[i]) - M) * s, p = exp2_fast(t);
+            e += p;
+            h = fmaf(p, fmaxf(t, -1e4f), h);
+        }
+        __syncthreads();
+        E = block_sum_all<NT>(e, sh[0]);
+        H = block_sum_all<NT>(h, sh[1]);
     }
+    if ((int)(threadIdx.x & ~31u) >= max(TOP ? parts * a.k : 1, 1)) return;
     const bool none = E != E || M > 3.402823466e38f, empty = !none && E == 0.0f;
     const double l2 = none ? (double)NAN : empty ? (double)kNegInf : log2((double)E);
     if (threadIdx.x == 0) {
@@ -518,7 +592,7 @@ __device__ __forceinline__ void slice_gradient(uint4 *buf, int nv, const Origin 
 }
 
 template <typename T, int NT>
-__global__ void __launch_bounds__(NT) k_distill(Distill a, int parts)
+__global__ void __launch_bounds__(NT) k_distill(Distill a, int log_parts)
 {
     constexpr int V = Vec<T>::n, kWarps = kMaxList / 32;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -530,12 +604,12 @@ __global__ void __launch_bounds__(NT) k_distill(Distill a, int parts)
     __shared__ uint64_t bar;
     uint4 *buf = reinterpret_cast<uint4 *>(smem);
     T *elem = reinterpret_cast<T *>(smem);
-    const int part = (int)(blockIdx.x % (unsigned)parts), j = threadIdx.x, k = a.k;
-    const int64_t row = blockIdx.x / (unsigned)parts;
+    const int parts = 1 << log_parts, part = (int)(blockIdx.x & (unsigned)(parts - 1)), j = threadIdx.x, k = a.k;
+    const int64_t row = blockIdx.x >> log_parts;
     cg::cluster_group cluster = cg::this_cluster();
     if (parts > 1) cluster_arrive();
 
-    const Slice<T> sl(a.z, a.stride, row, a.vocab, part, parts);
+    const Slice<T> sl(a.z, a.stride, row, a.vocab, part, log_parts);
     start_slice<T, NT>(sl, buf, &bar);
 
     // While the slice is on its way, the teacher's distribution over the list.  Thread j < k has
@@ -704,12 +778,21 @@ __global__ void __launch_bounds__(NT) k_distill(Distill a, int parts)
 constexpr int kSliceBytes = 64 * 1024 + 64;      // three blocks share an SM
 constexpr int kRowThreads = 256;
 
-// Blocks per row: as few as hold the row in slices of 64 KB.
-static int parts_for(int64_t bytes)
+// Blocks per row of the forward pass, as a power of two: one where the rows alone fill the GPU
+// (two for each SM); fewer rows are shared by up to 8 blocks of at least 8 KB.
+static int log_parts_for_rows(int64_t rows, int64_t bytes)
 {
-    int parts = 1;
-    while (parts < kMaxParts && (bytes + parts - 1) / parts > kSliceBytes - 64) parts *= 2;
-    return parts;
+    int n = 0;
+    while (n < 3 && rows << n < 2 * 148 && bytes >> (n + 1) >= 8 * 1024) ++n;
+    return n;
+}
+
+// Blocks per row where the row is held in shared memory: as few as hold it in slices of 64 KB.
+static int log_parts_for_slices(int64_t bytes)
+{
+    int n = 0;
+    while (n < 3 && ((bytes - 1) >> n) + 1 > kSliceBytes - 64) ++n;
+    return n;
 }
 
 template <typename F>
@@ -741,8 +824,10 @@ static void for_row_blocks(int64_t rows, int parts, F f)
 template <typename T>
 static void logprobs(const Logprobs &a, cudaStream_t st)
 {
-    int parts = parts_for(a.vocab * (int64_t)sizeof(T)), slice = (int)slice_bytes<T>(a.vocab, parts);
-    const size_t smem = slice + (a.k ? kCap * 12 + (size_t)parts * a.k * 8 : 0);
+    constexpr int NT = kRowThreads;
+    int log_parts = log_parts_for_rows(a.rows, a.vocab * (int64_t)sizeof(T)), parts = 1 << log_parts;
+    int rounds = (int)((slice_bytes<T>(a.vocab, parts) / 16 + kBatch * NT - 1) / (kBatch * NT));
+    const size_t smem = a.k ? kCap * 12 + (size_t)parts * a.k * 8 + (size_t)rounds * NT * 2 : 0;
     for_row_blocks(a.rows, parts, [&](int64_t at, int64_t n) {
         Logprobs b = a;
         b.z = static_cast<const T *>(a.z) + at * a.stride;
@@ -754,16 +839,16 @@ static void logprobs(const Logprobs &a, cudaStream_t st)
             b.top_ids = static_cast<char *>(a.top_ids) + at * a.k * (a.index64 ? 8 : 4);
             b.top_logprobs += at * a.k;
         }
-        const void *args[] = {&b, &parts, &slice};
-        if (a.k) launch_rows(k_logprobs<T, kRowThreads, true>, n, parts, kRowThreads, smem, st, args);
-        else launch_rows(k_logprobs<T, kRowThreads, false>, n, parts, kRowThreads, smem, st, args);
+        const void *args[] = {&b, &log_parts, &rounds};
+        if (a.k) launch_rows(k_logprobs<T, NT, true>, n, parts, NT, smem, st, args);
+        else launch_rows(k_logprobs<T, NT, false>, n, parts, NT, smem, st, args);
     });
 }
 
 template <typename T>
 static void distill(const Distill &a, cudaStream_t st)
 {
-    int parts = parts_for(a.vocab * (int64_t)sizeof(T));
+    int log_parts = log_parts_for_slices(a.vocab * (int64_t)sizeof(T)), parts = 1 << log_parts;
     const size_t smem = slice_bytes<T>(a.vocab, parts);
     for_row_blocks(a.rows, parts, [&](int64_t at, int64_t n) {
         Distill b = a;
@@ -773,7 +858,7 @@ static void distill(const Distill &a, cudaStream_t st)
         if (a.dloss) b.dloss += at;
         if (a.loss) b.loss += at;
         if (a.dz) b.dz = static_cast<T *>(a.dz) + at * a.dz_stride;
-        const void *args[] = {&b, &parts};
+        const void *args[] = {&b, &log_parts};
         launch_rows(k_distill<T, kRowThreads>, n, parts, kRowThreads, smem, st, args);
     });
 }
