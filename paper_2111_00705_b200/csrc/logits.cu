@@ -163,9 +163,9 @@ __device__ __forceinline__ double exponent64(float z, const Origin &row, float s
 
 // ---------------------------------------------------------------------------------------------
 // Alternatives.  Every slice gives its k first tokens in descending order, the cluster's first
-// block merges them.  Within a slice: 128 groups of threads have each met a largest value; the
-// k-th largest of these 128 is a value that at least k elements reach, and in a row without
-// structure hardly more (128 ln(128 / (128 - k)) are expected: 89 for k = 64).  It is found bit by
+// block merges them.  Within a slice the 256 threads have each met a largest value; the
+// k-th largest of these is a value that at least k elements reach, and in a row without
+// structure hardly more (256 ln(256 / (256 - k)) are expected: 74 for k = 64).  It is found bit by
 // bit in the upper 16 bits of the values' order (a bound a little too low only lets a few more
 // in).  The pass that adds up the exponentials notes the vectors that reach it; their elements
 // that do are collected, and counting for each how many are greater sorts them.  Only where more
@@ -173,9 +173,9 @@ __device__ __forceinline__ double exponent64(float z, const Origin &row, float s
 // threads' vectors) the slice is walked again in order, the best k so far always kept.
 // ---------------------------------------------------------------------------------------------
 constexpr int kCap = 512;
-constexpr int kGroups = 128;
+constexpr int kGroups = 256;
 
-// The upper 16 bits of the order of the k-th largest of the 4 x 32 values of a warp (1 <= k <= 128).
+// The upper 16 bits of the order of the k-th largest of the values of a warp's lanes (1 <= k <= kGroups).
 __device__ __forceinline__ int kth_of_groups(const float (&g)[kGroups / 32], int k)
 {
     uint32_t o[kGroups / 32], t = 0;
@@ -326,9 +326,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
     __shared__ Sums sums[kMaxParts];
     __shared__ int count[2], reach_sh;
     uint64_t *cand = reinterpret_cast<uint64_t *>(smem);            // kCap keys; before that every thread's maximum
-    uint64_t *lists = cand + kCap;                                  // first block: parts x k keys
-    int *hits = reinterpret_cast<int *>(lists + parts * a.k);       // kCap batches
+    int *hits = reinterpret_cast<int *>(cand + kCap);               // kCap batches
     uint16_t *keys = reinterpret_cast<uint16_t *>(hits + kCap);     // one of every batch
+    uint64_t *lists = reinterpret_cast<uint64_t *>(keys + rounds * NT);     // first block: parts x k keys
     const int part = (int)(blockIdx.x & (unsigned)(parts - 1));
     const int64_t row = blockIdx.x >> log_parts;
     cg::cluster_group cluster = cg::this_cluster();
@@ -399,23 +399,40 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
         const int reach16 = max(reach_sh, 0x80);                    // 0x7F: the order of -inf
         const float reach = key_value((uint64_t)reach16 << 48);
         const int batches = min(rounds, (sl.nv + kBatch * NT - 1) / (kBatch * NT)) * NT;
-        for (int i = threadIdx.x; i < batches; i += NT)
-            if (keys[i] >= reach16) {
-                const int at = atomicAdd(&count[0], 1);
-                if (at < kCap) hits[at] = i;
-            }
+        for (int i = threadIdx.x; i < batches / 8; i += NT) {
+            const uint4 q = reinterpret_cast<const uint4 *>(keys)[i];
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int b = 0; b < 8; ++b)
+                if ((int)(b & 1 ? w[b / 2] >> 16 : w[b / 2] & 0xFFFFu) >= reach16) {
+                    const int at = atomicAdd(&count[0], 1);
+                    if (at < kCap) hits[at] = 8 * i + b;
+                }
+        }
         __syncthreads();
         const int noted = count[0];
         if (noted <= kCap) {
-            for (int i = threadIdx.x >> 5; i < noted; i += NT / 32) {
-                const int b = hits[i], v = b / NT * (kBatch * NT) + b % NT + lane / V * NT, at = sl.start + v * V + lane % V;
-                if (lane < kBatch * V && v < sl.nv && at >= 0 && at < sl.vocab) {
-                    const float z = widen(sl.row[at]);
-                    if (z >= reach) {
-                        const int to = atomicAdd(&count[1], 1);
-                        if (to < kCap) cand[to] = order_key(z, at);
+            // a warp looks at kAhead batches at a time, a lane at one element of each
+            constexpr int kAhead = 8, W = NT / 32;
+            for (int i = threadIdx.x >> 5; i < noted; i += kAhead * W) {
+                float z[kAhead];
+                int at[kAhead];
+#pragma unroll
+                for (int o = 0; o < kAhead; ++o) {
+                    z[o] = kNegInf;
+                    at[o] = 0;
+                    if (i + o * W < noted && lane < kBatch * V) {
+                        const int b = hits[i + o * W], v = b / NT * (kBatch * NT) + b % NT + lane / V * NT;
+                        at[o] = sl.start + v * V + lane % V;
+                        if (v < sl.nv && at[o] >= 0 && at[o] < sl.vocab) z[o] = widen(sl.row[at[o]]);
                     }
                 }
+#pragma unroll
+                for (int o = 0; o < kAhead; ++o)
+                    if (z[o] >= reach) {
+                        const int to = atomicAdd(&count[1], 1);
+                        if (to < kCap) cand[to] = order_key(z[o], at[o]);
+                    }
             }
             __syncthreads();
             n = count[1];
