@@ -1,9 +1,9 @@
 // Layer norm, forward and backward.
 //
-// A row is held in registers: a group of THREADS threads (a warp, or a whole block) has N elements
-// of it each, loaded once, so mean, squared deviations and output come from one read.  Elements
-// are loaded in units of W consecutive ones: W elements of 16 bytes where every row starts on a
-// multiple of 16 bytes (and the row is a whole number of units), else single elements.
+// A row is held in registers: a group of threads has 8 or 16 elements of it each, loaded once,
+// so mean, squared deviations and output come from one read.  Elements are loaded in units of W
+// consecutive ones: 16 bytes where every row starts on a multiple of 16 bytes and is a whole
+// number of units, else single elements.
 #include "elements.cuh"
 
 namespace cdadam {
@@ -69,88 +69,180 @@ __device__ __forceinline__ void parameters(const AnyVec &v, bool wide4, int64_t 
 }
 __device__ __forceinline__ bool is_wide4(const AnyVec &v) { return v.type == 0 && ((uintptr_t)v.p & 15) == 0; }
 
-// Sum over a row's threads, the same in each: a warp's lanes, or the block (`sh`: 32 floats that
-// nothing else uses before the next barrier).
+// ---------------------------------------------------------------------------------------------
+// THREADS threads of a block (whole warps) work on a row; a block of BT threads has BT / THREADS
+// such groups.  Sums over a group: within warps by shuffles, then through shared memory behind a
+// barrier of the group's own.  `slot` has to alternate from one sum of a group to the next.
+// ---------------------------------------------------------------------------------------------
 template <int THREADS>
-__device__ __forceinline__ float row_sum(float v, float *sh)
+__device__ __forceinline__ void group_barrier(int group)
 {
-    return THREADS == 32 ? warp_sum(v) : block_sum_all<THREADS < 32 ? 32 : THREADS>(v, sh);
-}
-template <int THREADS>
-__device__ __forceinline__ float2 row_sum2(float a, float b, float2 *sh)
-{
-    a = warp_sum(a);
-    b = warp_sum(b);
-    if (THREADS == 32) return make_float2(a, b);
-    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = make_float2(a, b);
-    __syncthreads();
-    const int lane = threadIdx.x & 31;
-    const float2 v = lane < THREADS / 32 ? sh[lane] : make_float2(0.0f, 0.0f);
-    return make_float2(warp_sum(v.x), warp_sum(v.y));
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(THREADS) : "memory");
 }
 
-// ---------------------------------------------------------------------------------------------
-// Forward.  THREADS = 32: a block of 256 threads has eight rows; else a block has one.  U units of W
-// elements a thread.
-// ---------------------------------------------------------------------------------------------
-template <int THREADS> constexpr int kBlockOf = THREADS == 32 ? 256 : THREADS;
+template <int THREADS>
+__device__ __forceinline__ float group_sum(float v, float *slot, int group)
+{
+    constexpr int N = THREADS / 32;
+    v = warp_sum(v);
+    if (N == 1) return v;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32 % N;
+    if (lane == 0) slot[warp] = v;
+    group_barrier<THREADS>(group);
+    if (N <= 4) {
+        v = slot[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) v += slot[i];
+        return v;
+    }
+    v = slot[lane % N];
+#pragma unroll
+    for (int d = N / 2; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
 
+// Two sums at once: after the first exchange the lower half of a warp carries one, the upper half
+// the other.
+template <int THREADS>
+__device__ __forceinline__ float2 group_sum2(float a, float b, float2 *slot, int group)
+{
+    constexpr int N = THREADS / 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32 % N;
+    const bool upper = lane & 16;
+    float v = (upper ? b : a) + __shfl_xor_sync(0xffffffffu, upper ? a : b, 16);
+#pragma unroll
+    for (int d = 8; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    if (N == 1) return make_float2(__shfl_sync(0xffffffffu, v, 0), __shfl_sync(0xffffffffu, v, 16));
+    float *at = reinterpret_cast<float *>(slot);
+    if ((lane & 15) == 0) at[2 * warp + (upper ? 1 : 0)] = v;
+    group_barrier<THREADS>(group);
+    if (N <= 4) {
+        float2 s = slot[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) s = add2(s, slot[i]);
+        return s;
+    }
+    v = at[2 * (lane % N) + (upper ? 1 : 0)];       // N is 8 or 16: both halves of the warp cover all warps
+#pragma unroll
+    for (int d = (N > 16 ? 16 : N) / 2; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return make_float2(__shfl_sync(0xffffffffu, v, 0), __shfl_sync(0xffffffffu, v, 16));
+}
+
+// What a thread holds of a row: U units of W elements, N = U W, as N / 2 pairs when widened.
 template <typename T, int W, int U, int THREADS>
-__global__ void __launch_bounds__(kBlockOf<THREADS>) k_norm(NormForward a)
-{
-    __shared__ float sh[2][32];
-    const int t = threadIdx.x % THREADS;
-    const int64_t row = (int64_t)blockIdx.x * (kBlockOf<THREADS> / THREADS) + threadIdx.x / THREADS;
-    if (THREADS == 32 && row >= a.rows) return;
-    const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
-    const int cols = (int)a.cols;
+struct Held {
+    static constexpr int N = U * W;
     Unit<T, W> u[U];
+    __device__ __forceinline__ void load(const T *row, int t, int cols)
+    {
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const int j = (t + i * THREADS) * W;
-        if (j < cols) u[i].load(x + j);
-        else u[i].zero();
-    }
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        float f[W];
-        u[i].wide(f);
-#pragma unroll
-        for (int e = 0; e < W; ++e) s += f[e];
-    }
-    const float mean = row_sum<THREADS>(s, sh[0]) / (float)cols;
-    s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        float f[W];
-        u[i].wide(f);
-        const bool in = (t + i * THREADS) * W < cols;
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-            const float c = in ? f[e] - mean : 0.0f;
-            s = fmaf(c, c, s);
+        for (int i = 0; i < U; ++i) {
+            const int j = (t + i * THREADS) * W;
+            if (j < cols) u[i].load(row + j);
+            else u[i].zero();
         }
     }
-    const float rstd = 1.0f / sqrtf(row_sum<THREADS>(s, sh[1]) / (float)cols + a.eps);
-    T *y = static_cast<T *>(a.y) + row * a.y_stride;
-    const bool w4 = is_wide4(a.weight), b4 = is_wide4(a.bias);
+    __device__ __forceinline__ void wide(float2 (&f)[N / 2]) const
+    {
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const int j = (t + i * THREADS) * W;
-        if (j < cols) {
-            float f[W], w[W], b[W];
-            u[i].wide(f);
-            parameters<W>(a.weight, w4, j, 1.0f, w);
-            parameters<W>(a.bias, b4, j, 0.0f, b);
+        for (int i = 0; i < U; ++i) {
+            float g[W];
+            u[i].wide(g);
 #pragma unroll
-            for (int e = 0; e < W; ++e) f[e] = fmaf((f[e] - mean) * rstd, w[e], b[e]);
-            Unit<T, W>::store(y + j, f);
+            for (int e = 0; e < W; ++e) (((i * W + e) & 1) ? f[(i * W + e) / 2].y : f[(i * W + e) / 2].x) = g[e];
         }
     }
-    if (t == 0) {
-        if (a.mean) a.mean[row] = mean;
-        if (a.rstd) a.rstd[row] = rstd;
+    static __device__ __forceinline__ void store(T *row, int t, int cols, const float2 (&f)[N / 2])
+    {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int j = (t + i * THREADS) * W;
+            if (j < cols) {
+                float g[W];
+#pragma unroll
+                for (int e = 0; e < W; ++e) g[e] = ((i * W + e) & 1) ? f[(i * W + e) / 2].y : f[(i * W + e) / 2].x;
+                Unit<T, W>::store(row + j, g);
+            }
+        }
+    }
+    static __device__ __forceinline__ void params(const AnyVec &v, int t, int cols, float absent, float2 (&f)[N / 2])
+    {
+        const bool wide4 = is_wide4(v);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int j = (t + i * THREADS) * W;
+            float g[W];
+#pragma unroll
+            for (int e = 0; e < W; ++e) g[e] = 0.0f;
+            if (j < cols) parameters<W>(v, wide4, j, absent, g);
+#pragma unroll
+            for (int e = 0; e < W; ++e) (((i * W + e) & 1) ? f[(i * W + e) / 2].y : f[(i * W + e) / 2].x) = g[e];
+        }
+    }
+    // whether pair p's elements are columns of the row (N / 2 pairs; both of a pair when W > 1)
+    static __device__ __forceinline__ bool in(int i, int t, int cols) { return (t + i / W * THREADS) * W + i % W < cols; }
+};
+
+// ---------------------------------------------------------------------------------------------
+// Forward.  Every group takes rows at a distance of all groups, the next row on its way while one
+// is normalised.  KEEP: the parameters stay in registers (read for every row, 8 bytes of them
+// beside 4 of data, they took most of the time: 20000 x 4096 bf16 82 us); rows of more than 8192
+// columns leave no registers for them and for the next row.
+// ---------------------------------------------------------------------------------------------
+template <typename T, int W, int U, int THREADS, int BT, int PER_SM, bool KEEP>
+__global__ void __launch_bounds__(BT, PER_SM) k_norm(NormForward a)
+{
+    typedef Held<T, W, U, THREADS> H;
+    constexpr int N = H::N, GROUPS = BT / THREADS;
+    constexpr bool AHEAD = KEEP;
+    __shared__ float sh[GROUPS][2][THREADS / 32];
+    const int t = threadIdx.x % THREADS, group = threadIdx.x / THREADS, cols = (int)a.cols;
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    int64_t row = (int64_t)blockIdx.x * GROUPS + group;
+    const T *x = static_cast<const T *>(a.x);
+    H h, ahead;
+    float2 w[KEEP ? N / 2 : 1], b[KEEP ? N / 2 : 1];
+    if (row < a.rows) h.load(x + row * a.x_stride, t, cols);
+    if constexpr (KEEP) {
+        H::params(a.weight, t, cols, 1.0f, w);
+        H::params(a.bias, t, cols, 0.0f, b);
+    }
+    const float over = 1.0f / (float)cols;
+    for (; row < a.rows; row += step) {
+        if (AHEAD && row + step < a.rows) ahead.load(x + (row + step) * a.x_stride, t, cols);
+        float2 f[N / 2], s = both(0.0f);
+        h.wide(f);
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) s = add2(s, f[i]);
+        const float mean = group_sum<THREADS>(s.x + s.y, sh[group][0], group) * over;
+        s = both(0.0f);
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            f[i] = add2(f[i], both(-mean));
+            if (!H::in(2 * i, t, cols)) f[i].x = 0.0f;
+            if (!H::in(2 * i + 1, t, cols)) f[i].y = 0.0f;
+            s = fma2(f[i], f[i], s);
+        }
+        const float rstd = 1.0f / sqrtf(fmaf(group_sum<THREADS>(s.x + s.y, sh[group][1], group), over, a.eps));
+        if constexpr (KEEP) {
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) f[i] = fma2(mul2(f[i], both(rstd)), w[i], b[i]);
+        } else {
+            float2 p[N / 2];
+            H::params(a.weight, t, cols, 1.0f, p);
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) f[i] = mul2(mul2(f[i], both(rstd)), p[i]);
+            H::params(a.bias, t, cols, 0.0f, p);
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) f[i] = add2(f[i], p[i]);
+        }
+        H::store(static_cast<T *>(a.y) + row * a.y_stride, t, cols, f);
+        if (t == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        if (AHEAD) h = ahead;
+        else if (row + step < a.rows) h.load(x + (row + step) * a.x_stride, t, cols);
     }
 }
 
@@ -217,129 +309,91 @@ __device__ __forceinline__ void leave_sums(const NormBackward &a, int64_t g, int
     }
 }
 
-template <typename T, int W, int U, int THREADS>
-__global__ void __launch_bounds__(kBlockOf<THREADS>) k_norm_backward(NormBackward a, int blocks)
+template <typename T, int W, int U, int THREADS, int BT, int PER_SM>
+__global__ void __launch_bounds__(BT, PER_SM) k_norm_backward(NormBackward a, int blocks)
 {
-    constexpr int BT = kBlockOf<THREADS>, ROWS = BT / THREADS;
-    constexpr bool AHEAD = W > 1 ? U <= 2 : U <= 8;     // registers for the next row
-    extern __shared__ __align__(16) float wide_w[];     // the weight, binary32; at the end the block's sums
-    __shared__ float2 sh[2][32];
-    const int t = threadIdx.x % THREADS, sub = threadIdx.x / THREADS, cols = (int)a.cols;
+    typedef Held<T, W, U, THREADS> H;
+    constexpr int N = H::N, GROUPS = BT / THREADS;
+    extern __shared__ __align__(16) float sums[];       // GROUPS > 1: the block's sums, 2 x cols
+    __shared__ float2 sh[GROUPS][2][THREADS / 32];
+    const int t = threadIdx.x % THREADS, group = threadIdx.x / THREADS, cols = (int)a.cols;
     const int64_t per = a.rows / a.groups, first = blockIdx.y * per, end = first + per;
-    for (int j = threadIdx.x; j < (cols + 3) / 4 * 4; j += BT) wide_w[j] = a.weight.p && j < cols ? any_at(a.weight, j) : 1.0f;
-    __syncthreads();
     const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
-    float aw[U][W], ab[U][W];
+    float2 aw[N / 2], ab[N / 2], w[N / 2];
 #pragma unroll
-    for (int i = 0; i < U; ++i)
-#pragma unroll
-        for (int e = 0; e < W; ++e) aw[i][e] = ab[i][e] = 0.0f;
+    for (int i = 0; i < N / 2; ++i) aw[i] = ab[i] = both(0.0f);
 
-    Unit<T, W> ux[U], ud[U], nx[AHEAD ? U : 1], nd[AHEAD ? U : 1];
-    auto fetch = [&](int64_t row, Unit<T, W> *px, Unit<T, W> *pd) {
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int j = (t + i * THREADS) * W;
-            if (j < cols) {
-                px[i].load(x + row * a.x_stride + j);
-                pd[i].load(dy + row * a.dy_stride + j);
-            } else {
-                px[i].zero();
-                pd[i].zero();
-            }
-        }
-    };
-    const int64_t step = (int64_t)blocks * ROWS;
-    int64_t row = first + (int64_t)blockIdx.x * ROWS + sub;
+    H hx, hd, nx, nd;
+    const int64_t step = (int64_t)blocks * GROUPS;
+    int64_t row = first + (int64_t)blockIdx.x * GROUPS + group;
     float mean = 0.0f, rstd = 0.0f;
-    if (row < end) {
-        fetch(row, ux, ud);
-        mean = a.mean[row];
-        rstd = a.rstd[row];
-    }
+    auto fetch = [&](int64_t r, H &px, H &pd, float &m, float &s) {
+        px.load(x + r * a.x_stride, t, cols);
+        pd.load(dy + r * a.dy_stride, t, cols);
+        m = a.mean[r];
+        s = a.rstd[r];
+    };
+    if (row < end) fetch(row, hx, hd, mean, rstd);
+    H::params(a.weight, t, cols, 1.0f, w);
+    const float over = 1.0f / (float)cols;
     for (int flip = 0; row < end; row += step, flip ^= 1) {
         float nmean = 0.0f, nrstd = 0.0f;
-        if (AHEAD && row + step < end) {
-            fetch(row + step, nx, nd);
-            nmean = a.mean[row + step];
-            nrstd = a.rstd[row + step];
-        }
-        float s1 = 0.0f, s2 = 0.0f;
+        if (row + step < end) fetch(row + step, nx, nd, nmean, nrstd);
+        float2 s1 = both(0.0f), s2 = both(0.0f), fx[N / 2], fd[N / 2];
+        hx.wide(fx);
+        hd.wide(fd);
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int j = (t + i * THREADS) * W;
-            float fx[W], fd[W];
-            ux[i].wide(fx);
-            ud[i].wide(fd);
-#pragma unroll
-            for (int e = 0; e < W; ++e) {
-                const float xh = (fx[e] - mean) * rstd, h = fd[e] * (j < cols ? wide_w[j + e] : 0.0f);
-                s1 += h;
-                s2 = fmaf(h, xh, s2);
-                aw[i][e] = fmaf(fd[e], xh, aw[i][e]);
-                ab[i][e] += fd[e];
-            }
+        for (int i = 0; i < N / 2; ++i) {
+            const float2 xh = mul2(add2(fx[i], both(-mean)), both(rstd)), h = mul2(fd[i], w[i]);
+            s1 = add2(s1, h);
+            s2 = fma2(h, xh, s2);
+            aw[i] = fma2(fd[i], xh, aw[i]);
+            ab[i] = add2(ab[i], fd[i]);
         }
         if (a.dx) {
-            const float2 s = row_sum2<THREADS>(s1, s2, sh[flip]);
-            const float c1 = s.x / (float)cols, c2 = s.y / (float)cols;
-            T *dx = static_cast<T *>(a.dx) + row * a.dx_stride;
+            const float2 s = group_sum2<THREADS>(s1.x + s1.y, s2.x + s2.y, sh[group][flip], group);
+            const float2 c1 = both(-s.x * over), c2 = both(-s.y * over);
+            hx.wide(fx);                                // widened again rather than kept: registers
+            hd.wide(fd);
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int j = (t + i * THREADS) * W;
-                if (j < cols) {
-                    float fx[W], fd[W];
-                    ux[i].wide(fx);
-                    ud[i].wide(fd);
-#pragma unroll
-                    for (int e = 0; e < W; ++e) {
-                        const float xh = (fx[e] - mean) * rstd, h = fd[e] * wide_w[j + e];
-                        fx[e] = rstd * (h - c1 - xh * c2);
-                    }
-                    Unit<T, W>::store(dx + j, fx);
-                }
+            for (int i = 0; i < N / 2; ++i) {
+                const float2 xh = mul2(add2(fx[i], both(-mean)), both(rstd));
+                const float2 h = fma2(fd[i], w[i], c1);
+                fx[i] = mul2(fma2(xh, c2, h), both(rstd));
             }
+            H::store(static_cast<T *>(a.dx) + row * a.dx_stride, t, cols, fx);
         }
-        if (AHEAD) {
-#pragma unroll
-            for (int i = 0; i < U; ++i) { ux[i] = nx[i]; ud[i] = nd[i]; }
-            mean = nmean;
-            rstd = nrstd;
-        } else if (row + step < end) {
-            fetch(row + step, ux, ud);
-            mean = a.mean[row + step];
-            rstd = a.rstd[row + step];
-        }
+        hx = nx;
+        hd = nd;
+        mean = nmean;
+        rstd = nrstd;
     }
     grid_dep_launch();
     if (!a.dweight && !a.dbias) return;
-    if (ROWS > 1) {
-        float *sw = wide_w, *sb = wide_w + cols;
-        for (int r = 0; r < ROWS; ++r) {
+    if (GROUPS > 1) {
+        for (int r = 0; r < GROUPS; ++r) {
             __syncthreads();
-            if (sub == r) {
+            if (group == r) {
 #pragma unroll
-                for (int i = 0; i < U; ++i)
-#pragma unroll
-                    for (int e = 0; e < W; ++e) {
-                        const int j = (t + i * THREADS) * W + e;
-                        if (j < cols) {
-                            sw[j] = r == 0 ? aw[i][e] : sw[j] + aw[i][e];
-                            sb[j] = r == 0 ? ab[i][e] : sb[j] + ab[i][e];
-                        }
+                for (int i = 0; i < N; ++i) {
+                    const int j = (t + i / W * THREADS) * W + i % W;
+                    if (j < cols) {
+                        const float vw = i & 1 ? aw[i / 2].y : aw[i / 2].x, vb = i & 1 ? ab[i / 2].y : ab[i / 2].x;
+                        sums[j] = r == 0 ? vw : sums[j] + vw;
+                        sums[cols + j] = r == 0 ? vb : sums[cols + j] + vb;
                     }
+                }
             }
         }
         __syncthreads();
-        for (int j = threadIdx.x; j < cols; j += BT) leave_sums(a, blockIdx.y, blocks, j, sw[j], sb[j]);
+        for (int j = threadIdx.x; j < cols; j += BT) leave_sums(a, blockIdx.y, blocks, j, sums[j], sums[cols + j]);
     } else {
 #pragma unroll
-        for (int i = 0; i < U; ++i)
-#pragma unroll
-            for (int e = 0; e < W; ++e) {
-                const int j = (t + i * THREADS) * W + e;
-                if (j < cols) leave_sums(a, blockIdx.y, blocks, j, aw[i][e], ab[i][e]);
-            }
+        for (int i = 0; i < N; ++i) {
+            const int j = (t + i / W * THREADS) * W + i % W;
+            if (j < cols)
+                leave_sums(a, blockIdx.y, blocks, j, i & 1 ? aw[i / 2].y : aw[i / 2].x, i & 1 ? ab[i / 2].y : ab[i / 2].x);
+        }
     }
 }
 
@@ -400,7 +454,7 @@ __global__ void __launch_bounds__(kNormBlock) k_norm_dw(NormBackward a)
 template <typename T>
 __global__ void __launch_bounds__(kLongBlock) k_norm_dx(NormBackward a)
 {
-    __shared__ float2 sh[32];
+    __shared__ float sh[2][32];
     const int64_t row = blockIdx.x;
     const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
     const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride;
@@ -412,8 +466,7 @@ __global__ void __launch_bounds__(kLongBlock) k_norm_dx(NormBackward a)
         s1 += h;
         s2 = fmaf(h, (widen(x[j]) - mean) * rstd, s2);
     }
-    const float2 s = row_sum2<kLongBlock>(s1, s2, sh);
-    const float c1 = s.x / (float)a.cols, c2 = s.y / (float)a.cols;
+    const float c1 = block_sum_all<kLongBlock>(s1, sh[0]) / (float)a.cols, c2 = block_sum_all<kLongBlock>(s2, sh[1]) / (float)a.cols;
     for (int64_t j = threadIdx.x; j < a.cols; j += kLongBlock) {
         const float h = widen(dy[j]) * (a.weight.p ? any_at(a.weight, j) : 1.0f);
         const float xh = (widen(x[j]) - mean) * rstd;
@@ -424,7 +477,8 @@ __global__ void __launch_bounds__(kLongBlock) k_norm_dx(NormBackward a)
 // ---------------------------------------------------------------------------------------------
 // Launches
 // ---------------------------------------------------------------------------------------------
-constexpr int kSums = 2 * 148;          // blocks that leave sums, at most (two for each SM)
+constexpr int kSMs = 148;
+constexpr int kSums = 2 * kSMs;         // blocks that leave sums, at most (two for each SM)
 
 // Blocks that share a group's rows: as many as the GPU holds, no more than there are rows.
 static int blocks_per_group(int64_t rows, int64_t groups)
@@ -446,12 +500,14 @@ static bool aligned(const void *p, int64_t stride, int64_t rows, int size)
     return ((uintptr_t)p & 15) == 0 && (rows <= 1 || stride * size % 16 == 0);
 }
 
-template <typename T, int W, int U, int THREADS>
+template <typename T, int W, int U, int THREADS, int BT, int PER_SM, bool KEEP = true>
 static bool try_forward(const NormForward &a, cudaStream_t st)
 {
     if (a.cols > (int64_t)W * U * THREADS) return false;
-    constexpr int block = kBlockOf<THREADS>, rows = block / THREADS;
-    k_norm<T, W, U, THREADS><<<(unsigned)((a.rows + rows - 1) / rows), block, 0, st>>>(a);
+    constexpr int groups = BT / THREADS;
+    int64_t blocks = (a.rows + groups - 1) / groups;
+    if (blocks > kSMs * PER_SM) blocks = kSMs * PER_SM;
+    k_norm<T, W, U, THREADS, BT, PER_SM, KEEP><<<(unsigned)blocks, BT, 0, st>>>(a);
     return true;
 }
 
@@ -460,28 +516,32 @@ static void forward(const NormForward &a, cudaStream_t st)
 {
     constexpr int W = Vec<T>::n, F = 8 / W;             // binary32 needs twice the units
     if (a.cols % W == 0 && aligned(a.x, a.x_stride, a.rows, sizeof(T)) && aligned(a.y, a.y_stride, a.rows, sizeof(T))) {
-        if (try_forward<T, W, 1 * F, 32>(a, st) || try_forward<T, W, 2 * F, 32>(a, st) || try_forward<T, W, 4 * F, 32>(a, st) ||
-            try_forward<T, W, 2 * F, 128>(a, st) || try_forward<T, W, 4 * F, 128>(a, st) || try_forward<T, W, 4 * F, 256>(a, st) ||
-            try_forward<T, W, 4 * F, 512>(a, st) || try_forward<T, W, 4 * F, 1024>(a, st))
+        if (try_forward<T, W, 1 * F, 32, 512, 2>(a, st) || try_forward<T, W, 1 * F, 64, 512, 2>(a, st) ||
+            try_forward<T, W, 1 * F, 96, 480, 2>(a, st) || try_forward<T, W, 1 * F, 128, 512, 2>(a, st) ||
+            try_forward<T, W, 1 * F, 256, 512, 2>(a, st) || try_forward<T, W, 1 * F, 512, 512, 2>(a, st) ||
+            try_forward<T, W, 2 * F, 512, 512, 1>(a, st) || try_forward<T, W, 2 * F, 1024, 1024, 1, false>(a, st))
             return;
-    } else if (try_forward<T, 1, 8, 32>(a, st) || try_forward<T, 1, 32, 32>(a, st) || try_forward<T, 1, 16, 256>(a, st) ||
-               try_forward<T, 1, 32, 256>(a, st) || try_forward<T, 1, 32, 1024>(a, st)) {
+    } else if (try_forward<T, 1, 8, 32, 512, 2>(a, st) || try_forward<T, 1, 16, 32, 256, 2>(a, st) ||
+               try_forward<T, 1, 16, 64, 256, 2>(a, st) || try_forward<T, 1, 16, 128, 256, 2>(a, st) ||
+               try_forward<T, 1, 16, 256, 256, 2>(a, st) || try_forward<T, 1, 16, 512, 512, 1>(a, st) ||
+               try_forward<T, 1, 16, 1024, 1024, 1, false>(a, st)) {
         return;
     }
     k_norm_long<T><<<(unsigned)a.rows, kLongBlock, 0, st>>>(a);
 }
 
-template <typename T, int W, int U, int THREADS>
+template <typename T, int W, int U, int THREADS, int BT, int PER_SM>
 static bool try_backward(const NormBackward &a, int blocks, cudaStream_t st)
 {
     if (a.cols > (int64_t)W * U * THREADS) return false;
-    constexpr int BT = kBlockOf<THREADS>;
-    const int64_t per = a.rows / a.groups;
-    if (blocks > (per + BT / THREADS - 1) / (BT / THREADS)) blocks = (int)((per + BT / THREADS - 1) / (BT / THREADS));
+    constexpr int groups = BT / THREADS;
+    const int64_t per = a.rows / a.groups, most = (per + groups - 1) / groups;
+    if (PER_SM == 1 && blocks > 1) blocks = (blocks + 1) / 2;
+    if (blocks > most) blocks = (int)most;
     if (blocks < 1) blocks = 1;
-    const size_t smem = ((size_t)a.cols + 3) / 4 * 4 * 4 * (BT > THREADS ? 2 : 1);
-    cudaFuncSetAttribute(k_norm_backward<T, W, U, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    k_norm_backward<T, W, U, THREADS><<<dim3((unsigned)blocks, (unsigned)a.groups), BT, smem, st>>>(a, blocks);
+    const size_t smem = groups > 1 ? (size_t)a.cols * 8 : 0;
+    auto *kernel = k_norm_backward<T, W, U, THREADS, BT, PER_SM>;
+    kernel<<<dim3((unsigned)blocks, (unsigned)a.groups), BT, smem, st>>>(a, blocks);
     if (blocks > 1 && (a.dweight || a.dbias))
         launch_after(k_norm_sums, dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)a.groups), dim3(1024), 0, st, a, blocks);
     return true;
@@ -494,12 +554,14 @@ static void backward(const NormBackward &a, cudaStream_t st)
     const int n = blocks_per_group(a.rows, a.groups);
     if (a.cols % W == 0 && aligned(a.x, a.x_stride, a.rows, sizeof(T)) && aligned(a.dy, a.dy_stride, a.rows, sizeof(T)) &&
         (!a.dx || aligned(a.dx, a.dx_stride, a.rows, sizeof(T)))) {
-        if (try_backward<T, W, 1 * F, 32>(a, n, st) || try_backward<T, W, 3 * F, 32>(a, n, st) ||
-            try_backward<T, W, 1 * F, 256>(a, n, st) || try_backward<T, W, 1 * F, 512>(a, n, st) ||
-            try_backward<T, W, 2 * F, 512>(a, n, st) || try_backward<T, W, 4 * F, 512>(a, n, st))
+        if (try_backward<T, W, 1 * F, 32, 512, 2>(a, n, st) || try_backward<T, W, 1 * F, 64, 512, 2>(a, n, st) ||
+            try_backward<T, W, 1 * F, 96, 480, 2>(a, n, st) || try_backward<T, W, 1 * F, 128, 512, 2>(a, n, st) ||
+            try_backward<T, W, 1 * F, 256, 512, 2>(a, n, st) || try_backward<T, W, 1 * F, 512, 512, 2>(a, n, st) ||
+            try_backward<T, W, 2 * F, 512, 512, 1>(a, n, st))
             return;
-    } else if (try_backward<T, 1, 8, 32>(a, n, st) || try_backward<T, 1, 4, 256>(a, n, st) || try_backward<T, 1, 8, 256>(a, n, st) ||
-               try_backward<T, 1, 8, 512>(a, n, st) || try_backward<T, 1, 16, 512>(a, n, st)) {
+    } else if (try_backward<T, 1, 8, 32, 256, 2>(a, n, st) || try_backward<T, 1, 16, 32, 256, 2>(a, n, st) ||
+               try_backward<T, 1, 16, 64, 256, 2>(a, n, st) || try_backward<T, 1, 16, 128, 256, 2>(a, n, st) ||
+               try_backward<T, 1, 16, 256, 256, 2>(a, n, st) || try_backward<T, 1, 16, 512, 512, 1>(a, n, st)) {
         return;
     }
     if (a.dweight || a.dbias)
