@@ -494,65 +494,51 @@ _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 _INDEX_TYPES = {torch.int32: 0, torch.int64: 1}
 
 
-class _On:
-    """The device and stream a call runs on: the tensors' device, the given stream or the one
-    current there.  What the call allocates belongs to that stream."""
-    __slots__ = ("device", "stream", "guard")
+_FLOAT = (torch.float32,)
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 
-    def __init__(self, device, stream):
-        if device.type != "cuda":
-            raise ValueError("the operators take CUDA tensors")
-        if stream is not None and stream.device != device:
-            raise ValueError("the stream belongs to %s, the tensors to %s" % (stream.device, device))
-        self.device, self.stream, self.guard = device, stream, None
 
-    def __enter__(self):
-        if self.stream is not None:
-            self.guard = torch.cuda.stream(self.stream)
-        elif self.device.index != torch.cuda.current_device():
-            self.guard = torch.cuda.device(self.device)
-        if self.guard is not None:
-            self.guard.__enter__()
-        return (torch.cuda.current_stream() if self.stream is None else self.stream).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _elsewhere(t, stream):
+    """Context of a call that does not run on the current stream of the current device: the
+    tensors' device, the given stream.  What the call allocates then belongs to that stream."""
+    if not t.is_cuda:
+        raise ValueError("the operators take CUDA tensors")
+    if stream is None:
+        return torch.cuda.device(t.device)
+    if stream.device != t.device:
+        raise ValueError("the stream belongs to %s, the tensors to %s" % (stream.device, t.device))
+    return torch.cuda.stream(stream)
 
 
 def _matrix(t, what, device=None, shape=None, dtype=None):
     """(pointer, row stride) of a matrix with adjacent row elements."""
-    if t.dim() != 2 or t.dtype not in _TYPES or (t.shape[1] > 1 and t.stride(1) != 1):
+    stride = t.stride()
+    if len(stride) != 2 or (stride[1] != 1 and t.shape[1] > 1) or t.dtype not in _TYPES:
         raise ValueError("%s must be a matrix of float32, bfloat16 or float16 with adjacent row elements" % what)
-    if device is not None and t.device != device:
-        raise ValueError("%s is on %s, not on %s" % (what, t.device, device))
-    if shape is not None and t.shape != shape:
-        raise ValueError("%s has shape %s, not %s" % (what, tuple(t.shape), tuple(shape)))
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError("%s is %s, not %s" % (what, t.dtype, dtype))
-    return t.data_ptr(), t.stride(0)
+    if device is not None and (t.get_device() != device or t.shape != shape or t.dtype != dtype):
+        raise ValueError("%s is %s %s on %s, not %s %s on device %d"
+                         % (what, tuple(t.shape), t.dtype, t.device, tuple(shape), dtype, device))
+    return t.data_ptr(), stride[0]
 
 
 def _vector(t, what, device, shape, types):
     """Pointer of a contiguous tensor of the given shape and one of the types; None stays None."""
     if t is None:
         return None
-    if t.device != device or t.shape != shape or t.dtype not in types or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous tensor of shape %s on %s of one of the types %s"
+    if t.get_device() != device or t.shape != shape or t.dtype not in types or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous tensor of shape %s on device %d of one of the types %s"
                          % (what, tuple(shape), device, ", ".join(str(v) for v in types)))
     return t.data_ptr()
-
-
-_FLOAT = (torch.float32,)
 
 
 def _parameters(weight, bias, cols, device):
     w = _vector(weight, "weight", device, (cols,), _TYPES)
     b = _vector(bias, "bias", device, (cols,), _TYPES)
-    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+    if w is not None and b is not None and weight.dtype != bias.dtype:
         raise ValueError("weight and bias differ in type")
-    some = weight if weight is not None else bias
-    return w, b, F32 if some is None else _TYPES[some.dtype]
+    return w, b, _TYPES[weight.dtype] if w is not None else F32 if b is None else _TYPES[bias.dtype]
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
@@ -561,20 +547,24 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     instance).  out: (y, mean, rstd) to write into, each may be None: y is then allocated, mean
     and rstd are not computed."""
     px, sx = _matrix(x, "x")
-    device, shape = x.device, x.shape
-    w, b, wt = _parameters(weight, bias, shape[1], device)
-    with _On(device, stream) as st:
-        if out is None:
-            y, mean, rstd = torch.empty(shape, dtype=x.dtype, device=device), *torch.empty(2, shape[0], device=device).unbind(0)
-        else:
-            y, mean, rstd = out
-            if y is None:
-                y = torch.empty(shape, dtype=x.dtype, device=device)
-        py, sy = _matrix(y, "y", device, shape, x.dtype)
-        rows = shape[:1]
-        _check(lib().cdadam_layer_norm(px, sx, w, b, shape[0], shape[1], eps, _TYPES[x.dtype], wt, py, sy,
-                                       _vector(mean, "mean", device, rows, _FLOAT), _vector(rstd, "rstd", device, rows, _FLOAT),
-                                       st))
+    device, shape, dtype = x.get_device(), x.shape, x.dtype
+    if device < 0 or stream is not None or device != _current():
+        with _elsewhere(x, stream):
+            return layer_norm(x, weight, bias, eps, out)
+    rows, cols = shape
+    w, b, wt = _parameters(weight, bias, cols, device)
+    if out is None:
+        y, mean, rstd = torch.empty(shape, dtype=dtype, device=x.device), *torch.empty(2, rows, device=x.device).unbind(0)
+    else:
+        y, mean, rstd = out
+        if y is None:
+            y = torch.empty(shape, dtype=dtype, device=x.device)
+    py, sy = _matrix(y, "y", device, shape, dtype)
+    code = lib().cdadam_layer_norm(px, sx, w, b, rows, cols, eps, _TYPES[dtype], wt, py, sy,
+                                   _vector(mean, "mean", device, (rows,), _FLOAT),
+                                   _vector(rstd, "rstd", device, (rows,), _FLOAT), _raw_stream(device))
+    if code:
+        _check(code)
     return y, mean, rstd
 
 
@@ -585,34 +575,40 @@ def layer_norm_backward(dy, x, weight, mean, rstd, groups=1, accumulate=False, o
     gradient buffer and are added to with accumulate.  workspace: a contiguous CUDA tensor of at
     least layer_norm_workspace(rows, cols, groups) bytes to use instead of allocating one."""
     px, sx = _matrix(x, "x")
-    device, shape = x.device, x.shape
-    pdy, sdy = _matrix(dy, "dy", device, shape, x.dtype)
-    w, _, wt = _parameters(weight, None, shape[1], device)
-    rows, sums = shape[:1], (groups, shape[1])
-    with _On(device, stream) as st:
-        if out is None:
-            if accumulate:
-                raise ValueError("accumulate needs out")
-            dx = torch.empty(shape, dtype=x.dtype, device=device)
-            dweight, dbias = torch.empty((2,) + sums, device=device).unbind(0)
-        else:
-            dx, dweight, dbias = out
-        pdx, sdx = (None, 0) if dx is None else _matrix(dx, "dx", device, shape, x.dtype)
-        pw, sw = (None, 0) if dweight is None else _matrix(dweight, "dweight", device, sums)
-        pb, sb = (None, 0) if dbias is None else _matrix(dbias, "dbias", device, sums)
-        if dweight is not None and dbias is not None and dweight.dtype != dbias.dtype:
-            raise ValueError("dweight and dbias differ in type")
-        some = dweight if dweight is not None else dbias
-        if workspace is None:
-            need = lib().cdadam_layer_norm_workspace(shape[0], shape[1], groups) if some is not None else 0
-            workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-        elif workspace.device != device or not workspace.is_contiguous():
-            raise ValueError("workspace must be a contiguous tensor on %s" % device)
-        _check(lib().cdadam_layer_norm_backward(
-            pdy, sdy, px, sx, w, _vector(mean, "mean", device, rows, _FLOAT), _vector(rstd, "rstd", device, rows, _FLOAT),
-            shape[0], shape[1], groups, _TYPES[x.dtype], wt, F32 if some is None else _TYPES[some.dtype], pdx, sdx, pw, sw,
-            pb, sb, 1 if accumulate else 0, None if workspace is None else workspace.data_ptr(),
-            0 if workspace is None else workspace.numel() * workspace.element_size(), st))
+    device, shape, dtype = x.get_device(), x.shape, x.dtype
+    if device < 0 or stream is not None or device != _current():
+        with _elsewhere(x, stream):
+            return layer_norm_backward(dy, x, weight, mean, rstd, groups, accumulate, out, workspace)
+    rows, cols = shape
+    pdy, sdy = _matrix(dy, "dy", device, shape, dtype)
+    w, _, wt = _parameters(weight, None, cols, device)
+    sums = (groups, cols)
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        dx = torch.empty(shape, dtype=dtype, device=x.device)
+        dweight, dbias = torch.empty((2,) + sums, device=x.device).unbind(0)
+    else:
+        dx, dweight, dbias = out
+    pdx, sdx = (None, 0) if dx is None else _matrix(dx, "dx", device, shape, dtype)
+    some = dweight if dweight is not None else dbias
+    gt = None if some is None else some.dtype
+    pw, sw = (None, 0) if dweight is None else _matrix(dweight, "dweight", device, sums, gt)
+    pb, sb = (None, 0) if dbias is None else _matrix(dbias, "dbias", device, sums, gt)
+    if workspace is None:
+        need = lib().cdadam_layer_norm_workspace(rows, cols, groups) if some is not None else 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+        pws = None if workspace is None else workspace.data_ptr()
+    elif workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on %s" % x.device)
+    else:
+        need, pws = workspace.numel() * workspace.element_size(), workspace.data_ptr()
+    code = lib().cdadam_layer_norm_backward(
+        pdy, sdy, px, sx, w, _vector(mean, "mean", device, (rows,), _FLOAT), _vector(rstd, "rstd", device, (rows,), _FLOAT),
+        rows, cols, groups, _TYPES[dtype], wt, F32 if some is None else _TYPES[gt], pdx, sdx, pw, sw, pb, sb,
+        1 if accumulate else 0, pws, need, _raw_stream(device))
+    if code:
+        _check(code)
     return dx, dweight, dbias
 
 
@@ -627,27 +623,31 @@ def token_logprobs(logits, tokens=None, k=0, temperature=1.0, out=None, stream=N
     or int64, negative = none, or None (the first entry is then None).  out: the five to write
     into, each may be None: not computed.  Ids have the type of tokens (int64 without)."""
     pz, sz = _matrix(logits, "logits")
-    device, shape = logits.device, logits.shape
-    rows = shape[:1]
-    pt = _vector(tokens, "tokens", device, rows, _INDEX_TYPES)
-    with _On(device, stream) as st:
-        if out is None:
-            logprob, entropy, lse = torch.empty(3, shape[0], device=device).unbind(0)
-            if tokens is None:
-                logprob = None
-            ids = torch.empty(shape[0], k, dtype=torch.int64 if tokens is None else tokens.dtype, device=device)
-            top = torch.empty(shape[0], k, device=device)
-        else:
-            logprob, entropy, lse, ids, top = out
-        it = tokens if tokens is not None else ids
-        if tokens is not None and ids is not None and ids.dtype != tokens.dtype:
-            raise ValueError("tokens and ids differ in type")
-        lists = (shape[0], k)
-        _check(lib().cdadam_token_logprobs(
-            pz, sz, pt, shape[0], shape[1], _TYPES[logits.dtype], 1 if it is None else _INDEX_TYPES[it.dtype], temperature, k,
-            _vector(logprob, "logprob", device, rows, _FLOAT), _vector(entropy, "entropy", device, rows, _FLOAT),
-            _vector(lse, "lse", device, rows, _FLOAT), _vector(ids, "ids", device, lists, _INDEX_TYPES),
-            _vector(top, "top", device, lists, _FLOAT), st))
+    device, shape = logits.get_device(), logits.shape
+    if device < 0 or stream is not None or device != _current():
+        with _elsewhere(logits, stream):
+            return token_logprobs(logits, tokens, k, temperature, out)
+    rows, vocab = shape
+    per_row, lists = (rows,), (rows, k)
+    pt = _vector(tokens, "tokens", device, per_row, _INDEX_TYPES)
+    if out is None:
+        logprob, entropy, lse = torch.empty(3, rows, device=logits.device).unbind(0)
+        if tokens is None:
+            logprob = None
+        ids = torch.empty(lists, dtype=torch.int64 if tokens is None else tokens.dtype, device=logits.device)
+        top = torch.empty(lists, device=logits.device)
+    else:
+        logprob, entropy, lse, ids, top = out
+    it = tokens if tokens is not None else ids
+    if tokens is not None and ids is not None and ids.dtype != tokens.dtype:
+        raise ValueError("tokens and ids differ in type")
+    code = lib().cdadam_token_logprobs(
+        pz, sz, pt, rows, vocab, _TYPES[logits.dtype], 1 if it is None else _INDEX_TYPES.get(it.dtype, -1), temperature, k,
+        _vector(logprob, "logprob", device, per_row, _FLOAT), _vector(entropy, "entropy", device, per_row, _FLOAT),
+        _vector(lse, "lse", device, per_row, _FLOAT), _vector(ids, "ids", device, lists, _INDEX_TYPES),
+        _vector(top, "top", device, lists, _FLOAT), _raw_stream(device))
+    if code:
+        _check(code)
     return logprob, entropy, lse, ids, top
 
 
@@ -657,17 +657,21 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, dlogprob=None, de
     and entropy (dentropy per row), from the forward pass's lse and entropy.  out: where to write
     it (may be logits itself)."""
     pz, sz = _matrix(logits, "logits")
-    device, shape = logits.device, logits.shape
-    rows = shape[:1]
-    with _On(device, stream) as st:
-        if out is None:
-            out = torch.empty(shape, dtype=logits.dtype, device=device)
-        po, so = _matrix(out, "out", device, shape, logits.dtype)
-        _check(lib().cdadam_token_logprobs_backward(
-            pz, sz, _vector(tokens, "tokens", device, rows, _INDEX_TYPES), shape[0], shape[1], _TYPES[logits.dtype],
-            1 if tokens is None else _INDEX_TYPES[tokens.dtype], temperature, _vector(lse, "lse", device, rows, _FLOAT),
-            _vector(entropy, "entropy", device, rows, _FLOAT), _vector(dlogprob, "dlogprob", device, rows, _FLOAT),
-            _vector(dentropy, "dentropy", device, rows, _FLOAT), po, so, st))
+    device, shape, dtype = logits.get_device(), logits.shape, logits.dtype
+    if device < 0 or stream is not None or device != _current():
+        with _elsewhere(logits, stream):
+            return token_logprobs_backward(logits, tokens, lse, entropy, dlogprob, dentropy, temperature, out)
+    per_row = (shape[0],)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=logits.device)
+    po, so = _matrix(out, "out", device, shape, dtype)
+    code = lib().cdadam_token_logprobs_backward(
+        pz, sz, _vector(tokens, "tokens", device, per_row, _INDEX_TYPES), shape[0], shape[1], _TYPES[dtype],
+        1 if tokens is None else _INDEX_TYPES[tokens.dtype], temperature, _vector(lse, "lse", device, per_row, _FLOAT),
+        _vector(entropy, "entropy", device, per_row, _FLOAT), _vector(dlogprob, "dlogprob", device, per_row, _FLOAT),
+        _vector(dentropy, "dentropy", device, per_row, _FLOAT), po, so, _raw_stream(device))
+    if code:
+        _check(code)
     return out
 
 
@@ -678,22 +682,25 @@ def distill(logits, teacher_ids, teacher_logprobs, dloss=None, temperature=1.0, 
     count as one further outcome; otherwise the list is renormalised.  out: (loss, dlogits) to
     write into, each may be None: not computed."""
     pz, sz = _matrix(logits, "logits")
-    device, shape = logits.device, logits.shape
-    rows = shape[:1]
-    lists = teacher_ids.shape
+    device, shape, dtype, lists = logits.get_device(), logits.shape, logits.dtype, teacher_ids.shape
     if len(lists) != 2 or lists[0] != shape[0]:
         raise ValueError("teacher_ids has shape %s, not (%d, k)" % (tuple(lists), shape[0]))
+    if device < 0 or stream is not None or device != _current():
+        with _elsewhere(logits, stream):
+            return distill(logits, teacher_ids, teacher_logprobs, dloss, temperature, rest, out)
+    per_row = (shape[0],)
     pi = _vector(teacher_ids, "teacher_ids", device, lists, _INDEX_TYPES)
     pq = _vector(teacher_logprobs, "teacher_logprobs", device, lists, _FLOAT)
-    with _On(device, stream) as st:
-        if out is None:
-            loss = torch.empty(rows, device=device)
-            dz = None if dloss is None else torch.empty(shape, dtype=logits.dtype, device=device)
-        else:
-            loss, dz = out
-        po, so = (None, 0) if dz is None else _matrix(dz, "dlogits", device, shape, logits.dtype)
-        _check(lib().cdadam_distill(
-            pz, sz, pi, pq, shape[0], shape[1], lists[1], _TYPES[logits.dtype], _INDEX_TYPES[teacher_ids.dtype], temperature,
-            1 if rest else 0, _vector(dloss, "dloss", device, rows, _FLOAT), _vector(loss, "loss", device, rows, _FLOAT),
-            po, so, st))
+    if out is None:
+        loss = torch.empty(per_row, device=logits.device)
+        dz = None if dloss is None else torch.empty(shape, dtype=dtype, device=logits.device)
+    else:
+        loss, dz = out
+    po, so = (None, 0) if dz is None else _matrix(dz, "dlogits", device, shape, dtype)
+    code = lib().cdadam_distill(
+        pz, sz, pi, pq, shape[0], shape[1], lists[1], _TYPES[dtype], _INDEX_TYPES[teacher_ids.dtype], temperature,
+        1 if rest else 0, _vector(dloss, "dloss", device, per_row, _FLOAT), _vector(loss, "loss", device, per_row, _FLOAT),
+        po, so, _raw_stream(device))
+    if code:
+        _check(code)
     return loss, dz

@@ -12,7 +12,6 @@
 
 namespace cdadam {
 
-constexpr int kRowBlock = 256;
 constexpr int kMaxList = 128;
 constexpr double kLn2 = 0.693147180559945309417;
 
@@ -529,28 +528,97 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
         }
 }
 
-// One block per row.  dz_i = (g ([i = token] - p_i) - u p_i (log p_i + H)) / T.
-template <typename T>
-__global__ void __launch_bounds__(kRowBlock) k_logprobs_backward(LogprobsBackward a)
+// ---------------------------------------------------------------------------------------------
+// Gradient of log probability and entropy.  With t = z s - lse log2(e), p = 2^t,
+//   dz_i = p (a t + b) (+ g at the token),   a = -u ln2 / T,  b = -(g + u H) / T,
+// one pass over the logits: a block has kGradVecs vectors for each of its threads.  lse log2(e) is
+// taken off in two parts, so that only lse's own rounding is left in t.
+// ---------------------------------------------------------------------------------------------
+constexpr int kGradVecs = 4;
+constexpr float kLost = 16777216.0f;        // |lse| from which binary32 says nothing about p
+
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT) k_logprobs_backward(LogprobsBackward a, int chunks)
 {
-    const int64_t row = blockIdx.x;
-    const T *z = static_cast<const T *>(a.z) + row * a.stride;
-    T *dz = static_cast<T *>(a.dz) + row * a.dz_stride;
-    int64_t token = a.dlogprob ? index_at(a.tokens, row, a.index64) : -1;
-    if (token >= a.vocab) token = -1;
+    constexpr int V = Vec<T>::n;
+    const int64_t row = chunks == 1 ? blockIdx.x : blockIdx.x / (unsigned)chunks;
+    const int chunk = chunks == 1 ? 0 : (int)(blockIdx.x - (unsigned)row * (unsigned)chunks);
+    const Slice<T> sl(a.z, a.stride, row, a.vocab, 0, 0);
+    T *out = static_cast<T *>(a.dz) + row * a.dz_stride;
+    const bool same = (((uintptr_t)out - (uintptr_t)sl.row) & 15) == 0;
+
+    const int64_t at = a.dlogprob ? index_at(a.tokens, row, a.index64) : -1;
+    const int token = at >= 0 && at < a.vocab ? (int)at : -0x40000000;
     const float lse = a.lse[row], g = token >= 0 ? a.dlogprob[row] : 0.0f;
     const float u = a.dentropy ? a.dentropy[row] : 0.0f, H = a.dentropy ? a.entropy[row] : 0.0f;
-    const float s = (float)a.scale2;
-    const bool still = (g == 0.0f && u == 0.0f) || fabsf(lse) >= 16777216.0f;    // no gradient, or none that lse could give
-    const double l2 = (double)lse / kLn2;
-    const float hi = (float)l2, lo = lse == kNegInf ? 0.0f : (float)(l2 - (double)hi);
-    for (int64_t i = threadIdx.x; i < a.vocab; i += kRowBlock) {
-        const float v = widen(z[i]);
-        const float t = fmaf(v, s, -hi) - lo, p = exp2f(t);
-        const float lp = fmaxf(t, -1e4f) * (float)kLn2;
-        float d = -p * fmaf(u, lp + H, g);
-        if (i == token) d += g;
-        dz[i] = narrow<T>(v == kNegInf || still ? 0.0f : d * a.inv_temperature);
+    const bool zero = (g == 0.0f && u == 0.0f) || fabsf(lse) >= kLost;
+    const double l2 = (double)lse * (1.0 / kLn2);
+    const float hi = (float)l2, lo = (float)(l2 - (double)hi), s = (float)a.scale2;
+    const float ca = -u * ((float)kLn2 * a.inv_temperature), cb = -(fmaf(u, H, g)) * a.inv_temperature, cg = g * a.inv_temperature;
+
+    const int v0 = chunk * (NT * kGradVecs) + threadIdx.x;
+    uint4 q[kGradVecs];
+    if (!zero) {
+#pragma unroll
+        for (int i = 0; i < kGradVecs; ++i) {
+            const int v = v0 + i * NT, c = sl.start + v * V;
+            if (v < sl.nv) {
+                if (sl.whole(v)) {
+                    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                                 : "=r"(q[i].x), "=r"(q[i].y), "=r"(q[i].z), "=r"(q[i].w) : "l"(sl.row + c) : "memory");
+                } else {
+                    __align__(16) T e[V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) e[j] = c + j >= 0 && c + j < sl.vocab ? sl.row[c + j] : minus_inf<T>();
+                    q[i] = *reinterpret_cast<uint4 *>(e);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kGradVecs; ++i) {
+        const int v = v0 + i * NT, c = sl.start + v * V;
+        if (v >= sl.nv) break;
+        float2 f[V / 2];
+        if (zero) {
+#pragma unroll
+            for (int j = 0; j < V / 2; ++j) f[j] = both(0.0f);
+        } else {
+            Vec<T>::wide(q[i], f);
+            if (lse != lse) {                       // a row without a distribution
+#pragma unroll
+                for (int j = 0; j < V / 2; ++j) f[j] = make_float2(f[j].x == kNegInf ? 0.0f : NAN, f[j].y == kNegInf ? 0.0f : NAN);
+            } else {
+                const int k = token - c;            // which of the vector's elements is the token
+                float masked = 1.0f;                // 0: the token is masked
+#pragma unroll
+                for (int j = 0; j < V / 2; ++j) {
+                    if (2 * j == k && f[j].x == kNegInf) masked = 0.0f;
+                    if (2 * j + 1 == k && f[j].y == kNegInf) masked = 0.0f;
+                    const float2 t = add2(fma2(f[j], both(s), both(-hi)), both(-lo));
+                    const float2 p = make_float2(exp2_fast(t.x), exp2_fast(t.y));
+                    if (ca == 0.0f) f[j] = mul2(p, both(cb));
+                    else f[j] = mul2(p, fma2(make_float2(fmaxf(t.x, -1e4f), fmaxf(t.y, -1e4f)), both(ca), both(cb)));
+                }
+                if (k >= 0 && k < V) {
+#pragma unroll
+                    for (int j = 0; j < V / 2; ++j) {
+                        if (2 * j == k) f[j].x = fmaf(cg, masked, f[j].x);
+                        if (2 * j + 1 == k) f[j].y = fmaf(cg, masked, f[j].y);
+                    }
+                }
+            }
+        }
+        const uint4 r = Vec<T>::pack(f);
+        if (same && sl.whole(v)) {
+            __stcs(reinterpret_cast<uint4 *>(out + c), r);
+        } else {
+            __align__(16) T e[V];
+            *reinterpret_cast<uint4 *>(e) = r;
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (c + j >= 0 && c + j < sl.vocab) out[c + j] = e[j];
+        }
     }
 }
 
@@ -894,13 +962,32 @@ void launch_distill(const Distill &a, int type, cudaStream_t st)
     else distill<f16>(a, st);
 }
 
+template <typename T>
+static void logprobs_backward(const LogprobsBackward &a, cudaStream_t st)
+{
+    constexpr int V = Vec<T>::n;
+    const int64_t vecs = (a.vocab + 2 * V - 2) / V;
+    const int threads = vecs > 128 * kGradVecs ? 256 : 128;             // short rows in short blocks
+    const int chunks = (int)((vecs + threads * kGradVecs - 1) / (threads * kGradVecs));
+    for_row_blocks(a.rows, chunks, [&](int64_t at, int64_t n) {
+        LogprobsBackward b = a;
+        b.z = static_cast<const T *>(a.z) + at * a.stride;
+        b.dz = static_cast<T *>(a.dz) + at * a.dz_stride;
+        b.tokens = a.tokens ? static_cast<const char *>(a.tokens) + at * (a.index64 ? 8 : 4) : nullptr;
+        b.lse += at;
+        if (a.entropy) b.entropy += at;
+        if (a.dlogprob) b.dlogprob += at;
+        if (a.dentropy) b.dentropy += at;
+        if (threads == 256) k_logprobs_backward<T, 256><<<(unsigned)(n * chunks), 256, 0, st>>>(b, chunks);
+        else k_logprobs_backward<T, 128><<<(unsigned)(n * chunks), 128, 0, st>>>(b, chunks);
+    });
+}
+
 void launch_token_logprobs_backward(const LogprobsBackward &a, int type, cudaStream_t st)
 {
-    const unsigned g = (unsigned)a.rows;
-    if (g == 0) return;
-    if (type == 0) k_logprobs_backward<float><<<g, kRowBlock, 0, st>>>(a);
-    else if (type == 1) k_logprobs_backward<bf16><<<g, kRowBlock, 0, st>>>(a);
-    else k_logprobs_backward<f16><<<g, kRowBlock, 0, st>>>(a);
+    if (type == 0) logprobs_backward<float>(a, st);
+    else if (type == 1) logprobs_backward<bf16>(a, st);
+    else logprobs_backward<f16>(a, st);
 }
 
 }  // namespace cdadam
