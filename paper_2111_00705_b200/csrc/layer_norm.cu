@@ -1,85 +1,92 @@
 // Layer norm, forward and backward.
 //
-// A row is held in registers: a group of threads has 8 or 16 elements of it each, loaded once,
-// so mean, squared deviations and output come from one read.  Elements are loaded in units of W
-// consecutive ones: 16 bytes where every row starts on a multiple of 16 bytes and is a whole
-// number of units, else single elements.
+// Both are bound by memory: a row is read once and its output written once.  An SM runs one block
+// of 768 threads in groups; a group works on a row at a time, every thread on 8 or 16 of its
+// elements.  Rows reach a group through a ring of stages in shared memory, filled by bulk copies
+// that its first thread issues several rows ahead, so that what is on its way from memory does not
+// depend on registers or on where the warps are.  A bulk copy moves whole 16-byte vectors: of a row
+// that starts or ends between two it takes the neighbours' bytes along, and only at the very ends
+// of the matrix, where there are none, the row's last elements are read from memory directly.
+//
+// Elements are taken from the stage in units of W consecutive ones: 16 bytes where every row
+// starts on a multiple of 16 bytes and is a whole number of units, else one by one.
 #include "elements.cuh"
 
 namespace cdadam {
 
 // ---------------------------------------------------------------------------------------------
-// W consecutive elements, as they are in memory.
+// Rows of a matrix on their way through a group's stages.  A stage holds a chunk of up to 32 rows,
+// `pitch` bytes apart, each at its address modulo 16; lane i of the group's first warp issues the
+// copy of row i.
 // ---------------------------------------------------------------------------------------------
-template <typename T, int W> struct Unit;
-
 template <typename T>
-struct Unit<T, 1> {
-    T v;
-    __device__ __forceinline__ void load(const T *p) { v = *p; }
-    __device__ __forceinline__ void zero() { v = narrow<T>(0.0f); }
-    __device__ __forceinline__ void wide(float (&f)[1]) const { f[0] = widen(v); }
-    static __device__ __forceinline__ void store(T *p, const float (&f)[1]) { *p = narrow<T>(f[0]); }
-};
+struct Rows {
+    const T *base;
+    int64_t stride;
+    unsigned rows, near;        // within `near` rows of an end a copy's vectors may reach beyond the matrix
+    int cols;
 
-template <typename T, int W>
-struct Unit {
-    static_assert(W == Vec<T>::n, "16 bytes");
-    uint4 u;
-    __device__ __forceinline__ void load(const T *p)
+    __device__ __forceinline__ Rows(const void *p, int64_t row_stride, unsigned n, int c)
+        : base(static_cast<const T *>(p)), stride(row_stride), rows(n), cols(c)
     {
-        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                     : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p) : "memory");
+        near = stride * (int64_t)sizeof(T) >= 16 ? 1 : stride == 0 ? n : 16;
     }
-    __device__ __forceinline__ void zero() { u = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ void wide(float (&f)[W]) const
+    __device__ __forceinline__ const T *row(unsigned r) const { return base + r * stride; }
+    __device__ __forceinline__ bool edge(unsigned r) const { return r < near || rows - 1 - r < near; }
+    // The whole vectors around row r that lie within the matrix: [lo, hi).
+    __device__ __forceinline__ void window(unsigned r, uintptr_t &lo, uintptr_t &hi) const
     {
-        float2 g[W / 2];
-        Vec<T>::wide(u, g);
-#pragma unroll
-        for (int i = 0; i < W / 2; ++i) { f[2 * i] = g[i].x; f[2 * i + 1] = g[i].y; }
-    }
-    static __device__ __forceinline__ void store(T *p, const float (&f)[W])
-    {
-        float2 g[W / 2];
-#pragma unroll
-        for (int i = 0; i < W / 2; ++i) g[i] = make_float2(f[2 * i], f[2 * i + 1]);
-        const uint4 u = Vec<T>::pack(g);
-        asm volatile("st.global.cs.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w) : "memory");
-    }
-};
-
-// W consecutive parameters as binary32; `wide4`: binary32 parameters that start on 16 bytes.
-template <int W>
-__device__ __forceinline__ void parameters(const AnyVec &v, bool wide4, int64_t j, float absent, float (&f)[W])
-{
-    if (!v.p) {
-#pragma unroll
-        for (int i = 0; i < W; ++i) f[i] = absent;
-    } else if (W >= 4 && wide4) {
-#pragma unroll
-        for (int i = 0; i < W / 4; ++i) {
-            const float4 q = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(v.p) + j) + i);
-            f[4 * i] = q.x; f[(4 * i + 1) % W] = q.y; f[(4 * i + 2) % W] = q.z; f[(4 * i + 3) % W] = q.w;
+        lo = (uintptr_t)row(r) & ~(uintptr_t)15;
+        hi = ((uintptr_t)(row(r) + cols) + 15) & ~(uintptr_t)15;
+        if (edge(r)) {
+            if (lo < (uintptr_t)base) lo += 16;
+            if (hi > (uintptr_t)(row(rows - 1) + cols)) hi -= 16;
+            if (hi < lo) hi = lo;
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < W; ++i) f[i] = any_at(v, j + i);
     }
-}
-__device__ __forceinline__ bool is_wide4(const AnyVec &v) { return v.type == 0 && ((uintptr_t)v.p & 15) == 0; }
+    __device__ __forceinline__ uint32_t bytes(unsigned r) const
+    {
+        uintptr_t lo, hi;
+        window(r, lo, hi);
+        return (uint32_t)(hi - lo);
+    }
+    __device__ __forceinline__ void start(unsigned r, char *to, uint64_t *bar) const
+    {
+        uintptr_t lo, hi;
+        window(r, lo, hi);
+        if (hi > lo)
+            bulk_copy_g2s(to + (lo - ((uintptr_t)row(r) & ~(uintptr_t)15)), reinterpret_cast<const void *>(lo), (uint32_t)(hi - lo), bar);
+    }
+    // Where row r's first element is in the stage.
+    __device__ __forceinline__ const T *find(unsigned r, const char *at) const
+    {
+        return reinterpret_cast<const T *>(at + ((uintptr_t)row(r) & 15));
+    }
+    // Puts into the stage what the copy of row r could not bring; thread t of n.
+    __device__ __forceinline__ void complete(unsigned r, const char *at, int t, int n) const
+    {
+        uintptr_t lo, hi;
+        window(r, lo, hi);
+        T *to = const_cast<T *>(find(r, at));
+        for (int j = t; j < cols; j += n)
+            if ((uintptr_t)(row(r) + j) < lo || (uintptr_t)(row(r) + j) >= hi) to[j] = row(r)[j];
+    }
+};
+
+// Bytes from row to row of a stage.
+__host__ __device__ __forceinline__ int row_pitch(int cols, int size) { return (cols * size + 30) & ~15; }
 
 // ---------------------------------------------------------------------------------------------
-// THREADS threads of a block (whole warps) work on a row; a block of BT threads has BT / THREADS
-// such groups.  Sums over a group: within warps by shuffles, then through shared memory behind a
-// barrier of the group's own.  `slot` has to alternate from one sum of a group to the next.
+// A group: THREADS threads of a block (whole warps).  Sums over it: within warps by shuffles, then
+// through shared memory behind a barrier of the group's own.  `slot` has to alternate from one sum
+// of a group to the next.
 // ---------------------------------------------------------------------------------------------
 template <int THREADS>
 __device__ __forceinline__ void group_barrier(int group)
 {
-    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(THREADS) : "memory");
+    if (THREADS == 32) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(THREADS) : "memory");
 }
-
 template <int THREADS>
 __device__ __forceinline__ float group_sum(float v, float *slot, int group)
 {
@@ -128,122 +135,200 @@ __device__ __forceinline__ float2 group_sum2(float a, float b, float2 *slot, int
     return make_float2(__shfl_sync(0xffffffffu, v, 0), __shfl_sync(0xffffffffu, v, 16));
 }
 
-// What a thread holds of a row: U units of W elements, N = U W, as N / 2 pairs when widened.
-template <typename T, int W, int U, int THREADS>
-struct Held {
-    static constexpr int N = U * W;
-    Unit<T, W> u[U];
-    __device__ __forceinline__ void load(const T *row, int t, int cols)
+
+// ---------------------------------------------------------------------------------------------
+// A thread's N elements of a row, in STEPS steps of E (E / 2 pairs).  W > 1: a step is a unit, unit k
+// of thread t starts at column (t + k THREADS) W.  W = 1: a step is 8 single elements, element e of
+// step k is column t + (8 k + e) THREADS.  With N = 16 a launch has more than 8 THREADS columns, so
+// that the first half of a thread's elements needs no check.
+// ---------------------------------------------------------------------------------------------
+template <typename T, int W, int N_, int THREADS>
+struct Mine {
+    static constexpr int N = N_, E = W > 1 ? W : 8, STEPS = N / E, P = E / 2, SURE = N == 16 ? 8 : 0;
+    static __device__ __forceinline__ int column(int k, int e, int t)
     {
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int j = (t + i * THREADS) * W;
-            if (j < cols) u[i].load(row + j);
-            else u[i].zero();
-        }
+        return W > 1 ? (t + k * THREADS) * W + e : t + (k * E + e) * THREADS;
     }
-    __device__ __forceinline__ void wide(float2 (&f)[N / 2]) const
+    static __device__ __forceinline__ bool in(int k, int e, int t, int cols)
     {
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-            float g[W];
-            u[i].wide(g);
-#pragma unroll
-            for (int e = 0; e < W; ++e) (((i * W + e) & 1) ? f[(i * W + e) / 2].y : f[(i * W + e) / 2].x) = g[e];
-        }
+        return k * E + e < SURE || column(k, W > 1 ? 0 : e, t) < cols;
     }
-    static __device__ __forceinline__ void store(T *row, int t, int cols, const float2 (&f)[N / 2])
+    // From the stage; 0 beyond the row.
+    static __device__ __forceinline__ void load(const T *staged, int k, int t, int cols, float2 (&f)[P])
     {
+        if constexpr (W > 1) {
+            uint4 u = make_uint4(0, 0, 0, 0);
+            if (in(k, 0, t, cols)) u = *reinterpret_cast<const uint4 *>(staged + column(k, 0, t));
+            Vec<T>::wide(u, f);
+        } else {
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int j = (t + i * THREADS) * W;
-            if (j < cols) {
-                float g[W];
-#pragma unroll
-                for (int e = 0; e < W; ++e) g[e] = ((i * W + e) & 1) ? f[(i * W + e) / 2].y : f[(i * W + e) / 2].x;
-                Unit<T, W>::store(row + j, g);
+            for (int e = 0; e < E; ++e) {
+                const float v = in(k, e, t, cols) ? widen(staged[column(k, e, t)]) : 0.0f;
+                if (e & 1) f[e / 2].y = v; else f[e / 2].x = v;
             }
         }
     }
-    static __device__ __forceinline__ void params(const AnyVec &v, int t, int cols, float absent, float2 (&f)[N / 2])
+    static __device__ __forceinline__ void store(T *row, int k, int t, int cols, const float2 (&f)[P])
     {
-        const bool wide4 = is_wide4(v);
+        if constexpr (W > 1) {
+            if (in(k, 0, t, cols)) __stcs(reinterpret_cast<uint4 *>(row + column(k, 0, t)), Vec<T>::pack(f));
+        } else {
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int j = (t + i * THREADS) * W;
-            float g[W];
-#pragma unroll
-            for (int e = 0; e < W; ++e) g[e] = 0.0f;
-            if (j < cols) parameters<W>(v, wide4, j, absent, g);
-#pragma unroll
-            for (int e = 0; e < W; ++e) (((i * W + e) & 1) ? f[(i * W + e) / 2].y : f[(i * W + e) / 2].x) = g[e];
+            for (int e = 0; e < E; ++e)
+                if (in(k, e, t, cols)) row[column(k, e, t)] = narrow<T>(e & 1 ? f[e / 2].y : f[e / 2].x);
         }
     }
-    // whether pair p's elements are columns of the row (N / 2 pairs; both of a pair when W > 1)
-    static __device__ __forceinline__ bool in(int i, int t, int cols) { return (t + i / W * THREADS) * W + i % W < cols; }
 };
 
-// ---------------------------------------------------------------------------------------------
-// Forward.  Every group takes rows at a distance of all groups, the next row on its way while one
-// is normalised.  KEEP: the parameters stay in registers (read for every row, 8 bytes of them
-// beside 4 of data, they took most of the time: 20000 x 4096 bf16 82 us); rows of more than 8192
-// columns leave no registers for them and for the next row.
-// ---------------------------------------------------------------------------------------------
-template <typename T, int W, int U, int THREADS, int BT, int PER_SM, bool KEEP>
-__global__ void __launch_bounds__(BT, PER_SM) k_norm(NormForward a)
-{
-    typedef Held<T, W, U, THREADS> H;
-    constexpr int N = H::N, GROUPS = BT / THREADS;
-    constexpr bool AHEAD = KEEP;
-    __shared__ float sh[GROUPS][2][THREADS / 32];
-    const int t = threadIdx.x % THREADS, group = threadIdx.x / THREADS, cols = (int)a.cols;
-    const int64_t step = (int64_t)gridDim.x * GROUPS;
-    int64_t row = (int64_t)blockIdx.x * GROUPS + group;
-    const T *x = static_cast<const T *>(a.x);
-    H h, ahead;
-    float2 w[KEEP ? N / 2 : 1], b[KEEP ? N / 2 : 1];
-    if (row < a.rows) h.load(x + row * a.x_stride, t, cols);
-    if constexpr (KEEP) {
-        H::params(a.weight, t, cols, 1.0f, w);
-        H::params(a.bias, t, cols, 0.0f, b);
-    }
-    const float over = 1.0f / (float)cols;
-    for (; row < a.rows; row += step) {
-        if (AHEAD && row + step < a.rows) ahead.load(x + (row + step) * a.x_stride, t, cols);
-        float2 f[N / 2], s = both(0.0f);
-        h.wide(f);
-#pragma unroll
-        for (int i = 0; i < N / 2; ++i) s = add2(s, f[i]);
-        const float mean = group_sum<THREADS>(s.x + s.y, sh[group][0], group) * over;
-        s = both(0.0f);
-#pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            f[i] = add2(f[i], both(-mean));
-            if (!H::in(2 * i, t, cols)) f[i].x = 0.0f;
-            if (!H::in(2 * i + 1, t, cols)) f[i].y = 0.0f;
-            s = fma2(f[i], f[i], s);
+// Parameters, widened, in shared memory, 0 beyond the row: of units of 8 the first four floats in one
+// plane, the last four in another, so that a warp's 16-byte reads are adjacent.
+template <typename M, int W, int THREADS>
+struct Planes {
+    static constexpr int floats = M::N * THREADS, plane = floats / 2;
+    template <int BT>
+    static __device__ __forceinline__ void fill(float *p, const AnyVec &v, int cols, float absent)
+    {
+        for (int j = threadIdx.x; j < floats; j += BT) {
+            const float f = j >= cols ? 0.0f : v.p ? any_at(v, j) : absent;
+            if (W == 8) p[(j & 4 ? plane : 0) + (j >> 3) * 4 + (j & 3)] = f;
+            else p[j] = f;
         }
-        const float rstd = 1.0f / sqrtf(fmaf(group_sum<THREADS>(s.x + s.y, sh[group][1], group), over, a.eps));
-        if constexpr (KEEP) {
+    }
+    static __device__ __forceinline__ void load(const float *p, int k, int t, float2 (&f)[M::P])
+    {
+        if constexpr (W > 1) {
 #pragma unroll
-            for (int i = 0; i < N / 2; ++i) f[i] = fma2(mul2(f[i], both(rstd)), w[i], b[i]);
+            for (int h = 0; h < W / 4; ++h) {
+                const float4 q = *reinterpret_cast<const float4 *>(p + h * plane + (t + k * THREADS) * 4);
+                f[2 * h] = make_float2(q.x, q.y);
+                f[2 * h + 1] = make_float2(q.z, q.w);
+            }
         } else {
-            float2 p[N / 2];
-            H::params(a.weight, t, cols, 1.0f, p);
 #pragma unroll
-            for (int i = 0; i < N / 2; ++i) f[i] = mul2(mul2(f[i], both(rstd)), p[i]);
-            H::params(a.bias, t, cols, 0.0f, p);
-#pragma unroll
-            for (int i = 0; i < N / 2; ++i) f[i] = add2(f[i], p[i]);
+            for (int e = 0; e < M::E; ++e) {
+                const float v = p[M::column(k, e, t)];
+                if (e & 1) f[e / 2].y = v; else f[e / 2].x = v;
+            }
         }
-        H::store(static_cast<T *>(a.y) + row * a.y_stride, t, cols, f);
-        if (t == 0) {
-            if (a.mean) a.mean[row] = mean;
-            if (a.rstd) a.rstd[row] = rstd;
-        }
-        if (AHEAD) h = ahead;
-        else if (row + step < a.rows) h.load(x + (row + step) * a.x_stride, t, cols);
     }
+};
+
+// Rows of a chunk, stages of a ring, bytes from row to row: the shape of a launch's rings.
+struct Ring {
+    int rows, stages, pitch;
+};
+constexpr int kMaxStages = 6;
+
+// 1 / sqrt(v): the approximation and one Newton step, within 1 ulp or so and a third of the
+// instructions of the correctly rounded quotient and root.
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const float r = rsqrtf(v);
+    return v > 0.0f && r < 3e38f ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Forward.
+// ---------------------------------------------------------------------------------------------
+template <typename T, int W, int N, int THREADS, int BT>
+__global__ void __launch_bounds__(BT, 1) k_norm(NormForward a, Ring ring)
+{
+    typedef Mine<T, W, N, THREADS> M;
+    typedef Planes<M, W, THREADS> PL;
+    constexpr int GROUPS = BT / THREADS;
+    extern __shared__ __align__(16) char smem[];        // weight, bias; the rings
+    __shared__ float sh[GROUPS][2][THREADS / 32];
+    __shared__ uint64_t bars[GROUPS][kMaxStages];
+    const int t = threadIdx.x % THREADS, group = threadIdx.x / THREADS, cols = (int)a.cols;
+    const unsigned rows = (unsigned)a.rows, step = gridDim.x * GROUPS * ring.rows;
+    const Rows<T> x(a.x, a.x_stride, rows, cols);
+    float *const w = reinterpret_cast<float *>(smem), *const b = w + PL::floats;
+    const int stage_bytes = ring.rows * ring.pitch;
+    char *stages = smem + 2 * PL::floats * 4 + group * ring.stages * stage_bytes;
+    const uint32_t row_bytes = cols * (uint32_t)sizeof(T);
+    // the group's first warp: chunk at row r into stage s
+    auto start = [&](unsigned r, int s) {
+        const int n = min((unsigned)ring.rows, rows - r);
+        char *to = stages + s * stage_bytes + t * ring.pitch;
+        if (W > 1) {                                    // rows of whole vectors
+            if (t == 0) mbar_arrive_expect_tx(&bars[group][s], n * row_bytes);
+            __syncwarp();
+            if (t < n) bulk_copy_g2s(to, x.row(r + t), row_bytes, &bars[group][s]);
+            return;
+        }
+        uint32_t sum = t < n ? x.bytes(r + t) : 0;
+        sum = __reduce_add_sync(0xffffffffu, sum);
+        if (t == 0) mbar_arrive_expect_tx(&bars[group][s], sum);
+        __syncwarp();
+        if (t < n) x.start(r + t, to, &bars[group][s]);
+    };
+    unsigned row0 = (blockIdx.x * GROUPS + group) * ring.rows;
+    if (t < 32) {
+        if (t == 0) {
+            for (int i = 0; i < ring.stages; ++i) mbar_init(&bars[group][i], 1);
+            mbar_fence_init();
+        }
+        __syncwarp();
+        for (int i = 0; i < ring.stages; ++i)
+            if (row0 + (uint64_t)i * step < rows) start(row0 + i * step, i);
+    }
+    PL::template fill<BT>(w, a.weight, cols, 1.0f);
+    PL::template fill<BT>(b, a.bias, cols, 0.0f);
+    __syncthreads();
+    const float over = 1.0f / (float)cols;
+    bool late = false;
+    int s = 0, phase = 0;
+    for (; row0 < rows; row0 = row0 + (uint64_t)step < rows ? row0 + step : rows) {
+        late |= !mbar_wait_bounded(&bars[group][s], phase);
+        const int n = min((unsigned)ring.rows, rows - row0);
+        for (int i = 0; i < n; ++i) {
+            const unsigned row = row0 + i;
+            const char *at = stages + s * stage_bytes + i * ring.pitch;
+            const T *staged = W > 1 ? reinterpret_cast<const T *>(at) : x.find(row, at);
+            float2 f[M::STEPS][M::P], v = both(0.0f);
+            if (W == 1 && x.edge(row)) {
+                x.complete(row, at, t, THREADS);
+                group_barrier<THREADS>(group);
+            }
+#pragma unroll
+            for (int k = 0; k < M::STEPS; ++k) M::load(staged, k, t, cols, f[k]);
+#pragma unroll
+            for (int k = 0; k < M::STEPS; ++k)
+#pragma unroll
+                for (int e = 0; e < M::P; ++e) v = add2(v, f[k][e]);
+            const float mean = group_sum<THREADS>(v.x + v.y, sh[group][0], group) * over;
+            if (i == n - 1 && t < 32 && row0 + (uint64_t)ring.stages * step < rows) start(row0 + ring.stages * step, s);   // all have read
+            v = both(0.0f);
+#pragma unroll
+            for (int k = 0; k < M::STEPS; ++k)
+#pragma unroll
+                for (int e = 0; e < M::P; ++e) {
+                    const float2 d = add2(f[k][e], both(-mean));
+                    if (M::in(k, 2 * e + 1, t, cols)) v = fma2(d, d, v);
+                    else if (W == 1 && M::in(k, 2 * e, t, cols)) v.x = fmaf(d.x, d.x, v.x);
+                    f[k][e] = d;
+                }
+            float rstd = inverse_root(fmaf(group_sum<THREADS>(v.x + v.y, sh[group][1], group), over, a.eps));
+            if (late) rstd = NAN;                       // a copy that does not arrive within seconds
+            T *y = static_cast<T *>(a.y) + row * a.y_stride;
+#pragma unroll
+            for (int k = 0; k < M::STEPS; ++k) {
+                float2 pw[M::P], pb[M::P];
+                PL::load(w, k, t, pw);
+                PL::load(b, k, t, pb);
+#pragma unroll
+                for (int e = 0; e < M::P; ++e) f[k][e] = fma2(mul2(f[k][e], both(rstd)), pw[e], pb[e]);
+                M::store(y, k, t, cols, f[k]);
+            }
+            if (t == 0) {
+                if (a.mean) a.mean[row] = mean;
+                if (a.rstd) a.rstd[row] = rstd;
+            }
+        }
+        if (++s == ring.stages) { s = 0; phase ^= 1; }
+    }
+    if (late)                                           // no block leaves with copies in flight
+        for (int i = 0; i < ring.stages; ++i) mbar_wait_bounded(&bars[group][i], i < s ? phase : phase ^ 1);
 }
 
 // Rows too long for the registers of a block: three passes, the later two from L2.
@@ -309,90 +394,158 @@ __device__ __forceinline__ void leave_sums(const NormBackward &a, int64_t g, int
     }
 }
 
-template <typename T, int W, int U, int THREADS, int BT, int PER_SM>
-__global__ void __launch_bounds__(BT, PER_SM) k_norm_backward(NormBackward a, int blocks)
+template <typename T, int W, int N, int THREADS, int BT>
+__global__ void __launch_bounds__(BT, 1) k_norm_backward(NormBackward a, int blocks, Ring ring)
 {
-    typedef Held<T, W, U, THREADS> H;
-    constexpr int N = H::N, GROUPS = BT / THREADS;
-    extern __shared__ __align__(16) float sums[];       // GROUPS > 1: the block's sums, 2 x cols
+    typedef Mine<T, W, N, THREADS> M;
+    typedef Planes<M, W, THREADS> PL;
+    constexpr int GROUPS = BT / THREADS, STEPS = M::STEPS, P = M::P;
+    extern __shared__ __align__(16) char smem[];        // weight; the rings; at the end the groups' sums
     __shared__ float2 sh[GROUPS][2][THREADS / 32];
-    const int t = threadIdx.x % THREADS, group = threadIdx.x / THREADS, cols = (int)a.cols;
-    const int64_t per = a.rows / a.groups, first = blockIdx.y * per, end = first + per;
-    const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
-    float2 aw[N / 2], ab[N / 2], w[N / 2];
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) aw[i] = ab[i] = both(0.0f);
-
-    H hx, hd, nx, nd;
-    const int64_t step = (int64_t)blocks * GROUPS;
-    int64_t row = first + (int64_t)blockIdx.x * GROUPS + group;
-    float mean = 0.0f, rstd = 0.0f;
-    auto fetch = [&](int64_t r, H &px, H &pd, float &m, float &s) {
-        px.load(x + r * a.x_stride, t, cols);
-        pd.load(dy + r * a.dy_stride, t, cols);
-        m = a.mean[r];
-        s = a.rstd[r];
-    };
-    if (row < end) fetch(row, hx, hd, mean, rstd);
-    H::params(a.weight, t, cols, 1.0f, w);
-    const float over = 1.0f / (float)cols;
-    for (int flip = 0; row < end; row += step, flip ^= 1) {
-        float nmean = 0.0f, nrstd = 0.0f;
-        if (row + step < end) fetch(row + step, nx, nd, nmean, nrstd);
-        float2 s1 = both(0.0f), s2 = both(0.0f), fx[N / 2], fd[N / 2];
-        hx.wide(fx);
-        hd.wide(fd);
-#pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            const float2 xh = mul2(add2(fx[i], both(-mean)), both(rstd)), h = mul2(fd[i], w[i]);
-            s1 = add2(s1, h);
-            s2 = fma2(h, xh, s2);
-            aw[i] = fma2(fd[i], xh, aw[i]);
-            ab[i] = add2(ab[i], fd[i]);
-        }
-        if (a.dx) {
-            const float2 s = group_sum2<THREADS>(s1.x + s1.y, s2.x + s2.y, sh[group][flip], group);
-            const float2 c1 = both(-s.x * over), c2 = both(-s.y * over);
-            hx.wide(fx);                                // widened again rather than kept: registers
-            hd.wide(fd);
-#pragma unroll
-            for (int i = 0; i < N / 2; ++i) {
-                const float2 xh = mul2(add2(fx[i], both(-mean)), both(rstd));
-                const float2 h = fma2(fd[i], w[i], c1);
-                fx[i] = mul2(fma2(xh, c2, h), both(rstd));
+    __shared__ uint64_t bars[GROUPS][kMaxStages];
+    const int t = threadIdx.x % THREADS, group = threadIdx.x / THREADS, lane = threadIdx.x & 31, cols = (int)a.cols;
+    const unsigned rows = (unsigned)a.rows, per = rows / (unsigned)a.groups, end = (blockIdx.y + 1) * per;
+    const unsigned step = (unsigned)blocks * GROUPS * ring.rows;
+    const Rows<T> x(a.x, a.x_stride, rows, cols), dy(a.dy, a.dy_stride, rows, cols);
+    float *const w = reinterpret_cast<float *>(smem);
+    const int half = ring.rows * ring.pitch, stage_bytes = 2 * half;
+    const uint32_t row_bytes = cols * (uint32_t)sizeof(T);
+    char *stages = smem + PL::floats * 4 + group * ring.stages * stage_bytes;
+    auto start = [&](unsigned r, int s) {
+        const int n = min((unsigned)ring.rows, end - r);
+        char *to = stages + s * stage_bytes + t * ring.pitch;
+        if (W > 1) {                                    // rows of whole vectors
+            if (t == 0) mbar_arrive_expect_tx(&bars[group][s], 2 * n * row_bytes);
+            __syncwarp();
+            if (t < n) {
+                bulk_copy_g2s(to, x.row(r + t), row_bytes, &bars[group][s]);
+                bulk_copy_g2s(to + half, dy.row(r + t), row_bytes, &bars[group][s]);
             }
-            H::store(static_cast<T *>(a.dx) + row * a.dx_stride, t, cols, fx);
+            return;
         }
-        hx = nx;
-        hd = nd;
-        mean = nmean;
-        rstd = nrstd;
+        uint32_t sum = t < n ? x.bytes(r + t) + dy.bytes(r + t) : 0;
+        sum = __reduce_add_sync(0xffffffffu, sum);
+        if (t == 0) mbar_arrive_expect_tx(&bars[group][s], sum);
+        __syncwarp();
+        if (t < n) {
+            x.start(r + t, to, &bars[group][s]);
+            dy.start(r + t, to + half, &bars[group][s]);
+        }
+    };
+    unsigned row0 = blockIdx.y * per + (blockIdx.x * GROUPS + group) * ring.rows;
+    if (t < 32) {
+        if (t == 0) {
+            for (int i = 0; i < ring.stages; ++i) mbar_init(&bars[group][i], 1);
+            mbar_fence_init();
+        }
+        __syncwarp();
+        for (int i = 0; i < ring.stages; ++i)
+            if (row0 + (uint64_t)i * step < end) start(row0 + i * step, i);
     }
-    grid_dep_launch();
-    if (!a.dweight && !a.dbias) return;
-    if (GROUPS > 1) {
-        for (int r = 0; r < GROUPS; ++r) {
-            __syncthreads();
-            if (group == r) {
+    PL::template fill<BT>(w, a.weight, cols, 1.0f);
+    // lane l of every warp has the statistics of the chunk's row l, a chunk ahead
+    float mean_next = 0.0f, rstd_next = 0.0f;
+    if (row0 < end && lane < ring.rows && row0 + lane < end) { mean_next = a.mean[row0 + lane]; rstd_next = a.rstd[row0 + lane]; }
+    float2 aw[STEPS][P], ab[STEPS][P];
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int j = (t + i / W * THREADS) * W + i % W;
-                    if (j < cols) {
-                        const float vw = i & 1 ? aw[i / 2].y : aw[i / 2].x, vb = i & 1 ? ab[i / 2].y : ab[i / 2].x;
-                        sums[j] = r == 0 ? vw : sums[j] + vw;
-                        sums[cols + j] = r == 0 ? vb : sums[cols + j] + vb;
-                    }
+    for (int k = 0; k < STEPS; ++k)
+#pragma unroll
+        for (int e = 0; e < P; ++e) aw[k][e] = ab[k][e] = both(0.0f);
+    __syncthreads();
+    const float over = 1.0f / (float)cols;
+    bool late = false;
+    int s = 0, phase = 0, flip = 0;
+    while (row0 < end) {
+        const float means = mean_next, rstds = rstd_next;
+        const unsigned next = row0 + (uint64_t)step < end ? row0 + step : end;
+        if (lane < ring.rows && next + lane < end) { mean_next = a.mean[next + lane]; rstd_next = a.rstd[next + lane]; }
+        late |= !mbar_wait_bounded(&bars[group][s], phase);
+        const int n = min((unsigned)ring.rows, end - row0);
+        for (int i = 0; i < n; ++i, flip ^= 1) {
+            const unsigned row = row0 + i;
+            const float mean = __shfl_sync(0xffffffffu, means, i);
+            float rstd = __shfl_sync(0xffffffffu, rstds, i);
+            if (late) rstd = NAN;                       // a copy that does not arrive within seconds
+            const char *at = stages + s * stage_bytes + i * ring.pitch;
+            const T *sx = W > 1 ? reinterpret_cast<const T *>(at) : x.find(row, at);
+            const T *sd = W > 1 ? reinterpret_cast<const T *>(at + half) : dy.find(row, at + half);
+            if (W == 1 && (x.edge(row) || dy.edge(row))) {
+                x.complete(row, at, t, THREADS);
+                dy.complete(row, at + half, t, THREADS);
+                group_barrier<THREADS>(group);
+            }
+            float2 s1 = both(0.0f), s2 = both(0.0f), fx[STEPS][P], fd[STEPS][P];
+#pragma unroll
+            for (int k = 0; k < STEPS; ++k) {
+                float2 pw[P];
+                M::load(sx, k, t, cols, fx[k]);
+                M::load(sd, k, t, cols, fd[k]);
+                PL::load(w, k, t, pw);
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                    const float2 xh = mul2(add2(fx[k][e], both(-mean)), both(rstd)), h = mul2(fd[k][e], pw[e]);
+                    s1 = add2(s1, h);
+                    s2 = fma2(h, xh, s2);
+                    aw[k][e] = fma2(fd[k][e], xh, aw[k][e]);
+                    ab[k][e] = add2(ab[k][e], fd[k][e]);
+                    fx[k][e] = xh;
+                    fd[k][e] = h;
+                }
+            }
+            float2 v = both(0.0f);
+            if (a.dx) v = group_sum2<THREADS>(s1.x + s1.y, s2.x + s2.y, sh[group][flip], group);
+            else group_barrier<THREADS>(group);
+            if (i == n - 1 && t < 32 && row0 + (uint64_t)ring.stages * step < end) start(row0 + ring.stages * step, s);   // all have read
+            if (a.dx) {
+                const float2 c1 = both(-v.x * over), c2 = both(-v.y * over);
+                T *dx = static_cast<T *>(a.dx) + row * a.dx_stride;
+#pragma unroll
+                for (int k = 0; k < STEPS; ++k) {
+#pragma unroll
+                    for (int e = 0; e < P; ++e) fx[k][e] = mul2(fma2(fx[k][e], c2, add2(fd[k][e], c1)), both(rstd));
+                    M::store(dx, k, t, cols, fx[k]);
                 }
             }
         }
-        __syncthreads();
-        for (int j = threadIdx.x; j < cols; j += BT) leave_sums(a, blockIdx.y, blocks, j, sums[j], sums[cols + j]);
-    } else {
+        row0 = next;
+        if (++s == ring.stages) { s = 0; phase ^= 1; }
+    }
+    if (late) {                                                 // no block leaves with copies in flight
+        for (int i = 0; i < ring.stages; ++i) mbar_wait_bounded(&bars[group][i], i < s ? phase : phase ^ 1);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int j = (t + i / W * THREADS) * W + i % W;
-            if (j < cols)
-                leave_sums(a, blockIdx.y, blocks, j, i & 1 ? aw[i / 2].y : aw[i / 2].x, i & 1 ? ab[i / 2].y : ab[i / 2].x);
+        for (int k = 0; k < STEPS; ++k)
+#pragma unroll
+            for (int e = 0; e < P; ++e) aw[k][e] = ab[k][e] = both(NAN);
+    }
+    grid_dep_launch();
+    if (!a.dweight && !a.dbias) return;
+    float *sums = reinterpret_cast<float *>(smem);              // GROUPS x 2 x cols
+    if (GROUPS > 1) __syncthreads();                            // the rings are empty
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k)
+#pragma unroll
+        for (int e = 0; e < M::E; ++e) {
+            const int j = M::column(k, e, t);
+            const float vw = e & 1 ? aw[k][e / 2].y : aw[k][e / 2].x, vb = e & 1 ? ab[k][e / 2].y : ab[k][e / 2].x;
+            if (j < cols) {
+                if (GROUPS > 1) {
+                    sums[(group * 2) * cols + j] = vw;
+                    sums[(group * 2 + 1) * cols + j] = vb;
+                } else {
+                    leave_sums(a, blockIdx.y, blocks, j, vw, vb);
+                }
+            }
+        }
+    if (GROUPS > 1) {
+        __syncthreads();
+        for (int j = threadIdx.x; j < cols; j += BT) {
+            float vw = 0.0f, vb = 0.0f;
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                vw += sums[(g * 2) * cols + j];
+                vb += sums[(g * 2 + 1) * cols + j];
+            }
+            leave_sums(a, blockIdx.y, blocks, j, vw, vb);
         }
     }
 }
@@ -478,7 +631,7 @@ __global__ void __launch_bounds__(kLongBlock) k_norm_dx(NormBackward a)
 // Launches
 // ---------------------------------------------------------------------------------------------
 constexpr int kSMs = 148;
-constexpr int kSums = 2 * kSMs;         // blocks that leave sums, at most (two for each SM)
+constexpr int kSums = kSMs;             // blocks that leave sums, at most
 
 // Blocks that share a group's rows: as many as the GPU holds, no more than there are rows.
 static int blocks_per_group(int64_t rows, int64_t groups)
@@ -500,48 +653,70 @@ static bool aligned(const void *p, int64_t stride, int64_t rows, int size)
     return ((uintptr_t)p & 15) == 0 && (rows <= 1 || stride * size % 16 == 0);
 }
 
-template <typename T, int W, int U, int THREADS, int BT, int PER_SM, bool KEEP = true>
+// Rows in chunks of about 4 KB (one row where it is longer), fewer where that would leave groups
+// without a chunk; two stages to six, until the rings take 160 KB or the shared memory is full.
+static Ring ring_of(int64_t rows, int64_t groups, int pitch, int all_groups_and_matrices, int parameter_bytes)
+{
+    Ring r;
+    r.pitch = pitch;
+    r.rows = pitch >= 4096 ? 1 : 4096 / pitch;
+    if (r.rows > 32) r.rows = 32;
+    if (r.rows > rows / groups) r.rows = rows / groups < 1 ? 1 : (int)(rows / groups);
+    while (r.rows > 1 && r.rows * pitch * all_groups_and_matrices > 80 * 1024) --r.rows;
+    const int bytes = r.rows * pitch * all_groups_and_matrices, room = 216 * 1024 - parameter_bytes,
+              n = (room < 160 * 1024 ? room : 160 * 1024) / bytes;
+    r.stages = n < 2 ? 2 : n > kMaxStages ? kMaxStages : n;
+    return r;
+}
+
+template <typename T, int W, int N, int THREADS, int BT>
 static bool try_forward(const NormForward &a, cudaStream_t st)
 {
-    if (a.cols > (int64_t)W * U * THREADS) return false;
+    if (a.cols > (int64_t)N * THREADS) return false;
     constexpr int groups = BT / THREADS;
-    int64_t blocks = (a.rows + groups - 1) / groups;
-    if (blocks > kSMs * PER_SM) blocks = kSMs * PER_SM;
-    k_norm<T, W, U, THREADS, BT, PER_SM, KEEP><<<(unsigned)blocks, BT, 0, st>>>(a);
+    const int cols = (int)a.cols;
+    const Ring r = ring_of(a.rows, (int64_t)kSMs * groups, row_pitch(cols, sizeof(T)), groups, 2 * N * THREADS * 4);
+    const int64_t need = ((a.rows + r.rows - 1) / r.rows + groups - 1) / groups;
+    const int smem = 2 * N * THREADS * 4 + r.stages * r.rows * r.pitch * groups;
+    auto *kernel = k_norm<T, W, N, THREADS, BT>;
+    cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    kernel<<<(unsigned)(need < kSMs ? need : kSMs), BT, smem, st>>>(a, r);
     return true;
 }
 
 template <typename T>
 static void forward(const NormForward &a, cudaStream_t st)
 {
-    constexpr int W = Vec<T>::n, F = 8 / W;             // binary32 needs twice the units
+    constexpr int W = Vec<T>::n;
     if (a.cols % W == 0 && aligned(a.x, a.x_stride, a.rows, sizeof(T)) && aligned(a.y, a.y_stride, a.rows, sizeof(T))) {
-        if (try_forward<T, W, 1 * F, 32, 512, 2>(a, st) || try_forward<T, W, 1 * F, 64, 512, 2>(a, st) ||
-            try_forward<T, W, 1 * F, 96, 480, 2>(a, st) || try_forward<T, W, 1 * F, 128, 512, 2>(a, st) ||
-            try_forward<T, W, 1 * F, 256, 512, 2>(a, st) || try_forward<T, W, 1 * F, 512, 512, 2>(a, st) ||
-            try_forward<T, W, 2 * F, 512, 512, 1>(a, st) || try_forward<T, W, 2 * F, 1024, 1024, 1, false>(a, st))
+        if (try_forward<T, W, 8, 32, 768>(a, st) || try_forward<T, W, 16, 32, 768>(a, st) || try_forward<T, W, 8, 96, 768>(a, st) ||
+            try_forward<T, W, 16, 64, 768>(a, st) || try_forward<T, W, 16, 128, 768>(a, st) ||
+            try_forward<T, W, 16, 256, 768>(a, st) || try_forward<T, W, 16, 512, 512>(a, st))
             return;
-    } else if (try_forward<T, 1, 8, 32, 512, 2>(a, st) || try_forward<T, 1, 16, 32, 256, 2>(a, st) ||
-               try_forward<T, 1, 16, 64, 256, 2>(a, st) || try_forward<T, 1, 16, 128, 256, 2>(a, st) ||
-               try_forward<T, 1, 16, 256, 256, 2>(a, st) || try_forward<T, 1, 16, 512, 512, 1>(a, st) ||
-               try_forward<T, 1, 16, 1024, 1024, 1, false>(a, st)) {
+    } else if (try_forward<T, 1, 8, 32, 768>(a, st) || try_forward<T, 1, 16, 32, 768>(a, st) ||
+               try_forward<T, 1, 16, 64, 768>(a, st) || try_forward<T, 1, 16, 128, 768>(a, st) ||
+               try_forward<T, 1, 16, 256, 768>(a, st) || try_forward<T, 1, 16, 512, 512>(a, st)) {
         return;
     }
     k_norm_long<T><<<(unsigned)a.rows, kLongBlock, 0, st>>>(a);
 }
 
-template <typename T, int W, int U, int THREADS, int BT, int PER_SM>
+template <typename T, int W, int N, int THREADS, int BT>
 static bool try_backward(const NormBackward &a, int blocks, cudaStream_t st)
 {
-    if (a.cols > (int64_t)W * U * THREADS) return false;
+    if (a.cols > (int64_t)N * THREADS) return false;
     constexpr int groups = BT / THREADS;
-    const int64_t per = a.rows / a.groups, most = (per + groups - 1) / groups;
-    if (PER_SM == 1 && blocks > 1) blocks = (blocks + 1) / 2;
+    const int64_t per = a.rows / a.groups;
+    const int cols = (int)a.cols;
+    const Ring r = ring_of(per, (int64_t)blocks * groups, row_pitch(cols, sizeof(T)), 2 * groups, N * THREADS * 4);
+    const int64_t most = ((per + r.rows - 1) / r.rows + groups - 1) / groups;
     if (blocks > most) blocks = (int)most;
     if (blocks < 1) blocks = 1;
-    const size_t smem = groups > 1 ? (size_t)a.cols * 8 : 0;
-    auto *kernel = k_norm_backward<T, W, U, THREADS, BT, PER_SM>;
-    kernel<<<dim3((unsigned)blocks, (unsigned)a.groups), BT, smem, st>>>(a, blocks);
+    const int rings = N * THREADS * 4 + 2 * r.stages * r.rows * r.pitch * groups, sums = groups > 1 ? groups * 2 * cols * 4 : 0;
+    const int smem = rings > sums ? rings : sums;
+    auto *kernel = k_norm_backward<T, W, N, THREADS, BT>;
+    cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    kernel<<<dim3((unsigned)blocks, (unsigned)a.groups), BT, smem, st>>>(a, blocks, r);
     if (blocks > 1 && (a.dweight || a.dbias))
         launch_after(k_norm_sums, dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)a.groups), dim3(1024), 0, st, a, blocks);
     return true;
@@ -550,18 +725,18 @@ static bool try_backward(const NormBackward &a, int blocks, cudaStream_t st)
 template <typename T>
 static void backward(const NormBackward &a, cudaStream_t st)
 {
-    constexpr int W = Vec<T>::n, F = 8 / W;
+    constexpr int W = Vec<T>::n;
     const int n = blocks_per_group(a.rows, a.groups);
     if (a.cols % W == 0 && aligned(a.x, a.x_stride, a.rows, sizeof(T)) && aligned(a.dy, a.dy_stride, a.rows, sizeof(T)) &&
         (!a.dx || aligned(a.dx, a.dx_stride, a.rows, sizeof(T)))) {
-        if (try_backward<T, W, 1 * F, 32, 512, 2>(a, n, st) || try_backward<T, W, 1 * F, 64, 512, 2>(a, n, st) ||
-            try_backward<T, W, 1 * F, 96, 480, 2>(a, n, st) || try_backward<T, W, 1 * F, 128, 512, 2>(a, n, st) ||
-            try_backward<T, W, 1 * F, 256, 512, 2>(a, n, st) || try_backward<T, W, 1 * F, 512, 512, 2>(a, n, st) ||
-            try_backward<T, W, 2 * F, 512, 512, 1>(a, n, st))
+        if (try_backward<T, W, 8, 32, 768>(a, n, st) || try_backward<T, W, 16, 32, 512>(a, n, st) ||
+            try_backward<T, W, 8, 96, 768>(a, n, st) || try_backward<T, W, 16, 64, 512>(a, n, st) ||
+            try_backward<T, W, 16, 128, 512>(a, n, st) || try_backward<T, W, 16, 256, 512>(a, n, st) ||
+            try_backward<T, W, 16, 512, 512>(a, n, st))
             return;
-    } else if (try_backward<T, 1, 8, 32, 256, 2>(a, n, st) || try_backward<T, 1, 16, 32, 256, 2>(a, n, st) ||
-               try_backward<T, 1, 16, 64, 256, 2>(a, n, st) || try_backward<T, 1, 16, 128, 256, 2>(a, n, st) ||
-               try_backward<T, 1, 16, 256, 256, 2>(a, n, st) || try_backward<T, 1, 16, 512, 512, 1>(a, n, st)) {
+    } else if (try_backward<T, 1, 8, 32, 768>(a, n, st) || try_backward<T, 1, 16, 32, 512>(a, n, st) ||
+               try_backward<T, 1, 16, 64, 512>(a, n, st) || try_backward<T, 1, 16, 128, 512>(a, n, st) ||
+               try_backward<T, 1, 16, 256, 512>(a, n, st) || try_backward<T, 1, 16, 512, 512>(a, n, st)) {
         return;
     }
     if (a.dweight || a.dbias)
