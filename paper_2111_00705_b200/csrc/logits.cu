@@ -46,6 +46,38 @@ namespace cg = cooperative_groups;
 // Cluster barrier in two halves, for threads that need not be converged: writes before an
 // arrival, also to other blocks' shared memory, are visible after the wait.
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
+// Stores into block `rank`'s shared memory (at the place of `here` in this block's) that are
+// counted on its barrier `bar`: no fence, the receiver waits for the bytes.
+__device__ __forceinline__ uint32_t cluster_addr(const void *here, int rank)
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(here)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void send32(const void *here, int rank, uint64_t *bar, float v)
+{
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(cluster_addr(here, rank)),
+                 "r"(__float_as_uint(v)), "r"(cluster_addr(bar, rank)) : "memory");
+}
+__device__ __forceinline__ void send64(const void *here, int rank, uint64_t *bar, float x, float y)
+{
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(cluster_addr(here, rank)),
+                 "l"(bits64(make_float2(x, y))), "r"(cluster_addr(bar, rank)) : "memory");
+}
+// As mbar_wait_bounded, for what other blocks of the cluster have sent.
+__device__ __forceinline__ bool wait_told(uint64_t *bar)
+{
+    for (int spin = 0; spin < kWaitLimit; ++spin) {
+        uint32_t done;
+        asm volatile("{\n.reg .pred p;\n"
+                     "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+                     "selp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(done) : "r"(smem_addr(bar)), "r"(0) : "memory");
+        if (done) return true;
+    }
+    return false;
+}
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 // ---------------------------------------------------------------------------------------------
@@ -681,41 +713,47 @@ __global__ void __launch_bounds__(NT) k_distill(Distill a, int log_parts)
 {
     constexpr int V = Vec<T>::n, kWarps = kMaxList / 32;
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ float sh[2][NT / 32], shm[kWarps], she[kWarps];
+    __shared__ float sh[2][NT / 32], top32[kWarps], zl[kMaxList];
     __shared__ __align__(16) int32_t id[kMaxList];
-    __shared__ double w[kMaxList], sum64[kWarps];
-    __shared__ float top32[kWarps];
-    __shared__ Rest rest_sh[kMaxParts];
-    __shared__ uint64_t bar;
+    __shared__ double w[kMaxList], sum64[2][kWarps];
+    __shared__ __align__(8) Rest rest_sh[kMaxParts];
+    __shared__ uint64_t bar, told;              // the slice has arrived; the cluster's sums have
+    __shared__ bool listed[kMaxList];
+    __shared__ int repeated;
     uint4 *buf = reinterpret_cast<uint4 *>(smem);
     T *elem = reinterpret_cast<T *>(smem);
-    const int parts = 1 << log_parts, part = (int)(blockIdx.x & (unsigned)(parts - 1)), j = threadIdx.x, k = a.k;
+    const int parts = 1 << log_parts, part = (int)(blockIdx.x & (unsigned)(parts - 1)), j = threadIdx.x, k = a.k, lane = j & 31;
     const int64_t row = blockIdx.x >> log_parts;
     cg::cluster_group cluster = cg::this_cluster();
-    if (parts > 1) cluster_arrive();
-
     const Slice<T> sl(a.z, a.stride, row, a.vocab, part, log_parts);
-    start_slice<T, NT>(sl, buf, &bar);
 
-    // While the slice is on its way, the teacher's distribution over the list.  Thread j < k has
-    // entry j; an index listed again is left to its first entry.  Unused: id -1, weight 0.
+    // The list is asked for ahead of the slice, and worked on while that is on its way: the teacher's
+    // distribution.  Thread j < k has entry j; an index listed again is left to its first entry.
+    // Unused: id -1, weight 0.
     int mine = -1;
-    float zj = kNegInf, lq = kNegInf;
+    float lq = kNegInf;
     double q = 0.0;
+    int64_t listed_id = -1;
+    if (j < k) {
+        listed_id = index_at(a.ids, row * k + j, a.index64);
+        lq = a.teacher[row * k + j];
+    }
+    if (j == 0) {
+        repeated = 0;
+        mbar_init(&told, 1);
+    }
+    start_slice<T, NT>(sl, buf, &bar);
+    if (parts > 1) cluster_arrive_relaxed();            // this block runs, its barriers exist
     if (j < kMaxList) {
-        if (j < k) {
-            const int64_t i = index_at(a.ids, row * k + j, a.index64);
-            lq = a.teacher[row * k + j];
-            mine = i >= 0 && i < a.vocab && (a.rest || lq != kNegInf) ? (int)i : -1;
-            if (mine >= 0) zj = widen(sl.row[mine]);
-            else lq = kNegInf;
-        }
-        id[j] = j < k ? mine : -1;
+        mine = listed_id >= 0 && listed_id < a.vocab && (a.rest || lq != kNegInf) ? (int)listed_id : -1;
+        if (mine < 0) lq = kNegInf;
+        id[j] = mine;
         if (!a.rest) {
             const float m = warp_max(lq);
-            if ((j & 31) == 0) top32[j >> 5] = m;
+            if (lane == 0) top32[j >> 5] = m;
         }
     }
+    const float g = a.dz ? a.dloss[row] * a.inv_temperature : 0.0f;
     __syncthreads();
     bool again = false;
     if (j < kMaxList) {
@@ -731,83 +769,80 @@ __global__ void __launch_bounds__(NT) k_distill(Distill a, int log_parts)
                 const int4 d = *reinterpret_cast<const int4 *>(id + i);
                 again |= (d.x == mine) | (d.y == mine && i + 1 < j) | (d.z == mine && i + 2 < j) | (d.w == mine && i + 3 < j);
             }
+            if (again) repeated = 1;
         }
         w[j] = q;
+        listed[j] = mine >= 0 && !again;
         const double sum = warp_sum64(q);
-        if ((j & 31) == 0) sum64[j >> 5] = sum;
+        if (lane == 0) sum64[0][j >> 5] = sum;
     }
-    const bool late = !mbar_wait_bounded(&bar, 0);
-    const int used = __syncthreads_count(mine >= 0 && !again);
-    if (__syncthreads_or(again) && mine >= 0) {          // some index is listed more than once
-        if (again) { q = 0.0; zj = kNegInf; }
-        else
-            for (int i = j + 1; i < k; ++i)
-                if (id[i] == mine) q += w[i];
-    }
-    const bool first = mine >= 0 && !again;
-    const double mass = (sum64[0] + sum64[1]) + (sum64[2] + sum64[3]);
-    if (!a.rest && mass != 0.0) q /= mass;
-    const double r = !a.rest || used >= a.vocab ? 0.0 : mass != mass ? mass : fmax(0.0, 1.0 - mass);
-    const float s = (float)a.scale2;
-    const bool here = first && mine >= sl.start && mine < sl.start + sl.nv * V;
-    if (here) elem[mine - sl.start] = minus_inf<T>();
-    if (j < kMaxList) {
-        const float m = warp_max(zj), p = zj == kNegInf ? 0.0f : exp2_fast((zj - m) * s);
-        const float e = warp_sum(p);
-        if ((j & 31) == 0) { shm[j >> 5] = m; she[j >> 5] = e; }
+    const bool first = mine >= 0 && !again, here = first && mine >= sl.start && mine < sl.start + sl.nv * V;
+    bool late = !mbar_wait_bounded(&bar, 0);
+    const int used = __syncthreads_count(first);
+    float zj = kNegInf;
+    if (here) {
+        zj = widen(elem[mine - sl.start]);
+        elem[mine - sl.start] = minus_inf<T>();
     }
     __syncthreads();
-
+    const float s = (float)a.scale2;
     const float m = block_max_all<NT>(late ? kLate : slice_max<T, NT>(buf, sl.nv), sh[0]);
     const Origin own(m, s);
     float e = own.far ? slice_sum<T, NT, true>(buf, sl.nv, own, s) : slice_sum<T, NT, false>(buf, sl.nv, own, s);
     e = block_sum_all<NT>(e, sh[1]);
+
+    // every block learns the others' sums and the listed tokens' logits
     if (parts > 1) {
         cluster_wait();
-        if (j < parts) cluster.map_shared_rank(rest_sh, j)[part] = Rest{m, e};
-        cluster_arrive();
-        cluster_wait();
+        if (j == 0) mbar_arrive_expect_tx(&told, (uint32_t)(parts * sizeof(Rest) + used * sizeof(float)));
+        for (int i = 0; i < parts; ++i) {
+            if (here) send32(&zl[j], i, &told, zj);
+            if (j == i) send64(&rest_sh[part], i, &told, m, e);
+        }
     } else {
+        if (here) zl[j] = zj;
         if (j == 0) rest_sh[0] = Rest{m, e};
-        __syncthreads();
     }
+    // meanwhile the teacher's weights of this thread's entry
+    if (repeated && mine >= 0) {
+        if (again) q = 0.0;
+        else
+            for (int i = j + 1; i < k; ++i)
+                if (id[i] == mine) q += w[i];
+    }
+    const double mass = (sum64[0][0] + sum64[0][1]) + (sum64[0][2] + sum64[0][3]);
+    if (!a.rest && mass != 0.0) q /= mass;
+    const double r = !a.rest || used >= a.vocab ? 0.0 : mass != mass ? mass : fmax(0.0, 1.0 - mass);
+    if (parts > 1) late |= !wait_told(&told);
+    else __syncthreads();
 
-    // rest and list, each relative to its own origin; then both relative to the larger
-    float mr = kNegInf, er = 0.0f, ml = kNegInf, el = 0.0f;
-    for (int i = 0; i < parts; ++i) mr = fmaxf(mr, rest_sh[i].m);
-    for (int i = 0; i < kWarps; ++i) ml = fmaxf(ml, shm[i]);
+    // Rest and list, each relative to its own origin; then both relative to the larger.  Every warp
+    // does this for itself.
+    const Rest mine_rest = rest_sh[lane < parts ? lane : 0];
+    const float mr = warp_max(mine_rest.m);
+    float zk[kWarps], ml = kNegInf;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+        zk[i] = listed[lane + 32 * i] ? zl[lane + 32 * i] : kNegInf;
+        ml = fmaxf(ml, zk[i]);
+    }
+    ml = warp_max(ml);
     const Origin rest(mr, s), top(fmaxf(mr, ml), s);
     const float mlu = ml == kNegInf ? 0.0f : ml;
-    for (int i = 0; i < parts; ++i) {
-        const Rest p = rest_sh[i];
-        if (p.e != 0.0f) er = fmaf(p.e != p.e ? 1.0f : exp2_fast(shift(Origin(p.m, s), rest, s)), p.e, er);
-    }
-    for (int i = 0; i < kWarps; ++i)
-        if (she[i] != 0.0f) el = fmaf(she[i] != she[i] ? 1.0f : exp2_fast((shm[i] - mlu) * s), she[i], el);
-    const bool bad = er != er || el != el || fmaxf(mr, ml) > 3.402823466e38f, empty = !bad && fmaxf(mr, ml) == kNegInf;
+    float er = mine_rest.e != mine_rest.e ? mine_rest.e : mine_rest.e == 0.0f || lane >= parts ? 0.0f
+        : exp2_fast(shift(Origin(mine_rest.m, s), rest, s)) * mine_rest.e;
+    float el = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) el += zk[i] == kNegInf ? 0.0f : exp2_fast((zk[i] - mlu) * s);
+    er = warp_sum(er);
+    el = warp_sum(el);
+    const bool bad = late || er != er || el != el || fmaxf(mr, ml) > 3.402823466e38f, empty = !bad && fmaxf(mr, ml) == kNegInf;
     // the list's sum is relative to ml s, the origin's c is rounded: exponents of the difference
     const float fr = er == 0.0f ? 0.0f : exp2_fast(shift(rest, top, s)), fl = el == 0.0f ? 0.0f
         : exp2_fast(top.far ? (mlu - top.m) * s : fmaf(mlu, s, -top.c));
     const float E = fmaf(fr, er, fl * el);
 
-    const bool loss = part == 0 && a.loss;
-    if (loss && j < kMaxList) {
-        // in 64 bits from here: the only roundings are those of the sums
-        const double l2 = log2((double)E);
-        double t = 0.0;
-        if (first && !(q == 0.0)) t = q * (log(q) - (exponent64(zj, top, s) - l2) * kLn2);
-        if (j == 0 && r > 0.0) {
-            const double at = top.far ? ((double)rest.m - (double)top.m) * (double)s
-                : (rest.far ? exponent64(rest.m, top, s) : (double)rest.c - (double)top.c);
-            t += r * (log(r) - (at + log2((double)er) - l2) * kLn2);
-        }
-        if (j == 0 && r != r) t = r;
-        t = warp_sum64(t);
-        if ((j & 31) == 0) sum64[j >> 5] = t;
-    }
-
     if (a.dz) {
-        const float g = a.dloss[row] * a.inv_temperature;
         const bool zero = g == 0.0f || empty || (used == 0 && !bad);
         const float others = er == 0.0f ? 0.0f : g * (fr / E - (float)r / er);
         if (zero || bad) {
@@ -848,12 +883,31 @@ __global__ void __launch_bounds__(NT) k_distill(Distill a, int log_parts)
         } else {
             for (int c = lo + threadIdx.x; c < hi; c += NT) out[c] = elem[c - sl.start];
         }
-    } else {
-        __syncthreads();
     }
-    if (loss && j == 0)
-        a.loss[row] = bad ? NAN : used == 0 ? 0.0f : empty ? INFINITY : (float)((sum64[0] + sum64[1]) + (sum64[2] + sum64[3]));
-    if (late) mbar_wait_bounded(&bar, 0);                               // no block leaves with copies in flight
+    if (part == 0 && a.loss) {
+        if (j < kMaxList) {
+            // relative to `top` and in 64 bits: the only roundings are those of the sums
+            const double l2 = log2((double)E);
+            double t = 0.0;
+            if (first && !(q == 0.0)) t = q * (log(q) - (exponent64(zl[j], top, s) - l2) * kLn2);
+            if (j == 0 && r > 0.0) {
+                const double at = top.far ? ((double)rest.m - (double)top.m) * (double)s
+                    : (rest.far ? exponent64(rest.m, top, s) : (double)rest.c - (double)top.c);
+                t += r * (log(r) - (at + log2((double)er) - l2) * kLn2);
+            }
+            if (j == 0 && r != r) t = r;
+            t = warp_sum64(t);
+            if (lane == 0) sum64[1][j >> 5] = t;
+        }
+        __syncthreads();
+        if (j == 0)
+            a.loss[row] = bad ? NAN : used == 0 ? 0.0f : empty ? INFINITY
+                : (float)((sum64[1][0] + sum64[1][1]) + (sum64[1][2] + sum64[1][3]));
+    }
+    if (late) {                                                         // no block leaves with copies in flight
+        mbar_wait_bounded(&bar, 0);
+        if (parts > 1) wait_told(&told);
+    }
     if (a.dz && threadIdx.x == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
 }
 
