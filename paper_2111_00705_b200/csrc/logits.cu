@@ -194,33 +194,40 @@ __device__ __forceinline__ double exponent64(float z, const Origin &row, float s
 
 // ---------------------------------------------------------------------------------------------
 // Alternatives.  Every slice gives its k first tokens in descending order, the cluster's first
-// block merges them.  Within a slice the 256 threads have each met a largest value; the
-// k-th largest of these is a value that at least k elements reach, and in a row without
-// structure hardly more (256 ln(256 / (256 - k)) are expected: 74 for k = 64).  It is found bit by
-// bit in the upper 16 bits of the values' order (a bound a little too low only lets a few more
-// in).  The pass that adds up the exponentials notes the vectors that reach it; their elements
-// that do are collected, and counting for each how many are greater sorts them.  Only where more
-// than kCap are noted or collected (thousands of equal values, or the largest all in a few
-// threads' vectors) the slice is walked again in order, the best k so far always kept.
+// block merges them.  Within a slice each of the NT threads meets a largest value; the k-th largest
+// of these is one that at least k elements reach, and in a row without structure hardly more (NT ln(
+// NT / (NT - k)) are expected: 74 for NT = 256, k = 64).  It is found in the upper 16 bits of the
+// values' order (a bound a little too low only lets a few more in).  A thread keeps a copy of the
+// best batch of its even and of its odd rounds; almost all elements that reach the bound are in
+// these, and the few other batches that do are read again.  Counting for each collected element how
+// many are greater sorts them.  Only where more than kCap are collected (thousands of equal values,
+// or the largest all in a few threads' vectors) the slice is walked again in order, the best k so
+// far always kept.
 // ---------------------------------------------------------------------------------------------
 constexpr int kCap = 512;
-constexpr int kGroups = 256;
 
-// The upper 16 bits of the order of the k-th largest of the values of a warp's lanes (1 <= k <= kGroups).
-__device__ __forceinline__ int kth_of_groups(const float (&g)[kGroups / 32], int k)
+// The upper 16 bits of the order of the k-th largest of the 32 N values of a warp's lanes (1 <= k <=
+// 32 N), by bisection between the smallest and the largest.
+template <int N>
+__device__ __forceinline__ int kth_of_groups(const float (&g)[N], int k)
 {
-    uint32_t o[kGroups / 32], t = 0;
+    int o[N], lo = 0xFFFF, hi = 0;
 #pragma unroll
-    for (int i = 0; i < kGroups / 32; ++i) o[i] = (uint32_t)(order_key(g[i], 0) >> 48);
-#pragma unroll
-    for (int b = 15; b >= 0; --b) {
-        const uint32_t next = t | (1u << b);
+    for (int i = 0; i < N; ++i) {
+        o[i] = (int)(order_key(g[i], 0) >> 48);
+        lo = min(lo, o[i]);
+        hi = max(hi, o[i]);
+    }
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
         int n = 0;
 #pragma unroll
-        for (int i = 0; i < kGroups / 32; ++i) n += o[i] >= next;
-        if (__reduce_add_sync(0xffffffffu, n) >= k) t = next;
+        for (int i = 0; i < N; ++i) n += o[i] >= mid;
+        if (__reduce_add_sync(0xffffffffu, n) >= k) lo = mid; else hi = mid - 1;
     }
-    return (int)t;
+    return lo;
 }
 
 __device__ __forceinline__ int rank_of(uint64_t key, const uint64_t *keys, int n)
@@ -282,7 +289,9 @@ __device__ __noinline__ int collect_in_order(const Slice<T> &sl, float reach, in
 // lowest value, give no sums this way (infinite c, or e = 0): they are added up again relative to
 // their maximum.
 // For the alternatives each batch leaves the upper 16 bits of its maximum's order in shared
-// memory; after the pass only batches that reach the threshold are looked at again (in L2).
+// memory, and the batch itself where it is its group's best so far: with 4 blocks of 256 KB rows on
+// every SM a row's beginning has left L2 when its end arrives, and fetching 75 batches of it once
+// more took half as long as the row (0.249 instead of 0.206 ms for 4096 x 131072 bf16, k = 64).
 // ---------------------------------------------------------------------------------------------
 constexpr int kBatch = 4;
 constexpr float kFar = 1e30f;
@@ -356,9 +365,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
     __shared__ float sh[4][NT / 32];
     __shared__ Sums sums[kMaxParts];
     __shared__ int count[2], reach_sh;
-    uint64_t *cand = reinterpret_cast<uint64_t *>(smem);            // kCap keys; before that every thread's maximum
-    int *hits = reinterpret_cast<int *>(cand + kCap);               // kCap batches
-    uint16_t *keys = reinterpret_cast<uint16_t *>(hits + kCap);     // one of every batch
+    uint4 *kept = reinterpret_cast<uint4 *>(smem);                  // every group's best batch
+    uint64_t *cand = reinterpret_cast<uint64_t *>(kept + 2 * kBatch * NT);  // kCap keys; before that the groups' maxima
+    int2 *hits = reinterpret_cast<int2 *>(cand + kCap);             // kCap batches
+    uint16_t *kept_at = reinterpret_cast<uint16_t *>(hits + kCap);  // the round of every group's best batch
+    uint16_t *keys = kept_at + 2 * NT;                              // one of every batch
     uint64_t *lists = reinterpret_cast<uint64_t *>(keys + rounds * NT);     // first block: parts x k keys
     const int part = (int)(blockIdx.x & (unsigned)(parts - 1));
     const int64_t row = blockIdx.x >> log_parts;
@@ -368,6 +379,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
     const Slice<T> sl(a.z, a.stride, row, a.vocab, part, log_parts);
     const float s = (float)a.scale2, gap = 200.0f / s;
     Running r = {kNegInf, -kFar * s, {0.0f, 0.0f}, {0.0f, 0.0f}};
+    float best[2] = {kNegInf, kNegInf}, second[2] = {kNegInf, kNegInf};     // of the even and the odd rounds
     uint4 u[kBatch], next[kBatch];
     if (sl.nv > 0) load_batch<T, NT>(sl, threadIdx.x, u);
 #pragma unroll 2
@@ -377,7 +389,17 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
 #pragma unroll
         for (int b = 1; b < kBatch; ++b) mx = Vec<T>::max(mx, Vec<T>::top(u[b]));
         const float top = Vec<T>::value(mx);
-        if (TOP) keys[i * NT + threadIdx.x] = (uint16_t)(order_key(top, 0) >> 48);
+        if (TOP) {
+            keys[i * NT + threadIdx.x] = (uint16_t)(order_key(top, 0) >> 48);
+            const float was = i & 1 ? best[1] : best[0], next2 = fmaxf(i & 1 ? second[1] : second[0], fminf(was, top));
+            if (i & 1) second[1] = next2; else second[0] = next2;
+            if (top > was) {
+                if (i & 1) best[1] = top; else best[0] = top;
+                kept_at[(i & 1) * NT + threadIdx.x] = (uint16_t)i;
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b) kept[((i & 1) * kBatch + b) * NT + threadIdx.x] = u[b];
+            }
+        }
         r.m = fmaxf(r.m, top);
         const float m = fmaxf(r.m, -kFar), c = m * s, d = r.c - c, f = exp2_fast(d);
         r.c = c;
@@ -415,36 +437,44 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
         reinterpret_cast<float *>(cand)[threadIdx.x] = r.m;
         __syncthreads();
         if (threadIdx.x < 32) {
-            const float *all = reinterpret_cast<const float *>(cand);
-            float g[kGroups / 32];
+            float g[NT / 32];
 #pragma unroll
-            for (int i = 0; i < kGroups / 32; ++i) {
-                g[i] = all[threadIdx.x + 32 * i];
-#pragma unroll
-                for (int o = kGroups; o < NT; o += kGroups) g[i] = fmaxf(g[i], all[threadIdx.x + 32 * i + o]);
-            }
-            const int t = kth_of_groups(g, a.k);
+            for (int i = 0; i < NT / 32; ++i) g[i] = reinterpret_cast<const float *>(cand)[threadIdx.x + 32 * i];
+            const int t = kth_of_groups<NT / 32>(g, a.k);
             if (threadIdx.x == 0) { reach_sh = t; count[0] = count[1] = 0; }
         }
         __syncthreads();
         const int reach16 = max(reach_sh, 0x80);                    // 0x7F: the order of -inf
         const float reach = key_value((uint64_t)reach16 << 48);
-        const int batches = min(rounds, (sl.nv + kBatch * NT - 1) / (kBatch * NT)) * NT;
-        for (int i = threadIdx.x; i < batches / 8; i += NT) {
-            const uint4 q = reinterpret_cast<const uint4 *>(keys)[i];
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        // list the batches that reach it: where the first vector of a kept one is (the others of the
+        // batch are NT V elements apart there as in the row) and its column; -1 where it is not kept
+        const int place = (int)threadIdx.x * V, column = sl.start + place;
 #pragma unroll
-            for (int b = 0; b < 8; ++b)
-                if ((int)(b & 1 ? w[b / 2] >> 16 : w[b / 2] & 0xFFFFu) >= reach16) {
-                    const int at = atomicAdd(&count[0], 1);
-                    if (at < kCap) hits[at] = 8 * i + b;
-                }
+        for (int o = 0; o < 2; ++o) {
+            const bool in = best[o] >= reach;
+            const unsigned all = __ballot_sync(0xffffffffu, in);
+            if (all == 0) continue;
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&count[0], __popc(all));
+            at = __shfl_sync(0xffffffffu, at, 0) + __popc(all & ((1u << lane) - 1));
+            if (in) {
+                const int own = kept_at[o * NT + threadIdx.x];
+                if (at < kCap) hits[at] = make_int2(o * (kBatch * NT * V) + place, own * (kBatch * NT * V) + column);
+                if (second[o] >= reach)
+                    for (int i = o; i < rounds && i * (kBatch * NT) < sl.nv; i += 2)
+                        if (keys[i * NT + threadIdx.x] >= reach16 && i != own) {
+                            const int to = atomicAdd(&count[0], 1);
+                            if (to < kCap) hits[to] = make_int2(-1, i * (kBatch * NT * V) + column);
+                        }
+            }
         }
         __syncthreads();
         const int noted = count[0];
         if (noted <= kCap) {
             // a warp looks at kAhead batches at a time, a lane at one element of each
-            constexpr int kAhead = 8, W = NT / 32;
+            constexpr int kAhead = 4, W = NT / 32;
+            const T *elem = reinterpret_cast<const T *>(kept);
+            const int mine = lane / V * (NT * V) + lane % V;
             for (int i = threadIdx.x >> 5; i < noted; i += kAhead * W) {
                 float z[kAhead];
                 int at[kAhead];
@@ -453,17 +483,22 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
                     z[o] = kNegInf;
                     at[o] = 0;
                     if (i + o * W < noted && lane < kBatch * V) {
-                        const int b = hits[i + o * W], v = b / NT * (kBatch * NT) + b % NT + lane / V * NT;
-                        at[o] = sl.start + v * V + lane % V;
-                        if (v < sl.nv && at[o] >= 0 && at[o] < sl.vocab) z[o] = widen(sl.row[at[o]]);
+                        const int2 h = hits[i + o * W];
+                        at[o] = h.y + mine;
+                        if (h.x >= 0) z[o] = widen(elem[h.x + mine]);
+                        else if (at[o] >= max(sl.start, 0) && at[o] < min(sl.vocab, sl.start + sl.nv * V)) z[o] = widen(sl.row[at[o]]);
                     }
                 }
 #pragma unroll
-                for (int o = 0; o < kAhead; ++o)
-                    if (z[o] >= reach) {
-                        const int to = atomicAdd(&count[1], 1);
-                        if (to < kCap) cand[to] = order_key(z[o], at[o]);
-                    }
+                for (int o = 0; o < kAhead; ++o) {
+                    const bool in = z[o] >= reach;
+                    const unsigned all = __ballot_sync(0xffffffffu, in);
+                    if (all == 0) continue;
+                    int to = 0;
+                    if (lane == 0) to = atomicAdd(&count[1], __popc(all));
+                    to = __shfl_sync(0xffffffffu, to, 0) + __popc(all & ((1u << lane) - 1));
+                    if (in && to < kCap) cand[to] = order_key(z[o], at[o]);
+                }
             }
             __syncthreads();
             n = count[1];
@@ -919,7 +954,7 @@ __global__ void __launch_bounds__(NT) k_distill(Distill a, int log_parts)
 // Launches
 // ---------------------------------------------------------------------------------------------
 constexpr int kSliceBytes = 32 * 1024;           // six blocks share an SM
-constexpr int kRowThreads = 256;
+constexpr int64_t kShortSlice = 64 * 1024;       // slices of the forward pass up to this: blocks of 128 threads
 
 // Blocks per row of the forward pass, as a power of two: one where the rows alone fill the GPU
 // (two for each SM); fewer rows are shared by up to 8 blocks of at least 8 KB.
@@ -966,13 +1001,12 @@ static void for_row_blocks(int64_t rows, int parts, F f)
     for (int64_t at = 0; at < rows; at += most) f(at, rows - at < most ? rows - at : most);
 }
 
-template <typename T>
-static void logprobs(const Logprobs &a, cudaStream_t st)
+template <typename T, int NT>
+static void logprobs(const Logprobs &a, int log_parts, cudaStream_t st)
 {
-    constexpr int NT = kRowThreads;
-    int log_parts = log_parts_for_rows(a.rows, a.vocab * (int64_t)sizeof(T)), parts = 1 << log_parts;
+    const int parts = 1 << log_parts;
     int rounds = (int)((slice_bytes<T>(a.vocab, parts) / 16 + kBatch * NT - 1) / (kBatch * NT));
-    const size_t smem = a.k ? kCap * 12 + (size_t)parts * a.k * 8 + (size_t)rounds * NT * 2 : 0;
+    const size_t smem = a.k ? 2 * kBatch * NT * 16 + kCap * 16 + (size_t)(rounds + 2) * NT * 2 + (size_t)parts * a.k * 8 : 0;
     for_row_blocks(a.rows, parts, [&](int64_t at, int64_t n) {
         Logprobs b = a;
         b.z = static_cast<const T *>(a.z) + at * a.stride;
@@ -988,6 +1022,15 @@ static void logprobs(const Logprobs &a, cudaStream_t st)
         if (a.k) launch_rows(k_logprobs<T, NT, true>, n, parts, NT, smem, st, args);
         else launch_rows(k_logprobs<T, NT, false>, n, parts, NT, smem, st, args);
     });
+}
+
+template <typename T>
+static void logprobs(const Logprobs &a, cudaStream_t st)
+{
+    const int64_t bytes = a.vocab * (int64_t)sizeof(T);
+    const int log_parts = log_parts_for_rows(a.rows, bytes);
+    if (bytes >> log_parts <= kShortSlice) logprobs<T, 128>(a, log_parts, st);
+    else logprobs<T, 256>(a, log_parts, st);
 }
 
 template <typename T>
