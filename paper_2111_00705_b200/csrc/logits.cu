@@ -193,8 +193,8 @@ __device__ __forceinline__ double exponent64(float z, const Origin &row, float s
 }
 
 // ---------------------------------------------------------------------------------------------
-// Alternatives.  Every slice gives its k first tokens in descending order, the cluster's first
-// block merges them.  Within a slice each of the NT threads meets a largest value; the k-th largest
+// Alternatives.  Every slice gives its k first tokens in descending order to all blocks of the
+// cluster, and each places its own among them.  Within a slice each of the NT threads meets a largest value; the k-th largest
 // of these is one that at least k elements reach, and in a row without structure hardly more (NT ln(
 // NT / (NT - k)) are expected: 74 for NT = 256, k = 64).  It is found in the upper 16 bits of the
 // values' order (a bound a little too low only lets a few more in).  A thread keeps a copy of the
@@ -370,11 +370,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
     int2 *hits = reinterpret_cast<int2 *>(cand + kCap);             // kCap batches
     uint16_t *kept_at = reinterpret_cast<uint16_t *>(hits + kCap);  // the round of every group's best batch
     uint16_t *keys = kept_at + 2 * NT;                              // one of every batch
-    uint64_t *lists = reinterpret_cast<uint64_t *>(keys + rounds * NT);     // first block: parts x k keys
+    uint64_t *lists = reinterpret_cast<uint64_t *>(keys + rounds * NT);     // of all slices: parts x k keys
     const int part = (int)(blockIdx.x & (unsigned)(parts - 1));
     const int64_t row = blockIdx.x >> log_parts;
     cg::cluster_group cluster = cg::this_cluster();
-    if (parts > 1) cluster_arrive();                // the first block runs before anything is written to it
+    if (parts > 1) cluster_arrive();                // a block runs before anything is written to it
 
     const Slice<T> sl(a.z, a.stride, row, a.vocab, part, log_parts);
     const float s = (float)a.scale2, gap = 200.0f / s;
@@ -472,32 +472,42 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
         const int noted = count[0];
         if (noted <= kCap) {
             // a warp looks at kAhead batches at a time, a lane at one element of each
-            constexpr int kAhead = 4, W = NT / 32;
+            constexpr int kAhead = 8, W = NT / 32;
             const T *elem = reinterpret_cast<const T *>(kept);
-            const int mine = lane / V * (NT * V) + lane % V;
+            const int mine = lane / V * (NT * V) + lane % V, lo = max(sl.start, 0), hi = min(sl.vocab, sl.start + sl.nv * V);
             for (int i = threadIdx.x >> 5; i < noted; i += kAhead * W) {
-                float z[kAhead];
+                T raw[kAhead];                      // all on their way before the first is looked at
                 int at[kAhead];
 #pragma unroll
                 for (int o = 0; o < kAhead; ++o) {
-                    z[o] = kNegInf;
-                    at[o] = 0;
-                    if (i + o * W < noted && lane < kBatch * V) {
-                        const int2 h = hits[i + o * W];
-                        at[o] = h.y + mine;
-                        if (h.x >= 0) z[o] = widen(elem[h.x + mine]);
-                        else if (at[o] >= max(sl.start, 0) && at[o] < min(sl.vocab, sl.start + sl.nv * V)) z[o] = widen(sl.row[at[o]]);
-                    }
+                    const bool there = i + o * W < noted && lane < kBatch * V;
+                    const int2 h = hits[there ? i + o * W : 0];
+                    at[o] = h.y + mine;
+                    const bool in = there && at[o] >= lo && at[o] < hi;
+                    const T *p = h.x >= 0 ? elem + (h.x + mine) : sl.row + at[o];
+                    raw[o] = minus_inf<T>();
+                    if (in) raw[o] = *p;
                 }
+                float z[kAhead];
+#pragma unroll
+                for (int o = 0; o < kAhead; ++o) z[o] = widen(raw[o]);
+                // one reservation for all of them
+                int total = 0, to = 0;
+                unsigned all[kAhead];
 #pragma unroll
                 for (int o = 0; o < kAhead; ++o) {
-                    const bool in = z[o] >= reach;
-                    const unsigned all = __ballot_sync(0xffffffffu, in);
-                    if (all == 0) continue;
-                    int to = 0;
-                    if (lane == 0) to = atomicAdd(&count[1], __popc(all));
-                    to = __shfl_sync(0xffffffffu, to, 0) + __popc(all & ((1u << lane) - 1));
-                    if (in && to < kCap) cand[to] = order_key(z[o], at[o]);
+                    all[o] = __ballot_sync(0xffffffffu, z[o] >= reach);
+                    total += __popc(all[o]);
+                }
+                if (lane == 0 && total) to = atomicAdd(&count[1], total);
+                to = __shfl_sync(0xffffffffu, to, 0);
+#pragma unroll
+                for (int o = 0; o < kAhead; ++o) {
+                    if (z[o] >= reach) {
+                        const int here = to + __popc(all[o] & ((1u << lane) - 1));
+                        if (here < kCap) cand[here] = order_key(z[o], at[o]);
+                    }
+                    to += __popc(all[o]);
                 }
             }
             __syncthreads();
@@ -507,14 +517,16 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
     }
     __syncthreads();
     if (parts > 1) cluster_wait();
-    if (TOP) {
-        uint64_t *list = parts > 1 ? cluster.map_shared_rank(lists, 0) : lists;
+    // every block gets all slices' lists and sums, and places its own alternatives among them
+    if (TOP)
         for (int i = threadIdx.x; i < n; i += NT) {
             const uint64_t key = cand[i];
             const int at = rank_of(key, cand, n);
-            if (at < a.k) list[part * a.k + at] = key;
+            if (at >= a.k) continue;
+            if (parts == 1) lists[at] = key;
+            else
+                for (int o = 0; o < parts; ++o) cluster.map_shared_rank(lists, o)[part * a.k + at] = key;
         }
-    }
     if (threadIdx.x < 32) {
         const bool is = threadIdx.x < NT / 32;
         m = warp_max(is ? sh[0][threadIdx.x] : kNegInf);
@@ -522,14 +534,12 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
         e = is ? sh[2][threadIdx.x] : 0.0f;
         h = is ? sh[3][threadIdx.x] : 0.0f;
         join_warp(c, e, h);
-        if (threadIdx.x == 0) {
-            Sums *to = parts > 1 ? cluster.map_shared_rank(sums, 0) : sums;
-            to[part] = Sums{m, c, e, h, min(n, a.k)};
-        }
+        // (without alternatives to the first block alone: the others do not wait for anything)
+        if (lane < (TOP ? parts : 1)) (parts > 1 ? cluster.map_shared_rank(sums, lane) : sums)[part] = Sums{m, c, e, h, min(n, a.k)};
     }
     if (parts > 1) {
         cluster_arrive();
-        if (part != 0) return;                       // nothing reads this block's shared memory
+        if (!TOP && part != 0) return;               // nothing is sent to this block
         cluster_wait();
     } else {
         __syncthreads();
@@ -555,10 +565,10 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
         E = block_sum_all<NT>(e, sh[0]);
         H = block_sum_all<NT>(h, sh[1]);
     }
-    if ((int)(threadIdx.x & ~31u) >= max(TOP ? parts * a.k : 1, 1)) return;
+    if ((int)(threadIdx.x & ~31u) >= (TOP ? a.k : 1)) return;
     const bool none = E != E || M > 3.402823466e38f, empty = !none && E == 0.0f;
     const double l2 = none ? (double)NAN : empty ? (double)kNegInf : log2((double)E);
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && part == 0) {
         if (a.logprob) {
             const int64_t t = index_at(a.tokens, row, a.index64);
             a.logprob[row] = t < 0 ? 0.0f : t >= a.vocab || none ? NAN : empty ? kNegInf
@@ -569,13 +579,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
         if (a.lse) a.lse[row] = (float)(((all.far ? (double)all.m * a.scale2 : (double)all.c * (a.scale2 / (double)s)) + l2) * kLn2);
     }
     if (!TOP) return;
-    for (int t = threadIdx.x; t < parts * a.k; t += NT) {
-        const int r = t / a.k, j = t - r * a.k;
-        if (none || j >= sums[r].n) continue;
-        const uint64_t key = lists[t];
+    for (int j = threadIdx.x; j < (none ? 0 : sums[part].n); j += NT) {
+        const uint64_t key = lists[part * a.k + j];
         int at = j;
         for (int o = 0; o < parts; ++o) {
-            if (o == r) continue;
+            if (o == part) continue;
             int lo = 0, hi = sums[o].n;              // first entry of list o that is not greater
             while (lo < hi) {
                 const int mid = (lo + hi) >> 1;
@@ -588,7 +596,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
             a.top_logprobs[row * a.k + at] = (float)((exponent64(key_value(key), all, s) - l2) * kLn2);
         }
     }
-    for (int t = threadIdx.x; t < a.k; t += NT)
+    for (int t = threadIdx.x; t < a.k && part == 0; t += NT)
         if (none || t >= total) {
             store_index(a.top_ids, row * a.k + t, a.index64, -1);
             a.top_logprobs[row * a.k + t] = none ? NAN : kNegInf;
