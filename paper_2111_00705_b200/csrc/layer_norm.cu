@@ -1,8 +1,8 @@
 // Layer norm, forward and backward.
 //
 // Both are bound by memory: a row is read once and its output written once.  An SM runs one block
-// of 768 threads in groups; a group works on a row at a time, every thread on 8 or 16 of its
-// elements.  Rows reach a group through a ring of stages in shared memory, filled by bulk copies
+// of 512 or 768 threads in groups; a group works on a row at a time, every thread on 8, 16 or 24 of
+// its elements.  Rows reach a group through a ring of stages in shared memory, filled by bulk copies
 // that its first thread issues several rows ahead, so that what is on its way from memory does not
 // depend on registers or on where the warps are.  A bulk copy moves whole 16-byte vectors: of a row
 // that starts or ends between two it takes the neighbours' bytes along, and only at the very ends
@@ -139,12 +139,12 @@ __device__ __forceinline__ float2 group_sum2(float a, float b, float2 *slot, int
 // ---------------------------------------------------------------------------------------------
 // A thread's N elements of a row, in STEPS steps of E (E / 2 pairs).  W > 1: a step is a unit, unit k
 // of thread t starts at column (t + k THREADS) W.  W = 1: a step is 8 single elements, element e of
-// step k is column t + (8 k + e) THREADS.  With N = 16 a launch has more than 8 THREADS columns, so
-// that the first half of a thread's elements needs no check.
+// step k is column t + (8 k + e) THREADS.  A launch with N = 16 (24) has more than 8 (16) THREADS
+// columns, so that all but a thread's last 8 elements need no check.
 // ---------------------------------------------------------------------------------------------
 template <typename T, int W, int N_, int THREADS>
 struct Mine {
-    static constexpr int N = N_, E = W > 1 ? W : 8, STEPS = N / E, P = E / 2, SURE = N == 16 ? 8 : 0;
+    static constexpr int N = N_, E = W > 1 ? W : 8, STEPS = N / E, P = E / 2, SURE = N > 8 ? N - 8 : 0;
     static __device__ __forceinline__ int column(int k, int e, int t)
     {
         return W > 1 ? (t + k * THREADS) * W + e : t + (k * E + e) * THREADS;
@@ -188,10 +188,24 @@ struct Planes {
     template <int BT>
     static __device__ __forceinline__ void fill(float *p, const AnyVec &v, int cols, float absent)
     {
-        for (int j = threadIdx.x; j < floats; j += BT) {
-            const float f = j >= cols ? 0.0f : v.p ? any_at(v, j) : absent;
-            if (W == 8) p[(j & 4 ? plane : 0) + (j >> 3) * 4 + (j & 3)] = f;
-            else p[j] = f;
+        constexpr int each = (floats + BT - 1) / BT;    // all loads of a thread on their way at once
+        float f[each];
+#pragma unroll
+        for (int i = 0; i < each; ++i) {
+            const int j = threadIdx.x + i * BT;
+            f[i] = j >= cols ? 0.0f : absent;
+            if (v.p && v.type == 0 && j < cols) f[i] = __ldg(static_cast<const float *>(v.p) + j);
+        }
+        if (v.p && v.type != 0)
+#pragma unroll
+            for (int i = 0; i < each; ++i)
+                if (threadIdx.x + i * BT < cols) f[i] = any_at(v, threadIdx.x + i * BT);
+#pragma unroll
+        for (int i = 0; i < each; ++i) {
+            const int j = threadIdx.x + i * BT;
+            if (j >= floats) break;
+            if (W == 8) p[(j & 4 ? plane : 0) + (j >> 3) * 4 + (j & 3)] = f[i];
+            else p[j] = f[i];
         }
     }
     static __device__ __forceinline__ void load(const float *p, int k, int t, float2 (&f)[M::P])
@@ -522,20 +536,32 @@ __global__ void __launch_bounds__(BT, 1) k_norm_backward(NormBackward a, int blo
     float *sums = reinterpret_cast<float *>(smem);              // GROUPS x 2 x cols
     if (GROUPS > 1) __syncthreads();                            // the rings are empty
 #pragma unroll
-    for (int k = 0; k < STEPS; ++k)
+    for (int k = 0; k < STEPS; ++k) {
+        float *gw = sums + (group * 2) * cols, *gb = gw + cols;
+        if (GROUPS > 1 && W > 1) {                              // 16 bytes at a time
+            const int j = M::column(k, 0, t);
+            if (j < cols)
 #pragma unroll
-        for (int e = 0; e < M::E; ++e) {
-            const int j = M::column(k, e, t);
-            const float vw = e & 1 ? aw[k][e / 2].y : aw[k][e / 2].x, vb = e & 1 ? ab[k][e / 2].y : ab[k][e / 2].x;
-            if (j < cols) {
-                if (GROUPS > 1) {
-                    sums[(group * 2) * cols + j] = vw;
-                    sums[(group * 2 + 1) * cols + j] = vb;
-                } else {
-                    leave_sums(a, blockIdx.y, blocks, j, vw, vb);
+                for (int e = 0; e < P; e += 2) {
+                    *reinterpret_cast<float4 *>(gw + j + 2 * e) = make_float4(aw[k][e].x, aw[k][e].y, aw[k][e + 1].x, aw[k][e + 1].y);
+                    *reinterpret_cast<float4 *>(gb + j + 2 * e) = make_float4(ab[k][e].x, ab[k][e].y, ab[k][e + 1].x, ab[k][e + 1].y);
+                }
+        } else {
+#pragma unroll
+            for (int e = 0; e < M::E; ++e) {
+                const int j = M::column(k, e, t);
+                const float vw = e & 1 ? aw[k][e / 2].y : aw[k][e / 2].x, vb = e & 1 ? ab[k][e / 2].y : ab[k][e / 2].x;
+                if (j < cols) {
+                    if (GROUPS > 1) {
+                        gw[j] = vw;
+                        gb[j] = vb;
+                    } else {
+                        leave_sums(a, blockIdx.y, blocks, j, vw, vb);
+                    }
                 }
             }
         }
+    }
     if (GROUPS > 1) {
         __syncthreads();
         for (int j = threadIdx.x; j < cols; j += BT) {
@@ -550,29 +576,32 @@ __global__ void __launch_bounds__(BT, 1) k_norm_backward(NormBackward a, int blo
     }
 }
 
-// The blocks' sums of a group, added in the order of the blocks: 32 columns a block, the 32 warps
-// a share of the blocks each.
-__global__ void __launch_bounds__(1024) k_norm_sums(NormBackward a, int blocks)
+// The blocks' sums of a group, added in the order of the blocks: 32 columns a block, its 8 warps a
+// share of the blocks each.
+constexpr int kSumWarps = 8;
+
+__global__ void __launch_bounds__(32 * kSumWarps) k_norm_sums(NormBackward a, int blocks)
 {
-    __shared__ float sh[32][33];
+    __shared__ float sh[kSumWarps][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t j = (int64_t)blockIdx.x * 32 + lane, n = 2 * a.cols;      // columns of dweight, then of dbias
     const float *p = a.parts + blockIdx.y * (int64_t)blocks * n + j;
-    const int share = (blocks + 31) / 32, lo = warp * share, hi = min(blocks, lo + share);
+    const int share = (blocks + kSumWarps - 1) / kSumWarps, lo = warp * share, hi = min(blocks, lo + share);
     grid_dep_wait();
     float s = 0.0f;
     if (j < n)
-#pragma unroll 8
+#pragma unroll 10
         for (int b = lo; b < hi; ++b) s += __ldcg(p + b * n);
     sh[warp][lane] = s;
     __syncthreads();
-    s = warp_sum(sh[lane][warp]);                       // column `warp` of the block's 32
-    const int64_t c = (int64_t)blockIdx.x * 32 + warp;
-    if (lane == 0 && c < n) {
-        if (c < a.cols) {
-            if (a.dweight) store_grad(a.dweight, blockIdx.y * a.dweight_stride + c, a.grad_type, a.accumulate, s);
+    if (warp == 0 && j < n) {
+        s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kSumWarps; ++w) s += sh[w][lane];
+        if (j < a.cols) {
+            if (a.dweight) store_grad(a.dweight, blockIdx.y * a.dweight_stride + j, a.grad_type, a.accumulate, s);
         } else if (a.dbias) {
-            store_grad(a.dbias, blockIdx.y * a.dbias_stride + c - a.cols, a.grad_type, a.accumulate, s);
+            store_grad(a.dbias, blockIdx.y * a.dbias_stride + j - a.cols, a.grad_type, a.accumulate, s);
         }
     }
 }
@@ -689,12 +718,12 @@ static void forward(const NormForward &a, cudaStream_t st)
 {
     constexpr int W = Vec<T>::n;
     if (a.cols % W == 0 && aligned(a.x, a.x_stride, a.rows, sizeof(T)) && aligned(a.y, a.y_stride, a.rows, sizeof(T))) {
-        if (try_forward<T, W, 8, 32, 768>(a, st) || try_forward<T, W, 16, 32, 768>(a, st) || try_forward<T, W, 8, 96, 768>(a, st) ||
+        if (try_forward<T, W, 8, 32, 768>(a, st) || try_forward<T, W, 16, 32, 768>(a, st) || try_forward<T, W, 24, 32, 768>(a, st) ||
             try_forward<T, W, 16, 64, 768>(a, st) || try_forward<T, W, 16, 128, 768>(a, st) ||
             try_forward<T, W, 16, 256, 768>(a, st) || try_forward<T, W, 16, 512, 512>(a, st))
             return;
     } else if (try_forward<T, 1, 8, 32, 768>(a, st) || try_forward<T, 1, 16, 32, 768>(a, st) ||
-               try_forward<T, 1, 16, 64, 768>(a, st) || try_forward<T, 1, 16, 128, 768>(a, st) ||
+               try_forward<T, 1, 24, 32, 768>(a, st) || try_forward<T, 1, 16, 64, 768>(a, st) || try_forward<T, 1, 16, 128, 768>(a, st) ||
                try_forward<T, 1, 16, 256, 768>(a, st) || try_forward<T, 1, 16, 512, 512>(a, st)) {
         return;
     }
@@ -718,7 +747,7 @@ static bool try_backward(const NormBackward &a, int blocks, cudaStream_t st)
     cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     kernel<<<dim3((unsigned)blocks, (unsigned)a.groups), BT, smem, st>>>(a, blocks, r);
     if (blocks > 1 && (a.dweight || a.dbias))
-        launch_after(k_norm_sums, dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)a.groups), dim3(1024), 0, st, a, blocks);
+        launch_after(k_norm_sums, dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)a.groups), dim3(32 * kSumWarps), 0, st, a, blocks);
     return true;
 }
 
