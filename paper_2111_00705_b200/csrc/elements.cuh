@@ -145,7 +145,6 @@ template <> struct Vec<float> {
         return make_uint4(__float_as_uint(max_nan(__uint_as_float(u.x), t)), __float_as_uint(max_nan(__uint_as_float(u.y), t)),
                           __float_as_uint(max_nan(__uint_as_float(u.z), t)), __float_as_uint(max_nan(__uint_as_float(u.w), t)));
     }
-    static __device__ __forceinline__ bool reaches(running a, running t) { return a >= t; }
 };
 
 template <> struct Vec<bf16> {
@@ -184,7 +183,6 @@ template <> struct Vec<bf16> {
         return make_uint4(word(__hmax2_nan(two(u.x), t)), word(__hmax2_nan(two(u.y), t)), word(__hmax2_nan(two(u.z), t)),
                           word(__hmax2_nan(two(u.w), t)));
     }
-    static __device__ __forceinline__ bool reaches(running a, running t) { return !__hblt2(a, t); }
 };
 
 template <> struct Vec<f16> {
@@ -220,20 +218,8 @@ template <> struct Vec<f16> {
         return make_uint4(word(__hmax2_nan(two(u.x), t)), word(__hmax2_nan(two(u.y), t)), word(__hmax2_nan(two(u.z), t)),
                           word(__hmax2_nan(two(u.w), t)));
     }
-    static __device__ __forceinline__ bool reaches(running a, running t) { return !__hblt2(a, t); }
 };
 
 template <typename T> __device__ __forceinline__ T minus_inf() { return narrow<T>(kNegInf); }
-
-// 16 bytes global -> shared without passing through registers; complete for the issuing thread
-// after copies_done().
-__device__ __forceinline__ void copy16(void *dst, const void *src)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copies_done()
-{
-    asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
-}
 
 }  // namespace cdadam
