@@ -87,27 +87,6 @@ __device__ __forceinline__ void group_barrier(int group)
     if (THREADS == 32) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(THREADS) : "memory");
 }
-template <int THREADS>
-__device__ __forceinline__ float group_sum(float v, float *slot, int group)
-{
-    constexpr int N = THREADS / 32;
-    v = warp_sum(v);
-    if (N == 1) return v;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32 % N;
-    if (lane == 0) slot[warp] = v;
-    group_barrier<THREADS>(group);
-    if (N <= 4) {
-        v = slot[0];
-#pragma unroll
-        for (int i = 1; i < N; ++i) v += slot[i];
-        return v;
-    }
-    v = slot[lane % N];
-#pragma unroll
-    for (int d = N / 2; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-    return v;
-}
-
 // Two sums at once: after the first exchange the lower half of a warp carries one, the upper half
 // the other.
 template <int THREADS>
@@ -242,7 +221,8 @@ __device__ __forceinline__ float inverse_root(float v)
 }
 
 // ---------------------------------------------------------------------------------------------
-// Forward.
+// Forward.  A group works on two rows at a time: their sums go through the same shuffles and
+// barriers, and parameters are taken from shared memory once for both.
 // ---------------------------------------------------------------------------------------------
 template <typename T, int W, int N, int THREADS, int BT>
 __global__ void __launch_bounds__(BT, 1) k_norm(NormForward a, Ring ring)
@@ -251,7 +231,7 @@ __global__ void __launch_bounds__(BT, 1) k_norm(NormForward a, Ring ring)
     typedef Planes<M, W, THREADS> PL;
     constexpr int GROUPS = BT / THREADS;
     extern __shared__ __align__(16) char smem[];        // weight, bias; the rings
-    __shared__ float sh[GROUPS][2][THREADS / 32];
+    __shared__ float2 sh[GROUPS][2][THREADS / 32];
     __shared__ uint64_t bars[GROUPS][kMaxStages];
     const int t = threadIdx.x % THREADS, group = threadIdx.x / THREADS, cols = (int)a.cols;
     const unsigned rows = (unsigned)a.rows, step = gridDim.x * GROUPS * ring.rows;
@@ -295,48 +275,64 @@ __global__ void __launch_bounds__(BT, 1) k_norm(NormForward a, Ring ring)
     for (; row0 < rows; row0 = row0 + (uint64_t)step < rows ? row0 + step : rows) {
         late |= !mbar_wait_bounded(&bars[group][s], phase);
         const int n = min((unsigned)ring.rows, rows - row0);
-        for (int i = 0; i < n; ++i) {
-            const unsigned row = row0 + i;
-            const char *at = stages + s * stage_bytes + i * ring.pitch;
-            const T *staged = W > 1 ? reinterpret_cast<const T *>(at) : x.find(row, at);
-            float2 f[M::STEPS][M::P], v = both(0.0f);
-            if (W == 1 && x.edge(row)) {
-                x.complete(row, at, t, THREADS);
-                group_barrier<THREADS>(group);
-            }
+        for (int i = 0; i < n; i += 2) {
+            const bool two = i + 1 < n;
+            float2 f[2][M::STEPS][M::P], v[2] = {both(0.0f), both(0.0f)};
 #pragma unroll
-            for (int k = 0; k < M::STEPS; ++k) M::load(staged, k, t, cols, f[k]);
-#pragma unroll
-            for (int k = 0; k < M::STEPS; ++k)
-#pragma unroll
-                for (int e = 0; e < M::P; ++e) v = add2(v, f[k][e]);
-            const float mean = group_sum<THREADS>(v.x + v.y, sh[group][0], group) * over;
-            if (i == n - 1 && t < 32 && row0 + (uint64_t)ring.stages * step < rows) start(row0 + ring.stages * step, s);   // all have read
-            v = both(0.0f);
-#pragma unroll
-            for (int k = 0; k < M::STEPS; ++k)
-#pragma unroll
-                for (int e = 0; e < M::P; ++e) {
-                    const float2 d = add2(f[k][e], both(-mean));
-                    if (M::in(k, 2 * e + 1, t, cols)) v = fma2(d, d, v);
-                    else if (W == 1 && M::in(k, 2 * e, t, cols)) v.x = fmaf(d.x, d.x, v.x);
-                    f[k][e] = d;
+            for (int r = 0; r < 2; ++r) {
+                if (r == 1 && !two) break;
+                const unsigned row = row0 + i + r;
+                const char *at = stages + s * stage_bytes + (i + r) * ring.pitch;
+                const T *staged = W > 1 ? reinterpret_cast<const T *>(at) : x.find(row, at);
+                if (W == 1 && x.edge(row)) {
+                    x.complete(row, at, t, THREADS);
+                    group_barrier<THREADS>(group);
                 }
-            float rstd = inverse_root(fmaf(group_sum<THREADS>(v.x + v.y, sh[group][1], group), over, a.eps));
-            if (late) rstd = NAN;                       // a copy that does not arrive within seconds
-            T *y = static_cast<T *>(a.y) + row * a.y_stride;
+#pragma unroll
+                for (int k = 0; k < M::STEPS; ++k) M::load(staged, k, t, cols, f[r][k]);
+#pragma unroll
+                for (int k = 0; k < M::STEPS; ++k)
+#pragma unroll
+                    for (int e = 0; e < M::P; ++e) v[r] = add2(v[r], f[r][k][e]);
+            }
+            const float2 mean = mul2(group_sum2<THREADS>(v[0].x + v[0].y, v[1].x + v[1].y, sh[group][0], group), both(over));
+            if (i + 2 >= n && t < 32 && row0 + (uint64_t)ring.stages * step < rows) start(row0 + ring.stages * step, s);   // all have read
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const float m = r ? mean.y : mean.x;
+                v[r] = both(0.0f);
+                if (r == 1 && !two) break;
+#pragma unroll
+                for (int k = 0; k < M::STEPS; ++k)
+#pragma unroll
+                    for (int e = 0; e < M::P; ++e) {
+                        const float2 d = add2(f[r][k][e], both(-m));
+                        if (M::in(k, 2 * e + 1, t, cols)) v[r] = fma2(d, d, v[r]);
+                        else if (W == 1 && M::in(k, 2 * e, t, cols)) v[r].x = fmaf(d.x, d.x, v[r].x);
+                        f[r][k][e] = d;
+                    }
+            }
+            const float2 squares = group_sum2<THREADS>(v[0].x + v[0].y, v[1].x + v[1].y, sh[group][1], group);
+            float2 rstd = make_float2(inverse_root(fmaf(squares.x, over, a.eps)), inverse_root(fmaf(squares.y, over, a.eps)));
+            if (late) rstd = both(NAN);                 // a copy that does not arrive within seconds
+            T *y = static_cast<T *>(a.y) + (int64_t)(row0 + i) * a.y_stride;
 #pragma unroll
             for (int k = 0; k < M::STEPS; ++k) {
                 float2 pw[M::P], pb[M::P];
                 PL::load(w, k, t, pw);
                 PL::load(b, k, t, pb);
 #pragma unroll
-                for (int e = 0; e < M::P; ++e) f[k][e] = fma2(mul2(f[k][e], both(rstd)), pw[e], pb[e]);
-                M::store(y, k, t, cols, f[k]);
+                for (int e = 0; e < M::P; ++e) f[0][k][e] = fma2(mul2(f[0][k][e], both(rstd.x)), pw[e], pb[e]);
+                M::store(y, k, t, cols, f[0][k]);
+                if (two) {
+#pragma unroll
+                    for (int e = 0; e < M::P; ++e) f[1][k][e] = fma2(mul2(f[1][k][e], both(rstd.y)), pw[e], pb[e]);
+                    M::store(y + a.y_stride, k, t, cols, f[1][k]);
+                }
             }
-            if (t == 0) {
-                if (a.mean) a.mean[row] = mean;
-                if (a.rstd) a.rstd[row] = rstd;
+            if (t < (two ? 2 : 1)) {
+                if (a.mean) a.mean[row0 + i + t] = t ? mean.y : mean.x;
+                if (a.rstd) a.rstd[row0 + i + t] = t ? rstd.y : rstd.x;
             }
         }
         if (++s == ring.stages) { s = 0; phase ^= 1; }
@@ -682,13 +678,13 @@ static bool aligned(const void *p, int64_t stride, int64_t rows, int size)
     return ((uintptr_t)p & 15) == 0 && (rows <= 1 || stride * size % 16 == 0);
 }
 
-// Rows in chunks of about 4 KB (one row where it is longer), fewer where that would leave groups
+// Rows in chunks of about 4 KB (`least` rows where they are longer), fewer where that would leave groups
 // without a chunk; two stages to six, until the rings take 160 KB or the shared memory is full.
-static Ring ring_of(int64_t rows, int64_t groups, int pitch, int all_groups_and_matrices, int parameter_bytes)
+static Ring ring_of(int64_t rows, int64_t groups, int pitch, int all_groups_and_matrices, int parameter_bytes, int least)
 {
     Ring r;
     r.pitch = pitch;
-    r.rows = pitch >= 4096 ? 1 : 4096 / pitch;
+    r.rows = pitch * least >= 4096 ? least : 4096 / pitch;
     if (r.rows > 32) r.rows = 32;
     if (r.rows > rows / groups) r.rows = rows / groups < 1 ? 1 : (int)(rows / groups);
     while (r.rows > 1 && r.rows * pitch * all_groups_and_matrices > 80 * 1024) --r.rows;
@@ -704,11 +700,11 @@ static bool try_forward(const NormForward &a, cudaStream_t st)
     if (a.cols > (int64_t)N * THREADS) return false;
     constexpr int groups = BT / THREADS;
     const int cols = (int)a.cols;
-    const Ring r = ring_of(a.rows, (int64_t)kSMs * groups, row_pitch(cols, sizeof(T)), groups, 2 * N * THREADS * 4);
+    const Ring r = ring_of(a.rows, (int64_t)kSMs * groups, row_pitch(cols, sizeof(T)), groups, 2 * N * THREADS * 4, 2);
     const int64_t need = ((a.rows + r.rows - 1) / r.rows + groups - 1) / groups;
     const int smem = 2 * N * THREADS * 4 + r.stages * r.rows * r.pitch * groups;
     auto *kernel = k_norm<T, W, N, THREADS, BT>;
-    cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    allow_shared(kernel, smem);
     kernel<<<(unsigned)(need < kSMs ? need : kSMs), BT, smem, st>>>(a, r);
     return true;
 }
@@ -718,12 +714,12 @@ static void forward(const NormForward &a, cudaStream_t st)
 {
     constexpr int W = Vec<T>::n;
     if (a.cols % W == 0 && aligned(a.x, a.x_stride, a.rows, sizeof(T)) && aligned(a.y, a.y_stride, a.rows, sizeof(T))) {
-        if (try_forward<T, W, 8, 32, 768>(a, st) || try_forward<T, W, 16, 32, 768>(a, st) || try_forward<T, W, 24, 32, 768>(a, st) ||
+        if (try_forward<T, W, 8, 32, 768>(a, st) || try_forward<T, W, 16, 32, 768>(a, st) || try_forward<T, W, 24, 32, 512>(a, st) ||
             try_forward<T, W, 16, 64, 768>(a, st) || try_forward<T, W, 16, 128, 768>(a, st) ||
             try_forward<T, W, 16, 256, 768>(a, st) || try_forward<T, W, 16, 512, 512>(a, st))
             return;
     } else if (try_forward<T, 1, 8, 32, 768>(a, st) || try_forward<T, 1, 16, 32, 768>(a, st) ||
-               try_forward<T, 1, 24, 32, 768>(a, st) || try_forward<T, 1, 16, 64, 768>(a, st) || try_forward<T, 1, 16, 128, 768>(a, st) ||
+               try_forward<T, 1, 24, 32, 512>(a, st) || try_forward<T, 1, 16, 64, 768>(a, st) || try_forward<T, 1, 16, 128, 768>(a, st) ||
                try_forward<T, 1, 16, 256, 768>(a, st) || try_forward<T, 1, 16, 512, 512>(a, st)) {
         return;
     }
@@ -737,14 +733,14 @@ static bool try_backward(const NormBackward &a, int blocks, cudaStream_t st)
     constexpr int groups = BT / THREADS;
     const int64_t per = a.rows / a.groups;
     const int cols = (int)a.cols;
-    const Ring r = ring_of(per, (int64_t)blocks * groups, row_pitch(cols, sizeof(T)), 2 * groups, N * THREADS * 4);
+    const Ring r = ring_of(per, (int64_t)blocks * groups, row_pitch(cols, sizeof(T)), 2 * groups, N * THREADS * 4, 1);
     const int64_t most = ((per + r.rows - 1) / r.rows + groups - 1) / groups;
     if (blocks > most) blocks = (int)most;
     if (blocks < 1) blocks = 1;
     const int rings = N * THREADS * 4 + 2 * r.stages * r.rows * r.pitch * groups, sums = groups > 1 ? groups * 2 * cols * 4 : 0;
     const int smem = rings > sums ? rings : sums;
     auto *kernel = k_norm_backward<T, W, N, THREADS, BT>;
-    cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    allow_shared(kernel, smem);
     kernel<<<dim3((unsigned)blocks, (unsigned)a.groups), BT, smem, st>>>(a, blocks, r);
     if (blocks > 1 && (a.dweight || a.dbias))
         launch_after(k_norm_sums, dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)a.groups), dim3(32 * kSumWarps), 0, st, a, blocks);

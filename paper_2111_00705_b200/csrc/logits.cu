@@ -986,7 +986,7 @@ static int log_parts_for_slices(int64_t bytes)
 template <typename F>
 static void launch_rows(F kernel, int64_t rows, int parts, int threads, size_t smem, cudaStream_t st, const void *args[])
 {
-    cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    allow_shared(kernel, smem);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows * parts));
     cfg.blockDim = dim3((unsigned)threads);

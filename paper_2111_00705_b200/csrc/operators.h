@@ -7,6 +7,16 @@
 
 namespace cdadam {
 
+// Lets `kernel` be launched with `bytes` of dynamic shared memory.  Up to 48 KB, of which its static
+// shared memory takes a few, that needs no call.
+// (A call for every launch costs the host less than a microsecond; no state is kept, so that any
+// thread may launch on any device.)
+template <typename F>
+inline void allow_shared(F *kernel, size_t bytes)
+{
+    if (bytes > 40 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
 // A read-only vector of any of the three element types, widened at every access.
 struct AnyVec {
     const void *p;      // NULL: not given
