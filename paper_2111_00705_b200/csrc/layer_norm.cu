@@ -108,9 +108,10 @@ __device__ __forceinline__ float2 group_sum2(float a, float b, float2 *slot, int
         for (int i = 1; i < N; ++i) s = add2(s, slot[i]);
         return s;
     }
-    v = at[2 * (lane % N) + (upper ? 1 : 0)];       // N is 8 or 16: both halves of the warp cover all warps
+    // each half of the warp adds up one of the sums: lane l of it has warp l's
+    v = (lane & 15) < N ? at[2 * (lane & 15) + (upper ? 1 : 0)] : 0.0f;
 #pragma unroll
-    for (int d = (N > 16 ? 16 : N) / 2; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    for (int d = 8; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
     return make_float2(__shfl_sync(0xffffffffu, v, 0), __shfl_sync(0xffffffffu, v, 16));
 }
 
@@ -716,11 +717,11 @@ static void forward(const NormForward &a, cudaStream_t st)
     if (a.cols % W == 0 && aligned(a.x, a.x_stride, a.rows, sizeof(T)) && aligned(a.y, a.y_stride, a.rows, sizeof(T))) {
         if (try_forward<T, W, 8, 32, 768>(a, st) || try_forward<T, W, 16, 32, 768>(a, st) || try_forward<T, W, 24, 32, 512>(a, st) ||
             try_forward<T, W, 16, 64, 768>(a, st) || try_forward<T, W, 16, 128, 768>(a, st) ||
-            try_forward<T, W, 16, 256, 768>(a, st) || try_forward<T, W, 16, 512, 512>(a, st))
+            try_forward<T, W, 16, 256, 768>(a, st) || try_forward<T, W, 16, 384, 768>(a, st) || try_forward<T, W, 16, 512, 512>(a, st))
             return;
     } else if (try_forward<T, 1, 8, 32, 768>(a, st) || try_forward<T, 1, 16, 32, 768>(a, st) ||
                try_forward<T, 1, 24, 32, 512>(a, st) || try_forward<T, 1, 16, 64, 768>(a, st) || try_forward<T, 1, 16, 128, 768>(a, st) ||
-               try_forward<T, 1, 16, 256, 768>(a, st) || try_forward<T, 1, 16, 512, 512>(a, st)) {
+               try_forward<T, 1, 16, 256, 768>(a, st) || try_forward<T, 1, 16, 384, 768>(a, st) || try_forward<T, 1, 16, 512, 512>(a, st)) {
         return;
     }
     k_norm_long<T><<<(unsigned)a.rows, kLongBlock, 0, st>>>(a);
@@ -761,7 +762,7 @@ static void backward(const NormBackward &a, cudaStream_t st)
             return;
     } else if (try_backward<T, 1, 8, 32, 768>(a, n, st) || try_backward<T, 1, 16, 32, 512>(a, n, st) ||
                try_backward<T, 1, 16, 64, 512>(a, n, st) || try_backward<T, 1, 16, 128, 512>(a, n, st) ||
-               try_backward<T, 1, 16, 256, 512>(a, n, st) || try_backward<T, 1, 16, 512, 512>(a, n, st)) {
+               try_backward<T, 1, 16, 256, 512>(a, n, st) || try_backward<T, 1, 16, 320, 640>(a, n, st) || try_backward<T, 1, 16, 512, 512>(a, n, st)) {
         return;
     }
     if (a.dweight || a.dbias)
