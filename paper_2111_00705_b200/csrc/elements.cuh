@@ -191,6 +191,7 @@ template <> struct Vec<f16> {
     typedef __half2 running;
     static __device__ __forceinline__ __half2 two(uint32_t w) { return *reinterpret_cast<__half2 *>(&w); }
     static __device__ __forceinline__ running lowest() { return two(0xFC00FC00u); }
+    static __device__ __forceinline__ float2 up(uint32_t w) { return __half22float2(two(w)); }
     static __device__ __forceinline__ void wide(const uint4 &u, float2 (&f)[4])
     {
         f[0] = __half22float2(two(u.x)); f[1] = __half22float2(two(u.y));

@@ -1,15 +1,16 @@
 // Layer norm, forward and backward.
 //
 // Both are bound by memory: a row is read once and its output written once.  An SM runs one block
-// of 512 or 768 threads in groups; a group works on a row at a time, every thread on 8, 16 or 24 of
-// its elements.  Rows reach a group through a ring of stages in shared memory, filled by bulk copies
+// of 512 to 768 threads in groups; a group works on a row or two at a time, every thread on 8, 16 or
+// 24 elements of a row.  Rows reach a group through a ring of stages in shared memory, filled by bulk copies
 // that its first thread issues several rows ahead, so that what is on its way from memory does not
 // depend on registers or on where the warps are.  A bulk copy moves whole 16-byte vectors: of a row
 // that starts or ends between two it takes the neighbours' bytes along, and only at the very ends
 // of the matrix, where there are none, the row's last elements are read from memory directly.
 //
 // Elements are taken from the stage in units of W consecutive ones: 16 bytes where every row
-// starts on a multiple of 16 bytes and is a whole number of units, else one by one.
+// starts on a multiple of 16 bytes and is a whole number of units, else two where rows allow that,
+// else one by one.
 #include "elements.cuh"
 
 namespace cdadam {
@@ -70,6 +71,7 @@ struct Rows {
         T *to = const_cast<T *>(find(r, at));
         for (int j = t; j < cols; j += n)
             if ((uintptr_t)(row(r) + j) < lo || (uintptr_t)(row(r) + j) >= hi) to[j] = row(r)[j];
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // a later copy writes there
     }
 };
 
@@ -116,30 +118,48 @@ __device__ __forceinline__ float2 group_sum2(float a, float b, float2 *slot, int
 }
 
 
+// Two adjacent elements (their address a multiple of their size together).
+template <typename T> struct Two {
+    static __device__ __forceinline__ float2 wide(const T *p) { return Vec<T>::up(*reinterpret_cast<const uint32_t *>(p)); }
+    static __device__ __forceinline__ void store(T *p, float2 f) { *reinterpret_cast<uint32_t *>(p) = Vec<T>::down(f); }
+};
+template <> struct Two<float> {
+    static __device__ __forceinline__ float2 wide(const float *p) { return *reinterpret_cast<const float2 *>(p); }
+    static __device__ __forceinline__ void store(float *p, float2 f) { *reinterpret_cast<float2 *>(p) = f; }
+};
+
 // ---------------------------------------------------------------------------------------------
-// A thread's N elements of a row, in STEPS steps of E (E / 2 pairs).  W > 1: a step is a unit, unit k
-// of thread t starts at column (t + k THREADS) W.  W = 1: a step is 8 single elements, element e of
-// step k is column t + (8 k + e) THREADS.  A launch with N = 16 (24) has more than 8 (16) THREADS
-// columns, so that all but a thread's last 8 elements need no check.
+// A thread's N elements of a row, in STEPS steps of E (E / 2 pairs).  BIG (W elements are 16 bytes):
+// a step is a unit, unit k of thread t starts at column (t + k THREADS) W.  W = 1 and 2: a step is
+// 8 / W units, unit i of step k starts at column (t + (8 k / W + i) THREADS) W.  A launch with N =
+// 16 (24) has more than 8 (16) THREADS columns, so that all but a thread's last 8 elements need no
+// check.
 // ---------------------------------------------------------------------------------------------
 template <typename T, int W, int N_, int THREADS>
 struct Mine {
-    static constexpr int N = N_, E = W > 1 ? W : 8, STEPS = N / E, P = E / 2, SURE = N > 8 ? N - 8 : 0;
+    static constexpr bool BIG = W * sizeof(T) == 16;
+    static constexpr int N = N_, E = BIG ? W : 8, STEPS = N / E, P = E / 2, SURE = N > 8 ? N - 8 : 0;
     static __device__ __forceinline__ int column(int k, int e, int t)
     {
-        return W > 1 ? (t + k * THREADS) * W + e : t + (k * E + e) * THREADS;
+        return BIG ? (t + k * THREADS) * W + e : (t + (k * (E / W) + e / W) * THREADS) * W + e % W;
     }
-    static __device__ __forceinline__ bool in(int k, int e, int t, int cols)
+    static __device__ __forceinline__ bool in(int k, int e, int t, int cols)    // rows are whole units
     {
-        return k * E + e < SURE || column(k, W > 1 ? 0 : e, t) < cols;
+        return k * E + e / W * W < SURE || column(k, e / W * W, t) < cols;
     }
     // From the stage; 0 beyond the row.
     static __device__ __forceinline__ void load(const T *staged, int k, int t, int cols, float2 (&f)[P])
     {
-        if constexpr (W > 1) {
+        if constexpr (BIG) {
             uint4 u = make_uint4(0, 0, 0, 0);
             if (in(k, 0, t, cols)) u = *reinterpret_cast<const uint4 *>(staged + column(k, 0, t));
             Vec<T>::wide(u, f);
+        } else if constexpr (W == 2) {
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                f[e / 2] = both(0.0f);
+                if (in(k, e, t, cols)) f[e / 2] = Two<T>::wide(staged + column(k, e, t));
+            }
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -150,8 +170,12 @@ struct Mine {
     }
     static __device__ __forceinline__ void store(T *row, int k, int t, int cols, const float2 (&f)[P])
     {
-        if constexpr (W > 1) {
+        if constexpr (BIG) {
             if (in(k, 0, t, cols)) __stcs(reinterpret_cast<uint4 *>(row + column(k, 0, t)), Vec<T>::pack(f));
+        } else if constexpr (W == 2) {
+#pragma unroll
+            for (int e = 0; e < E; e += 2)
+                if (in(k, e, t, cols)) Two<T>::store(row + column(k, e, t), f[e / 2]);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e)
@@ -190,13 +214,16 @@ struct Planes {
     }
     static __device__ __forceinline__ void load(const float *p, int k, int t, float2 (&f)[M::P])
     {
-        if constexpr (W > 1) {
+        if constexpr (M::BIG) {
 #pragma unroll
             for (int h = 0; h < W / 4; ++h) {
                 const float4 q = *reinterpret_cast<const float4 *>(p + h * plane + (t + k * THREADS) * 4);
                 f[2 * h] = make_float2(q.x, q.y);
                 f[2 * h + 1] = make_float2(q.z, q.w);
             }
+        } else if constexpr (W == 2) {
+#pragma unroll
+            for (int e = 0; e < M::E; e += 2) f[e / 2] = *reinterpret_cast<const float2 *>(p + M::column(k, e, t));
         } else {
 #pragma unroll
             for (int e = 0; e < M::E; ++e) {
@@ -247,7 +274,7 @@ __global__ void __launch_bounds__(BT, 1) k_norm(NormForward a, Ring ring)
     auto start = [&](unsigned r, int s) {
         const int n = min((unsigned)ring.rows, rows - r);
         char *to = stages + s * stage_bytes + t * ring.pitch;
-        if (W > 1) {                                    // rows of whole vectors
+        if (M::BIG) {                                   // rows of whole vectors
             if (t == 0) mbar_arrive_expect_tx(&bars[group][s], n * row_bytes);
             __syncwarp();
             if (t < n) bulk_copy_g2s(to, x.row(r + t), row_bytes, &bars[group][s]);
@@ -286,8 +313,8 @@ __global__ void __launch_bounds__(BT, 1) k_norm(NormForward a, Ring ring)
                 if (r == 1 && !two) break;
                 const unsigned row = row0 + i + r;
                 const char *at = stages + s * stage_bytes + (i + r) * ring.pitch;
-                const T *staged = W > 1 ? reinterpret_cast<const T *>(at) : x.find(row, at);
-                if (W == 1 && x.edge(row)) {
+                const T *staged = M::BIG ? reinterpret_cast<const T *>(at) : x.find(row, at);
+                if (!M::BIG && x.edge(row)) {
                     x.complete(row, at, t, THREADS);
                     group_barrier<THREADS>(group);
                 }
@@ -430,7 +457,7 @@ __global__ void __launch_bounds__(BT, 1) k_norm_backward(NormBackward a, int blo
     auto start = [&](unsigned r, int s) {
         const int n = min((unsigned)ring.rows, end - r);
         char *to = stages + s * stage_bytes + t * ring.pitch;
-        if (W > 1) {                                    // rows of whole vectors
+        if (M::BIG) {                                   // rows of whole vectors
             if (t == 0) mbar_arrive_expect_tx(&bars[group][s], 2 * n * row_bytes);
             __syncwarp();
             if (t < n) {
@@ -483,9 +510,9 @@ __global__ void __launch_bounds__(BT, 1) k_norm_backward(NormBackward a, int blo
             float rstd = __shfl_sync(0xffffffffu, rstds, i);
             if (late) rstd = NAN;                       // a copy that does not arrive within seconds
             const char *at = stages + s * stage_bytes + i * ring.pitch;
-            const T *sx = W > 1 ? reinterpret_cast<const T *>(at) : x.find(row, at);
-            const T *sd = W > 1 ? reinterpret_cast<const T *>(at + half) : dy.find(row, at + half);
-            if (W == 1 && (x.edge(row) || dy.edge(row))) {
+            const T *sx = M::BIG ? reinterpret_cast<const T *>(at) : x.find(row, at);
+            const T *sd = M::BIG ? reinterpret_cast<const T *>(at + half) : dy.find(row, at + half);
+            if (!M::BIG && (x.edge(row) || dy.edge(row))) {
                 x.complete(row, at, t, THREADS);
                 dy.complete(row, at + half, t, THREADS);
                 group_barrier<THREADS>(group);
@@ -540,7 +567,7 @@ __global__ void __launch_bounds__(BT, 1) k_norm_backward(NormBackward a, int blo
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) {
         float *gw = sums + (group * 2) * cols, *gb = gw + cols;
-        if (GROUPS > 1 && W > 1) {                              // 16 bytes at a time
+        if (GROUPS > 1 && M::BIG) {                             // 16 bytes at a time
             const int j = M::column(k, 0, t);
             if (j < cols)
 #pragma unroll
@@ -678,10 +705,10 @@ int64_t layer_norm_workspace(int64_t rows, int64_t cols, int64_t groups)
     return n > 1 ? groups * n * cols * 8 : 0;
 }
 
-// Whether every row of a matrix starts on 16 bytes.
-static bool aligned(const void *p, int64_t stride, int64_t rows, int size)
+// Whether every row of a matrix starts on a multiple of `to` bytes.
+static bool aligned(const void *p, int64_t stride, int64_t rows, int size, int to)
 {
-    return ((uintptr_t)p & 15) == 0 && (rows <= 1 || stride * size % 16 == 0);
+    return (uintptr_t)p % to == 0 && (rows <= 1 || stride * size % to == 0);
 }
 
 // Rows in chunks of about 4 KB (`least` rows where they are longer), fewer where that would leave groups
@@ -715,20 +742,23 @@ static bool try_forward(const NormForward &a, cudaStream_t st)
     return true;
 }
 
+// Rows that start on 16 bytes and are whole units of that go by those, others of an even number of
+// elements that start on two by two (20000 x 1022 bf16 25 us, one by one 29; 20000 x 4098 112 and
+// 138 us; backward of 32768 x 4090 211 and 233 us), the rest one by one.
+template <typename T, int W>
+static bool forward_by(const NormForward &a, cudaStream_t st)
+{
+    const int to = W * (int)sizeof(T);
+    if (a.cols % W || !aligned(a.x, a.x_stride, a.rows, sizeof(T), to) || !aligned(a.y, a.y_stride, a.rows, sizeof(T), to)) return false;
+    return try_forward<T, W, 8, 32, 768>(a, st) || try_forward<T, W, 16, 32, 768>(a, st) || try_forward<T, W, 24, 32, 512>(a, st) ||
+           try_forward<T, W, 16, 64, 768>(a, st) || try_forward<T, W, 16, 128, 768>(a, st) || try_forward<T, W, 16, 256, 768>(a, st) ||
+           try_forward<T, W, 16, 384, 768>(a, st) || try_forward<T, W, 16, 512, 512>(a, st);
+}
+
 template <typename T>
 static void forward(const NormForward &a, cudaStream_t st)
 {
-    constexpr int W = Vec<T>::n;
-    if (a.cols % W == 0 && aligned(a.x, a.x_stride, a.rows, sizeof(T)) && aligned(a.y, a.y_stride, a.rows, sizeof(T))) {
-        if (try_forward<T, W, 8, 32, 768>(a, st) || try_forward<T, W, 16, 32, 768>(a, st) || try_forward<T, W, 24, 32, 512>(a, st) ||
-            try_forward<T, W, 16, 64, 768>(a, st) || try_forward<T, W, 16, 128, 768>(a, st) ||
-            try_forward<T, W, 16, 256, 768>(a, st) || try_forward<T, W, 16, 384, 768>(a, st) || try_forward<T, W, 16, 512, 512>(a, st))
-            return;
-    } else if (try_forward<T, 1, 8, 32, 768>(a, st) || try_forward<T, 1, 16, 32, 768>(a, st) ||
-               try_forward<T, 1, 24, 32, 512>(a, st) || try_forward<T, 1, 16, 64, 768>(a, st) || try_forward<T, 1, 16, 128, 768>(a, st) ||
-               try_forward<T, 1, 16, 256, 768>(a, st) || try_forward<T, 1, 16, 384, 768>(a, st) || try_forward<T, 1, 16, 512, 512>(a, st)) {
-        return;
-    }
+    if (forward_by<T, Vec<T>::n>(a, st) || forward_by<T, 2>(a, st) || forward_by<T, 1>(a, st)) return;
     k_norm_long<T><<<(unsigned)a.rows, kLongBlock, 0, st>>>(a);
 }
 
@@ -753,23 +783,29 @@ static bool try_backward(const NormBackward &a, int blocks, cudaStream_t st)
     return true;
 }
 
+template <typename T, int W>
+static bool backward_by(const NormBackward &a, int n, cudaStream_t st)
+{
+    const int to = W * (int)sizeof(T);
+    if (a.cols % W || !aligned(a.x, a.x_stride, a.rows, sizeof(T), to) || !aligned(a.dy, a.dy_stride, a.rows, sizeof(T), to) ||
+        (a.dx && !aligned(a.dx, a.dx_stride, a.rows, sizeof(T), to)))
+        return false;
+    if (try_backward<T, W, 8, 32, 768>(a, n, st) || try_backward<T, W, 16, 32, 512>(a, n, st)) return true;
+    if constexpr (W * sizeof(T) == 16)
+        if (try_backward<T, W, 8, 96, 768>(a, n, st)) return true;
+    if (try_backward<T, W, 16, 64, 512>(a, n, st) || try_backward<T, W, 16, 128, 512>(a, n, st) ||
+        try_backward<T, W, 16, 256, 512>(a, n, st))
+        return true;
+    if constexpr (W * sizeof(T) != 16)
+        if (try_backward<T, W, 16, 320, 640>(a, n, st)) return true;
+    return try_backward<T, W, 16, 512, 512>(a, n, st);
+}
+
 template <typename T>
 static void backward(const NormBackward &a, cudaStream_t st)
 {
-    constexpr int W = Vec<T>::n;
     const int n = blocks_per_group(a.rows, a.groups);
-    if (a.cols % W == 0 && aligned(a.x, a.x_stride, a.rows, sizeof(T)) && aligned(a.dy, a.dy_stride, a.rows, sizeof(T)) &&
-        (!a.dx || aligned(a.dx, a.dx_stride, a.rows, sizeof(T)))) {
-        if (try_backward<T, W, 8, 32, 768>(a, n, st) || try_backward<T, W, 16, 32, 512>(a, n, st) ||
-            try_backward<T, W, 8, 96, 768>(a, n, st) || try_backward<T, W, 16, 64, 512>(a, n, st) ||
-            try_backward<T, W, 16, 128, 512>(a, n, st) || try_backward<T, W, 16, 256, 512>(a, n, st) ||
-            try_backward<T, W, 16, 512, 512>(a, n, st))
-            return;
-    } else if (try_backward<T, 1, 8, 32, 768>(a, n, st) || try_backward<T, 1, 16, 32, 512>(a, n, st) ||
-               try_backward<T, 1, 16, 64, 512>(a, n, st) || try_backward<T, 1, 16, 128, 512>(a, n, st) ||
-               try_backward<T, 1, 16, 256, 512>(a, n, st) || try_backward<T, 1, 16, 320, 640>(a, n, st) || try_backward<T, 1, 16, 512, 512>(a, n, st)) {
-        return;
-    }
+    if (backward_by<T, Vec<T>::n>(a, n, st) || backward_by<T, 2>(a, n, st) || backward_by<T, 1>(a, n, st)) return;
     if (a.dweight || a.dbias)
         k_norm_dw<T><<<dim3((unsigned)((a.cols + 31) / 32), (unsigned)a.groups), kNormBlock, 0, st>>>(a);
     if (a.dx && a.rows) k_norm_dx<T><<<(unsigned)a.rows, kLongBlock, 0, st>>>(a);

@@ -2,10 +2,11 @@
 // probable alternatives, its gradient, and distillation from a teacher's listed tokens.
 //
 // A row of logits is what bounds all three: each has to be read once, and its gradient written
-// once.  The sums need the row's maximum first, the gradient needs the sums, so a row is
-// worked on two or three times.  To read it from memory once it is held on the chip: a
-// thread-block cluster of 1, 2, 4 or 8 blocks takes a row, every block a slice of it in its
-// shared memory, and the blocks exchange a few sums through distributed shared memory.
+// once.  The log probabilities read it in one streaming pass with a running maximum and sums, and
+// their gradient needs no more than the saved normaliser.  The distillation's gradient needs the
+// sums of the whole row, so there the row is held on the chip: a thread-block cluster of 1, 2, 4
+// or 8 blocks takes it, every block a slice in its shared memory, and the blocks exchange a few
+// sums through distributed shared memory.
 #include <cooperative_groups.h>
 
 #include "elements.cuh"

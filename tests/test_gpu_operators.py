@@ -182,6 +182,18 @@ def test_norm_backward_every_width(cols, dtype):
         check_backward(dy, x, w[1:], groups)
 
 
+@pytest.mark.parametrize("cols", [2, 10, 66, 250, 258, 514, 766, 770, 1022, 2050, 4090, 4098, 5002, 6146, 8190, 8194])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_norm_rows_that_start_on_two_elements(cols, dtype):
+    g = gen(cols, 5 + len(dtype))
+    for rows, pad, shift, groups in ((1, 0, 0, 1), (6, 0, 2, 3), (35, 2, 0, 1), (300, 4, 2, 2), (7, 6, 4, 7), (4, 1, 0, 2)):
+        x = matrix(rows, cols, TYPES[dtype], g, 1.5, pad, shift)
+        dy = matrix(rows, cols, TYPES[dtype], g, 0.1, 2, shift)
+        w = torch.randn(2 * cols, generator=g, device="cuda")
+        check_norm(x, w[:cols], w[cols:])
+        check_backward(dy, x, w[cols:], groups)
+
+
 @pytest.mark.parametrize("rows,cols,groups", [(16384, 768, 8), (3001, 1021, 1), (5000, 64, 5), (70000, 8, 1), (1200, 4096, 4),
                                               (400, 10001, 2), (300, 16384, 1), (150, 33000, 3), (64, 3000, 64), (1999, 1, 1)])
 @pytest.mark.parametrize("dtype", list(TYPES))
