@@ -11,6 +11,8 @@
 // Elements are taken from the stage in units of W consecutive ones: 16 bytes where every row
 // starts on a multiple of 16 bytes and is a whole number of units, else two where rows allow that,
 // else one by one.
+#include <type_traits>
+
 #include "elements.cuh"
 
 namespace cdadam {
@@ -371,28 +373,85 @@ __global__ void __launch_bounds__(BT, 1) k_norm(NormForward a, Ring ring)
         for (int i = 0; i < ring.stages; ++i) mbar_wait_bounded(&bars[group][i], i < s ? phase : phase ^ 1);
 }
 
-// Rows too long for the registers of a block: three passes, the later two from L2.
-constexpr int kLongBlock = 1024;
+// Rows too long for the registers of a block: three passes, the later two from the caches, by
+// vectors of 16 bytes where rows are whole ones (4000 x 16384 bf16 70 us,
+// 16383 columns, one by one, 148).
+constexpr int kLongBlock = 512;
+
+// V elements: 16 bytes or one.
+template <typename T, int V> struct RawOf { typedef uint4 type; };
+template <typename T> struct RawOf<T, 1> { typedef T type; };
+template <typename T, int V> using Raw = typename RawOf<T, V>::type;
 
 template <typename T>
+__device__ __forceinline__ void widen_all(const uint4 &u, float (&f)[Vec<T>::n])
+{
+    float2 g[Vec<T>::n / 2];
+    Vec<T>::wide(u, g);
+#pragma unroll
+    for (int e = 0; e < Vec<T>::n; ++e) f[e] = e & 1 ? g[e / 2].y : g[e / 2].x;
+}
+template <typename T>
+__device__ __forceinline__ void widen_all(const T &u, float (&f)[1]) { f[0] = widen(u); }
+template <typename T, int V>
+__device__ __forceinline__ void take(const T *p, float (&f)[V]) { widen_all<T>(*reinterpret_cast<const Raw<T, V> *>(p), f); }
+template <typename T, int V>
+__device__ __forceinline__ void put(T *p, const float (&f)[V])
+{
+    if constexpr (V > 1) {
+        float2 g[V / 2];
+#pragma unroll
+        for (int e = 0; e < V; e += 2) g[e / 2] = make_float2(f[e], f[e + 1]);
+        __stcs(reinterpret_cast<uint4 *>(p), Vec<T>::pack(g));
+    } else {
+        *p = narrow<T>(f[0]);
+    }
+}
+template <int V>
+__device__ __forceinline__ void take(const AnyVec &v, int64_t j, float absent, float (&f)[V])
+{
+    if (V > 1 && v.p && v.type == 0 && ((uintptr_t)v.p & 15) == 0) {
+#pragma unroll
+        for (int e = 0; e + 3 < V; e += 4) {
+            const float4 q = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(v.p) + j + e));
+            f[e] = q.x; f[e + 1] = q.y; f[e + 2] = q.z; f[e + 3] = q.w;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[e] = v.p ? any_at(v, j + e) : absent;
+    }
+}
+
+template <typename T, int V>
 __global__ void __launch_bounds__(kLongBlock) k_norm_long(NormForward a)
 {
     __shared__ float sh[2][32];
     const int64_t row = blockIdx.x;
     const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
     T *y = static_cast<T *>(a.y) + row * a.y_stride;
-    float s = 0.0f;
-    for (int64_t j = threadIdx.x; j < a.cols; j += kLongBlock) s += widen(x[j]);
+    float s = 0.0f, f[V], w[V], b[V];
+#pragma unroll 4
+    for (int64_t j = threadIdx.x * V; j < a.cols; j += kLongBlock * V) {
+        take(x + j, f);
+#pragma unroll
+        for (int e = 0; e < V; ++e) s += f[e];
+    }
     const float mean = block_sum_all<kLongBlock>(s, sh[0]) / (float)a.cols;
     s = 0.0f;
-    for (int64_t j = threadIdx.x; j < a.cols; j += kLongBlock) {
-        const float c = widen(x[j]) - mean;
-        s = fmaf(c, c, s);
+#pragma unroll 4
+    for (int64_t j = threadIdx.x * V; j < a.cols; j += kLongBlock * V) {
+        take(x + j, f);
+#pragma unroll
+        for (int e = 0; e < V; ++e) s = fmaf(f[e] - mean, f[e] - mean, s);
     }
     const float rstd = 1.0f / sqrtf(block_sum_all<kLongBlock>(s, sh[1]) / (float)a.cols + a.eps);
-    for (int64_t j = threadIdx.x; j < a.cols; j += kLongBlock) {
-        const float w = a.weight.p ? any_at(a.weight, j) : 1.0f, b = a.bias.p ? any_at(a.bias, j) : 0.0f;
-        y[j] = narrow<T>(fmaf((widen(x[j]) - mean) * rstd, w, b));
+    for (int64_t j = threadIdx.x * V; j < a.cols; j += kLongBlock * V) {
+        take(x + j, f);
+        take(a.weight, j, 1.0f, w);
+        take(a.bias, j, 0.0f, b);
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[e] = fmaf((f[e] - mean) * rstd, w[e], b[e]);
+        put(y + j, f);
     }
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[row] = mean;
@@ -635,34 +694,69 @@ __global__ void __launch_bounds__(32 * kSumWarps) k_norm_sums(NormBackward a, in
     }
 }
 
-// Rows too long for that: the sums over rows first (dx may overwrite what they read), then dx.
+// Rows too long for that: the sums over rows first (dx may overwrite what they read), then dx; V as
+// in k_norm_long.  8192 x 16384 bf16 261 us, where reading x and dy twice takes 205 at the copy
+// rate; 16383 columns, one by one, 696.
+//
+// The sums: a block has 32 V columns and a share of a group's rows, its warps every eighth row of
+// that, AHEAD on their way at a time; the warps' sums are added in order.
 constexpr int kNormBlock = 256;
 
-template <typename T>
-__global__ void __launch_bounds__(kNormBlock) k_norm_dw(NormBackward a)
+template <typename T, int V>
+__global__ void __launch_bounds__(kNormBlock, 3) k_norm_dw(NormBackward a, int blocks)
 {
-    __shared__ float sw[kNormBlock / 32][33], sb[kNormBlock / 32][33];
+    constexpr int WARPS = kNormBlock / 32, AHEAD = V > 1 ? 4 : 8;
+    __shared__ float sw[WARPS][32 * V], sb[WARPS][32 * V];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t j = (int64_t)blockIdx.x * 32 + lane, per = a.rows / a.groups, first = blockIdx.y * per;
-    float w = 0.0f, b = 0.0f;
-    if (j < a.cols)
-        for (int64_t r = first + warp; r < first + per; r += kNormBlock / 32) {
-            const float dy = widen(static_cast<const T *>(a.dy)[r * a.dy_stride + j]);
-            const float x = widen(static_cast<const T *>(a.x)[r * a.x_stride + j]);
-            w = fmaf(dy, (x - a.mean[r]) * a.rstd[r], w);
-            b += dy;
-        }
-    sw[warp][lane] = w;
-    sb[warp][lane] = b;
+    const int64_t j0 = (int64_t)blockIdx.z * 32 * V, j = j0 + lane * V, per = a.rows / a.groups;
+    const int64_t share = (per + blocks - 1) / blocks, end = (blockIdx.y + 1) * per;
+    const int64_t first = blockIdx.y * per + blockIdx.x * share, last = first + share < end ? first + share : end;
+    float w[V], b[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) w[e] = b[e] = 0.0f;
+    if (j < a.cols) {
+        const T *x = static_cast<const T *>(a.x) + j, *dy = static_cast<const T *>(a.dy) + j;
+        auto rows = [&](int64_t r, auto count) {
+            constexpr int n = decltype(count)::value;
+            Raw<T, V> ux[n], ud[n];
+            float mean[n], rstd[n], fx[V], fd[V];
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                const int64_t q = r + i * WARPS;
+                ux[i] = *reinterpret_cast<const Raw<T, V> *>(x + q * a.x_stride);
+                ud[i] = *reinterpret_cast<const Raw<T, V> *>(dy + q * a.dy_stride);
+                mean[i] = a.mean[q];
+                rstd[i] = a.rstd[q];
+            }
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                widen_all<T>(ux[i], fx);
+                widen_all<T>(ud[i], fd);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    w[e] = fmaf(fd[e], (fx[e] - mean[i]) * rstd[i], w[e]);
+                    b[e] += fd[e];
+                }
+            }
+        };
+        int64_t r = first + warp;
+        for (; r + (AHEAD - 1) * WARPS < last; r += AHEAD * WARPS) rows(r, std::integral_constant<int, AHEAD>());
+        for (; r < last; r += WARPS) rows(r, std::integral_constant<int, 1>());
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        sw[warp][lane * V + e] = w[e];
+        sb[warp][lane * V + e] = b[e];
+    }
     __syncthreads();
-    if (warp == 0 && j < a.cols) {
-        w = b = 0.0f;
-        for (int i = 0; i < kNormBlock / 32; ++i) { w += sw[i][lane]; b += sb[i][lane]; }
-        leave_sums(a, blockIdx.y, 1, j, w, b);
+    for (int c = threadIdx.x; c < 32 * V; c += kNormBlock) {
+        float tw = 0.0f, tb = 0.0f;
+        for (int i = 0; i < WARPS; ++i) { tw += sw[i][c]; tb += sb[i][c]; }
+        if (j0 + c < a.cols) leave_sums(a, blockIdx.y, blocks, j0 + c, tw, tb);
     }
 }
 
-template <typename T>
+template <typename T, int V>
 __global__ void __launch_bounds__(kLongBlock) k_norm_dx(NormBackward a)
 {
     __shared__ float sh[2][32];
@@ -671,17 +765,27 @@ __global__ void __launch_bounds__(kLongBlock) k_norm_dx(NormBackward a)
     const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride;
     T *dx = static_cast<T *>(a.dx) + row * a.dx_stride;
     const float mean = a.mean[row], rstd = a.rstd[row];
-    float s1 = 0.0f, s2 = 0.0f;
-    for (int64_t j = threadIdx.x; j < a.cols; j += kLongBlock) {
-        const float h = widen(dy[j]) * (a.weight.p ? any_at(a.weight, j) : 1.0f);
-        s1 += h;
-        s2 = fmaf(h, (widen(x[j]) - mean) * rstd, s2);
+    float s1 = 0.0f, s2 = 0.0f, fx[V], fd[V], w[V];
+#pragma unroll 2
+    for (int64_t j = threadIdx.x * V; j < a.cols; j += kLongBlock * V) {
+        take(x + j, fx);
+        take(dy + j, fd);
+        take(a.weight, j, 1.0f, w);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float h = fd[e] * w[e];
+            s1 += h;
+            s2 = fmaf(h, (fx[e] - mean) * rstd, s2);
+        }
     }
     const float c1 = block_sum_all<kLongBlock>(s1, sh[0]) / (float)a.cols, c2 = block_sum_all<kLongBlock>(s2, sh[1]) / (float)a.cols;
-    for (int64_t j = threadIdx.x; j < a.cols; j += kLongBlock) {
-        const float h = widen(dy[j]) * (a.weight.p ? any_at(a.weight, j) : 1.0f);
-        const float xh = (widen(x[j]) - mean) * rstd;
-        dx[j] = narrow<T>(rstd * (h - c1 - xh * c2));
+    for (int64_t j = threadIdx.x * V; j < a.cols; j += kLongBlock * V) {
+        take(x + j, fx);
+        take(dy + j, fd);
+        take(a.weight, j, 1.0f, w);
+#pragma unroll
+        for (int e = 0; e < V; ++e) fx[e] = rstd * (fd[e] * w[e] - c1 - (fx[e] - mean) * rstd * c2);
+        put(dx + j, fx);
     }
 }
 
@@ -759,7 +863,11 @@ template <typename T>
 static void forward(const NormForward &a, cudaStream_t st)
 {
     if (forward_by<T, Vec<T>::n>(a, st) || forward_by<T, 2>(a, st) || forward_by<T, 1>(a, st)) return;
-    k_norm_long<T><<<(unsigned)a.rows, kLongBlock, 0, st>>>(a);
+    constexpr int V = Vec<T>::n;
+    if (a.cols % V == 0 && aligned(a.x, a.x_stride, a.rows, sizeof(T), 16) && aligned(a.y, a.y_stride, a.rows, sizeof(T), 16))
+        k_norm_long<T, V><<<(unsigned)a.rows, kLongBlock, 0, st>>>(a);
+    else
+        k_norm_long<T, 1><<<(unsigned)a.rows, kLongBlock, 0, st>>>(a);
 }
 
 template <typename T, int W, int N, int THREADS, int BT>
@@ -781,6 +889,23 @@ static bool try_backward(const NormBackward &a, int blocks, cudaStream_t st)
     if (blocks > 1 && (a.dweight || a.dbias))
         launch_after(k_norm_sums, dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)a.groups), dim3(32 * kSumWarps), 0, st, a, blocks);
     return true;
+}
+
+// Three blocks of k_norm_dw fit on an SM.  A share has 32 rows or more, one batch of a block's warps.
+template <typename T, int V>
+static void backward_long(const NormBackward &a, int most, cudaStream_t st)
+{
+    if (a.dweight || a.dbias) {
+        const int64_t per = a.rows / a.groups, columns = (a.cols + 32 * V - 1) / (32 * V);
+        int64_t blocks = 3 * kSMs / (a.groups * columns);
+        if (blocks > per / 32) blocks = per / 32;
+        if (blocks > most) blocks = most;
+        if (blocks < 1) blocks = 1;
+        k_norm_dw<T, V><<<dim3((unsigned)blocks, (unsigned)a.groups, (unsigned)columns), kNormBlock, 0, st>>>(a, (int)blocks);
+        if (blocks > 1)
+            k_norm_sums<<<dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)a.groups), 32 * kSumWarps, 0, st>>>(a, (int)blocks);
+    }
+    if (a.dx && a.rows) k_norm_dx<T, V><<<(unsigned)a.rows, kLongBlock, 0, st>>>(a);
 }
 
 template <typename T, int W>
@@ -806,9 +931,12 @@ static void backward(const NormBackward &a, cudaStream_t st)
 {
     const int n = blocks_per_group(a.rows, a.groups);
     if (backward_by<T, Vec<T>::n>(a, n, st) || backward_by<T, 2>(a, n, st) || backward_by<T, 1>(a, n, st)) return;
-    if (a.dweight || a.dbias)
-        k_norm_dw<T><<<dim3((unsigned)((a.cols + 31) / 32), (unsigned)a.groups), kNormBlock, 0, st>>>(a);
-    if (a.dx && a.rows) k_norm_dx<T><<<(unsigned)a.rows, kLongBlock, 0, st>>>(a);
+    constexpr int V = Vec<T>::n;
+    if (a.cols % V == 0 && aligned(a.x, a.x_stride, a.rows, sizeof(T), 16) && aligned(a.dy, a.dy_stride, a.rows, sizeof(T), 16) &&
+        (!a.dx || aligned(a.dx, a.dx_stride, a.rows, sizeof(T), 16)))
+        backward_long<T, V>(a, n, st);
+    else
+        backward_long<T, 1>(a, n, st);
 }
 
 void launch_layer_norm(const NormForward &a, int type, cudaStream_t st)
