@@ -885,8 +885,8 @@ static bool try_backward(const NormBackward &a, int blocks, cudaStream_t st)
     const int smem = rings > sums ? rings : sums;
     auto *kernel = k_norm_backward<T, W, N, THREADS, BT>;
     allow_shared(kernel, smem);
-    kernel<<<dim3((unsigned)blocks, (unsigned)a.groups), BT, smem, st>>>(a, blocks, r);
-    if (blocks > 1 && (a.dweight || a.dbias))
+    const bool queued = queue(kernel, dim3((unsigned)blocks, (unsigned)a.groups), BT, smem, st, a, blocks, r);
+    if (queued && blocks > 1 && (a.dweight || a.dbias))
         launch_after(k_norm_sums, dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)a.groups), dim3(32 * kSumWarps), 0, st, a, blocks);
     return true;
 }
@@ -901,7 +901,8 @@ static void backward_long(const NormBackward &a, int most, cudaStream_t st)
         if (blocks > per / 32) blocks = per / 32;
         if (blocks > most) blocks = most;
         if (blocks < 1) blocks = 1;
-        k_norm_dw<T, V><<<dim3((unsigned)blocks, (unsigned)a.groups, (unsigned)columns), kNormBlock, 0, st>>>(a, (int)blocks);
+        if (!queue(k_norm_dw<T, V>, dim3((unsigned)blocks, (unsigned)a.groups, (unsigned)columns), kNormBlock, 0, st, a, (int)blocks))
+            return;                 // dx may overwrite what the sums were to be taken from
         if (blocks > 1)
             k_norm_sums<<<dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)a.groups), 32 * kSumWarps, 0, st>>>(a, (int)blocks);
     }

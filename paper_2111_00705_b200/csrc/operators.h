@@ -17,6 +17,19 @@ inline void allow_shared(F *kernel, size_t bytes)
     if (bytes > 40 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
+// Queues a kernel; false where that was refused, so that what would read its results is not queued
+// either (the reason stays for the caller's cudaGetLastError()).
+template <typename... P, typename... A>
+inline bool queue(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, A... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess;
+}
+
 // A read-only vector of any of the three element types, widened at every access.
 struct AnyVec {
     const void *p;      // NULL: not given
