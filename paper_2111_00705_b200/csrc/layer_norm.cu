@@ -825,7 +825,7 @@ static Ring ring_of(int64_t rows, int64_t groups, int pitch, int all_groups_and_
     if (r.rows > 32) r.rows = 32;
     if (r.rows > rows / groups) r.rows = rows / groups < 1 ? 1 : (int)(rows / groups);
     while (r.rows > 1 && r.rows * pitch * all_groups_and_matrices > 80 * 1024) --r.rows;
-    const int bytes = r.rows * pitch * all_groups_and_matrices, room = 216 * 1024 - parameter_bytes,
+    const int bytes = r.rows * pitch * all_groups_and_matrices, room = kSharedLimit - parameter_bytes,
               n = (room < 160 * 1024 ? room : 160 * 1024) / bytes;
     r.stages = n < 2 ? 2 : n > kMaxStages ? kMaxStages : n;
     return r;

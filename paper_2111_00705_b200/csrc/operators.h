@@ -8,13 +8,17 @@
 namespace cdadam {
 
 // Lets `kernel` be launched with `bytes` of dynamic shared memory.  Up to 48 KB, of which its static
-// shared memory takes a few, that needs no call.
-// (A call for every launch costs the host less than a microsecond; no state is kept, so that any
-// thread may launch on any device.)
+// shared memory takes a few, that needs no call.  The limit belongs to the function and not to the
+// launch, and another host thread may be between setting it and its own launch of another size:
+// so every call sets the same one, the most that any launch takes, and none lowers it.  (A block has
+// 227 KB; the static part is at most 3 KB, k_distill's.  A call for every launch costs the host less
+// than a microsecond; nothing remembers which device has had it.)
+constexpr int kSharedLimit = 216 * 1024;
+
 template <typename F>
 inline void allow_shared(F *kernel, size_t bytes)
 {
-    if (bytes > 40 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (bytes > 40 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedLimit);
 }
 
 // Queues a kernel; false where that was refused, so that what would read its results is not queued

@@ -117,3 +117,16 @@ def test_a_refused_launch_leaves_the_sums_over_rows_alone():
             s.fill_(1e9)
         torch.cuda.synchronize()
         assert together([lambda c=c, w=w, s=s: body(c, w, s) for c, w, s in zip(calls, want, spaces)]) == [0] * len(calls)
+
+
+@pytest.mark.parametrize("which", list(SIZES))
+def test_calls_of_two_sizes_from_four_threads(which):
+    calls, want = prepared(which)
+    for c in calls:
+        for t in c.outputs:
+            t.fill_(-7)
+    torch.cuda.synchronize()
+    codes = together([lambda c=c: [c() for _ in range(4000)] for c in calls])
+    assert [sum(v != cd.OK for v in n) for n in codes] == [0] * len(calls), cd.last_error()
+    for c, w in zip(calls, want):
+        assert all(torch.equal(a, b) for a, b in zip(c.outputs, w))
