@@ -165,17 +165,23 @@ __device__ __forceinline__ float slice_max(const uint4 *buf, int nv)
 
 // Exponentials are taken relative to a slice's maximum m: t = z s - c with c = m s rounded to
 // binary32, one fused operation; the same c is used wherever sums of slices are joined, so its
-// rounding cancels.  Where c does not exist (nothing but masked logits: m is -inf or the type's
-// lowest value) t = (z - m) s.
+// rounding cancels.  The rounding is also what t is at the maximum itself: at most 4 while |c| is
+// below 2^27, but hundreds, and 2^t infinite or 0, from 2^32 or so on (a mask of -1e10).  Where |m s| is
+// not below half of that bound, or there is nothing but masked logits (m is -inf), the origin is far:
+// t = (z - m) s.
+constexpr float kFar = 134217728.0f;        // 2^27
+
 struct Origin {
     float m, c;
-    bool far;               // no c
+    bool far;               // m itself is the origin, not c
     __device__ __forceinline__ Origin(float top, float s)
     {
-        far = !(fabsf(top) < 1e30f);
+        far = !(fabsf(top) * s < 0.5f * kFar);
         m = top == kNegInf ? 0.0f : top;
         c = m * s;
     }
+    // What t is relative to (products of two binary32 values are exact in 64 bits).
+    __device__ __forceinline__ double at(float s) const { return far ? (double)m * (double)s : (double)c; }
 };
 template <bool FAR>
 __device__ __forceinline__ float2 exponents(float2 z, const Origin &o, float s)
@@ -185,12 +191,13 @@ __device__ __forceinline__ float2 exponents(float2 z, const Origin &o, float s)
 // Exponent of slice p's origin relative to the row's, at least -1e4.
 __device__ __forceinline__ float shift(const Origin &p, const Origin &row, float s)
 {
-    return row.far ? fmaxf((p.m - row.m) * s, -1e4f) : p.far ? -1e4f : fmaxf(p.c - row.c, -1e4f);
+    const float d = row.far ? (p.far ? (p.m - row.m) * s : -fmaf(row.m, s, -p.c)) : p.far ? fmaf(p.m, s, -row.c) : p.c - row.c;
+    return fmaxf(d, -1e4f);
 }
 // z relative to the row's origin, in 64 bits.
 __device__ __forceinline__ double exponent64(float z, const Origin &row, float s)
 {
-    return row.far ? ((double)z - (double)row.m) * (double)s : (double)z * (double)s - (double)row.c;
+    return (double)z * (double)s - row.at(s);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -281,14 +288,15 @@ __device__ __noinline__ int collect_in_order(const Slice<T> &sl, float reach, in
 // ---------------------------------------------------------------------------------------------
 // The forward pass reads every logit once, in batches of kBatch vectors a thread, the next batch
 // on its way while one is worked on.  A thread's sums are relative to the largest value it has
-// met, c = max(m, -1e30) s, and are rescaled when a batch raises it (about ten operations for 32
+// met, c = max(m s, -kFar), and are rescaled when a batch raises it (about ten operations for 32
 // logits): no barrier and no second look at a logit, so memory is never waited for together.
+// (A thread that meets nothing above the bound, in the masked part of a row, adds up 0 or, near it, finite
+// values that the row's maximum makes 0.)
 //   e = sum 2^t, h = sum 2^t t, t = z s - c (one fused operation for two logits).
 // Masked logits must not make 0 times -inf in h.  LOW raises them (four packed operations for
 // eight) to a value whose t is finite and far below -150; binary16 has no such value next to its
-// lowest and bounds t itself.  Rows beyond +-1e30, and rows where all is masked by the type's
-// lowest value, give no sums this way (infinite c, or e = 0): they are added up again relative to
-// their maximum.
+// lowest and bounds t itself.  Rows whose maximum is a far origin (|m s| from half of kFar on: where all
+// is masked by a large finite value, for instance) are added up again relative to it.
 // For the alternatives each batch leaves the upper 16 bits of its maximum's order in shared
 // memory, and the batch itself where it is the best so far of its thread's even or odd rounds: with
 // 4 blocks on every SM, each at its own row of 256 KB, a row's beginning has left L2 when its end
@@ -299,7 +307,6 @@ __device__ __noinline__ int collect_in_order(const Slice<T> &sl, float reach, in
 // 20 alternatives 10 us.
 // ---------------------------------------------------------------------------------------------
 constexpr int kBatch = 4;
-constexpr float kFar = 1e30f;
 
 template <typename T>
 __device__ __noinline__ uint4 edge_vector(const Slice<T> sl, int v)
@@ -382,8 +389,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
     if (parts > 1) cluster_arrive();                // a block runs before anything is written to it
 
     const Slice<T> sl(a.z, a.stride, row, a.vocab, part, log_parts);
-    const float s = (float)a.scale2, gap = 200.0f / s;
-    Running r = {kNegInf, -kFar * s, {0.0f, 0.0f}, {0.0f, 0.0f}};
+    const float s = (float)a.scale2, inv_s = 1.0f / s;
+    Running r = {kNegInf, -kFar, {0.0f, 0.0f}, {0.0f, 0.0f}};
     float best[2] = {kNegInf, kNegInf}, second[2] = {kNegInf, kNegInf};     // of the even and the odd rounds
     uint4 u[kBatch], next[kBatch];
     if (sl.nv > 0) load_batch<T, NT>(sl, threadIdx.x, u);
@@ -406,11 +413,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
             }
         }
         r.m = fmaxf(r.m, top);
-        const float m = fmaxf(r.m, -kFar), c = m * s, d = r.c - c, f = exp2_fast(d);
+        const float c = fmaxf(r.m * s, -kFar), d = r.c - c, f = exp2_fast(d);
         r.c = c;
         r.h = mul2(fma2(both(d), r.e, r.h), both(f));
         r.e = mul2(r.e, both(f));
-        const typename Vec<T>::running low = Vec<T>::below(m - fmaxf(gap, 0.015625f * fabsf(m)));
+        const typename Vec<T>::running low = Vec<T>::below((c - fmaxf(200.0f, 0.015625f * fabsf(c))) * inv_s);
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
             float2 z[V / 2];
@@ -535,7 +542,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
     if (threadIdx.x < 32) {
         const bool is = threadIdx.x < NT / 32;
         m = warp_max(is ? sh[0][threadIdx.x] : kNegInf);
-        c = is ? sh[1][threadIdx.x] : -kFar * s;
+        c = is ? sh[1][threadIdx.x] : -kFar;
         e = is ? sh[2][threadIdx.x] : 0.0f;
         h = is ? sh[3][threadIdx.x] : 0.0f;
         join_warp(c, e, h);
@@ -558,7 +565,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
     const int total = TOP ? (int)__reduce_add_sync(0xffffffffu, is ? p.n : 0) : 0;
     Origin all(M, s);
     all.c = C;
-    all.far = fabsf(M) >= kFar && M > kNegInf && M <= 3.402823466e38f;
+    all.far &= M > kNegInf && M <= 3.402823466e38f;
     if (all.far) {                                   // relative to the maximum, by this block alone
         e = h = 0.0f;
         for (int64_t i = threadIdx.x; i < a.vocab; i += NT) {
@@ -957,9 +964,7 @@ __global__ void __launch_bounds__(NT) k_distill(Distill a, int log_parts)
             double t = 0.0;
             if (first && !(q == 0.0)) t = q * (log(q) - (exponent64(zl[j], top, s) - l2) * kLn2);
             if (j == 0 && r > 0.0) {
-                const double at = top.far ? ((double)rest.m - (double)top.m) * (double)s
-                    : (rest.far ? exponent64(rest.m, top, s) : (double)rest.c - (double)top.c);
-                t += r * (log(r) - (at + log2((double)er) - l2) * kLn2);
+                t += r * (log(r) - (rest.at(s) - top.at(s) + log2((double)er) - l2) * kLn2);
             }
             if (j == 0 && r != r) t = r;
             t = warp_sum64(t);
