@@ -529,6 +529,9 @@ enum { CDADAM_I32 = 0, CDADAM_I64 = 1 };
  *            own binary32 parameters or a copy in `type`); NULL means 1 and 0
  *   mean, rstd     device, rows floats: mu and s, which the backward pass needs; may be NULL
  *   eps >= 0, 1 <= cols <= CDADAM_MAX_NORM_COLS, rows < 2^31
+ * A row that holds a NaN or an infinity, or whose sum leaves binary32's range, is NaN.  A row of
+ * finite values whose squared deviations sum to more than binary32 holds (magnitudes of 1e18 and
+ * more) has s = 0 and y = b.
  */
 int cdadam_layer_norm(const void *x, int64_t x_stride, const void *weight, const void *bias,
                       int64_t rows, int64_t cols, float eps, int type, int weight_type,

@@ -243,11 +243,12 @@ struct Ring {
 constexpr int kMaxStages = 6;
 
 // 1 / sqrt(v): the approximation and one Newton step, within 1 ulp or so and a third of the
-// instructions of the correctly rounded quotient and root.
+// instructions of the correctly rounded quotient and root.  0 and infinity have no step to take (0
+// times infinity): v = 0 gives infinity, a sum of squares that overflowed gives 0.
 __device__ __forceinline__ float inverse_root(float v)
 {
     const float r = rsqrtf(v);
-    return v > 0.0f && r < 3e38f ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
+    return r > 0.0f && r < 3e38f ? r * fmaf(-0.5f * r * v, r, 1.5f) : r;
 }
 
 // ---------------------------------------------------------------------------------------------
