@@ -78,7 +78,7 @@ struct LogprobsBackward {
     const void *tokens;
     int64_t rows, vocab;
     int index64;
-    double scale2;
+    double scale2, lse_scale;   // log2(e) / temperature; the same as rounded to binary32, times temperature
     float inv_temperature;
     const float *lse, *entropy, *dlogprob, *dentropy;
     void *dz; int64_t dz_stride;

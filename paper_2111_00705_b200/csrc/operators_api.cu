@@ -188,8 +188,10 @@ int cdadam_token_logprobs_backward(const void *logits, int64_t logits_stride, co
         misaligned(dentropy, 4))
         return refuse(fn, "a vector is not aligned to its elements");
     if (rows == 0) return CDADAM_OK;
-    cdadam::LogprobsBackward a = {logits, logits_stride, tokens, rows, vocab, index_type == CDADAM_I64, scale2(temperature),
-                                  (float)(1.0 / (double)temperature), lse, entropy, dlogprob, dentropy, dlogits, dlogits_stride};
+    const double s = scale2(temperature);
+    cdadam::LogprobsBackward a = {logits, logits_stride, tokens, rows, vocab, index_type == CDADAM_I64, s,
+                                  (double)(float)s * (double)temperature, (float)(1.0 / (double)temperature), lse, entropy,
+                                  dlogprob, dentropy, dlogits, dlogits_stride};
     cdadam::launch_token_logprobs_backward(a, type, (cudaStream_t)stream);
     return launched(fn);
 }
