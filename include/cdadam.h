@@ -510,6 +510,13 @@ int cdadam_compress_sign_static(const float *x, int64_t d, uint32_t *bits, float
  * only; rows whose address is a multiple of 16 bytes are read and written fastest.  `type` is
  * the element type of activations and logits; all arithmetic is binary32 or wider and every
  * output is rounded once.  rows = 0 is allowed and queues only what an empty sum defines.
+ *
+ * Layer norms of up to 8192 columns and the distillation wait inside their kernels for bulk
+ * asynchronous copies, with a limit (2^22 polls, seconds, never reached by a copy that is merely
+ * slow).  There is no context whose status could tell of a wait that ran out: the outputs that
+ * depend on the copy are NaN then (a layer norm's mean and rstd among them, and what the same threads
+ * compute after it).  A block waits a second time, with the default limit, before it goes on, and no copy
+ * is started behind one that has not arrived.
  */
 
 /* element types */
@@ -520,6 +527,13 @@ enum { CDADAM_I32 = 0, CDADAM_I64 = 1 };
 #define CDADAM_MAX_LIST 128              /* longest list of alternatives / of a teacher */
 #define CDADAM_MAX_VOCAB 393216          /* longest row of logits */
 #define CDADAM_MAX_NORM_COLS 1048576     /* longest row of a layer norm */
+
+/*
+ * That limit for the calling thread's following calls; polls < 0 restores the default.  0 makes
+ * every such wait run out at once, which is how the NaN outcome can be exercised without anything
+ * going wrong on the device.
+ */
+int cdadam_set_operator_wait_limit(int polls);
 
 /*
  * Layer norm of every row: with mu = mean(x), v = mean((x - mu)^2), s = 1 / sqrt(v + eps),

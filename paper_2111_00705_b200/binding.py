@@ -70,6 +70,7 @@ _SIGNATURES = {
                                         _c.c_void_p, _c.c_void_p]),
     "cdadam_compress_sign_static": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_void_p,
                                                _c.c_void_p]),
+    "cdadam_set_operator_wait_limit": (_c.c_int, [_c.c_int]),
     "cdadam_layer_norm": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_float,
                                      _c.c_int, _c.c_int, _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_void_p]),
     "cdadam_layer_norm_backward": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_void_p,
@@ -539,6 +540,12 @@ def _parameters(weight, bias, cols, device):
     if w is not None and b is not None and weight.dtype != bias.dtype:
         raise ValueError("weight and bias differ in type")
     return w, b, _TYPES[weight.dtype] if w is not None else F32 if b is None else _TYPES[bias.dtype]
+
+
+def set_operator_wait_limit(polls):
+    """Polls before the operators' kernels, in this thread's following calls, give up a wait on an
+    asynchronous copy (< 0: the default); what depends on the copy is then NaN."""
+    _check(lib().cdadam_set_operator_wait_limit(int(polls)))
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):

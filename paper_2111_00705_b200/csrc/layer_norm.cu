@@ -236,11 +236,34 @@ struct Planes {
     }
 };
 
-// Rows of a chunk, stages of a ring, bytes from row to row: the shape of a launch's rings.
+// Rows of a chunk, stages of a ring, bytes from row to row: the shape of a launch's rings; polls of a
+// wait for a chunk.
 struct Ring {
-    int rows, stages, pitch;
+    int rows, stages, pitch, wait_limit;
 };
 constexpr int kMaxStages = 6;
+
+// What has become of a thread's waits for its group's chunks (`late`): 0: all came; 1: from one on
+// a wait ran out, the thread then waited a second time, with the default limit: its rows are NaN;
+// 2: that was in vain too: the thread waits for nothing any more, after the other stages' copies
+// (rows up to `end`), so that no block leaves with copies in flight, and its group's first warp
+// starts nothing.  All of a wait behind the first poll is in a function, for the loop's registers'
+// sake (inline: 32768 x 4096 bf16 backward 151 us instead of 145).
+__device__ __noinline__ int wait_slowly(uint64_t *bars, int stages, int limit, int late, int s, int phase, unsigned row0,
+                                        unsigned step, unsigned end)
+{
+    if (late == 2 || mbar_wait_bounded(&bars[s], phase, limit)) return late;
+    if (mbar_wait_bounded(&bars[s], phase)) return 1;
+    for (int i = 1; i < stages && row0 + (uint64_t)i * step < end; ++i)
+        mbar_wait_bounded(&bars[(s + i) % stages], s + i < stages ? phase : phase ^ 1);
+    return 2;
+}
+__device__ __forceinline__ int wait_chunk(uint64_t *bars, const Ring &ring, int late, int s, int phase, unsigned row0, unsigned step,
+                                          unsigned end)
+{
+    if (ring.wait_limit != 0 && mbar_try_wait(&bars[s], phase)) return late;
+    return wait_slowly(bars, ring.stages, ring.wait_limit, late, s, phase, row0, step, end);
+}
 
 // 1 / sqrt(v): the approximation and one Newton step, within 1 ulp or so and a third of the
 // instructions of the correctly rounded quotient and root.  0 and infinity have no step to take (0
@@ -303,14 +326,14 @@ __global__ void __launch_bounds__(BT, 1) k_norm(NormForward a, Ring ring)
     PL::template fill<BT>(b, a.bias, cols, 0.0f);
     __syncthreads();
     const float over = 1.0f / (float)cols;
-    bool late = false;
-    int s = 0, phase = 0;
+    int s = 0, phase = 0, late = 0;
     for (; row0 < rows; row0 = row0 + (uint64_t)step < rows ? row0 + step : rows) {
-        late |= !mbar_wait_bounded(&bars[group][s], phase);
+        late = wait_chunk(bars[group], ring, late, s, phase, row0, step, rows);
+        const float none = late ? NAN : 0.0f;           // one thread that was late is enough for the row
         const int n = min((unsigned)ring.rows, rows - row0);
         for (int i = 0; i < n; i += 2) {
             const bool two = i + 1 < n;
-            float2 f[2][M::STEPS][M::P], v[2] = {both(0.0f), both(0.0f)};
+            float2 f[2][M::STEPS][M::P], v[2] = {both(none), both(none)};
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 if (r == 1 && !two) break;
@@ -329,7 +352,8 @@ __global__ void __launch_bounds__(BT, 1) k_norm(NormForward a, Ring ring)
                     for (int e = 0; e < M::P; ++e) v[r] = add2(v[r], f[r][k][e]);
             }
             const float2 mean = mul2(group_sum2<THREADS>(v[0].x + v[0].y, v[1].x + v[1].y, sh[group][0], group), both(over));
-            if (i + 2 >= n && t < 32 && row0 + (uint64_t)ring.stages * step < rows) start(row0 + ring.stages * step, s);   // all have read
+            if (i + 2 >= n && t < 32 && row0 + (uint64_t)ring.stages * step < rows && __all_sync(0xffffffffu, late < 2))
+                start(row0 + ring.stages * step, s);    // all have read
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 const float m = r ? mean.y : mean.x;
@@ -346,8 +370,7 @@ __global__ void __launch_bounds__(BT, 1) k_norm(NormForward a, Ring ring)
                     }
             }
             const float2 squares = group_sum2<THREADS>(v[0].x + v[0].y, v[1].x + v[1].y, sh[group][1], group);
-            float2 rstd = make_float2(inverse_root(fmaf(squares.x, over, a.eps)), inverse_root(fmaf(squares.y, over, a.eps)));
-            if (late) rstd = both(NAN);                 // a copy that does not arrive within seconds
+            const float2 rstd = make_float2(inverse_root(fmaf(squares.x, over, a.eps)), inverse_root(fmaf(squares.y, over, a.eps)));
             T *y = static_cast<T *>(a.y) + (int64_t)(row0 + i) * a.y_stride;
 #pragma unroll
             for (int k = 0; k < M::STEPS; ++k) {
@@ -370,8 +393,6 @@ __global__ void __launch_bounds__(BT, 1) k_norm(NormForward a, Ring ring)
         }
         if (++s == ring.stages) { s = 0; phase ^= 1; }
     }
-    if (late)                                           // no block leaves with copies in flight
-        for (int i = 0; i < ring.stages; ++i) mbar_wait_bounded(&bars[group][i], i < s ? phase : phase ^ 1);
 }
 
 // Rows too long for the registers of a block: three passes, the later two from the caches, by
@@ -556,19 +577,18 @@ __global__ void __launch_bounds__(BT, 1) k_norm_backward(NormBackward a, int blo
         for (int e = 0; e < P; ++e) aw[k][e] = ab[k][e] = both(0.0f);
     __syncthreads();
     const float over = 1.0f / (float)cols;
-    bool late = false;
-    int s = 0, phase = 0, flip = 0;
+    int s = 0, phase = 0, flip = 0, late = 0;
     while (row0 < end) {
         const float means = mean_next, rstds = rstd_next;
         const unsigned next = row0 + (uint64_t)step < end ? row0 + step : end;
         if (lane < ring.rows && next + lane < end) { mean_next = a.mean[next + lane]; rstd_next = a.rstd[next + lane]; }
-        late |= !mbar_wait_bounded(&bars[group][s], phase);
+        late = wait_chunk(bars[group], ring, late, s, phase, row0, step, end);
         const int n = min((unsigned)ring.rows, end - row0);
         for (int i = 0; i < n; ++i, flip ^= 1) {
             const unsigned row = row0 + i;
             const float mean = __shfl_sync(0xffffffffu, means, i);
             float rstd = __shfl_sync(0xffffffffu, rstds, i);
-            if (late) rstd = NAN;                       // a copy that does not arrive within seconds
+            if (late) rstd = NAN;                       // and with it the group's sums over the row
             const char *at = stages + s * stage_bytes + i * ring.pitch;
             const T *sx = M::BIG ? reinterpret_cast<const T *>(at) : x.find(row, at);
             const T *sd = M::BIG ? reinterpret_cast<const T *>(at + half) : dy.find(row, at + half);
@@ -598,7 +618,8 @@ __global__ void __launch_bounds__(BT, 1) k_norm_backward(NormBackward a, int blo
             float2 v = both(0.0f);
             if (a.dx) v = group_sum2<THREADS>(s1.x + s1.y, s2.x + s2.y, sh[group][flip], group);
             else group_barrier<THREADS>(group);
-            if (i == n - 1 && t < 32 && row0 + (uint64_t)ring.stages * step < end) start(row0 + ring.stages * step, s);   // all have read
+            if (i == n - 1 && t < 32 && row0 + (uint64_t)ring.stages * step < end && __all_sync(0xffffffffu, late < 2))
+                start(row0 + ring.stages * step, s);    // all have read
             if (a.dx) {
                 const float2 c1 = both(-v.x * over), c2 = both(-v.y * over);
                 T *dx = static_cast<T *>(a.dx) + row * a.dx_stride;
@@ -613,8 +634,7 @@ __global__ void __launch_bounds__(BT, 1) k_norm_backward(NormBackward a, int blo
         row0 = next;
         if (++s == ring.stages) { s = 0; phase ^= 1; }
     }
-    if (late) {                                                 // no block leaves with copies in flight
-        for (int i = 0; i < ring.stages; ++i) mbar_wait_bounded(&bars[group][i], i < s ? phase : phase ^ 1);
+    if (late) {
 #pragma unroll
         for (int k = 0; k < STEPS; ++k)
 #pragma unroll
@@ -818,9 +838,10 @@ static bool aligned(const void *p, int64_t stride, int64_t rows, int size, int t
 
 // Rows in chunks of about 4 KB (`least` rows where they are longer), fewer where that would leave groups
 // without a chunk; two stages to six, until the rings take 160 KB or the shared memory is full.
-static Ring ring_of(int64_t rows, int64_t groups, int pitch, int all_groups_and_matrices, int parameter_bytes, int least)
+static Ring ring_of(int64_t rows, int64_t groups, int pitch, int all_groups_and_matrices, int parameter_bytes, int least, int wait_limit)
 {
     Ring r;
+    r.wait_limit = wait_limit < 0 ? kWaitLimit : wait_limit;
     r.pitch = pitch;
     r.rows = pitch * least >= 4096 ? least : 4096 / pitch;
     if (r.rows > 32) r.rows = 32;
@@ -838,7 +859,7 @@ static bool try_forward(const NormForward &a, cudaStream_t st)
     if (a.cols > (int64_t)N * THREADS) return false;
     constexpr int groups = BT / THREADS;
     const int cols = (int)a.cols;
-    const Ring r = ring_of(a.rows, (int64_t)kSMs * groups, row_pitch(cols, sizeof(T)), groups, 2 * N * THREADS * 4, 2);
+    const Ring r = ring_of(a.rows, (int64_t)kSMs * groups, row_pitch(cols, sizeof(T)), groups, 2 * N * THREADS * 4, 2, a.wait_limit);
     const int64_t need = ((a.rows + r.rows - 1) / r.rows + groups - 1) / groups;
     const int smem = 2 * N * THREADS * 4 + r.stages * r.rows * r.pitch * groups;
     auto *kernel = k_norm<T, W, N, THREADS, BT>;
@@ -878,7 +899,7 @@ static bool try_backward(const NormBackward &a, int blocks, cudaStream_t st)
     constexpr int groups = BT / THREADS;
     const int64_t per = a.rows / a.groups;
     const int cols = (int)a.cols;
-    const Ring r = ring_of(per, (int64_t)blocks * groups, row_pitch(cols, sizeof(T)), 2 * groups, N * THREADS * 4, 1);
+    const Ring r = ring_of(per, (int64_t)blocks * groups, row_pitch(cols, sizeof(T)), 2 * groups, N * THREADS * 4, 1, a.wait_limit);
     const int64_t most = ((per + r.rows - 1) / r.rows + groups - 1) / groups;
     if (blocks > most) blocks = (int)most;
     if (blocks < 1) blocks = 1;

@@ -67,9 +67,9 @@ __device__ __forceinline__ void send64(const void *here, int rank, uint64_t *bar
                  "l"(bits64(make_float2(x, y))), "r"(cluster_addr(bar, rank)) : "memory");
 }
 // As mbar_wait_bounded, for what other blocks of the cluster have sent.
-__device__ __forceinline__ bool wait_told(uint64_t *bar)
+__device__ __forceinline__ bool wait_told(uint64_t *bar, int limit)
 {
-    for (int spin = 0; spin < kWaitLimit; ++spin) {
+    for (int spin = 0; spin < limit; ++spin) {
         uint32_t done;
         asm volatile("{\n.reg .pred p;\n"
                      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
@@ -120,7 +120,8 @@ struct Slice {
 // while the next one's is on its way.  (Copies issued by all threads share the bandwidth evenly,
 // all blocks then wait together and compute together.)
 // A copy that does not arrive within the limit of a wait (seconds) makes the row one without a
-// distribution: its maximum counts as +inf, its outputs are NaN.
+// distribution: its maximum counts as +inf, its outputs are NaN.  A second wait, with the default limit,
+// follows at once, so that nothing is still in flight when the slice is written or the block leaves.
 constexpr float kLate = __builtin_huge_valf();
 constexpr uint32_t kCopyBytes = 16 * 1024;
 
@@ -852,7 +853,8 @@ __global__ void __launch_bounds__(NT) k_distill(Distill a, int log_parts)
         if (lane == 0) sum64[0][j >> 5] = sum;
     }
     const bool first = mine >= 0 && !again, here = first && mine >= sl.start && mine < sl.start + sl.nv * V;
-    bool late = !mbar_wait_bounded(&bar, 0);
+    bool late = !mbar_wait_bounded(&bar, 0, a.wait_limit);
+    if (late) mbar_wait_bounded(&bar, 0);
     const int used = __syncthreads_count(first);
     float zj = kNegInf;
     if (here) {
@@ -888,8 +890,14 @@ __global__ void __launch_bounds__(NT) k_distill(Distill a, int log_parts)
     const double mass = (sum64[0][0] + sum64[0][1]) + (sum64[0][2] + sum64[0][3]);
     if (!a.rest && mass != 0.0) q /= mass;
     const double r = !a.rest || used >= a.vocab ? 0.0 : mass != mass ? mass : fmax(0.0, 1.0 - mass);
-    if (parts > 1) late |= !wait_told(&told);
-    else __syncthreads();
+    if (parts > 1) {
+        if (!wait_told(&told, a.wait_limit)) {
+            late = true;
+            wait_told(&told, kWaitLimit);
+        }
+    } else {
+        __syncthreads();
+    }
 
     // Rest and list, each relative to its own origin; then both relative to the larger.  Every warp
     // does this for itself.
@@ -976,10 +984,6 @@ __global__ void __launch_bounds__(NT) k_distill(Distill a, int log_parts)
         if (j == 0)
             a.loss[row] = bad ? NAN : used == 0 ? 0.0f : empty ? INFINITY
                 : (float)((sum64[1][0] + sum64[1][1]) + (sum64[1][2] + sum64[1][3]));
-    }
-    if (late) {                                                         // no block leaves with copies in flight
-        mbar_wait_bounded(&bar, 0);
-        if (parts > 1) wait_told(&told);
     }
     if (a.dz && threadIdx.x == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
 }
@@ -1074,6 +1078,7 @@ static void distill(const Distill &a, cudaStream_t st)
     const size_t smem = slice_bytes<T>(a.vocab, parts);
     for_row_blocks(a.rows, parts, [&](int64_t at, int64_t n) {
         Distill b = a;
+        if (a.wait_limit < 0) b.wait_limit = kWaitLimit;
         b.z = static_cast<const T *>(a.z) + at * a.stride;
         b.ids = static_cast<const char *>(a.ids) + at * a.k * (a.index64 ? 8 : 4);
         b.teacher += at * a.k;

@@ -47,6 +47,7 @@ struct NormForward {
     float eps;
     void *y; int64_t y_stride;
     float *mean, *rstd;
+    int wait_limit;     // polls; < 0: the kernels' default
 };
 
 struct NormBackward {
@@ -60,6 +61,7 @@ struct NormBackward {
     void *dbias; int64_t dbias_stride;
     int grad_type, accumulate;
     float *parts;       // workspace
+    int wait_limit;
 };
 
 struct Logprobs {
@@ -95,6 +97,7 @@ struct Distill {
     const float *dloss;
     float *loss;
     void *dz; int64_t dz_stride;   // dz NULL: the loss alone
+    int wait_limit;
 };
 
 // type: 0 binary32, 1 bfloat16, 2 binary16 (the CDADAM_* codes)

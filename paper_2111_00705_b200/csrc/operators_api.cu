@@ -77,12 +77,20 @@ int check_logits(const char *fn, const void *logits, int64_t stride, int64_t row
     return check_matrix(fn, "logits", logits, stride, rows, vocab, type, false);
 }
 
+thread_local int wait_limit = -1;
+
 double scale2(float temperature) { return 1.4426950408889634074 / (double)temperature; }
 int index_size(int index_type) { return index_type == CDADAM_I64 ? 8 : 4; }
 
 }  // namespace
 
 extern "C" {
+
+int cdadam_set_operator_wait_limit(int polls)
+{
+    wait_limit = polls < 0 ? -1 : polls;
+    return CDADAM_OK;
+}
 
 int cdadam_layer_norm(const void *x, int64_t x_stride, const void *weight, const void *bias, int64_t rows, int64_t cols,
                       float eps, int type, int weight_type, void *y, int64_t y_stride, float *mean, float *rstd, void *stream)
@@ -99,7 +107,8 @@ int cdadam_layer_norm(const void *x, int64_t x_stride, const void *weight, const
     if (misaligned(weight, size_of(weight_type)) || misaligned(bias, size_of(weight_type)) || misaligned(mean, 4) ||
         misaligned(rstd, 4))
         return refuse(fn, "weight, bias, mean or rstd is not aligned to its elements");
-    cdadam::NormForward a = {x, x_stride, {weight, weight_type}, {bias, weight_type}, rows, cols, eps, y, y_stride, mean, rstd};
+    cdadam::NormForward a = {x, x_stride, {weight, weight_type}, {bias, weight_type}, rows, cols, eps, y, y_stride, mean, rstd,
+                             wait_limit};
     if (rows == 0) return CDADAM_OK;
     cdadam::launch_layer_norm(a, type, (cudaStream_t)stream);
     return launched(fn);
@@ -143,7 +152,8 @@ int cdadam_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x,
         return refuse(fn, "workspace: %lld bytes, 16-byte aligned, are needed, %lld given", (long long)need,
                       (long long)(workspace ? workspace_bytes : 0));
     cdadam::NormBackward a = {dy, dy_stride, x, x_stride, {weight, weight_type}, mean, rstd, rows, cols, groups, dx, dx_stride,
-                              dweight, dweight_stride, dbias, dbias_stride, grad_type, accumulate != 0, (float *)workspace};
+                              dweight, dweight_stride, dbias, dbias_stride, grad_type, accumulate != 0, (float *)workspace,
+                              wait_limit};
     cdadam::launch_layer_norm_backward(a, type, (cudaStream_t)stream);
     return launched(fn);
 }
@@ -216,7 +226,7 @@ int cdadam_distill(const void *logits, int64_t logits_stride, const void *teache
     if (rows == 0) return CDADAM_OK;
     cdadam::Distill a = {logits, logits_stride, teacher_ids, teacher_logprobs, rows, vocab, k, index_type == CDADAM_I64,
                          scale2(temperature), (float)(1.0 / (double)temperature), rest != 0, dloss, loss, dlogits,
-                         dlogits_stride};
+                         dlogits_stride, wait_limit};
     cdadam::launch_distill(a, type, (cudaStream_t)stream);
     return launched(fn);
 }
