@@ -611,7 +611,8 @@ int cdadam_token_logprobs(const void *logits, int64_t logits_stride, const void 
  *   dlogprob, dentropy   rows floats, the gradients of the two outputs; either may be NULL: 0
  *   tokens   NULL only where dlogprob is.  A token that is negative or >= vocab has no gradient
  *   dlogits  rows x vocab of `type`; may be logits itself (same address and stride)
- * A masked logit (-inf) gets gradient 0.  A row without any gradient coming in (no token or
+ * A masked logit (-inf) gets gradient 0 (also where the gradient coming in is not finite, which makes
+ * the row's others infinite or NaN).  A row without any gradient coming in (no token or
  * dlogprob 0, and dentropy 0) gets 0 whatever its logits are, so that padding may hold anything,
  * and so does a row with |lse| >= 2^24 (every token masked by the type's lowest value, for
  * instance): a binary32 lse of that size says nothing about the probabilities.

@@ -646,6 +646,8 @@ __global__ void __launch_bounds__(NT) k_logprobs_backward(LogprobsBackward a, in
     const double l2 = (double)lse * a.lse_scale;
     const float hi = (float)l2, lo = (float)(l2 - (double)hi);
     const float ca = -u * ((float)kLn2 * a.inv_temperature), cb = -(fmaf(u, H, g)) * a.inv_temperature, cg = g * a.inv_temperature;
+    // a row without a distribution, or a gradient that is not finite: 0 times that is NaN, and masked logits have 0
+    const bool careful = lse != lse || !(fabsf(ca) + fabsf(cb) < __builtin_huge_valf());
 
     const int v0 = chunk * (NT * kGradVecs) + threadIdx.x;
     uint4 q[kGradVecs];
@@ -676,33 +678,35 @@ __global__ void __launch_bounds__(NT) k_logprobs_backward(LogprobsBackward a, in
             for (int j = 0; j < V / 2; ++j) f[j] = both(0.0f);
         } else {
             Vec<T>::wide(q[i], f);
-            if (lse != lse) {                       // a row without a distribution
+            const int k = token - c;                // which of the vector's elements is the token, if one is
+            float at_token = kNegInf;
+            if (k >= 0 && k < V) at_token = widen(sl.row[token]);
+            if (careful) {
 #pragma unroll
-                for (int j = 0; j < V / 2; ++j) f[j] = make_float2(f[j].x == kNegInf ? 0.0f : NAN, f[j].y == kNegInf ? 0.0f : NAN);
-            } else {
-                const int k = token - c;            // which of the vector's elements is the token, if one is
-                float at_token = kNegInf;
-                if (k >= 0 && k < V) at_token = widen(sl.row[token]);
-                if (ca == 0.0f) {
-#pragma unroll
-                    for (int j = 0; j < V / 2; ++j) {
-                        const float2 t = add2(fma2(f[j], both(s), both(-hi)), both(-lo));
-                        f[j] = mul2(make_float2(exp2_fast(t.x), exp2_fast(t.y)), both(cb));
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < V / 2; ++j) {
-                        const float2 t = add2(fma2(f[j], both(s), both(-hi)), both(-lo));
-                        f[j] = mul2(make_float2(exp2_fast(t.x), exp2_fast(t.y)),
-                                    fma2(make_float2(fmaxf(t.x, -1e4f), fmaxf(t.y, -1e4f)), both(ca), both(cb)));
-                    }
+                for (int j = 0; j < V / 2; ++j) {
+                    const float2 t = add2(fma2(f[j], both(s), both(-hi)), both(-lo));
+                    const float x = exp2_fast(t.x) * fmaf(fmaxf(t.x, -1e4f), ca, cb), y = exp2_fast(t.y) * fmaf(fmaxf(t.y, -1e4f), ca, cb);
+                    f[j] = make_float2(f[j].x == kNegInf ? 0.0f : x, f[j].y == kNegInf ? 0.0f : y);
                 }
-                if (at_token != kNegInf) {          // (a masked token has no gradient)
+            } else if (ca == 0.0f) {
 #pragma unroll
-                    for (int j = 0; j < V / 2; ++j) {
-                        if (2 * j == k) f[j].x += cg;
-                        if (2 * j + 1 == k) f[j].y += cg;
-                    }
+                for (int j = 0; j < V / 2; ++j) {
+                    const float2 t = add2(fma2(f[j], both(s), both(-hi)), both(-lo));
+                    f[j] = mul2(make_float2(exp2_fast(t.x), exp2_fast(t.y)), both(cb));
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < V / 2; ++j) {
+                    const float2 t = add2(fma2(f[j], both(s), both(-hi)), both(-lo));
+                    f[j] = mul2(make_float2(exp2_fast(t.x), exp2_fast(t.y)),
+                                fma2(make_float2(fmaxf(t.x, -1e4f), fmaxf(t.y, -1e4f)), both(ca), both(cb)));
+                }
+            }
+            if (at_token != kNegInf) {              // (a masked token has no gradient)
+#pragma unroll
+                for (int j = 0; j < V / 2; ++j) {
+                    if (2 * j == k) f[j].x += cg;
+                    if (2 * j + 1 == k) f[j].y += cg;
                 }
             }
         }
@@ -928,13 +932,13 @@ __global__ void __launch_bounds__(NT) k_distill(Distill a, int log_parts)
     if (a.dz) {
         const bool zero = g == 0.0f || empty || (used == 0 && !bad);
         const float others = er == 0.0f ? 0.0f : g * (fr / E - (float)r / er);
-        if (zero || bad) {
+        if (zero || bad || !(fabsf(others) < __builtin_huge_valf())) {      // (0 times infinity is no masked logit's gradient)
+            const float all = zero ? 0.0f : bad ? NAN : others;
             for (int v = threadIdx.x; v < sl.nv; v += NT) {
                 float2 f[V / 2];
                 Vec<T>::wide(buf[v], f);
 #pragma unroll
-                for (int i = 0; i < V / 2; ++i)
-                    f[i] = zero ? both(0.0f) : make_float2(f[i].x == kNegInf ? 0.0f : NAN, f[i].y == kNegInf ? 0.0f : NAN);
+                for (int i = 0; i < V / 2; ++i) f[i] = make_float2(f[i].x == kNegInf ? 0.0f : all, f[i].y == kNegInf ? 0.0f : all);
                 buf[v] = Vec<T>::pack(f);
             }
         } else if (rest.far) {

@@ -110,3 +110,31 @@ def test_distillation_beside_large_finite_values(vocab, dtype, rest):
         want, size, grad, gsize = distill64(z, ids, lq, dloss[:, None], temperature, rest)
         near(loss, want, TERM * size.nan_to_num(posinf=0.0) + round_tol(want, torch.float32).nan_to_num(posinf=0.0), "loss")
         near(dz, grad, TERM * gsize + round_tol(grad, z.dtype), "dlogits")
+
+
+@pytest.mark.parametrize("bad", [INF, -INF, math.nan])
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("vocab", [40, 1003, 30522, 131072])
+def test_masked_logits_have_no_gradient_whatever_comes_in(vocab, dtype, bad):
+    """A gradient coming in that is not finite (a loss scaled too far) reaches the row's unmasked logits only."""
+    g = gen(vocab, 47)
+    z = torch.randn(5, vocab, generator=g, device="cuda").to(TYPES[dtype])
+    masked = torch.zeros(5, vocab, dtype=torch.bool, device="cuda")
+    masked[:, vocab // 3:vocab // 2] = True
+    masked[3, ::2] = True
+    z[masked] = -INF
+    tokens = torch.tensor([0, 1, 2, 3, vocab // 3], device="cuda")         # the last one is masked
+    lp, ent, lse, _, _ = cd.token_logprobs(z, tokens)
+    one, odd = torch.ones(5, device="cuda"), torch.tensor([1.0, bad, 1.0, bad, bad], device="cuda")
+    hit = odd != 1.0
+    good = cd.token_logprobs_backward(z, tokens, lse, ent, one, one)
+    for dlp, dent in ((odd, None), (odd, one), (one, odd)):
+        got = cd.token_logprobs_backward(z, tokens, lse, ent, dlp, dent)
+        assert not got[masked].any() and not got[hit][~masked[hit]].isfinite().any()
+        assert torch.equal(got[~hit], good[~hit]) or dent is None
+    ids, lq = teacher_list(5, vocab, 8, g)
+    ids[:, 0] = vocab // 3                                                  # listed and masked
+    loss, good = cd.distill(z, ids, lq, one)
+    got_loss, got = cd.distill(z, ids, lq, odd)
+    assert torch.equal(loss, got_loss) and torch.equal(got[~hit], good[~hit])
+    assert not got[masked].any() and not got[hit][~masked[hit]].isfinite().any()
