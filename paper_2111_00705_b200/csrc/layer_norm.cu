@@ -134,13 +134,14 @@ template <> struct Two<float> {
 // A thread's N elements of a row, in STEPS steps of E (E / 2 pairs).  BIG (W elements are 16 bytes):
 // a step is a unit, unit k of thread t starts at column (t + k THREADS) W.  W = 1 and 2: a step is
 // 8 / W units, unit i of step k starts at column (t + (8 k / W + i) THREADS) W.  A launch with N =
-// 16 (24) has more than 8 (16) THREADS columns, so that all but a thread's last 8 elements need no
-// check.
+// 16 (24) has at least 8 (16) THREADS columns, `fits` sees to that, so that all but a thread's last 8
+// elements need no check.
 // ---------------------------------------------------------------------------------------------
 template <typename T, int W, int N_, int THREADS>
 struct Mine {
     static constexpr bool BIG = W * sizeof(T) == 16;
     static constexpr int N = N_, E = BIG ? W : 8, STEPS = N / E, P = E / 2, SURE = N > 8 ? N - 8 : 0;
+    static bool fits(int64_t cols) { return cols >= (int64_t)SURE * THREADS && cols <= (int64_t)N * THREADS; }
     static __device__ __forceinline__ int column(int k, int e, int t)
     {
         return BIG ? (t + k * THREADS) * W + e : (t + (k * (E / W) + e / W) * THREADS) * W + e % W;
@@ -856,7 +857,7 @@ static Ring ring_of(int64_t rows, int64_t groups, int pitch, int all_groups_and_
 template <typename T, int W, int N, int THREADS, int BT>
 static bool try_forward(const NormForward &a, cudaStream_t st)
 {
-    if (a.cols > (int64_t)N * THREADS) return false;
+    if (!Mine<T, W, N, THREADS>::fits(a.cols)) return false;
     constexpr int groups = BT / THREADS;
     const int cols = (int)a.cols;
     const Ring r = ring_of(a.rows, (int64_t)kSMs * groups, row_pitch(cols, sizeof(T)), groups, 2 * N * THREADS * 4, 2, a.wait_limit);
@@ -895,7 +896,7 @@ static void forward(const NormForward &a, cudaStream_t st)
 template <typename T, int W, int N, int THREADS, int BT>
 static bool try_backward(const NormBackward &a, int blocks, cudaStream_t st)
 {
-    if (a.cols > (int64_t)N * THREADS) return false;
+    if (!Mine<T, W, N, THREADS>::fits(a.cols)) return false;
     constexpr int groups = BT / THREADS;
     const int64_t per = a.rows / a.groups;
     const int cols = (int)a.cols;
