@@ -14,7 +14,7 @@ import pytest
 import torch
 
 from paper_2111_00705_b200 import binding as cd
-from test_gpu_operators import INF, SUM, TYPES, check_logprobs, gen, round_tol, teacher_list
+from test_gpu_operators import INF, SUM, TYPES, backward_logprobs64, check_logprobs, gen, hard_rows, round_tol, teacher_list
 
 pytestmark = pytest.mark.gpu
 
@@ -62,18 +62,18 @@ def softmax64(y):
 
 
 def distill64(z, ids, teacher, g, temperature, rest):
-    """From the definition, distinct valid ids, every row with something unmasked.  Differences of logits are
+    """From the definition, valid ids, every row with something unmasked.  Differences of logits are
     formed before anything of ordinary size is added to them: 1e20 + log 16 is 1e20 in 64 bits too."""
     y = z.double() / temperature
     e, total, m = softmax64(y)
     p = e / total
     q = teacher.double().exp() if rest else torch.softmax(teacher.double(), 1)
-    full = torch.zeros_like(y).scatter_(1, ids, q)
+    full = torch.zeros_like(y).scatter_add_(1, ids, q)                  # an index listed twice: one token with the sum
     inside = torch.zeros_like(y, dtype=torch.bool).scatter_(1, ids, True)
-    r = (1.0 - q.sum(1, keepdim=True)).clamp(min=0.0) if rest and ids.shape[1] < y.shape[1] else torch.zeros_like(m)
-    log_p = (y.gather(1, ids) - m) - total.log()
-    term = torch.where(q == 0, 0.0, q * (q.log() - log_p))
-    size = torch.where(q == 0, 0.0, q * (q.log().abs() + log_p.abs() + 1))
+    r = (1.0 - q.sum(1, keepdim=True)).clamp(min=0.0) * (~inside).any(1, keepdim=True) if rest else torch.zeros_like(m)
+    log_p = (y - m) - total.log()
+    term = torch.where(full == 0, 0.0, full * (full.log() - log_p))
+    size = torch.where(full == 0, 0.0, full * (full.log().abs() + log_p.abs() + 1))
     er, sum_r, mr = softmax64(y.masked_fill(inside, -INF))
     log_r = torch.where(sum_r == 0, -INF, (mr - m) + (sum_r.log() - total.log()))
     loss = term.sum(1) + torch.where(r > 0, r * (r.log() - log_r), 0.0)[:, 0]
@@ -138,3 +138,43 @@ def test_masked_logits_have_no_gradient_whatever_comes_in(vocab, dtype, bad):
     got_loss, got = cd.distill(z, ids, lq, odd)
     assert torch.equal(loss, got_loss) and torch.equal(got[~hit], good[~hit])
     assert not got[masked].any() and not got[hit][~masked[hit]].isfinite().any()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("vocab", VOCABS)
+def test_gradient_beside_large_finite_values(vocab, dtype):
+    """Given lse and entropy.  A probability's exponent is off by 1.25 times 2^-23 of its own size, below
+    126 where the probability is not 0: 2^-15 with everything else."""
+    g = gen(vocab, 45)
+    z = torch.cat([masked_rows(vocab, TYPES[dtype], g), hard_rows(vocab, TYPES[dtype], g)[:14]])
+    n = z.shape[0]
+    tokens = torch.arange(n, device="cuda") * 977 % vocab
+    dlp, dent = torch.randn(2, n, generator=g, device="cuda").unbind(0)
+    for temperature in (1.0, 0.5, 3.0):
+        _, ent, lse, _, _ = cd.token_logprobs(z, tokens, temperature=temperature)
+        for gl, ge in ((dlp, dent), (dlp, None)):
+            got = cd.token_logprobs_backward(z, tokens, lse, ent, gl, ge, temperature)
+            torch.cuda.synchronize()
+            want, size = backward_logprobs64(z, tokens, lse, ent, gl, ge, temperature)
+            near(got, want, 2.0 ** -15 * size + round_tol(want, z.dtype), "dlogits")
+
+
+@pytest.mark.parametrize("rest", [True, False])
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("vocab", [40, 1000, 5003, 32768, 70001])
+def test_distillation_of_hard_rows(vocab, dtype, rest):
+    """The hard rows again (without the one that is empty), where a logit at the type's lowest value allows nothing."""
+    g = gen(vocab, 46)
+    z = hard_rows(vocab, TYPES[dtype], g)[[0] + list(range(2, 14))]
+    n, k = z.shape[0], 24
+    ids, lq = teacher_list(n, vocab, k, g)
+    ids[4, 0] = vocab // 3                                                  # the one token left in that row
+    ids[5, :2] = torch.tensor([0, vocab - 1], device="cuda")                # the two that are not at the lowest value
+    ids[5, 2:] = torch.arange(1, k - 1, device="cuda")
+    dloss = torch.full((n,), 64.0, device="cuda")
+    for temperature in (1.0, 0.5):
+        loss, dz = cd.distill(z, ids, lq, dloss, temperature, rest)
+        torch.cuda.synchronize()
+        want, size, grad, gsize = distill64(z, ids, lq, dloss[:, None], temperature, rest)
+        near(loss, want, TERM * size.nan_to_num(posinf=0.0) + round_tol(want, torch.float32).nan_to_num(posinf=0.0), "loss")
+        near(dz, grad, TERM * gsize + round_tol(grad, z.dtype), "dlogits")
