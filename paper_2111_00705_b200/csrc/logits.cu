@@ -320,6 +320,10 @@ __device__ __noinline__ uint4 edge_vector(const Slice<T> sl, int v)
     return *reinterpret_cast<uint4 *>(e);
 }
 
+// A log probability, an entropy: rounding takes neither beyond 0.  NaN stays.
+__device__ __forceinline__ float at_most_0(double v) { return v > 0.0 ? 0.0f : (float)v; }
+__device__ __forceinline__ float at_least_0(double v) { return v < 0.0 ? 0.0f : (float)v; }
+
 __device__ __forceinline__ uint4 ld_stream(const void *p)
 {
     uint4 v;
@@ -585,9 +589,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
         if (a.logprob) {
             const int64_t t = index_at(a.tokens, row, a.index64);
             a.logprob[row] = t < 0 ? 0.0f : t >= a.vocab || none ? NAN : empty ? kNegInf
-                : (float)((exponent64(widen(sl.row[t]), all, s) - l2) * kLn2);
+                : at_most_0((exponent64(widen(sl.row[t]), all, s) - l2) * kLn2);
         }
-        if (a.entropy) a.entropy[row] = empty ? 0.0f : (float)((l2 - (double)H / (double)E) * kLn2);
+        if (a.entropy) a.entropy[row] = empty ? 0.0f : at_least_0((l2 - (double)H / (double)E) * kLn2);
         // z s - c - l2 is the log of p_i for s as rounded; the exact scale for the origin itself
         if (a.lse) a.lse[row] = (float)(((all.far ? (double)all.m * a.scale2 : (double)all.c * (a.scale2 / (double)s)) + l2) * kLn2);
     }
@@ -606,7 +610,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
         }
         if (at < a.k) {
             store_index(a.top_ids, row * a.k + at, a.index64, key_index(key));
-            a.top_logprobs[row * a.k + at] = (float)((exponent64(key_value(key), all, s) - l2) * kLn2);
+            a.top_logprobs[row * a.k + at] = at_most_0((exponent64(key_value(key), all, s) - l2) * kLn2);
         }
     }
     for (int t = threadIdx.x; t < a.k && part == 0; t += NT)
