@@ -489,6 +489,10 @@ def compress_sign_static(x, bits=None, scale=None, stream=None):
 
 
 # -- operators of a worker around its loss ---------------------------------------------------
+# They are plain calls: their results have no automatic-differentiation graph, whatever requires_grad
+# their inputs have, each gradient is a call of its own, and writing into `out` does not raise a tensor's
+# version.  With `stream` a call runs there, and so belongs there what it allocates: other streams have
+# to wait for it.
 F32, BF16, F16 = 0, 1, 2
 MAX_LIST, MAX_VOCAB, MAX_NORM_COLS = 128, 393216, 1048576
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
@@ -552,7 +556,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     """Layer norm of every row of x (rows x cols): (y, mean, rstd).  weight and bias: cols
     elements of any of the three types (slices of the optimizer's parameter vector, for
     instance).  out: (y, mean, rstd) to write into, each may be None: y is then allocated, mean
-    and rstd are not computed."""
+    and rstd are not computed.  No automatic differentiation: layer_norm_backward is the gradient."""
     px, sx = _matrix(x, "x")
     device, shape, dtype = x.get_device(), x.shape, x.dtype
     if device < 0 or stream is not None or device != _current():
@@ -628,7 +632,8 @@ def token_logprobs(logits, tokens=None, k=0, temperature=1.0, out=None, stream=N
     """Per row of logits (rows x vocab): (log probability of tokens[row], entropy, log normaliser,
     the k most probable tokens, their log probabilities), at logits / temperature.  tokens: int32
     or int64, negative = none, or None (the first entry is then None).  out: the five to write
-    into, each may be None: not computed.  Ids have the type of tokens (int64 without)."""
+    into, each may be None: not computed.  Ids have the type of tokens (int64 without).  No automatic
+    differentiation: token_logprobs_backward is the gradient."""
     pz, sz = _matrix(logits, "logits")
     device, shape = logits.get_device(), logits.shape
     if device < 0 or stream is not None or device != _current():
@@ -687,7 +692,7 @@ def distill(logits, teacher_ids, teacher_logprobs, dloss=None, temperature=1.0, 
     token_logprobs gives them), and with dloss (the gradient of every row's loss) its gradient
     with respect to the logits: (loss, dlogits or None).  rest: the tokens that are not listed
     count as one further outcome; otherwise the list is renormalised.  out: (loss, dlogits) to
-    write into, each may be None: not computed."""
+    write into, each may be None: not computed.  No automatic differentiation: dlogits is the gradient."""
     pz, sz = _matrix(logits, "logits")
     device, shape, dtype, lists = logits.get_device(), logits.shape, logits.dtype, teacher_ids.shape
     if len(lists) != 2 or lists[0] != shape[0]:
