@@ -872,6 +872,15 @@ static bool try_forward(const NormForward &a, cudaStream_t st)
 // Rows that start on 16 bytes and are whole units of that go by those, others of an even number of
 // elements that start on two by two (20000 x 1022 bf16 25 us, one by one 29; 20000 x 4098 112 and
 // 138 us; backward of 32768 x 4090 211 and 233 us), the rest one by one.
+//
+// A row has the smallest group of 32, 64, 128, 256 or 512 threads whose 16 elements a thread hold
+// it (8 up to 256 columns), with two exceptions where more of a group's elements would be empty than
+// in use: 24 elements a thread of one warp for 513 to 768 columns, 384 threads for 4097 to 6144.  bf16, 82 M elements,
+// us with and without them:
+//     columns        520       640       768       518       766       519       767
+//     24 elements    67/100    62/84     63/69     77/134    61/95     100/162   70/114
+//     columns        4104      5120      6144      4098      6142      4099      6143
+//     384 threads    79/108    67/90     61/79     110/132   81/98     141/170   102/122
 template <typename T, int W>
 static bool forward_by(const NormForward &a, cudaStream_t st)
 {
@@ -932,6 +941,16 @@ static void backward_long(const NormBackward &a, int most, cudaStream_t st)
     if (a.dx && a.rows) k_norm_dx<T, V><<<(unsigned)a.rows, kLongBlock, 0, st>>>(a);
 }
 
+// As forward, but the sums over rows beside the row leave no room for 24 elements a thread, and the
+// exceptions are others.  96 threads of 8 elements for 513 to 768 columns of whole vectors; two by
+// two or one by one is slower so.  320 threads for 4097 to 5120 columns that go two by two or one
+// by one, although up to 90 bytes of every thread's registers go to memory; whole vectors of 16-bit
+// elements would gain less, those of binary32 lose.  bf16 of 100 M elements (f32: 67 M), us with and
+// without them (*: not taken):
+//     columns        520       640       768       518       766       519       767
+//     96 threads     151/160   126/134   116/121   285*/200  242*/153  256*/227  210*/172
+//     columns        4104      5120      4104 f32  4098      5118      4099      5119
+//     320 threads    184*/211  163*/173  160*/155  230/274   200/223   257/316   224/266
 template <typename T, int W>
 static bool backward_by(const NormBackward &a, int n, cudaStream_t st)
 {
