@@ -1000,10 +1000,15 @@ __global__ void __launch_bounds__(NT) k_distill(Distill a, int log_parts)
 // Launches
 // ---------------------------------------------------------------------------------------------
 constexpr int kSliceBytes = 32 * 1024;           // six blocks share an SM
-constexpr int64_t kShortSlice = 64 * 1024;       // slices of the forward pass up to this: blocks of 128 threads
+// Slices of the forward pass up to this: blocks of 128 threads instead of 256.  bf16, us with 128 / 256
+// threads, without alternatives and with 64: 40000 x 1000 134/275, 428/686; 8192 x 4001 31/62, 88/139;
+// 4096 x 30522 54/61, 104/112; 2000 x 131072 95/92, 145/129; 1000 x 250000 88/92, 169/134.
+constexpr int64_t kShortSlice = 64 * 1024;
 
 // Blocks per row of the forward pass, as a power of two: one where the rows alone fill the GPU
-// (two for each SM); fewer rows are shared by up to 8 blocks of at least 8 KB.
+// (two for each SM); fewer rows are shared by up to 8 blocks of at least 8 KB.  bf16, us with / without
+// sharing, 0 and 20 alternatives: 1 x 30522 9.7/10.2, 10.3/12.3; 8 x 131072 8.9/12.0, 12.3/17.0; 64 x 131072
+// 11.2/15.1, 16.5/21.4; 200 x 30522 9.3/10.8, 14.1/15.8; 250 x 131072 18.7/18.1, 26.3/26.6.
 static int log_parts_for_rows(int64_t rows, int64_t bytes)
 {
     int n = 0;
@@ -1094,6 +1099,8 @@ static void distill(const Distill &a, cudaStream_t st)
         if (a.loss) b.loss += at;
         if (a.dz) b.dz = static_cast<T *>(a.dz) + at * a.dz_stride;
         const void *args[] = {&b, &log_parts};
+        // longer slices than 48 KB (8 blocks do not hold the row in less): 256 threads; us with them / with 128:
+        // 2000 x 131072 f32 402/424, 1000 x 393216 bf16 385/430, 700 x 393216 f32 653/749
         if (smem > 48 * 1024) launch_rows(k_distill<T, 256>, n, parts, 256, smem, st, args);
         else launch_rows(k_distill<T, 128>, n, parts, 128, smem, st, args);
     });
