@@ -1124,9 +1124,9 @@ template <typename T>
 static void logprobs_backward(const LogprobsBackward &a, cudaStream_t st)
 {
     constexpr int V = Vec<T>::n;
+    constexpr int NT = 128;
     const int64_t vecs = (a.vocab + 2 * V - 2) / V;
-    const int threads = vecs > 128 * kGradVecs ? 256 : 128;             // short rows in short blocks
-    const int chunks = (int)((vecs + threads * kGradVecs - 1) / (threads * kGradVecs));
+    const int chunks = (int)((vecs + NT * kGradVecs - 1) / (NT * kGradVecs));
     for_row_blocks(a.rows, chunks, [&](int64_t at, int64_t n) {
         LogprobsBackward b = a;
         b.z = static_cast<const T *>(a.z) + at * a.stride;
@@ -1136,8 +1136,7 @@ static void logprobs_backward(const LogprobsBackward &a, cudaStream_t st)
         if (a.entropy) b.entropy += at;
         if (a.dlogprob) b.dlogprob += at;
         if (a.dentropy) b.dentropy += at;
-        if (threads == 256) k_logprobs_backward<T, 256><<<(unsigned)(n * chunks), 256, 0, st>>>(b, chunks);
-        else k_logprobs_backward<T, 128><<<(unsigned)(n * chunks), 128, 0, st>>>(b, chunks);
+        k_logprobs_backward<T, NT><<<(unsigned)(n * chunks), NT, 0, st>>>(b, chunks);
     });
 }
 
