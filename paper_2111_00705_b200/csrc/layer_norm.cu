@@ -278,8 +278,10 @@ __device__ __forceinline__ float inverse_root(float v)
 // ---------------------------------------------------------------------------------------------
 // Forward.  A group works on two rows at a time: their sums go through the same shuffles and
 // barriers, and parameters are taken from shared memory once for both (20000 x 4096 bf16: 71 us a
-// row at a time, 59 us so, 5.5 TB/s or 84 % of the copy rate; 16384 x 768 f32 20 us).  Rows that do
-// not start on 16 bytes cost about twice the instructions: 20000 x 1021 bf16 29 us, 43 %.
+// row at a time, 61 us so, 5.3 TB/s or 82 % of the copy rate; 16384 x 768 f32 20 us, bf16 14.5, of
+// which 9 are the rows at 5.7 TB/s and the rest is the start of the rings and the end of the
+// launch).  Rows that do not start on 16 bytes cost about twice the instructions: 20000 x 1021 bf16
+// 29 us, 43 %.
 // ---------------------------------------------------------------------------------------------
 template <typename T, int W, int N, int THREADS, int BT>
 __global__ void __launch_bounds__(BT, 1) k_norm(NormForward a, Ring ring)
@@ -397,8 +399,8 @@ __global__ void __launch_bounds__(BT, 1) k_norm(NormForward a, Ring ring)
 }
 
 // Rows too long for the registers of a block: three passes, the later two from the caches, by
-// vectors of 16 bytes where rows are whole ones (4000 x 16384 bf16 70 us,
-// 16383 columns, one by one, 148).
+// vectors of 16 bytes where rows are whole ones (4000 x 16384 bf16 69 us, 58 % of the copy rate;
+// 16383 columns, one by one, 147, 27 %).
 constexpr int kLongBlock = 512;
 
 // V elements: 16 bytes or one.
@@ -488,9 +490,11 @@ __global__ void __launch_bounds__(kLongBlock) k_norm_long(NormForward a)
 // dbias together.  THREADS = 32: the block's warps have a row each and add their sums up at the
 // end, in order.  `blocks` blocks share a group; with more than one each leaves its sums in the
 // workspace and k_norm_sums adds them, in order: no atomics, the same bits every time.
-// Measured: 32768 x 4096 bf16 0.141 ms (5.7 TB/s, 87 % of the copy rate); 16384 x 768 bf16 for 8 workers
-// 25 us, of which the rows take 12, the second kernel 5 and the start of the rings 3; 30000 x 1021
-// f16 58 us (48 %: single elements).
+// Measured: 32768 x 4096 bf16 145 to 154 us (5.2 to 5.5 TB/s, 80 to 85 % of the copy rate); 16384 x 768
+// bf16 for 8 workers 25 us, of which the rows take 12, the second kernel 5 and the start of the
+// rings 3; 30000 x 1021 f16 60 us (47 %: single elements).  Narrow rows, from two numbers of rows each:
+// 1024 columns 6.3 TB/s and 16 us beside that, 500 columns 6.0 TB/s and 15 us, 128 columns 3.4 TB/s (the
+// sums over a row) and 12 us: 32768 rows take 48, 31 and 19.5 us.
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ void store_grad(void *p, int64_t i, int type, int accumulate, float v)
 {
@@ -717,7 +721,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) k_norm_sums(NormBackward a, in
 }
 
 // Rows too long for that: the sums over rows first (dx may overwrite what they read), then dx; V as
-// in k_norm_long.  8192 x 16384 bf16 261 us, where reading x and dy twice takes 205 at the copy
+// in k_norm_long.  8192 x 16384 bf16 256 us, where reading x and dy twice takes 205 at the copy
 // rate; 16383 columns, one by one, 696.
 //
 // The sums: a block has 32 V columns and a share of a group's rows, its warps every eighth row of
@@ -871,7 +875,7 @@ static bool try_forward(const NormForward &a, cudaStream_t st)
 
 // Rows that start on 16 bytes and are whole units of that go by those, others of an even number of
 // elements that start on two by two (20000 x 1022 bf16 25 us, one by one 29; 20000 x 4098 112 and
-// 138 us; backward of 32768 x 4090 211 and 233 us), the rest one by one.
+// 141 us; backward of 32768 x 4090 199 and 233 us), the rest one by one.
 //
 // A row has the smallest group of 32, 64, 128, 256 or 512 threads whose 16 elements a thread hold
 // it (8 up to 256 columns), with two exceptions where more of a group's elements would be empty than
