@@ -166,18 +166,19 @@ __device__ __forceinline__ float slice_max(const uint4 *buf, int nv)
 
 // Exponentials are taken relative to a slice's maximum m: t = z s - c with c = m s rounded to
 // binary32, one fused operation; the same c is used wherever sums of slices are joined, so its
-// rounding cancels.  The rounding is also what t is at the maximum itself: at most 4 while |c| is
-// below 2^27, but hundreds, and 2^t infinite or 0, from 2^32 or so on (a mask of -1e10).  Where |m s| is
-// not below half of that bound, or there is nothing but masked logits (m is -inf), the origin is far:
-// t = (z - m) s.
-constexpr float kFar = 134217728.0f;        // 2^27
+// rounding cancels.  The rounding is also what t is at the maximum itself: at most 64 while |c| is
+// below 2^31, which leaves binary32's sums of 2^t room on both sides, but hundreds, and 2^t infinite
+// or 0, from 2^32 or so on (a mask of -1e10).  Where |m s| is not below that bound, or there is
+// nothing but masked logits (m is -inf), the origin is far: t = (z - m) s.  (What lies between kNear
+// and kFar keeps a near maximum and a bound of -kFar on c further apart than 2^t reaches.)
+constexpr float kFar = 2147483648.0f, kNear = kFar - 4096.0f;       // 2^31
 
 struct Origin {
     float m, c;
     bool far;               // m itself is the origin, not c
     __device__ __forceinline__ Origin(float top, float s)
     {
-        far = !(fabsf(top) * s < 0.5f * kFar);
+        far = !(fabsf(top) * s < kNear);
         m = top == kNegInf ? 0.0f : top;
         c = m * s;
     }
@@ -296,8 +297,8 @@ __device__ __noinline__ int collect_in_order(const Slice<T> &sl, float reach, in
 //   e = sum 2^t, h = sum 2^t t, t = z s - c (one fused operation for two logits).
 // Masked logits must not make 0 times -inf in h.  LOW raises them (four packed operations for
 // eight) to a value whose t is finite and far below -150; binary16 has no such value next to its
-// lowest and bounds t itself.  Rows whose maximum is a far origin (|m s| from half of kFar on: where all
-// is masked by a large finite value, for instance) are added up again relative to it.
+// lowest and bounds t itself.  Rows whose maximum is a far origin (where all is masked by -1e10, for
+// instance) are added up again relative to it.
 // For the alternatives each batch leaves the upper 16 bits of its maximum's order in shared
 // memory, and the batch itself where it is the best so far of its thread's even or odd rounds: with
 // 4 blocks on every SM, each at its own row of 256 KB, a row's beginning has left L2 when its end
