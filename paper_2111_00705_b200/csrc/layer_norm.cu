@@ -490,7 +490,7 @@ __global__ void __launch_bounds__(kLongBlock) k_norm_long(NormForward a)
 // dbias together.  THREADS = 32: the block's warps have a row each and add their sums up at the
 // end, in order.  `blocks` blocks share a group; with more than one each leaves its sums in the
 // workspace and k_norm_sums adds them, in order: no atomics, the same bits every time.
-// Measured: 32768 x 4096 bf16 145 to 154 us (5.2 to 5.5 TB/s, 80 to 85 % of the copy rate); 16384 x 768
+// Measured: 32768 x 4096 bf16 145 to 156 us (5.2 to 5.5 TB/s, 79 to 85 % of the copy rate); 16384 x 768
 // bf16 for 8 workers 25 us, of which the rows take 12, the second kernel 5 and the start of the
 // rings 3; 30000 x 1021 f16 60 us (47 %: single elements).  Narrow rows, from two numbers of rows each:
 // 1024 columns 6.3 TB/s and 16 us beside that, 500 columns 6.0 TB/s and 15 us, 128 columns 3.4 TB/s (the

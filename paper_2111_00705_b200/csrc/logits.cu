@@ -304,7 +304,7 @@ __device__ __noinline__ int collect_in_order(const Slice<T> &sl, float reach, in
 // 4 blocks on every SM, each at its own row of 256 KB, a row's beginning has left L2 when its end
 // arrives.
 // Measured: 4096 x 131072 bf16 without alternatives 0.166 ms (6.5 TB/s, 98 % of the copy rate: bound
-// by memory); with 64 of them 0.240 to 0.254 ms: what follows the pass, some 12,000 warp instructions in
+// by memory); with 64 of them 0.240 to 0.255 ms: what follows the pass, some 12,000 warp instructions in
 // short dependent pieces, does not all hide behind the other blocks' loads.  One row of 30522 with
 // 20 alternatives 10 us.
 // ---------------------------------------------------------------------------------------------
@@ -627,7 +627,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_logprobs(Logprobs a, int log_
 // one pass over the logits: a block has kGradVecs vectors for each of its threads.  lse T s is taken
 // off in two parts, and with s as rounded for the logits, so that t has a relative error of 2^-23
 // however large z and lse are (beside what lse's own rounding means).  Bound by memory: 4096 x
-// 30522 bf16 with both gradients 86 to 90 us (5.5 to 5.8 TB/s, 85 to 89 % of the copy rate).
+// 30522 bf16 with both gradients 86 to 91 us (5.5 to 5.8 TB/s, 84 to 89 % of the copy rate).
 // ---------------------------------------------------------------------------------------------
 constexpr int kGradVecs = 4;
 constexpr float kLost = 16777216.0f;        // |lse| from which binary32 says nothing about p
@@ -734,7 +734,7 @@ __global__ void __launch_bounds__(NT) k_logprobs_backward(LogprobsBackward a, in
 // from a sum of positive terms instead of from 1 - sum p_j, and neither part underflows however
 // far the other is above it.  The gradient replaces the slice in shared memory, the listed
 // tokens' entries are put in afterwards, and the slice leaves as one bulk copy.
-// Measured: 4096 x 131072 bf16, 64 listed, loss and gradient 0.405 to 0.435 ms (4.9 to 5.3 TB/s, 75 to
+// Measured: 4096 x 131072 bf16, 64 listed, loss and gradient 0.405 to 0.440 ms (4.9 to 5.3 TB/s, 75 to
 // 81 % of the copy rate), the loss alone 0.274 (60 %); 1023 x 50021 f16 48 us, the loss alone 33.  A
 // block's own chain (list, slice, maximum, sum, the cluster's sums, gradient) is about four times
 // as long as its slice takes in memory, and six blocks on an SM do not quite cover that.  Half of what an exchange through cluster barriers cost was their fences:
