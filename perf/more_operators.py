@@ -319,6 +319,11 @@ def exact(case, seed):
             "product": _exact_product}[case["op"]](case, s)
 
 
+def _two_to(e):
+    """2^e, whole numbers e of a normal binary64 power."""
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
 def _exact_whole(p):
     """Of binary32 rows p: the q nearest to 127 p / max |p| (even ones at a half), and the value of one step."""
     p = p.double()
@@ -356,7 +361,7 @@ def _exact_backward(case, s):
             a = slice(i * per + part.start, i * per + part.stop)
             if case["checkpoint"]:
                 q, e = (v[a].double() for v in s["x"])
-                x = torch.ldexp(q, e.repeat_interleave(BLOCK, 1)[:, :cols] - 127.0)
+                x = q * _two_to(e.repeat_interleave(BLOCK, 1)[:, :cols] - 127.0)
             else:
                 x = s["x"][a].double()
             r, dy = s["rstd"][a].double(), s["dy"][a].double()
@@ -373,10 +378,10 @@ def _exact_checkpoint(case, s):
         v = torch.nn.functional.pad(s["x"][a].double(), (0, -cols % BLOCK)).unflatten(1, (-1, BLOCK))
         top = v.abs().amax(2, keepdim=True)
         e = torch.where(top > 0, torch.frexp(top).exponent - 7, -126).clamp(min=-126)      # the largest is 64 to 128 steps
-        t = torch.ldexp(v, -e)
+        t = v * _two_to(-e)
         low = torch.floor(t)
         q = low + ((t - low > 0.5) | ((t - low == 0.5) & (torch.remainder(low, 2.0) == 1.0)))
-        got.append(torch.ldexp(q.clamp(-127, 127), e).flatten(1)[:, :cols])
+        got.append((q.clamp(-127, 127) * _two_to(e)).flatten(1)[:, :cols])
     return torch.cat(got), None
 
 
