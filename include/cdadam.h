@@ -655,6 +655,106 @@ int cdadam_distill(const void *logits, int64_t logits_stride,
                    float temperature, int rest, const float *dloss,
                    float *loss, void *dlogits, int64_t dlogits_stride, void *stream);
 
+/*
+ * A worker's operators in 8 bits.
+ *
+ * Four more parts of the same computation: the root-mean-square norm with the residual's addition
+ * in front of it, activations kept in 8 bits until the backward pass needs them (a checkpoint),
+ * products of 8-bit matrices, and what turns rows into 8 bits and back.  Matrices, types, streams and
+ * errors are as above; no wait inside these kernels has a limit that the caller sets
+ * unless said otherwise.  8-bit matrices are signed, row-major, elements of a row adjacent, rows any
+ * stride >= the row's length apart; rows that start on 16 bytes are fastest (a product takes no others).
+ *
+ * Two formats of 8 bits:
+ *   rows     q_j and one binary32 step per row: the value is q_j * scale.  With m = max |p_j| over the row,
+ *            scale = m / 127 and q_j is the integer nearest to 127 p_j / m, to the even one at a half, as
+ *            exact arithmetic on the binary32 p_j has it (no other rounding gets in).  A row of zeros has
+ *            scale 0; one with a NaN or an infinity has scale NaN and q = 0.
+ *   checkpoint   q_j and one byte E for every CDADAM_CHECKPOINT_BLOCK = 32 columns (the last block of a row may
+ *            be shorter): the value is q_j 2^(E - 127).  With 2^f <= max |x_j| < 2^(f+1) over the block,
+ *            E = max(f - 6 + 127, 1) and q_j = x_j 2^(127 - E) rounded to the nearest integer (to even at
+ *            a half), at most 127 in magnitude.  So a value is off by at most half a step 2^(E - 127) (by
+ *            less than a whole one where it is above 127 steps), and every value that a checkpoint stands
+ *            for is a bfloat16 (and, kept from binary16, a binary16).  A block with a NaN or an infinity has
+ *            E = 255 and q = 0 and stands for NaN.
+ */
+#define CDADAM_CHECKPOINT_BLOCK 32       /* columns of a checkpoint that share an exponent */
+#define CDADAM_MAX_INNER 131071          /* longest row of an 8-bit product: its sums fit 32 bits */
+
+/*
+ * Root-mean-square norm of every row of h = x + residual (rounded to `type`; h = x without residual):
+ * with s = 1 / sqrt(mean(h^2) + eps) and p_j = h_j w_j (rounded to binary32),
+ *     total_j = h_j,   y_j = p_j s,   (q, scale) = the rows format of p_j s (q is that of p),
+ *     (kept, exponents) = the checkpoint of h,   rstd = s.
+ *   x, residual, total, y   rows x cols of `type`; residual, total and y may be NULL
+ *   q, scale   rows x cols bytes and rows floats; both or neither
+ *   kept, exponents   rows x cols bytes and rows x ceil(cols / 32) bytes; both or neither
+ *   weight   cols elements of `weight_type`, NULL means 1;   rstd   rows floats, may be NULL
+ *   total may be x or residual, y may be x or residual (same address and stride), not the same one;
+ *   eps >= 0, 1 <= cols <= CDADAM_MAX_NORM_COLS, rows < 2^31.  At least one output must be given.
+ * A row with a NaN is NaN; with an infinity, or finite with a sum of squares beyond binary32, s = 0 (y is
+ * NaN at the infinities and 0 elsewhere).
+ */
+int cdadam_rms_norm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride,
+                    const void *weight, int64_t rows, int64_t cols, float eps, int type, int weight_type,
+                    void *total, int64_t total_stride, void *y, int64_t y_stride,
+                    int8_t *q, int64_t q_stride, float *scale,
+                    int8_t *kept, int64_t kept_stride, uint8_t *exponents, int64_t exponents_stride,
+                    float *rstd, void *stream);
+
+/*
+ * Its gradient.  With xh_j = x_j s and g_j = dy_j w_j, for every row
+ *     dx_j = s (g_j - xh_j mean(g xh)) + dtotal_j,
+ * the gradient of x and of residual alike, and summed over the rows of a group
+ *     dweight_j = sum dy_j xh_j.
+ *   x        h of the forward pass (its total, or x where there was no residual): rows x cols of `type`
+ *            where exponents is NULL, else the checkpoint of it: rows x cols bytes, exponents rows x ceil(cols / 32)
+ *   dtotal   rows x cols of `type`: the gradient that comes along the residual; NULL means 0
+ *   rstd     rows floats, the forward pass's
+ *   dx, dweight   either may be NULL; dx may be dy, dtotal or x (where it is of `type`), same address and stride
+ * Groups, grad_type, accumulate and workspace (cdadam_rms_norm_workspace bytes) are those of
+ * cdadam_layer_norm_backward.
+ */
+int cdadam_rms_norm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride,
+                             const uint8_t *exponents, int64_t exponents_stride, const void *weight,
+                             const float *rstd, const void *dtotal, int64_t dtotal_stride,
+                             int64_t rows, int64_t cols, int64_t groups,
+                             int type, int weight_type, int grad_type, void *dx, int64_t dx_stride,
+                             void *dweight, int64_t dweight_stride, int accumulate,
+                             void *workspace, int64_t workspace_bytes, void *stream);
+int64_t cdadam_rms_norm_workspace(int64_t rows, int64_t cols, int64_t groups);
+
+/* Rows format of x (p = x) and back: y_j = q_j scale (one binary32 product, rounded to `type`). */
+int cdadam_quantize_rows(const void *x, int64_t x_stride, int64_t rows, int64_t cols, int type,
+                         int8_t *q, int64_t q_stride, float *scale, void *stream);
+int cdadam_dequantize_rows(const int8_t *q, int64_t q_stride, const float *scale, int64_t rows, int64_t cols,
+                           int type, void *y, int64_t y_stride, void *stream);
+
+/* Checkpoint of x and back (rounded to `type`, which changes nothing where x had that type). */
+int cdadam_checkpoint8(const void *x, int64_t x_stride, int64_t rows, int64_t cols, int type,
+                       int8_t *kept, int64_t kept_stride, uint8_t *exponents, int64_t exponents_stride,
+                       void *stream);
+int cdadam_checkpoint8_restore(const int8_t *kept, int64_t kept_stride,
+                               const uint8_t *exponents, int64_t exponents_stride,
+                               int64_t rows, int64_t cols, int type, void *x, int64_t x_stride, void *stream);
+
+/*
+ * Product of 8-bit matrices in the rows format: for every token t and channel c
+ *     y_tc = (sum_k x_tk w_ck) x_scale_t w_scale_c + bias_c,
+ * the sum exact (32-bit integers), the rest in binary32 in this order, rounded once to `type`.
+ *   x        tokens x inner bytes, w channels x inner bytes; rows start on 16 bytes (address and strides are
+ *            multiples of 16); 1 <= inner <= CDADAM_MAX_INNER, tokens, channels < 2^31
+ *   x_scale, w_scale   tokens and channels floats;   bias   channels elements of `bias_type`, or NULL: 0
+ *   y        tokens x channels of `type`
+ * There is no gradient: it is for passes that need none (a teacher's, an evaluation, decoding).
+ * More than 8 tokens: the kernel waits for its own copies with the limit of cdadam_set_operator_wait_limit;
+ * what depends on one that did not arrive is NaN.
+ */
+int cdadam_matmul8(const int8_t *x, int64_t x_stride, const float *x_scale,
+                   const int8_t *w, int64_t w_stride, const float *w_scale, const void *bias,
+                   int64_t tokens, int64_t channels, int64_t inner, int type, int bias_type,
+                   void *y, int64_t y_stride, void *stream);
+
 /* Message of the calling thread's most recent failure ("" if none).  Never NULL. */
 const char *cdadam_last_error(void);
 

@@ -87,6 +87,26 @@ _SIGNATURES = {
     "cdadam_distill": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int,
                                   _c.c_int, _c.c_int, _c.c_float, _c.c_int, _c.c_void_p, _c.c_void_p, _c.c_void_p,
                                   _c.c_int64, _c.c_void_p]),
+    "cdadam_rms_norm": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_int64,
+                                   _c.c_float, _c.c_int, _c.c_int, _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64,
+                                   _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64,
+                                   _c.c_void_p, _c.c_void_p]),
+    "cdadam_rms_norm_backward": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64,
+                                            _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64,
+                                            _c.c_int64, _c.c_int, _c.c_int, _c.c_int, _c.c_void_p, _c.c_int64, _c.c_void_p,
+                                            _c.c_int64, _c.c_int, _c.c_void_p, _c.c_int64, _c.c_void_p]),
+    "cdadam_rms_norm_workspace": (_c.c_int64, [_c.c_int64, _c.c_int64, _c.c_int64]),
+    "cdadam_quantize_rows": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_int, _c.c_void_p, _c.c_int64,
+                                        _c.c_void_p, _c.c_void_p]),
+    "cdadam_dequantize_rows": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int,
+                                          _c.c_void_p, _c.c_int64, _c.c_void_p]),
+    "cdadam_checkpoint8": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_int, _c.c_void_p, _c.c_int64,
+                                      _c.c_void_p, _c.c_int64, _c.c_void_p]),
+    "cdadam_checkpoint8_restore": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64,
+                                              _c.c_int, _c.c_void_p, _c.c_int64, _c.c_void_p]),
+    "cdadam_matmul8": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_void_p,
+                                  _c.c_int64, _c.c_int64, _c.c_int64, _c.c_int, _c.c_int, _c.c_void_p, _c.c_int64,
+                                  _c.c_void_p]),
     "cdadam_profile_enable": (_c.c_int, [_c.c_void_p, _c.c_int]),
     "cdadam_profile_read": (_c.c_int, [_c.c_void_p, _c.POINTER(_c.c_double), _c.POINTER(_c.c_int64)]),
     "cdadam_profile_name": (_c.c_char_p, [_c.c_void_p, _c.c_int]),
@@ -716,3 +736,239 @@ def distill(logits, teacher_ids, teacher_logprobs, dloss=None, temperature=1.0, 
     if code:
         _check(code)
     return loss, dz
+
+
+# -- operators in 8 bits ---------------------------------------------------------------------
+# Two formats of 8-bit rows, each a pair of tensors: (q int8, scale float32[rows]), a step for every row; and a
+# checkpoint (kept int8, exponents uint8[rows, ceil(cols / 32)]), a power of two for every 32 columns.  Those that
+# are allocated here have rows that start on 16 bytes, which matmul8 needs.
+CHECKPOINT_BLOCK, MAX_INNER = 32, 131071
+
+
+def _rows8(rows, cols, device):
+    return torch.empty(rows, (cols + 15) // 16 * 16, dtype=torch.int8, device=device)[:, :cols]
+
+
+def _bytes(t, what, device, shape, dtype=torch.int8):
+    """(pointer, row stride) of a matrix of bytes."""
+    if t.get_device() != device or t.shape != shape or t.dtype != dtype or (shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be %s %s on device %d with adjacent row elements, not %s %s on %s"
+                         % (what, tuple(shape), dtype, device, tuple(t.shape), t.dtype, t.device))
+    return t.data_ptr(), t.stride(0)
+
+
+def _checkpoint(pair, device, shape):
+    """(pointer, row stride) of both parts of a checkpoint."""
+    kept, exponents = pair
+    return _bytes(kept, "kept", device, shape) + _bytes(exponents, "exponents", device, (shape[0], -(-shape[1] // CHECKPOINT_BLOCK)),
+                                                        torch.uint8)
+
+
+def checkpoint8_like(x):
+    """A checkpoint (kept, exponents) of a matrix of x's shape to be written into."""
+    rows, cols = x.shape
+    return _rows8(rows, cols, x.device), torch.empty(rows, -(-cols // CHECKPOINT_BLOCK), dtype=torch.uint8, device=x.device)
+
+
+def _rms_norm(x, weight, residual, eps, y, q, scale, total, rstd, checkpoint):
+    device, shape, dtype = x.get_device(), x.shape, x.dtype
+    px, sx = _matrix(x, "x")
+    rows, cols = shape
+    pr, sr = (None, 0) if residual is None else _matrix(residual, "residual", device, shape, dtype)
+    pt, st = (None, 0) if total is None else _matrix(total, "total", device, shape, dtype)
+    py, sy = (None, 0) if y is None else _matrix(y, "y", device, shape, dtype)
+    pq, sq = (None, 0) if q is None else _bytes(q, "q", device, shape)
+    pk, sk, pe, se = (None, 0, None, 0) if checkpoint is None else _checkpoint(checkpoint, device, shape)
+    w, _, wt = _parameters(weight, None, cols, device)
+    code = lib().cdadam_rms_norm(px, sx, pr, sr, w, rows, cols, eps, _TYPES[dtype], wt, pt, st, py, sy, pq, sq,
+                                 _vector(scale, "scale", device, (rows,), _FLOAT), pk, sk, pe, se,
+                                 _vector(rstd, "rstd", device, (rows,), _FLOAT), _raw_stream(device))
+    if code:
+        _check(code)
+
+
+def rms_norm(x, weight=None, residual=None, eps=1e-6, out=None, checkpoint=None, stream=None):
+    """Root-mean-square norm of every row of x (rows x cols), or of x + residual where that is given:
+    (y, total, rstd), total being the sum as x's type holds it (None without residual).  weight: cols elements of
+    any of the three types.  out: (y, total, rstd) to write into, each may be None: y is then allocated, total and
+    rstd are not computed.  checkpoint: (kept, exponents) to write the sum's checkpoint into
+    (checkpoint8_like).  No automatic differentiation: rms_norm_backward is the gradient."""
+    _matrix(x, "x")
+    device = x.get_device()
+    if device < 0 or stream is not None or device != _current():
+        with _elsewhere(x, stream):
+            return rms_norm(x, weight, residual, eps, out, checkpoint)
+    if out is None:
+        y, rstd = torch.empty(x.shape, dtype=x.dtype, device=x.device), torch.empty(x.shape[0], device=x.device)
+        total = None if residual is None else torch.empty_like(y)
+    else:
+        y, total, rstd = out
+        if y is None:
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _rms_norm(x, weight, residual, eps, y, None, None, total, rstd, checkpoint)
+    return y, total, rstd
+
+
+def rms_norm8(x, weight=None, residual=None, eps=1e-6, out=None, checkpoint=None, stream=None):
+    """rms_norm with its output in 8 bits: (q, scale, total, rstd), as matmul8 takes it.  out: the four to write
+    into; total and rstd may be None: not computed."""
+    _matrix(x, "x")
+    device = x.get_device()
+    if device < 0 or stream is not None or device != _current():
+        with _elsewhere(x, stream):
+            return rms_norm8(x, weight, residual, eps, out, checkpoint)
+    if out is None:
+        q = _rows8(*x.shape, x.device)
+        scale, rstd = torch.empty(2, x.shape[0], device=x.device).unbind(0)
+        total = None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        q, scale, total, rstd = out
+        if q is None or scale is None:
+            raise ValueError("out needs q and scale")
+    _rms_norm(x, weight, residual, eps, None, q, scale, total, rstd, checkpoint)
+    return q, scale, total, rstd
+
+
+def rms_norm_backward(dy, x, weight, rstd, dtotal=None, groups=1, accumulate=False, out=None, workspace=None, stream=None):
+    """Gradient of rms_norm: (dx, dweight).  x: what was normed (the total, or x where there was no residual),
+    or its checkpoint (kept, exponents).  dtotal: the gradient that comes along the residual; dx is the gradient of x and
+    of the residual alike.  dweight is groups x cols, summed over the rows of each of `groups` equal parts of the
+    batch (one per worker).  out: the two to write into, each may be None: not computed; dweight may be a strided slice
+    of the n x d gradient buffer and is added to with accumulate.  workspace: a contiguous CUDA tensor of at least
+    rms_norm_workspace(rows, cols, groups) bytes to use instead of allocating one."""
+    pdy, sdy = _matrix(dy, "dy")
+    device, shape, dtype = dy.get_device(), dy.shape, dy.dtype
+    if device < 0 or stream is not None or device != _current():
+        with _elsewhere(dy, stream):
+            return rms_norm_backward(dy, x, weight, rstd, dtotal, groups, accumulate, out, workspace)
+    rows, cols = shape
+    if isinstance(x, (tuple, list)):
+        px, sx, pe, se = _checkpoint(x, device, shape)
+    else:
+        (px, sx), pe, se = _matrix(x, "x", device, shape, dtype), None, 0
+    w, _, wt = _parameters(weight, None, cols, device)
+    pdt, sdt = (None, 0) if dtotal is None else _matrix(dtotal, "dtotal", device, shape, dtype)
+    sums = (groups, cols)
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        dx, dweight = torch.empty(shape, dtype=dtype, device=dy.device), torch.empty(sums, device=dy.device)
+    else:
+        dx, dweight = out
+    pdx, sdx = (None, 0) if dx is None else _matrix(dx, "dx", device, shape, dtype)
+    gt = None if dweight is None else dweight.dtype
+    pw, sw = (None, 0) if dweight is None else _matrix(dweight, "dweight", device, sums, gt)
+    if workspace is None:
+        need = lib().cdadam_rms_norm_workspace(rows, cols, groups) if dweight is not None else 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=dy.device) if need else None
+        pws = None if workspace is None else workspace.data_ptr()
+    elif workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on %s" % dy.device)
+    else:
+        need, pws = workspace.numel() * workspace.element_size(), workspace.data_ptr()
+    code = lib().cdadam_rms_norm_backward(
+        pdy, sdy, px, sx, pe, se, w, _vector(rstd, "rstd", device, (rows,), _FLOAT), pdt, sdt, rows, cols, groups, _TYPES[dtype], wt,
+        F32 if gt is None else _TYPES[gt], pdx, sdx, pw, sw, 1 if accumulate else 0, pws, need, _raw_stream(device))
+    if code:
+        _check(code)
+    return dx, dweight
+
+
+def rms_norm_workspace(rows, cols, groups=1):
+    """Bytes of workspace rms_norm_backward needs for dweight."""
+    return lib().cdadam_rms_norm_workspace(rows, cols, groups)
+
+
+def quantize_rows(x, out=None, stream=None):
+    """Rows of x in 8 bits, a step for each row: (q, scale).  out: the two to write into."""
+    px, sx = _matrix(x, "x")
+    device, shape = x.get_device(), x.shape
+    if device < 0 or stream is not None or device != _current():
+        with _elsewhere(x, stream):
+            return quantize_rows(x, out)
+    q, scale = (_rows8(*shape, x.device), torch.empty(shape[0], device=x.device)) if out is None else out
+    pq, sq = _bytes(q, "q", device, shape)
+    code = lib().cdadam_quantize_rows(px, sx, shape[0], shape[1], _TYPES[x.dtype], pq, sq,
+                                      _vector(scale, "scale", device, shape[:1], _FLOAT), _raw_stream(device))
+    if code:
+        _check(code)
+    return q, scale
+
+
+def dequantize_rows(q, scale, dtype=torch.float32, out=None, stream=None):
+    """The values q * scale of 8-bit rows, in dtype, or in out and its type."""
+    device, shape = q.get_device(), q.shape
+    if device < 0 or stream is not None or device != _current():
+        with _elsewhere(q, stream):
+            return dequantize_rows(q, scale, dtype, out)
+    if len(shape) != 2:
+        raise ValueError("q must be a matrix")
+    pq, sq = _bytes(q, "q", device, shape)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=q.device)
+    po, so = _matrix(out, "out", device, shape, out.dtype)
+    code = lib().cdadam_dequantize_rows(pq, sq, _vector(scale, "scale", device, shape[:1], _FLOAT), shape[0], shape[1],
+                                        _TYPES[out.dtype], po, so, _raw_stream(device))
+    if code:
+        _check(code)
+    return out
+
+
+def checkpoint8(x, out=None, stream=None):
+    """Checkpoint of x in 8 bits, a power of two for every 32 columns of a row: (kept, exponents).  out: the two to
+    write into."""
+    px, sx = _matrix(x, "x")
+    device, shape = x.get_device(), x.shape
+    if device < 0 or stream is not None or device != _current():
+        with _elsewhere(x, stream):
+            return checkpoint8(x, out)
+    out = checkpoint8_like(x) if out is None else out
+    code = lib().cdadam_checkpoint8(px, sx, shape[0], shape[1], _TYPES[x.dtype], *_checkpoint(out, device, shape),
+                                    _raw_stream(device))
+    if code:
+        _check(code)
+    return tuple(out)
+
+
+def checkpoint8_restore(kept, exponents, dtype=torch.float32, out=None, stream=None):
+    """The values of a checkpoint, in dtype, or in out and its type; exact in the type it was kept from and in
+    bfloat16."""
+    device, shape = kept.get_device(), kept.shape
+    if device < 0 or stream is not None or device != _current():
+        with _elsewhere(kept, stream):
+            return checkpoint8_restore(kept, exponents, dtype, out)
+    if len(shape) != 2:
+        raise ValueError("kept must be a matrix")
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=kept.device)
+    po, so = _matrix(out, "out", device, shape, out.dtype)
+    code = lib().cdadam_checkpoint8_restore(*_checkpoint((kept, exponents), device, shape), shape[0], shape[1],
+                                            _TYPES[out.dtype], po, so, _raw_stream(device))
+    if code:
+        _check(code)
+    return out
+
+
+def matmul8(x, x_scale, w, w_scale, bias=None, dtype=torch.bfloat16, out=None, stream=None):
+    """Product of 8-bit rows: y[t, c] = (sum_k x[t, k] w[c, k]) x_scale[t] w_scale[c] + bias[c], tokens x channels in
+    dtype, or in out and its type.  x: tokens x inner, w: channels x inner, as rms_norm8 and quantize_rows give them
+    (rows start on 16 bytes); bias: channels elements of any of the three types.  There is no gradient."""
+    device = x.get_device()
+    if device < 0 or stream is not None or device != _current():
+        with _elsewhere(x, stream):
+            return matmul8(x, x_scale, w, w_scale, bias, dtype, out)
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x and w must be matrices")
+    (tokens, inner), channels = x.shape, w.shape[0]
+    px, sx = _bytes(x, "x", device, (tokens, inner))
+    pw, sw = _bytes(w, "w", device, (channels, inner))
+    pb = _vector(bias, "bias", device, (channels,), _TYPES)
+    if out is None:
+        out = torch.empty(tokens, channels, dtype=dtype, device=x.device)
+    po, so = _matrix(out, "out", device, (tokens, channels), out.dtype)
+    code = lib().cdadam_matmul8(
+        px, sx, _vector(x_scale, "x_scale", device, (tokens,), _FLOAT), pw, sw, _vector(w_scale, "w_scale", device, (channels,), _FLOAT),
+        pb, tokens, channels, inner, _TYPES[out.dtype], F32 if bias is None else _TYPES[bias.dtype], po, so, _raw_stream(device))
+    if code:
+        _check(code)
+    return out

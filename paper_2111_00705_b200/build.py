@@ -9,13 +9,15 @@ multiply-add contraction is off so that every operation rounds once.
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcdadam.so")
 SOURCES = ["cdadam_api.cu", "sign_kernels.cu", "dense_kernels.cu", "topk_kernels.cu",
-           "static_scratch.cu", "operators_api.cu", "layer_norm.cu", "logits.cu"]
+           "static_scratch.cu", "operators_api.cu", "layer_norm.cu", "logits.cu",
+           "rms_norm.cu", "matmul8.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-fmad=false", "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 
@@ -40,16 +42,14 @@ def build(force=False, verbose=False):
         return LIB
     os.makedirs(OBJ, exist_ok=True)
     nvcc = _nvcc()
-    objs = []
+    objs = [os.path.join(OBJ, src.replace(".cu", ".o")) for src in SOURCES]
+    cmds = [[nvcc] + NVCC_FLAGS + ["-c", os.path.join(CSRC, src), "-o", obj] for src, obj in zip(SOURCES, objs)]
     log = []
-    for src in SOURCES:
-        obj = os.path.join(OBJ, src.replace(".cu", ".o"))
-        cmd = [nvcc] + NVCC_FLAGS + ["-c", os.path.join(CSRC, src), "-o", obj]
-        r = subprocess.run(cmd, capture_output=True, text=True)
-        log.append("$ " + " ".join(cmd) + "\n" + r.stdout + r.stderr)
-        if r.returncode != 0:
-            raise RuntimeError("nvcc failed:\n" + log[-1])
-        objs.append(obj)
+    with ThreadPoolExecutor(os.cpu_count() or 1) as pool:
+        for cmd, r in zip(cmds, pool.map(lambda c: subprocess.run(c, capture_output=True, text=True), cmds)):
+            log.append("$ " + " ".join(cmd) + "\n" + r.stdout + r.stderr)
+            if r.returncode != 0:
+                raise RuntimeError("nvcc failed:\n" + log[-1])
     tmp = LIB + ".%d.tmp" % os.getpid()
     cmd = [nvcc, "-shared", "-o", tmp] + objs
     r = subprocess.run(cmd, capture_output=True, text=True)

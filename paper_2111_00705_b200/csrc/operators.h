@@ -100,6 +100,54 @@ struct Distill {
     int wait_limit;
 };
 
+// A matrix of elements of the operator's type.
+struct Matrix {
+    void *p; int64_t stride;            // NULL: not given
+};
+// An 8-bit matrix and what goes with it: a step per row (rows format) or an exponent for every 32 columns of a row
+// (checkpoint).
+struct Rows8 {
+    int8_t *p; int64_t stride;
+    float *scale;
+};
+struct Kept8 {
+    int8_t *p; int64_t stride;
+    uint8_t *exponents; int64_t exponents_stride;
+};
+
+struct RmsNorm {
+    Matrix x, residual;
+    AnyVec weight;
+    int64_t rows, cols;
+    float eps;
+    int normalise;      // 0: s = 1 (the rows format of x itself)
+    Matrix total, y;
+    Rows8 q;
+    Kept8 kept;
+    float *rstd;
+};
+
+struct RmsNormBackward {
+    Matrix dy, x;       // x.p NULL: kept
+    Kept8 kept;
+    AnyVec weight;
+    const float *rstd;
+    Matrix dtotal;
+    int64_t rows, cols, groups;
+    Matrix dx;
+    void *dweight; int64_t dweight_stride;
+    int grad_type, accumulate;
+    float *parts;       // workspace
+};
+
+struct Matmul8 {
+    Rows8 x, w;
+    AnyVec bias;
+    int64_t tokens, channels, inner;
+    void *y; int64_t y_stride;
+    int wait_limit;     // polls; < 0: the kernel's default
+};
+
 // type: 0 binary32, 1 bfloat16, 2 binary16 (the CDADAM_* codes)
 void launch_layer_norm(const NormForward &a, int type, cudaStream_t st);
 void launch_layer_norm_backward(const NormBackward &a, int type, cudaStream_t st);
@@ -107,5 +155,13 @@ int64_t layer_norm_workspace(int64_t rows, int64_t cols, int64_t groups);
 void launch_token_logprobs(const Logprobs &a, int type, cudaStream_t st);
 void launch_token_logprobs_backward(const LogprobsBackward &a, int type, cudaStream_t st);
 void launch_distill(const Distill &a, int type, cudaStream_t st);
+void launch_rms_norm(const RmsNorm &a, int type, cudaStream_t st);
+void launch_rms_norm_backward(const RmsNormBackward &a, int type, cudaStream_t st);
+int64_t rms_norm_workspace(int64_t rows, int64_t cols, int64_t groups);
+void launch_checkpoint8(const Matrix &x, const Kept8 &kept, int64_t rows, int64_t cols, int type, cudaStream_t st);
+// values of the rows format (kept.p NULL) or of a checkpoint
+void launch_restore8(const Rows8 &q, const Kept8 &kept, const Matrix &to, int64_t rows, int64_t cols, int type, cudaStream_t st);
+// false: the matrices could not be described to the copy engine (the driver refused)
+bool launch_matmul8(const Matmul8 &a, int type, cudaStream_t st);
 
 }  // namespace cdadam
