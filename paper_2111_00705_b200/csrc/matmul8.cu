@@ -7,6 +7,8 @@
 // cluster of blocks shares the row's length and adds its sums up through shared memory.
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "elements.cuh"
 
 namespace cdadam {
@@ -46,6 +48,17 @@ __device__ __forceinline__ void read_sums(uint32_t addr, int (&v)[16])
                  "tcgen05.wait::ld.sync.aligned;"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
                    "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void read_sums32(uint32_t addr, int (&v)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
+                 "%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+                   "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+                   "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+                   "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
                  : "r"(addr) : "memory");
 }
 __device__ __forceinline__ void cluster_barrier()
@@ -195,6 +208,192 @@ __global__ void __launch_bounds__(128) k_matmul8(const __grid_constant__ CUtenso
 }
 
 // ---------------------------------------------------------------------------------------------
+// Many tokens: pairs of blocks, one on each SM, that stay and take one tile of 256 channels and 256 tokens after
+// the other.  Each holds half of the channels' rows and half of the tokens', the tensor cores of the two read both
+// halves, and each ends up with the sums of its 128 channels and all 256 tokens.  Two sets of sums in tensor memory:
+// eight warps turn one into outputs while the other is being added up, four of them each half of the tokens, some tokens
+// at a time through shared memory, so that a token's 128 channels leave together.  The first block of a pair issues the products for both;
+// its `full` barriers count the copies of both, `empty` and `ready` are told to both, `drained` counts the warps of both.
+// ---------------------------------------------------------------------------------------------
+constexpr int kPairTile = 256, kPairRing = 5, kPairStage = 2 * kRowsP * kBytesK, kPairThreads = 320, kLeaveBytes = 8192;
+
+__device__ __forceinline__ uint32_t at_rank(const void *p, int rank)
+{
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(p)), "r"(rank));
+    return at;
+}
+__device__ __forceinline__ void tma_2d_pair(void *dst, const CUtensorMap *map, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(smem_addr(dst)), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint64_t *bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(smem_addr(bar)), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void mma8_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add)
+{
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
+                 "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add) : "memory");
+}
+
+__device__ __forceinline__ void half_barrier(int half) { asm volatile("bar.sync %0, 128;" ::"r"(half + 1) : "memory"); }
+
+// N tokens' outputs of a thread's channel to the staging place: row i is token i's 128 channels.
+template <typename T, int N>
+__device__ __forceinline__ void leave_tokens(T *to, const int (&v)[N], const float *x_scale, float w_scale, float bias)
+{
+#pragma unroll
+    for (int e = 0; e < N; e += 4) {
+        const float4 x = *reinterpret_cast<const float4 *>(x_scale + e);
+        const float2 a = add2(mul2(mul2(make_float2((float)v[e], (float)v[e + 1]), make_float2(x.x, x.y)), both(w_scale)), both(bias));
+        const float2 b = add2(mul2(mul2(make_float2((float)v[e + 2], (float)v[e + 3]), make_float2(x.z, x.w)), both(w_scale)), both(bias));
+        if constexpr (sizeof(T) == 4) {
+            to[e * kRowsP] = a.x; to[(e + 1) * kRowsP] = a.y; to[(e + 2) * kRowsP] = b.x; to[(e + 3) * kRowsP] = b.y;
+        } else {
+            const uint32_t p = Vec<T>::down(a), q = Vec<T>::down(b);
+            unsigned short *u = reinterpret_cast<unsigned short *>(to);
+            u[e * kRowsP] = (unsigned short)p; u[(e + 1) * kRowsP] = (unsigned short)(p >> 16);
+            u[(e + 2) * kRowsP] = (unsigned short)q; u[(e + 3) * kRowsP] = (unsigned short)(q >> 16);
+        }
+    }
+}
+
+// TILED: the outputs' rows start on 16 bytes and leave by tiled bulk copies.
+template <typename T, bool TILED>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap, Matmul8 a,
+               int tiles, int token_tiles)
+{
+    extern __shared__ char raw[];
+    char *const stages = raw + (-smem_addr(raw) & 1023);
+    __shared__ uint64_t full[kPairRing], empty[kPairRing], ready[2], drained[2];
+    __shared__ uint32_t tmem;
+    __shared__ __align__(16) float x_scale[2][kPairTile];
+    const int warp = threadIdx.x >> 5, rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int blocks = (int)((a.inner + kBytesK - 1) / kBytesK);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kPairRing; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&ready[i], 1);
+            mbar_init(&drained[i], 16);
+        }
+        mbar_fence_init();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem)), "r"(2 * kPairTile) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+    fence_before();
+    __syncthreads();
+    cluster_barrier();
+    fence_after();
+    const uint32_t sums = tmem;
+    int late = 0;
+    if (threadIdx.x == 0) {
+        int i = 0;
+        for (int tile = pair; tile < tiles && late < 2; tile += pairs) {
+            const int channel = tile / token_tiles * kPairTile + rank * kRowsP, token = tile % token_tiles * kPairTile + rank * kRowsP;
+            for (int b = 0; b < blocks; ++b, ++i) {
+                const int s = i % kPairRing, phase = i / kPairRing & 1;
+                if (i >= kPairRing) late = wait_for(&empty[s], phase ^ 1, a.wait_limit, late);
+                if (late == 2) break;
+                if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * kPairStage);
+                char *to = stages + s * kPairStage;
+                const uint32_t bar = at_rank(&full[s], 0);
+                tma_2d_pair(to, &wmap, b * kBytesK, channel, bar);
+                tma_2d_pair(to + kRowsP * kBytesK, &xmap, b * kBytesK, token, bar);
+            }
+        }
+        // what is under way lands before the pair leaves
+        if (late == 2 && rank == 0)
+            for (int k = max(0, i - kPairRing); k < i; ++k) mbar_wait_bounded(&full[k % kPairRing], k / kPairRing & 1);
+    } else if (threadIdx.x == 32 && rank == 0) {
+        int i = 0, set = 0;
+        for (int tile = pair; tile < tiles && late < 2; tile += pairs, ++set) {
+            const int buffer = set & 1;
+            if (set >= 2) late = wait_for(&drained[buffer], (set >> 1 & 1) ^ 1, a.wait_limit, late);
+            fence_after();
+            for (int b = 0; b < blocks; ++b, ++i) {
+                const int s = i % kPairRing, phase = i / kPairRing & 1;
+                late = wait_for(&full[s], phase, a.wait_limit, late);
+                if (late == 2) break;
+                fence_after();
+                const uint64_t w = operand(stages + s * kPairStage), x = operand(stages + s * kPairStage + kRowsP * kBytesK);
+#pragma unroll
+                for (int k = 0; k < kBytesK / 32; ++k)
+                    mma8_pair(sums + buffer * kPairTile, w + 2 * k, x + 2 * k, shape8(2 * kRowsP, kPairTile), b > 0 || k > 0);
+                commit_pair(&empty[s]);
+            }
+            if (late < 2) commit_pair(&ready[buffer]);
+        }
+    } else if (warp >= 2) {
+        constexpr int CHUNK = kLeaveBytes / kRowsP / (int)sizeof(T), HALF = kPairTile / 2;  // tokens at a time: 16 or 32
+        const int lane = threadIdx.x & 31, quarter = warp & 3, half = (warp - 2) >> 2, row = quarter * 32 + lane;
+        const bool first = (threadIdx.x - 64) % 128 == 0;
+        char *const leave = stages + kPairRing * kPairStage + half * 2 * kLeaveBytes;
+        int set = 0, place = 0;
+        for (int tile = pair; tile < tiles; tile += pairs, ++set) {
+            const int buffer = set & 1;
+            const int64_t token0 = (int64_t)(tile % token_tiles) * kPairTile + half * HALF;
+            const int64_t channel0 = (int64_t)(tile / token_tiles) * kPairTile + rank * kRowsP;
+            const bool mine = channel0 + row < a.channels;
+            float w_scale = mine ? a.w.scale[channel0 + row] : 0.0f;
+            const float bias = mine && a.bias.p ? any_at(a.bias, channel0 + row) : 0.0f;
+            float *const xs = &x_scale[buffer][half * HALF];
+            xs[row] = token0 + row < a.tokens ? a.x.scale[token0 + row] : 0.0f;
+            late = wait_for(&ready[buffer], set >> 1 & 1, a.wait_limit, late);
+            if (late) w_scale = __uint_as_float(0x7fc00000u);
+            __syncwarp();
+            fence_after();
+            const uint32_t at = sums + buffer * kPairTile + half * HALF + ((uint32_t)quarter << 21);
+#pragma unroll 1
+            for (int c = 0; c < HALF; c += CHUNK, place ^= 1) {
+                int v[CHUNK];
+                if constexpr (CHUNK == 32) read_sums32(at + c, v); else read_sums(at + c, v);
+                T *const to = reinterpret_cast<T *>(leave + place * kLeaveBytes);
+                if (TILED && first) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                half_barrier(half);                     // what was here before has left; the scales are there
+                leave_tokens<T, CHUNK>(to + row, v, xs + c, w_scale, bias);
+                if (TILED) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                half_barrier(half);
+                if (token0 + c >= a.tokens) continue;
+                if (TILED) {
+                    if (first) {
+                        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+                                     ::"l"(&ymap), "r"((int)channel0), "r"((int)(token0 + c)), "r"(smem_addr(to)) : "memory");
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
+                } else {
+#pragma unroll 4
+                    for (int i = quarter; i < CHUNK; i += 4)
+#pragma unroll
+                        for (int k = 0; k < kRowsP; k += 32)
+                            if (channel0 + k + lane < a.channels && token0 + c + i < a.tokens)
+                                static_cast<T *>(a.y)[(token0 + c + i) * a.y_stride + channel0 + k + lane] = to[i * kRowsP + k + lane];
+                }
+            }
+            fence_before();
+            __syncwarp();
+            if (lane == 0)
+                asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(at_rank(&drained[buffer], 0)) : "memory");
+        }
+        if (TILED && first) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    cluster_barrier();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(sums), "r"(2 * kPairTile));
+}
+
+// ---------------------------------------------------------------------------------------------
 // Launches
 // ---------------------------------------------------------------------------------------------
 typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
@@ -222,6 +421,23 @@ static bool describe(CUtensorMap *map, const Rows8 &m, int64_t rows, int64_t inn
     const cuuint32_t box[2] = {kBytesK, (cuuint32_t)box_rows}, ones[2] = {1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, m.p, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T> static CUtensorMapDataType type_of()
+{
+    return std::is_same<T, float>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+           : std::is_same<T, bf16>::value ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+}
+// Boxes of 128 channels of some tokens.
+static bool describe_outputs(CUtensorMap *map, const Matmul8 &a, CUtensorMapDataType type, int size, int box_rows)
+{
+    const EncodeTiled fn = encode_tiled();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)a.channels, (cuuint64_t)a.tokens};
+    const cuuint64_t strides[1] = {(cuuint64_t)(a.tokens > 1 ? a.y_stride * size : (a.channels * size + 15) / 16 * 16)};
+    const cuuint32_t box[2] = {kRowsP, (cuuint32_t)box_rows}, ones[2] = {1, 1};
+    return fn(map, type, 2, a.y, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+              CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <typename T, int BN>
@@ -254,8 +470,24 @@ static bool product_as(const Matmul8 &a, cudaStream_t st)
     return true;
 }
 template <typename T>
+static bool product_by_pairs(const Matmul8 &a, cudaStream_t st)
+{
+    CUtensorMap wmap, xmap;
+    if (!describe(&wmap, a.w, a.channels, a.inner, kRowsP) || !describe(&xmap, a.x, a.tokens, a.inner, kRowsP)) return false;
+    const int64_t token_tiles = (a.tokens + kPairTile - 1) / kPairTile, tiles = (a.channels + kPairTile - 1) / kPairTile * token_tiles;
+    CUtensorMap ymap = {};
+    const bool tiled = ((uintptr_t)a.y & 15) == 0 && (a.tokens == 1 || a.y_stride * (int64_t)sizeof(T) % 16 == 0);
+    if (tiled && !describe_outputs(&ymap, a, type_of<T>(), sizeof(T), kLeaveBytes / kRowsP / (int)sizeof(T))) return false;
+    const size_t smem = kPairRing * kPairStage + 4 * kLeaveBytes + 1024;
+    auto kernel = tiled ? k_matmul8_pair<T, true> : k_matmul8_pair<T, false>;
+    allow_shared(kernel, smem);
+    queue(kernel, dim3((unsigned)(2 * (tiles < 74 ? tiles : 74))), kPairThreads, smem, st, wmap, xmap, ymap, a, (int)tiles, (int)token_tiles);
+    return true;
+}
+template <typename T>
 static bool product(const Matmul8 &a, cudaStream_t st)
 {
+    if (a.tokens > 128 && (a.tokens + 255) / 256 * ((a.channels + 255) / 256) >= 74) return product_by_pairs<T>(a, st);
     if (a.tokens <= 16) return product_as<T, 16>(a, st);
     if (a.tokens <= 32) return product_as<T, 32>(a, st);
     if (a.tokens <= 64) return product_as<T, 64>(a, st);
