@@ -65,14 +65,13 @@ __device__ __forceinline__ void cluster_barrier()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ int load_peer(const void *p, int rank)
+__device__ __forceinline__ uint32_t at_rank(const void *p, int rank)
 {
     uint32_t at;
-    int v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(p)), "r"(rank));
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-    return v;
+    return at;
 }
+__device__ __forceinline__ void store_at(uint32_t at, int v) { asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
 
 // What has become of a thread's waits: 0: all in time; 1: one ran out and the thread waited a second time, with the
 // default limit: the block's results are NaN; 2: that was in vain too: nothing more is waited for or started.
@@ -178,29 +177,32 @@ __global__ void __launch_bounds__(128) k_matmul8(const __grid_constant__ CUtenso
                     store_product<T>(a, token0 + c + e, channel, v[e], x_scale[c + e], w_scale, bias, none);
         }
     } else {
-        // every block leaves its sums in the stages' place and adds up a share of the tokens
-        int *const left = reinterpret_cast<int *>(stages);
-        __shared__ int any_late;
-        if (threadIdx.x == 0) any_late = 0;
-        __syncthreads();
-        if (none) any_late = 1;
+        // every block adds up a share of the tokens: the others send it their sums, in the place of its stages
+        const int share = BN / splits;
+        __shared__ int late_of[8];
+        __syncwarp();
+        cluster_barrier();                              // the stages of all are free
+        if ((int)threadIdx.x < splits) store_at(at_rank(&late_of[rank], threadIdx.x), none);
 #pragma unroll 1
         for (int c = 0; c < BN; c += 16) {
             int v[16];
+            __syncwarp();
             read_sums(lane_at + c, v);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) left[(c + e) * kRowsP + threadIdx.x] = v[e];
-        }
-        cluster_barrier();
-        for (int r = 0; r < splits; ++r) none |= load_peer(&any_late, r) != 0;
-        for (int c = BN * rank / splits; c < BN * (rank + 1) / splits; ++c) {
-            if (token0 + c >= a.tokens) break;
-            int v = 0;
-            for (int r = 0; r < splits; ++r) v += load_peer(&left[c * kRowsP + threadIdx.x], r);
-            if (mine) store_product<T>(a, token0 + c, channel, v, x_scale[c], w_scale, bias, none);
+            for (int e = 0; e < 16; ++e)
+                store_at(at_rank(stages, (c + e) / share) + (((rank * share + (c + e) % share) * kRowsP + threadIdx.x) << 2), v[e]);
         }
         __syncwarp();
-        cluster_barrier();                              // no block leaves while others read from it
+        cluster_barrier();
+        for (int r = 0; r < splits; ++r) none |= late_of[r] != 0;
+        const int *const sent = reinterpret_cast<const int *>(stages) + threadIdx.x;
+#pragma unroll 4
+        for (int c = 0; c < share; ++c) {
+            int v = 0;
+            for (int r = 0; r < splits; ++r) v += sent[(r * share + c) * kRowsP];
+            const int64_t token = token0 + rank * share + c;
+            if (mine && token < a.tokens) store_product<T>(a, token, channel, v, x_scale[rank * share + c], w_scale, bias, none);
+        }
     }
     fence_before();
     __syncthreads();
@@ -217,12 +219,6 @@ __global__ void __launch_bounds__(128) k_matmul8(const __grid_constant__ CUtenso
 // ---------------------------------------------------------------------------------------------
 constexpr int kPairTile = 256, kPairRing = 5, kPairStage = 2 * kRowsP * kBytesK, kPairThreads = 320, kLeaveBytes = 8192;
 
-__device__ __forceinline__ uint32_t at_rank(const void *p, int rank)
-{
-    uint32_t at;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(p)), "r"(rank));
-    return at;
-}
 __device__ __forceinline__ void tma_2d_pair(void *dst, const CUtensorMap *map, int x, int y, uint32_t bar)
 {
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
