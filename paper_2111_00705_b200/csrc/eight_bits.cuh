@@ -9,30 +9,26 @@ namespace cdadam {
 template <typename T> struct Raw8 { uint32_t w[2 * sizeof(T)]; };
 
 template <typename T>
-__device__ __forceinline__ void widen8(const Raw8<T> &u, float (&f)[8])
+__device__ __forceinline__ void widen8(const Raw8<T> &u, float2 (&f)[4])
 {
-    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(u.w[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float2 v = Vec<T>::up(u.w[e]);
-            f[2 * e] = v.x;
-            f[2 * e + 1] = v.y;
-        }
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 4) f[e] = make_float2(__uint_as_float(u.w[2 * e]), __uint_as_float(u.w[2 * e + 1]));
+        else f[e] = Vec<T>::up(u.w[e]);
     }
 }
 template <typename T>
-__device__ __forceinline__ Raw8<T> narrow8(const float (&f)[8])
+__device__ __forceinline__ Raw8<T> narrow8(const float2 (&f)[4])
 {
     Raw8<T> u;
-    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u.w[e] = __float_as_uint(f[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) u.w[e] = Vec<T>::down(make_float2(f[2 * e], f[2 * e + 1]));
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 4) {
+            u.w[2 * e] = __float_as_uint(f[e].x);
+            u.w[2 * e + 1] = __float_as_uint(f[e].y);
+        } else {
+            u.w[e] = Vec<T>::down(f[e]);
+        }
     }
     return u;
 }
@@ -41,20 +37,38 @@ __device__ __forceinline__ uint32_t element_bits(const float *p) { return __floa
 __device__ __forceinline__ uint32_t element_bits(const bf16 *p) { return __ldcs(reinterpret_cast<const unsigned short *>(p)); }
 __device__ __forceinline__ uint32_t element_bits(const f16 *p) { return __ldcs(reinterpret_cast<const unsigned short *>(p)); }
 
-// Columns j .. j + 7 of a row, 0 beyond its end.  VEC: every row starts on 16 bytes.
-template <typename T, bool VEC>
-__device__ __forceinline__ Raw8<T> load8(const T *row, int64_t j, int64_t cols)
+// A matrix as units are taken from it.  VEC: every row starts on 16 bytes, a unit is one or two vectors.  Otherwise a
+// unit is cut out of the aligned vectors around it (and put into those that it shares with its
+// neighbours, which are the neighbouring threads' units): a third of the time of eight elements one by one.  A
+// vector may hold bytes of the rows before and after; of the first and last rows, where those would lie
+// outside the matrix, what is not inside the row is taken element by element.
+template <typename T> struct Place {
+    T *p;
+    int64_t stride, rows, near;     // rows this near to an end of the matrix have no neighbours on both sides
+    __device__ __forceinline__ T *row(int64_t r) const { return p + r * stride; }
+    __device__ __forceinline__ bool edge(int64_t r) const { return r < near || rows - 1 - r < near; }
+};
+template <typename T>
+__device__ __forceinline__ Place<T> place(const Matrix &m, int64_t rows)
+{
+    // the vectors around a unit reach less than 48 bytes beyond it
+    return {static_cast<T *>(m.p), m.stride, rows, m.stride > 0 ? 47 / (m.stride * (int64_t)sizeof(T)) + 1 : rows};
+}
+
+// w[i + k] for i = 0 .. N - 1, 0 <= k < 4.
+template <int N>
+__device__ __forceinline__ void skip_words(uint32_t (&w)[N + 4], unsigned k)
+{
+#pragma unroll
+    for (int i = 0; i < N + 2; ++i) w[i] = k & 2 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < N + 1; ++i) w[i] = k & 1 ? w[i + 1] : w[i];
+}
+
+template <typename T>
+__device__ __forceinline__ Raw8<T> load_elements(const T *row, int64_t j, int64_t cols)
 {
     Raw8<T> u;
-    if (VEC && j + 8 <= cols) {
-        const uint4 *p = reinterpret_cast<const uint4 *>(row + j);
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-            const uint4 v = __ldcs(p + i);
-            u.w[4 * i] = v.x; u.w[4 * i + 1] = v.y; u.w[4 * i + 2] = v.z; u.w[4 * i + 3] = v.w;
-        }
-        return u;
-    }
 #pragma unroll
     for (int i = 0; i < 2 * (int)sizeof(T); ++i) u.w[i] = 0;
 #pragma unroll
@@ -62,21 +76,104 @@ __device__ __forceinline__ Raw8<T> load8(const T *row, int64_t j, int64_t cols)
         if (j + e < cols) u.w[e * sizeof(T) / 4] |= element_bits(row + j + e) << (e * sizeof(T) % 4 * 8);
     return u;
 }
+
+// Columns j .. j + 7 of row r, 0 beyond its end.
 template <typename T, bool VEC>
-__device__ __forceinline__ void store8(T *row, int64_t j, int64_t cols, const Raw8<T> &u)
+__device__ __forceinline__ Raw8<T> load8(const Place<T> &m, int64_t r, int64_t j, int64_t cols)
 {
-    if (VEC && j + 8 <= cols) {
-        uint4 *p = reinterpret_cast<uint4 *>(row + j);
+    constexpr int W = 2 * sizeof(T);
+    const T *const row = m.row(r);
+    Raw8<T> u;
+    if (VEC) {
+        if (j + 8 > cols) return load_elements(row, j, cols);
+        const uint4 *p = reinterpret_cast<const uint4 *>(row + j);
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) __stcs(p + i, make_uint4(u.w[4 * i], u.w[4 * i + 1], u.w[4 * i + 2], u.w[4 * i + 3]));
+        for (int i = 0; i < W / 4; ++i) {
+            const uint4 v = __ldcs(p + i);
+            u.w[4 * i] = v.x; u.w[4 * i + 1] = v.y; u.w[4 * i + 2] = v.z; u.w[4 * i + 3] = v.w;
+        }
+        return u;
+    }
+    if (j >= cols || (m.edge(r) && (j * (int64_t)sizeof(T) < 16 || (j + 8) * (int64_t)sizeof(T) + 16 > cols * (int64_t)sizeof(T))))
+        return load_elements(row, j, cols);
+    const uintptr_t at = (uintptr_t)(row + j);
+    const uint4 *p = reinterpret_cast<const uint4 *>(at & ~(uintptr_t)15);
+    uint32_t w[W + 4];
+#pragma unroll
+    for (int i = 0; i < W / 4 + 1; ++i) {
+        const uint4 v = p[i];               // the neighbours' next one: in the first-level cache
+        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+    }
+    skip_words<W>(w, (unsigned)(at >> 2) & 3);
+    const unsigned bits = sizeof(T) == 4 ? 0 : (unsigned)(at & 3) * 8;
+#pragma unroll
+    for (int i = 0; i < W; ++i) u.w[i] = sizeof(T) == 4 ? w[i] : __funnelshift_r(w[i], w[i + 1], bits);
+    if (j + 8 > cols)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (j + e >= cols) u.w[e * sizeof(T) / 4] &= sizeof(T) == 4 ? 0u : e & 1 ? 0x0000ffffu : 0xffff0000u;
+    return u;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_element(T *row, int64_t j, const Raw8<T> &u, int e)
+{
+    if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t *>(row)[j + e] = u.w[e];
+    else reinterpret_cast<unsigned short *>(row)[j + e] = (unsigned short)(u.w[e / 2] >> (e % 2 * 16));
+}
+// All lanes of the warp call it (with j >= cols: nothing is stored); lane l + 1 has the unit behind lane l's, or
+// one of another row.
+template <typename T, bool VEC>
+__device__ __forceinline__ void store8(const Place<T> &m, int64_t r, int64_t j, int64_t cols, const Raw8<T> &u)
+{
+    constexpr int W = 2 * sizeof(T);
+    T *const row = m.row(r);
+    if (VEC) {
+        if (j + 8 <= cols) {
+            uint4 *p = reinterpret_cast<uint4 *>(row + j);
+#pragma unroll
+            for (int i = 0; i < W / 4; ++i) __stcs(p + i, make_uint4(u.w[4 * i], u.w[4 * i + 1], u.w[4 * i + 2], u.w[4 * i + 3]));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (j + e < cols) store_element(row, j, u, e);
+        }
         return;
     }
+    // the aligned vectors whose last bytes are the unit's first ones begin with the last `over` elements of the
+    // unit before
+    const uintptr_t at = (uintptr_t)(row + j);
+    const unsigned over = (unsigned)(at & 15) / (unsigned)sizeof(T), lane = threadIdx.x & 31;
+    uint32_t w[W + 4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (j + e < cols) {
-            if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t *>(row)[j + e] = u.w[e];
-            else reinterpret_cast<unsigned short *>(row)[j + e] = (unsigned short)(u.w[e / 2] >> (e % 2 * 16));
+    for (int i = 0; i < 4; ++i) w[i] = __shfl_up_sync(0xffffffffu, u.w[W - 4 + i], 1);
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[4 + i] = u.w[i];
+    const int64_t j_before = __shfl_up_sync(0xffffffffu, j, 1);
+    const bool whole = j + 8 - over <= cols && (over == 0 || (lane > 0 && j > 0 && j_before == j - 8));
+    if (whole) {
+        const unsigned from = 16 - (unsigned)(at & 15);         // byte of w where the vectors begin
+        skip_words<W>(w, from >> 2 & 3);
+        if (from < 16 || over) {
+            const unsigned bits = (from & 3) * 8;
+            if (sizeof(T) != 4)
+#pragma unroll
+                for (int i = 0; i < W; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
         }
+        uint4 *p = reinterpret_cast<uint4 *>(at & ~(uintptr_t)15);
+#pragma unroll
+        for (int i = 0; i < W / 4; ++i)
+            __stcs(p + i, over ? make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3])
+                               : make_uint4(u.w[4 * i], u.w[4 * i + 1], u.w[4 * i + 2], u.w[4 * i + 3]));
+    }
+    // what no vector takes: the first elements where there is none, the last where the next lane has none
+    const bool next = __shfl_down_sync(0xffffffffu, whole && over > 0, 1) && lane < 31;
+    const int64_t j_next = __shfl_down_sync(0xffffffffu, j, 1);
+    const int first = whole ? 8 - (int)over : 0, last = over > 0 && next && j_next == j + 8 ? 8 - (int)over : 8;
+    if (first < last)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e >= first && e < last && j + e < cols) store_element(row, j, u, e);
 }
 
 // Eight bytes; `vec`: rows start on 8 bytes.
@@ -108,13 +205,16 @@ __device__ __forceinline__ uint2 low_bytes(const uint32_t (&q)[8])
     return v;
 }
 // A byte b of v ^ 0x80 in the last place of 2^23 is 2^23 + 128 + (signed) b.
-__device__ __forceinline__ void unpack_bytes(uint2 v, float (&f)[8])
+__device__ __forceinline__ void unpack_bytes(uint2 v, float2 (&f)[4])
 {
     v.x ^= 0x80808080u;
     v.y ^= 0x80808080u;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        f[e] = __fadd_rn(__uint_as_float(__byte_perm(e < 4 ? v.x : v.y, 0x4B000000u, 0x7440 | e % 4)), -8388736.0f);
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t w = e < 2 ? v.x : v.y;
+        f[e] = add2(make_float2(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440 | e % 2 * 2)),
+                                __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7441 | e % 2 * 2))), both(-8388736.0f));
+    }
 }
 // t + kWhole, |t| < 2^22, is t rounded to the nearest integer (to even at a half) and has that integer's lowest byte as its own.
 constexpr float kWhole = 12582912.0f;       // 3 * 2^22
@@ -123,13 +223,16 @@ __device__ __forceinline__ bool on(const void *p, int64_t stride_bytes, int byte
     return (((uintptr_t)p | (uintptr_t)stride_bytes) & (uintptr_t)(bytes - 1)) == 0;
 }
 
-__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }   // ordered as |v|, NaN largest
-__device__ __forceinline__ uint32_t magnitude8(const float (&f)[8])
+// The largest of m and |f|; NaN if any is NaN.  As bits, NaN is above infinity and that above all others.
+__device__ __forceinline__ float largest(float m, float2 f)
 {
-    uint32_t m = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) m = max(m, magnitude(f[e]));
-    return m;
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(fabsf(f.x)), "f"(fabsf(f.y)));
+    return r;
+}
+__device__ __forceinline__ float largest8(float m, const float2 (&f)[4])
+{
+    return largest(largest(largest(largest(m, f[0]), f[1]), f[2]), f[3]);
 }
 constexpr uint32_t kInfBits = 0x7f800000u;
 
@@ -158,32 +261,47 @@ __device__ __noinline__ inline int nearest_exactly(float p, float m)
     if (b > 0.0 && (a > half || (a == half && (k & 1)))) ++k;
     return p < 0.0f ? -k : k;
 }
-__device__ __forceinline__ uint2 to_rows8(const float (&p)[8], const Step &s)
+__device__ __noinline__ inline uint2 to_rows8_exactly(float2 a, float2 b, float2 c, float2 d, float m)
 {
-    bool near = s.tiny;
+    const float p[8] = {a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
     uint32_t q[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float t = __fmul_rn(p[e], s.inverse), n = __fadd_rn(t, kWhole);
-        q[e] = __float_as_uint(n);
-        near |= fabsf(__fsub_rn(t, __fsub_rn(n, kWhole))) > 0.49998f;
-    }
-    if (near)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) q[e] = (uint32_t)nearest_exactly(p[e], s.m);
+    for (int e = 0; e < 8; ++e) q[e] = (uint32_t)nearest_exactly(p[e], m);
     return low_bytes(q);
+}
+__device__ __forceinline__ uint2 to_rows8(const float2 (&p)[4], const Step &s)
+{
+    float off = 0.0f;                       // furthest from an integer; NaN where 127 / m is beyond binary32
+    uint32_t q[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float2 t = mul2(p[e], both(s.inverse)), n = add2(t, both(kWhole));
+        q[2 * e] = __float_as_uint(n.x);
+        q[2 * e + 1] = __float_as_uint(n.y);
+        const float2 whole = add2(n, both(-kWhole));
+        off = largest(off, add2(t, make_float2(-whole.x, -whole.y)));
+    }
+    if (off <= 0.49998f && !s.tiny) return low_bytes(q);
+    return to_rows8_exactly(p[0], p[1], p[2], p[3], s.m);
 }
 
 // Checkpoint.  All steps are exact but the rounding itself: a power of two scales.
 __device__ __forceinline__ uint32_t kept_exponent(uint32_t bits) { return bits >= kInfBits ? 255u : max((int)(bits >> 23) - 6, 1); }
-__device__ __forceinline__ uint2 to_kept8(const float (&x)[8], uint32_t exponent)
+// m: the bits of the block's largest magnitude.  Only where that is above 127 steps can a value round to 128.
+__device__ __forceinline__ uint2 to_kept8(const float2 (&x)[4], uint32_t m, uint32_t exponent)
 {
     if (exponent == 255) return make_uint2(0, 0);
     const float up = __uint_as_float((254u - exponent) << 23);
+    const bool clamp = (m & 0x7fffffu) >= 0x7e0000u;
     uint32_t q[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        q[e] = __float_as_uint(__fadd_rn(fminf(fmaxf(__fmul_rn(x[e], up), -127.0f), 127.0f), kWhole));
+    for (int e = 0; e < 4; ++e) {
+        float2 t = mul2(x[e], both(up));
+        if (clamp) t = make_float2(fminf(fmaxf(t.x, -127.0f), 127.0f), fminf(fmaxf(t.y, -127.0f), 127.0f));
+        const float2 n = add2(t, both(kWhole));
+        q[2 * e] = __float_as_uint(n.x);
+        q[2 * e + 1] = __float_as_uint(n.y);
+    }
     return low_bytes(q);
 }
 __device__ __forceinline__ float kept_step(uint32_t exponent)

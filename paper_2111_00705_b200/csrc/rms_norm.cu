@@ -16,23 +16,26 @@ __device__ __forceinline__ void group_wait(int group)
     if (THREADS > 32) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(THREADS) : "memory");
 }
 template <int THREADS>
-__device__ __forceinline__ void group_sum_max(float &sum, uint32_t &top, float2 *slot, int group)
+__device__ __forceinline__ float2 group_sum_max(float sum, uint32_t top, float2 *slot, int group)
 {
     constexpr int N = THREADS / 32;
     sum = warp_sum(sum);
     top = __reduce_max_sync(0xffffffffu, top);
-    if (N == 1) return;
+    if (N == 1) return make_float2(sum, __uint_as_float(top));
     if ((threadIdx.x & 31) == 0) slot[threadIdx.x / 32 % N] = make_float2(sum, __uint_as_float(top));
     group_wait<THREADS>(group);
+    if (N > 8) {
+        const float2 v = (threadIdx.x & 31) < N ? slot[threadIdx.x & 31] : both(0.0f);
+        return make_float2(warp_sum(v.x), __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v.y))));
+    }
     float2 v = slot[0];
-    sum = v.x;
-    top = __float_as_uint(v.y);
 #pragma unroll
     for (int i = 1; i < N; ++i) {
-        v = slot[i];
-        sum += v.x;
-        top = max(top, __float_as_uint(v.y));
+        const float2 f = slot[i];
+        v.x += f.x;
+        v.y = __uint_as_float(max(__float_as_uint(v.y), __float_as_uint(f.y)));
     }
+    return v;
 }
 template <int THREADS>
 __device__ __forceinline__ float group_sum(float sum, float *slot, int group)
@@ -42,6 +45,7 @@ __device__ __forceinline__ float group_sum(float sum, float *slot, int group)
     if (N == 1) return sum;
     if ((threadIdx.x & 31) == 0) slot[threadIdx.x / 32 % N] = sum;
     group_wait<THREADS>(group);
+    if (N > 8) return warp_sum((threadIdx.x & 31) < N ? slot[threadIdx.x & 31] : 0.0f);
     sum = slot[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) sum += slot[i];
@@ -62,35 +66,35 @@ __device__ __forceinline__ void fill_weight(float *w, const AnyVec &v, int cols,
     for (int j = threadIdx.x; j < 8 * units; j += blockDim.x)
         w[(j & 4 ? 4 * units : 0) + (j >> 3) * 4 + (j & 3)] = j >= cols ? 0.0f : v.p ? any_at(v, j) : 1.0f;
 }
-__device__ __forceinline__ void weight8(const float *w, int u, int units, float (&f)[8])
+__device__ __forceinline__ void weight8(const float *w, int u, int units, float2 (&f)[4])
 {
     const float4 a = *reinterpret_cast<const float4 *>(w + 4 * u), b = *reinterpret_cast<const float4 *>(w + 4 * (units + u));
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    f[0] = make_float2(a.x, a.y);
+    f[1] = make_float2(a.z, a.w);
+    f[2] = make_float2(b.x, b.y);
+    f[3] = make_float2(b.z, b.w);
 }
 
+// The sum with the residual, as the activations' type holds it.
 template <typename T>
-__device__ __forceinline__ T *row_of(const Matrix &m, int64_t r) { return static_cast<T *>(m.p) + r * m.stride; }
-
-// h of a unit: x, or the sum with the residual as the activations' type holds it.
-template <typename T>
-__device__ __forceinline__ void add_residual(float (&f)[8], const Raw8<T> &r)
+__device__ __forceinline__ Raw8<T> sum8(const Raw8<T> &x, const Raw8<T> &residual)
 {
-    float g[8];
-    widen8<T>(r, g);
+    float2 f[4], g[4];
+    widen8<T>(x, f);
+    widen8<T>(residual, g);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = widen(narrow<T>(__fadd_rn(f[e], g[e])));
+    for (int e = 0; e < 4; ++e) f[e] = add2(f[e], g[e]);
+    return narrow8<T>(f);
 }
 
 // A block of 32 columns of a checkpoint: four neighbouring threads' units.
-template <typename T>
-__device__ __forceinline__ void keep8(const Kept8 &k, int64_t row, int64_t j, int64_t cols, const float (&f)[8], bool vec)
+__device__ __forceinline__ void keep8(const Kept8 &k, int64_t row, int64_t j, int64_t cols, const float2 (&f)[4], bool vec)
 {
-    uint32_t m = magnitude8(f);
+    uint32_t m = __float_as_uint(largest8(0.0f, f));
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
     const uint32_t e = kept_exponent(m);
-    store_bytes(k.p + row * k.stride, j, cols, vec, to_kept8(f, e));
+    store_bytes(k.p + row * k.stride, j, cols, vec, to_kept8(f, m, e));
     if ((threadIdx.x & 3) == 0 && j < cols) k.exponents[row * k.exponents_stride + (j >> 5)] = (uint8_t)e;
 }
 
@@ -113,13 +117,13 @@ __device__ __forceinline__ RowStats stats_of(const RmsNorm &a, float squares, ui
     return r;
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void finish8(const RmsNorm &a, const RowStats &st, int64_t row, int64_t j, const float (&p)[8], bool q_vec)
+__device__ __forceinline__ void finish8(const RmsNorm &a, const Place<T> &y, const RowStats &st, int64_t row, int64_t j, const float2 (&p)[4], bool q_vec)
 {
     if (a.y.p) {
-        float f[8];
+        float2 f[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = __fmul_rn(p[e], st.s);
-        store8<T, VEC>(row_of<T>(a.y, row), j, a.cols, narrow8<T>(f));
+        for (int e = 0; e < 4; ++e) f[e] = mul2(p[e], both(st.s));
+        store8<T, VEC>(y, row, j, a.cols, narrow8<T>(f));
     }
     if (a.q.p) store_bytes(a.q.p + row * a.q.stride, j, a.cols, q_vec, st.finite ? to_rows8(p, st.step) : make_uint2(0, 0));
 }
@@ -127,56 +131,65 @@ __device__ __forceinline__ void finish8(const RmsNorm &a, const RowStats &st, in
 // ---------------------------------------------------------------------------------------------
 // Forward.
 // ---------------------------------------------------------------------------------------------
+// Blocks an SM holds: as many as the registers of a thread's units allow.
+constexpr int forward_blocks(int size, int steps, int threads)
+{
+    return (size * steps <= 4 ? 1024 : size * steps <= 8 ? 768 : 512) / threads > 0 ? (size * steps <= 4 ? 1024 : size * steps <= 8 ? 768 : 512) / threads : 1;
+}
 template <typename T, int THREADS, int STEPS, int BT, bool VEC>
-__global__ void __launch_bounds__(BT, BT == 256 ? 2 : 1) k_rms_norm(RmsNorm a)
+__global__ void __launch_bounds__(BT, forward_blocks(sizeof(T), STEPS, BT)) k_rms_norm(RmsNorm a)
 {
     constexpr int GROUPS = BT / THREADS, UNITS = THREADS * STEPS;
-    constexpr bool AHEAD = STEPS * sizeof(T) < 16;       // the next row's units fit into the registers
+    constexpr bool AHEAD = BT < 1024 || sizeof(T) == 2;       // the next row's units fit into the registers
     extern __shared__ __align__(16) float w[];
     __shared__ float2 slots[GROUPS][2][THREADS / 32];
     const int t = threadIdx.x % THREADS, group = threadIdx.x / THREADS, cols = (int)a.cols;
     const int64_t step = (int64_t)gridDim.x * GROUPS;
     const bool q_vec = on(a.q.p, a.q.stride, 8), kept_vec = on(a.kept.p, a.kept.stride, 8);
+    const Place<T> x_ = place<T>(a.x, a.rows), residual_ = place<T>(a.residual, a.rows), total_ = place<T>(a.total, a.rows), y_ = place<T>(a.y, a.rows);
     int64_t row = (int64_t)blockIdx.x * GROUPS + group;
     Raw8<T> x[STEPS], r[STEPS];
     auto fetch = [&](int64_t n) {
 #pragma unroll
-        for (int k = 0; k < STEPS; ++k) x[k] = load8<T, VEC>(row_of<T>(a.x, n), 8 * (t + k * THREADS), cols);
+        for (int k = 0; k < STEPS; ++k) x[k] = load8<T, VEC>(x_, n, 8 * (t + k * THREADS), cols);
         if (a.residual.p)
 #pragma unroll
-            for (int k = 0; k < STEPS; ++k) r[k] = load8<T, VEC>(row_of<T>(a.residual, n), 8 * (t + k * THREADS), cols);
+            for (int k = 0; k < STEPS; ++k) r[k] = load8<T, VEC>(residual_, n, 8 * (t + k * THREADS), cols);
     };
     if (AHEAD && row < a.rows) fetch(row);
     fill_weight(w, a.weight, cols, UNITS);
     __syncthreads();
     for (int slot = 0; row < a.rows; row += step, slot ^= 1) {
-        float p[STEPS][8], squares = 0.0f;
-        uint32_t top = 0;
+        float2 p[STEPS][4], squares = both(0.0f);
+        float top = 0.0f;
         if (!AHEAD) fetch(row);
+        if (a.residual.p)
+#pragma unroll
+            for (int k = 0; k < STEPS; ++k) x[k] = sum8<T>(x[k], r[k]);
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
+            const int u = t + k * THREADS;
+            if (a.total.p) store8<T, VEC>(total_, row, 8 * u, cols, x[k]);
             widen8<T>(x[k], p[k]);
-            if (a.residual.p) add_residual<T>(p[k], r[k]);
         }
         if (AHEAD && row + step < a.rows) fetch(row + step);
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
             const int u = t + k * THREADS;
-            if (a.total.p) store8<T, VEC>(row_of<T>(a.total, row), 8 * u, cols, narrow8<T>(p[k]));
-            if (a.kept.p) keep8<T>(a.kept, row, 8 * u, cols, p[k], kept_vec);
-            float f[8];
+            if (a.kept.p) keep8(a.kept, row, 8 * u, cols, p[k], kept_vec);
+            float2 f[4];
             weight8(w, u, UNITS, f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                squares = fmaf(p[k][e], p[k][e], squares);
-                p[k][e] = __fmul_rn(p[k][e], f[e]);
+            for (int e = 0; e < 4; ++e) {
+                squares = fma2(p[k][e], p[k][e], squares);
+                p[k][e] = mul2(p[k][e], f[e]);
             }
-            if (a.q.p) top = max(top, magnitude8(p[k]));
+            if (a.q.p) top = largest8(top, p[k]);
         }
-        group_sum_max<THREADS>(squares, top, slots[group][slot], group);
-        const RowStats st = stats_of(a, squares, top);
+        const float2 sums = group_sum_max<THREADS>(squares.x + squares.y, __float_as_uint(top), slots[group][slot], group);
+        const RowStats st = stats_of(a, sums.x, __float_as_uint(sums.y));
 #pragma unroll
-        for (int k = 0; k < STEPS; ++k) finish8<T, VEC>(a, st, row, 8 * (t + k * THREADS), p[k], q_vec);
+        for (int k = 0; k < STEPS; ++k) finish8<T, VEC>(a, y_, st, row, 8 * (t + k * THREADS), p[k], q_vec);
         if (t == 0) {
             if (a.rstd) a.rstd[row] = st.s;
             if (a.q.scale) a.q.scale[row] = st.scale();
@@ -187,10 +200,10 @@ __global__ void __launch_bounds__(BT, BT == 256 ? 2 : 1) k_rms_norm(RmsNorm a)
 // Rows too long for the registers of a block: read twice, the second time from the caches.
 constexpr int kLongThreads = 1024;
 
-__device__ __forceinline__ void weight8_long(const AnyVec &v, int64_t j, int64_t cols, float (&f)[8])
+__device__ __forceinline__ void weight8_long(const AnyVec &v, int64_t j, int64_t cols, float2 (&f)[4])
 {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = j + e >= cols ? 0.0f : v.p ? any_at(v, j + e) : 1.0f;
+    for (int e = 0; e < 8; ++e) (e & 1 ? f[e / 2].y : f[e / 2].x) = j + e >= cols ? 0.0f : v.p ? any_at(v, j + e) : 1.0f;
 }
 
 template <typename T, bool VEC>
@@ -199,40 +212,46 @@ __global__ void __launch_bounds__(kLongThreads, 1) k_rms_norm_long(RmsNorm a)
     __shared__ float2 slots[kLongThreads / 32];
     const int64_t row = blockIdx.x, cols = a.cols;
     const bool q_vec = on(a.q.p, a.q.stride, 8), kept_vec = on(a.kept.p, a.kept.stride, 8);
-    float f[8], w[8], squares = 0.0f;
-    uint32_t top = 0;
+    const Place<T> x_ = place<T>(a.x, a.rows), residual_ = place<T>(a.residual, a.rows), total_ = place<T>(a.total, a.rows), y_ = place<T>(a.y, a.rows);
+    float2 f[4], w[4], squares = both(0.0f);
+    float top = 0.0f;
     for (int64_t base = 0; base < cols; base += 8 * kLongThreads) {
         const int64_t j = base + 8 * threadIdx.x;
-        widen8<T>(load8<T, VEC>(row_of<T>(a.x, row), j, cols), f);
-        if (a.residual.p) add_residual<T>(f, load8<T, VEC>(row_of<T>(a.residual, row), j, cols));
-        if (a.total.p) store8<T, VEC>(row_of<T>(a.total, row), j, cols, narrow8<T>(f));
-        if (a.kept.p) keep8<T>(a.kept, row, j, cols, f, kept_vec);
+        Raw8<T> h = load8<T, VEC>(x_, row, j, cols);
+        if (a.residual.p) h = sum8<T>(h, load8<T, VEC>(residual_, row, j, cols));
+        if (a.total.p) store8<T, VEC>(total_, row, j, cols, h);
+        widen8<T>(h, f);
+        if (a.kept.p) keep8(a.kept, row, j, cols, f, kept_vec);
         weight8_long(a.weight, j, cols, w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            squares = fmaf(f[e], f[e], squares);
-            w[e] = __fmul_rn(f[e], w[e]);
+        for (int e = 0; e < 4; ++e) {
+            squares = fma2(f[e], f[e], squares);
+            w[e] = mul2(f[e], w[e]);
         }
-        top = max(top, magnitude8(w));
+        top = largest8(top, w);
     }
-    group_sum_max<kLongThreads>(squares, top, slots, 0);
-    const RowStats st = stats_of(a, squares, top);
+    const float2 sums = group_sum_max<kLongThreads>(squares.x + squares.y, __float_as_uint(top), slots, 0);
+    const RowStats st = stats_of(a, sums.x, __float_as_uint(sums.y));
     if (threadIdx.x == 0) {
         if (a.rstd) a.rstd[row] = st.s;
         if (a.q.scale) a.q.scale[row] = st.scale();
     }
     if (!a.y.p && !a.q.p) return;
-    for (int64_t j = 8 * threadIdx.x; j < cols; j += 8 * kLongThreads) {
+    if (!VEC && a.total.p) __syncthreads();             // units are put together with their neighbours' threads
+    for (int64_t base = 0; base < cols; base += 8 * kLongThreads) {
+        const int64_t j = base + 8 * threadIdx.x;
+        Raw8<T> h;
         if (a.total.p) {                                // may have been written over x
-            widen8<T>(load8<T, VEC>(row_of<T>(a.total, row), j, cols), f);
+            h = load8<T, VEC>(total_, row, j, cols);
         } else {
-            widen8<T>(load8<T, VEC>(row_of<T>(a.x, row), j, cols), f);
-            if (a.residual.p) add_residual<T>(f, load8<T, VEC>(row_of<T>(a.residual, row), j, cols));
+            h = load8<T, VEC>(x_, row, j, cols);
+            if (a.residual.p) h = sum8<T>(h, load8<T, VEC>(residual_, row, j, cols));
         }
+        widen8<T>(h, f);
         weight8_long(a.weight, j, cols, w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = __fmul_rn(f[e], w[e]);
-        finish8<T, VEC>(a, st, row, j, w, q_vec);
+        for (int e = 0; e < 4; ++e) w[e] = mul2(f[e], w[e]);
+        finish8<T, VEC>(a, y_, st, row, j, w, q_vec);
     }
 }
 
@@ -258,39 +277,33 @@ __device__ __forceinline__ void store_gradient(void *p, int64_t i, int type, int
 // A unit of the activations, as they were or as a checkpoint.
 template <typename T, bool KEPT> struct Source {
     Raw8<T> u;
-    __device__ __forceinline__ void load(const RmsNormBackward &a, int64_t row, int64_t j, int64_t cols, bool)
+    template <bool VEC>
+    __device__ __forceinline__ void load(const RmsNormBackward &, const Place<T> &x, int64_t row, int64_t j, int64_t cols, bool)
     {
-        u = load8<T, false>(row_of<T>(a.x, row), j, cols);
+        u = load8<T, VEC>(x, row, j, cols);
     }
-    __device__ __forceinline__ void load_vec(const RmsNormBackward &a, int64_t row, int64_t j, int64_t cols, bool)
-    {
-        u = load8<T, true>(row_of<T>(a.x, row), j, cols);
-    }
-    __device__ __forceinline__ void values(float s, float (&f)[8]) const
+    __device__ __forceinline__ void values(float s, float2 (&f)[4]) const
     {
         widen8<T>(u, f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = __fmul_rn(f[e], s);
+        for (int e = 0; e < 4; ++e) f[e] = mul2(f[e], both(s));
     }
 };
 template <typename T> struct Source<T, true> {
     uint2 u;
     uint32_t exponent;
-    __device__ __forceinline__ void load(const RmsNormBackward &a, int64_t row, int64_t j, int64_t cols, bool vec)
+    template <bool VEC>
+    __device__ __forceinline__ void load(const RmsNormBackward &a, const Place<T> &, int64_t row, int64_t j, int64_t cols, bool vec)
     {
         u = load_bytes(a.kept.p + row * a.kept.stride, j, cols, vec);
         exponent = j < cols ? __ldg(a.kept.exponents + row * a.kept.exponents_stride + (j >> 5)) : 1;
     }
-    __device__ __forceinline__ void load_vec(const RmsNormBackward &a, int64_t row, int64_t j, int64_t cols, bool vec)
-    {
-        load(a, row, j, cols, vec);
-    }
-    __device__ __forceinline__ void values(float s, float (&f)[8]) const
+    __device__ __forceinline__ void values(float s, float2 (&f)[4]) const
     {
         const float step = kept_step(exponent);
         unpack_bytes(u, f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = __fmul_rn(__fmul_rn(f[e], step), s);
+        for (int e = 0; e < 4; ++e) f[e] = mul2(mul2(f[e], both(step)), both(s));
     }
 };
 
@@ -304,6 +317,7 @@ __global__ void __launch_bounds__(BT, BT == 256 ? 2 : 1) k_rms_norm_backward(Rms
     const int64_t per = a.rows / a.groups, end = (blockIdx.y + 1) * per, step = (int64_t)gridDim.x * GROUPS;
     const bool vec = KEPT && on(a.kept.p, a.kept.stride, 8);
     const float over = __frcp_rn((float)cols);
+    const Place<T> dy_ = place<T>(a.dy, a.rows), x_ = place<T>(a.x, a.rows), dtotal_ = place<T>(a.dtotal, a.rows), dx_ = place<T>(a.dx, a.rows);
     int64_t row = blockIdx.y * per + (int64_t)blockIdx.x * GROUPS + group;
     Raw8<T> dy[STEPS];
     Source<T, KEPT> x[STEPS];
@@ -313,20 +327,20 @@ __global__ void __launch_bounds__(BT, BT == 256 ? 2 : 1) k_rms_norm_backward(Rms
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
             const int j = 8 * (t + k * THREADS);
-            dy[k] = load8<T, VEC>(row_of<T>(a.dy, n), j, cols);
-            if (VEC) x[k].load_vec(a, n, j, cols, vec); else x[k].load(a, n, j, cols, vec);
+            dy[k] = load8<T, VEC>(dy_, n, j, cols);
+            x[k].template load<VEC>(a, x_, n, j, cols, vec);
         }
     };
     if (row < end) fetch(row);
     fill_weight(w, a.weight, cols, UNITS);
     __syncthreads();
-    float sums[STEPS][8];
+    float2 sums[STEPS][4];
 #pragma unroll
     for (int k = 0; k < STEPS; ++k)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sums[k][e] = 0.0f;
+        for (int e = 0; e < 4; ++e) sums[k][e] = both(0.0f);
     for (int slot = 0; row < end; row += step, slot ^= 1) {
-        float dot = 0.0f;
+        float2 dot = both(0.0f);
         const float s = rstd;
         Raw8<T> dy_now[STEPS], more[STEPS];
         Source<T, KEPT> x_now[STEPS];
@@ -337,38 +351,39 @@ __global__ void __launch_bounds__(BT, BT == 256 ? 2 : 1) k_rms_norm_backward(Rms
         }
         if (a.dtotal.p)
 #pragma unroll
-            for (int k = 0; k < STEPS; ++k) more[k] = load8<T, VEC>(row_of<T>(a.dtotal, row), 8 * (t + k * THREADS), cols);
+            for (int k = 0; k < STEPS; ++k) more[k] = load8<T, VEC>(dtotal_, row, 8 * (t + k * THREADS), cols);
         if (row + step < end) fetch(row + step);
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
-            float g[8], xh[8], f[8];
+            float2 g[4], xh[4], f[4];
             x_now[k].values(s, xh);
             widen8<T>(dy_now[k], g);
             weight8(w, t + k * THREADS, UNITS, f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                sums[k][e] = fmaf(g[e], xh[e], sums[k][e]);
-                dot = fmaf(__fmul_rn(g[e], f[e]), xh[e], dot);
+            for (int e = 0; e < 4; ++e) {
+                sums[k][e] = fma2(g[e], xh[e], sums[k][e]);
+                dot = fma2(mul2(g[e], f[e]), xh[e], dot);
             }
         }
         if (!a.dx.p) continue;
-        const float mean = __fmul_rn(group_sum<THREADS>(dot, slots[group][slot], group), over);
+        const float mean = __fmul_rn(group_sum<THREADS>(dot.x + dot.y, slots[group][slot], group), over);
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
-            float g[8], xh[8], f[8];
+            float2 g[4], xh[4], f[4];
             x_now[k].values(s, xh);
             widen8<T>(dy_now[k], g);
             weight8(w, t + k * THREADS, UNITS, f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) g[e] = fmaf(-xh[e], mean, __fmul_rn(g[e], f[e]));
+            for (int e = 0; e < 4; ++e) g[e] = fma2(xh[e], both(-mean), mul2(g[e], f[e]));
             if (a.dtotal.p) widen8<T>(more[k], f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) g[e] = a.dtotal.p ? fmaf(g[e], s, f[e]) : __fmul_rn(g[e], s);
-            store8<T, VEC>(row_of<T>(a.dx, row), 8 * (t + k * THREADS), cols, narrow8<T>(g));
+            for (int e = 0; e < 4; ++e) g[e] = a.dtotal.p ? fma2(g[e], both(s), f[e]) : mul2(g[e], both(s));
+            store8<T, VEC>(dx_, row, 8 * (t + k * THREADS), cols, narrow8<T>(g));
         }
     }
     if (!a.dweight) return;
     // the groups' sums one after the other, as planes
+#pragma unroll 1
     for (int i = 0; i < GROUPS; ++i) {
         __syncthreads();
         if (i == group)
@@ -378,7 +393,7 @@ __global__ void __launch_bounds__(BT, BT == 256 ? 2 : 1) k_rms_norm_backward(Rms
                 for (int h = 0; h < 2; ++h) {
                     float4 *p = reinterpret_cast<float4 *>(w + 4 * (h * UNITS + t + k * THREADS));
                     float4 v = i ? *p : make_float4(0, 0, 0, 0);
-                    v.x += sums[k][4 * h]; v.y += sums[k][4 * h + 1]; v.z += sums[k][4 * h + 2]; v.w += sums[k][4 * h + 3];
+                    v.x += sums[k][2 * h].x; v.y += sums[k][2 * h].y; v.z += sums[k][2 * h + 1].x; v.w += sums[k][2 * h + 1].y;
                     *p = v;
                 }
     }
@@ -397,32 +412,34 @@ __global__ void __launch_bounds__(kLongThreads, 1) k_rms_dx_long(RmsNormBackward
     __shared__ float slots[kLongThreads / 32];
     const int64_t row = blockIdx.x, cols = a.cols;
     const bool vec = KEPT && on(a.kept.p, a.kept.stride, 8);
+    const Place<T> dy_ = place<T>(a.dy, a.rows), x_ = place<T>(a.x, a.rows), dtotal_ = place<T>(a.dtotal, a.rows), dx_ = place<T>(a.dx, a.rows);
     const float s = a.rstd[row];
     Source<T, KEPT> x;
-    float g[8], xh[8], w[8], dot = 0.0f;
+    float2 g[4], xh[4], w[4], dot = both(0.0f);
     auto take = [&](int64_t j) {
-        if (VEC) x.load_vec(a, row, j, cols, vec); else x.load(a, row, j, cols, vec);
+        x.template load<VEC>(a, x_, row, j, cols, vec);
         x.values(s, xh);
-        widen8<T>(load8<T, VEC>(row_of<T>(a.dy, row), j, cols), g);
+        widen8<T>(load8<T, VEC>(dy_, row, j, cols), g);
         weight8_long(a.weight, j, cols, w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] = __fmul_rn(g[e], w[e]);
+        for (int e = 0; e < 4; ++e) g[e] = mul2(g[e], w[e]);
     };
     for (int64_t j = 8 * threadIdx.x; j < cols; j += 8 * kLongThreads) {
         take(j);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dot = fmaf(g[e], xh[e], dot);
+        for (int e = 0; e < 4; ++e) dot = fma2(g[e], xh[e], dot);
     }
-    const float mean = __fmul_rn(group_sum<kLongThreads>(dot, slots, 0), __frcp_rn((float)cols));
-    for (int64_t j = 8 * threadIdx.x; j < cols; j += 8 * kLongThreads) {
+    const float mean = __fmul_rn(group_sum<kLongThreads>(dot.x + dot.y, slots, 0), __frcp_rn((float)cols));
+    for (int64_t base = 0; base < cols; base += 8 * kLongThreads) {
+        const int64_t j = base + 8 * threadIdx.x;
         take(j);
-        if (a.dtotal.p) widen8<T>(load8<T, VEC>(row_of<T>(a.dtotal, row), j, cols), w);
+        if (a.dtotal.p) widen8<T>(load8<T, VEC>(dtotal_, row, j, cols), w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float d = fmaf(-xh[e], mean, g[e]);
-            g[e] = a.dtotal.p ? fmaf(d, s, w[e]) : __fmul_rn(d, s);
+        for (int e = 0; e < 4; ++e) {
+            const float2 d = fma2(xh[e], both(-mean), g[e]);
+            g[e] = a.dtotal.p ? fma2(d, both(s), w[e]) : mul2(d, both(s));
         }
-        store8<T, VEC>(row_of<T>(a.dx, row), j, cols, narrow8<T>(g));
+        store8<T, VEC>(dx_, row, j, cols, narrow8<T>(g));
     }
 }
 constexpr int kLongRows = 128;         // rows of a block of the next kernel, at least
@@ -433,23 +450,25 @@ __global__ void __launch_bounds__(128) k_rms_dw_long(RmsNormBackward a)
     const int parts = gridDim.y, part = blockIdx.y;
     const int64_t first = blockIdx.z * per + per * part / parts, end = blockIdx.z * per + per * (part + 1) / parts;
     const bool vec = KEPT && on(a.kept.p, a.kept.stride, 8);
-    float sums[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    const Place<T> dy_ = place<T>(a.dy, a.rows), x_ = place<T>(a.x, a.rows);
+    float2 sums[4] = {both(0.0f), both(0.0f), both(0.0f), both(0.0f)};
     if (j >= cols) return;
 #pragma unroll 4
     for (int64_t row = first; row < end; ++row) {
         Source<T, KEPT> x;
-        float g[8], xh[8];
-        if (VEC) x.load_vec(a, row, j, cols, vec); else x.load(a, row, j, cols, vec);
-        widen8<T>(load8<T, VEC>(row_of<T>(a.dy, row), j, cols), g);
+        float2 g[4], xh[4];
+        x.template load<VEC>(a, x_, row, j, cols, vec);
+        widen8<T>(load8<T, VEC>(dy_, row, j, cols), g);
         x.values(__ldg(a.rstd + row), xh);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sums[e] = fmaf(g[e], xh[e], sums[e]);
+        for (int e = 0; e < 4; ++e) sums[e] = fma2(g[e], xh[e], sums[e]);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         if (j + e >= cols) break;
-        if (parts > 1) a.parts[((int64_t)blockIdx.z * parts + part) * cols + j + e] = sums[e];
-        else store_gradient(a.dweight, blockIdx.z * a.dweight_stride + j + e, a.grad_type, a.accumulate, sums[e]);
+        const float v = e & 1 ? sums[e / 2].y : sums[e / 2].x;
+        if (parts > 1) a.parts[((int64_t)blockIdx.z * parts + part) * cols + j + e] = v;
+        else store_gradient(a.dweight, blockIdx.z * a.dweight_stride + j + e, a.grad_type, a.accumulate, v);
     }
 }
 
@@ -475,39 +494,80 @@ __global__ void __launch_bounds__(1024) k_rms_sums(RmsNormBackward a, int parts)
 // The formats by themselves, unit by unit.  Rows are padded to whole blocks of four units, so that a
 // checkpoint's block is four neighbouring threads.
 // ---------------------------------------------------------------------------------------------
-constexpr int kFlat = 256;
+constexpr int kFlat = 256, kAhead = 4;     // a thread asks for that many units before it works on the first
+
+// Rows of `units` units each: the row of unit i is i / units, for i < 2^31 by a product (`magic` = ceil(2^(31 + s) / units),
+// 2^s >= units: the excess adds less than 1 / units).
+struct Units {
+    unsigned units, magic, shift;
+    int64_t all;
+};
+static Units units_of(int64_t rows, int64_t units)
+{
+    unsigned s = 0;
+    while (((int64_t)1 << s) < units) ++s;
+    return {(unsigned)units, (unsigned)((((uint64_t)1 << (31 + s)) + units - 1) / units), s, rows * units};
+}
+// Unit i; of those behind the last row: none (j = cols).
+struct UnitAt {
+    int64_t row, j;
+};
+__device__ __forceinline__ UnitAt unit_at(int64_t i, const Units &n, int64_t cols)
+{
+    if (i >= n.all) return {0, cols};
+    const int64_t row = n.all >> 31 ? i / n.units : n.shift ? __umulhi((unsigned)i, n.magic) >> (n.shift - 1) : i;
+    return {row, 8 * (i - row * n.units)};
+}
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kFlat) k_checkpoint8(Matrix x, Kept8 kept, int64_t rows, int64_t cols)
+__global__ void __launch_bounds__(kFlat) k_checkpoint8(Matrix x, Kept8 kept, int64_t rows, int64_t cols, Units n)
 {
-    const unsigned units = (unsigned)((cols + 31) / 32 * 4);
     const bool vec = on(kept.p, kept.stride, 8);
-    const int64_t all = rows * units;
-    for (int64_t base = (int64_t)blockIdx.x * kFlat; base < all; base += (int64_t)gridDim.x * kFlat) {
-        const int64_t i = base + threadIdx.x;
-        const int64_t row = i < all ? (all >> 32 ? i / units : (unsigned)i / units) : rows - 1, j = i < all ? 8 * (i - row * units) : cols;
-        float f[8];
-        widen8<T>(load8<T, VEC>(row_of<T>(x, row), j, cols), f);
-        keep8<T>(kept, row, j, cols, f, vec);
+    const Place<T> x_ = place<T>(x, rows);
+    for (int64_t base = (int64_t)blockIdx.x * kFlat * kAhead; base < n.all; base += (int64_t)gridDim.x * kFlat * kAhead) {
+        UnitAt at[kAhead];
+        Raw8<T> u[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            at[k] = unit_at(base + k * kFlat + threadIdx.x, n, cols);
+            u[k] = load8<T, VEC>(x_, at[k].row, at[k].j, cols);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            float2 f[4];
+            widen8<T>(u[k], f);
+            keep8(kept, at[k].row, at[k].j, cols, f, vec);
+        }
     }
 }
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kFlat) k_restore8(Rows8 q, Kept8 kept, Matrix to, int64_t rows, int64_t cols)
+__global__ void __launch_bounds__(kFlat) k_restore8(Rows8 q, Kept8 kept, Matrix to, int64_t rows, int64_t cols, Units n)
 {
-    const unsigned units = (unsigned)((cols + 7) / 8);
     const int8_t *p = kept.p ? kept.p : q.p;
-    const int64_t stride = kept.p ? kept.stride : q.stride, all = rows * units;
+    const int64_t stride = kept.p ? kept.stride : q.stride;
     const bool vec = on(p, stride, 8);
-    for (int64_t i = (int64_t)blockIdx.x * kFlat + threadIdx.x; i < all; i += (int64_t)gridDim.x * kFlat) {
-        const int64_t row = all >> 32 ? i / units : (unsigned)i / units, j = 8 * (i - row * units);
-        float f[8];
-        const uint2 b = load_bytes(p + row * stride, j, cols, vec);
-        const float s = kept.p ? kept_step(__ldg(kept.exponents + row * kept.exponents_stride + (j >> 5))) : __ldg(q.scale + row);
-        unpack_bytes(b, f);
+    const Place<T> to_ = place<T>(to, rows);
+    for (int64_t base = (int64_t)blockIdx.x * kFlat * kAhead; base < n.all; base += (int64_t)gridDim.x * kFlat * kAhead) {
+        UnitAt at[kAhead];
+        uint2 b[kAhead];
+        float s[kAhead];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = __fmul_rn(f[e], s);
-        store8<T, VEC>(row_of<T>(to, row), j, cols, narrow8<T>(f));
+        for (int k = 0; k < kAhead; ++k) {
+            at[k] = unit_at(base + k * kFlat + threadIdx.x, n, cols);
+            b[k] = load_bytes(p + at[k].row * stride, at[k].j, cols, vec);
+            s[k] = 0.0f;
+            if (at[k].j < cols)
+                s[k] = kept.p ? kept_step(__ldg(kept.exponents + at[k].row * kept.exponents_stride + (at[k].j >> 5))) : __ldg(q.scale + at[k].row);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            float2 f[4];
+            unpack_bytes(b[k], f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] = mul2(f[e], both(s[k]));
+            store8<T, VEC>(to_, at[k].row, at[k].j, cols, narrow8<T>(f));
+        }
     }
 }
 
@@ -523,7 +583,7 @@ template <typename T, int THREADS, int STEPS, int BT>
 static void forward_as(const RmsNorm &a, bool vec, cudaStream_t st)
 {
     auto kernel = vec ? k_rms_norm<T, THREADS, STEPS, BT, true> : k_rms_norm<T, THREADS, STEPS, BT, false>;
-    const int64_t groups = BT / THREADS, need = (a.rows + groups - 1) / groups, most = kSms * (BT == 256 ? 4 : BT == 512 ? 2 : 1);
+    const int64_t groups = BT / THREADS, need = (a.rows + groups - 1) / groups, most = kSms * forward_blocks(sizeof(T), STEPS, BT);
     const size_t smem = (size_t)THREADS * STEPS * 32;
     allow_shared(kernel, smem);
     queue(kernel, dim3((unsigned)(need < most ? need : most)), BT, smem, st, a);
@@ -538,15 +598,15 @@ static void forward(const RmsNorm &a, cudaStream_t st)
     if (units <= 32) forward_as<T, 32, 1, 256>(a, vec, st);
     else if (units <= 64) forward_as<T, 32, 2, 256>(a, vec, st);
     else if (units <= 96) forward_as<T, 32, 3, 256>(a, vec, st);
-    else if (units <= 128) forward_as<T, 32, 4, 256>(a, vec, st);
+    else if (units <= 128) forward_as<T, 64, 2, 256>(a, vec, st);
     else if (units <= 192) forward_as<T, 64, 3, 256>(a, vec, st);
-    else if (units <= 256) forward_as<T, 64, 4, 256>(a, vec, st);
+    else if (units <= 256) forward_as<T, 128, 2, 256>(a, vec, st);
     else if (units <= 384) forward_as<T, 128, 3, 256>(a, vec, st);
-    else if (units <= 512) forward_as<T, 128, 4, 256>(a, vec, st);
+    else if (units <= 512) forward_as<T, 256, 2, 256>(a, vec, st);
     else if (units <= 768) forward_as<T, 256, 3, 256>(a, vec, st);
-    else if (units <= 1024) forward_as<T, 256, 4, 256>(a, vec, st);
+    else if (units <= 1024) forward_as<T, 512, 2, 512>(a, vec, st);
     else if (units <= 1536) forward_as<T, 512, 3, 512>(a, vec, st);
-    else if (units <= 2048) forward_as<T, 512, 4, 512>(a, vec, st);
+    else if (units <= 2048) forward_as<T, 1024, 2, 1024>(a, vec, st);
     else queue(vec ? k_rms_norm_long<T, true> : k_rms_norm_long<T, false>, dim3((unsigned)a.rows), kLongThreads, 0, st, a);
 }
 void launch_rms_norm(const RmsNorm &a, int type, cudaStream_t st)
@@ -629,16 +689,17 @@ void launch_rms_norm_backward(const RmsNormBackward &a, int type, cudaStream_t s
     else backward<f16>(a, st);
 }
 
-static dim3 flat_grid(int64_t rows, int64_t units)
+static dim3 flat_grid(const Units &n)
 {
-    const int64_t need = (rows * units + kFlat - 1) / kFlat, most = kSms * 64;
+    const int64_t each = kFlat * kAhead, need = (n.all + each - 1) / each, most = kSms * 32;
     return dim3((unsigned)(need < most ? need : most));
 }
 template <typename T>
 static void checkpoint(const Matrix &x, const Kept8 &kept, int64_t rows, int64_t cols, cudaStream_t st)
 {
     auto kernel = starts_on_16(x, rows, sizeof(T)) ? k_checkpoint8<T, true> : k_checkpoint8<T, false>;
-    queue(kernel, flat_grid(rows, (cols + 31) / 32 * 4), kFlat, 0, st, x, kept, rows, cols);
+    const Units n = units_of(rows, (cols + 31) / 32 * 4);
+    queue(kernel, flat_grid(n), kFlat, 0, st, x, kept, rows, cols, n);
 }
 void launch_checkpoint8(const Matrix &x, const Kept8 &kept, int64_t rows, int64_t cols, int type, cudaStream_t st)
 {
@@ -650,7 +711,8 @@ template <typename T>
 static void restore(const Rows8 &q, const Kept8 &kept, const Matrix &to, int64_t rows, int64_t cols, cudaStream_t st)
 {
     auto kernel = starts_on_16(to, rows, sizeof(T)) ? k_restore8<T, true> : k_restore8<T, false>;
-    queue(kernel, flat_grid(rows, (cols + 7) / 8), kFlat, 0, st, q, kept, to, rows, cols);
+    const Units n = units_of(rows, (cols + 7) / 8);
+    queue(kernel, flat_grid(n), kFlat, 0, st, q, kept, to, rows, cols, n);
 }
 void launch_restore8(const Rows8 &q, const Kept8 &kept, const Matrix &to, int64_t rows, int64_t cols, int type, cudaStream_t st)
 {
