@@ -66,7 +66,7 @@ __device__ __forceinline__ void skip_words(uint32_t (&w)[N + 4], unsigned k)
 }
 
 template <typename T>
-__device__ __forceinline__ Raw8<T> load_elements(const T *row, int64_t j, int64_t cols)
+__device__ __forceinline__ Raw8<T> load_elements(const T *row, int j, int cols)
 {
     Raw8<T> u;
 #pragma unroll
@@ -79,7 +79,7 @@ __device__ __forceinline__ Raw8<T> load_elements(const T *row, int64_t j, int64_
 
 // Columns j .. j + 7 of row r, 0 beyond its end.
 template <typename T, bool VEC>
-__device__ __forceinline__ Raw8<T> load8(const Place<T> &m, int64_t r, int64_t j, int64_t cols)
+__device__ __forceinline__ Raw8<T> load8(const Place<T> &m, int64_t r, int j, int cols)
 {
     constexpr int W = 2 * sizeof(T);
     const T *const row = m.row(r);
@@ -94,7 +94,7 @@ __device__ __forceinline__ Raw8<T> load8(const Place<T> &m, int64_t r, int64_t j
         }
         return u;
     }
-    if (j >= cols || (m.edge(r) && (j * (int64_t)sizeof(T) < 16 || (j + 8) * (int64_t)sizeof(T) + 16 > cols * (int64_t)sizeof(T))))
+    if (j >= cols || (m.edge(r) && (j * (int)sizeof(T) < 16 || (j + 8) * (int)sizeof(T) + 16 > cols * (int)sizeof(T))))
         return load_elements(row, j, cols);
     const uintptr_t at = (uintptr_t)(row + j);
     const uint4 *p = reinterpret_cast<const uint4 *>(at & ~(uintptr_t)15);
@@ -116,7 +116,7 @@ __device__ __forceinline__ Raw8<T> load8(const Place<T> &m, int64_t r, int64_t j
 }
 
 template <typename T>
-__device__ __forceinline__ void store_element(T *row, int64_t j, const Raw8<T> &u, int e)
+__device__ __forceinline__ void store_element(T *row, int j, const Raw8<T> &u, int e)
 {
     if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t *>(row)[j + e] = u.w[e];
     else reinterpret_cast<unsigned short *>(row)[j + e] = (unsigned short)(u.w[e / 2] >> (e % 2 * 16));
@@ -124,7 +124,7 @@ __device__ __forceinline__ void store_element(T *row, int64_t j, const Raw8<T> &
 // All lanes of the warp call it (with j >= cols: nothing is stored); lane l + 1 has the unit behind lane l's, or
 // one of another row.
 template <typename T, bool VEC>
-__device__ __forceinline__ void store8(const Place<T> &m, int64_t r, int64_t j, int64_t cols, const Raw8<T> &u)
+__device__ __forceinline__ void store8(const Place<T> &m, int64_t r, int j, int cols, const Raw8<T> &u)
 {
     constexpr int W = 2 * sizeof(T);
     T *const row = m.row(r);
@@ -149,8 +149,8 @@ __device__ __forceinline__ void store8(const Place<T> &m, int64_t r, int64_t j, 
     for (int i = 0; i < 4; ++i) w[i] = __shfl_up_sync(0xffffffffu, u.w[W - 4 + i], 1);
 #pragma unroll
     for (int i = 0; i < W; ++i) w[4 + i] = u.w[i];
-    const int64_t j_before = __shfl_up_sync(0xffffffffu, j, 1);
-    const bool whole = j + 8 - over <= cols && (over == 0 || (lane > 0 && j > 0 && j_before == j - 8));
+    const int j_before = __shfl_up_sync(0xffffffffu, j, 1);
+    const bool whole = j + 8 - (int)over <= cols && (over == 0 || (lane > 0 && j > 0 && j_before == j - 8));
     if (whole) {
         const unsigned from = 16 - (unsigned)(at & 15);         // byte of w where the vectors begin
         skip_words<W>(w, from >> 2 & 3);
@@ -168,7 +168,7 @@ __device__ __forceinline__ void store8(const Place<T> &m, int64_t r, int64_t j, 
     }
     // what no vector takes: the first elements where there is none, the last where the next lane has none
     const bool next = __shfl_down_sync(0xffffffffu, whole && over > 0, 1) && lane < 31;
-    const int64_t j_next = __shfl_down_sync(0xffffffffu, j, 1);
+    const int j_next = __shfl_down_sync(0xffffffffu, j, 1);
     const int first = whole ? 8 - (int)over : 0, last = over > 0 && next && j_next == j + 8 ? 8 - (int)over : 8;
     if (first < last)
 #pragma unroll
@@ -177,7 +177,7 @@ __device__ __forceinline__ void store8(const Place<T> &m, int64_t r, int64_t j, 
 }
 
 // Eight bytes; `vec`: rows start on 8 bytes.
-__device__ __forceinline__ uint2 load_bytes(const int8_t *row, int64_t j, int64_t cols, bool vec)
+__device__ __forceinline__ uint2 load_bytes(const int8_t *row, int j, int cols, bool vec)
 {
     if (vec && j + 8 <= cols) return __ldcs(reinterpret_cast<const uint2 *>(row + j));
     uint32_t w[2] = {0, 0};
@@ -186,7 +186,7 @@ __device__ __forceinline__ uint2 load_bytes(const int8_t *row, int64_t j, int64_
         if (j + e < cols) w[e / 4] |= (uint32_t)(uint8_t)row[j + e] << (e % 4 * 8);
     return make_uint2(w[0], w[1]);
 }
-__device__ __forceinline__ void store_bytes(int8_t *row, int64_t j, int64_t cols, bool vec, uint2 v)
+__device__ __forceinline__ void store_bytes(int8_t *row, int j, int cols, bool vec, uint2 v)
 {
     if (vec && j + 8 <= cols) {
         *reinterpret_cast<uint2 *>(row + j) = v;

@@ -88,7 +88,7 @@ __device__ __forceinline__ Raw8<T> sum8(const Raw8<T> &x, const Raw8<T> &residua
 }
 
 // A block of 32 columns of a checkpoint: four neighbouring threads' units.
-__device__ __forceinline__ void keep8(const Kept8 &k, int64_t row, int64_t j, int64_t cols, const float2 (&f)[4], bool vec)
+__device__ __forceinline__ void keep8(const Kept8 &k, int64_t row, int j, int cols, const float2 (&f)[4], bool vec)
 {
     uint32_t m = __float_as_uint(largest8(0.0f, f));
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
@@ -117,15 +117,15 @@ __device__ __forceinline__ RowStats stats_of(const RmsNorm &a, float squares, ui
     return r;
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void finish8(const RmsNorm &a, const Place<T> &y, const RowStats &st, int64_t row, int64_t j, const float2 (&p)[4], bool q_vec)
+__device__ __forceinline__ void finish8(const RmsNorm &a, const Place<T> &y, const RowStats &st, int64_t row, int j, const float2 (&p)[4], bool q_vec)
 {
     if (a.y.p) {
         float2 f[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = mul2(p[e], both(st.s));
-        store8<T, VEC>(y, row, j, a.cols, narrow8<T>(f));
+        store8<T, VEC>(y, row, j, (int)a.cols, narrow8<T>(f));
     }
-    if (a.q.p) store_bytes(a.q.p + row * a.q.stride, j, a.cols, q_vec, st.finite ? to_rows8(p, st.step) : make_uint2(0, 0));
+    if (a.q.p) store_bytes(a.q.p + row * a.q.stride, j, (int)a.cols, q_vec, st.finite ? to_rows8(p, st.step) : make_uint2(0, 0));
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(BT, forward_blocks(sizeof(T), STEPS, BT)) k_rm
 // Rows too long for the registers of a block: read twice, the second time from the caches.
 constexpr int kLongThreads = 1024;
 
-__device__ __forceinline__ void weight8_long(const AnyVec &v, int64_t j, int64_t cols, float2 (&f)[4])
+__device__ __forceinline__ void weight8_long(const AnyVec &v, int j, int cols, float2 (&f)[4])
 {
 #pragma unroll
     for (int e = 0; e < 8; ++e) (e & 1 ? f[e / 2].y : f[e / 2].x) = j + e >= cols ? 0.0f : v.p ? any_at(v, j + e) : 1.0f;
@@ -210,13 +210,14 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(kLongThreads, 1) k_rms_norm_long(RmsNorm a)
 {
     __shared__ float2 slots[kLongThreads / 32];
-    const int64_t row = blockIdx.x, cols = a.cols;
+    const int64_t row = blockIdx.x;
+    const int cols = (int)a.cols;
     const bool q_vec = on(a.q.p, a.q.stride, 8), kept_vec = on(a.kept.p, a.kept.stride, 8);
     const Place<T> x_ = place<T>(a.x, a.rows), residual_ = place<T>(a.residual, a.rows), total_ = place<T>(a.total, a.rows), y_ = place<T>(a.y, a.rows);
     float2 f[4], w[4], squares = both(0.0f);
     float top = 0.0f;
-    for (int64_t base = 0; base < cols; base += 8 * kLongThreads) {
-        const int64_t j = base + 8 * threadIdx.x;
+    for (int base = 0; base < cols; base += 8 * kLongThreads) {
+        const int j = base + 8 * (int)threadIdx.x;
         Raw8<T> h = load8<T, VEC>(x_, row, j, cols);
         if (a.residual.p) h = sum8<T>(h, load8<T, VEC>(residual_, row, j, cols));
         if (a.total.p) store8<T, VEC>(total_, row, j, cols, h);
@@ -238,8 +239,8 @@ __global__ void __launch_bounds__(kLongThreads, 1) k_rms_norm_long(RmsNorm a)
     }
     if (!a.y.p && !a.q.p) return;
     if (!VEC && a.total.p) __syncthreads();             // units are put together with their neighbours' threads
-    for (int64_t base = 0; base < cols; base += 8 * kLongThreads) {
-        const int64_t j = base + 8 * threadIdx.x;
+    for (int base = 0; base < cols; base += 8 * kLongThreads) {
+        const int j = base + 8 * (int)threadIdx.x;
         Raw8<T> h;
         if (a.total.p) {                                // may have been written over x
             h = load8<T, VEC>(total_, row, j, cols);
@@ -278,7 +279,7 @@ __device__ __forceinline__ void store_gradient(void *p, int64_t i, int type, int
 template <typename T, bool KEPT> struct Source {
     Raw8<T> u;
     template <bool VEC>
-    __device__ __forceinline__ void load(const RmsNormBackward &, const Place<T> &x, int64_t row, int64_t j, int64_t cols, bool)
+    __device__ __forceinline__ void load(const RmsNormBackward &, const Place<T> &x, int64_t row, int j, int cols, bool)
     {
         u = load8<T, VEC>(x, row, j, cols);
     }
@@ -293,7 +294,7 @@ template <typename T> struct Source<T, true> {
     uint2 u;
     uint32_t exponent;
     template <bool VEC>
-    __device__ __forceinline__ void load(const RmsNormBackward &a, const Place<T> &, int64_t row, int64_t j, int64_t cols, bool vec)
+    __device__ __forceinline__ void load(const RmsNormBackward &a, const Place<T> &, int64_t row, int j, int cols, bool vec)
     {
         u = load_bytes(a.kept.p + row * a.kept.stride, j, cols, vec);
         exponent = j < cols ? __ldg(a.kept.exponents + row * a.kept.exponents_stride + (j >> 5)) : 1;
@@ -410,13 +411,14 @@ template <typename T, bool VEC, bool KEPT>
 __global__ void __launch_bounds__(kLongThreads, 1) k_rms_dx_long(RmsNormBackward a)
 {
     __shared__ float slots[kLongThreads / 32];
-    const int64_t row = blockIdx.x, cols = a.cols;
+    const int64_t row = blockIdx.x;
+    const int cols = (int)a.cols;
     const bool vec = KEPT && on(a.kept.p, a.kept.stride, 8);
     const Place<T> dy_ = place<T>(a.dy, a.rows), x_ = place<T>(a.x, a.rows), dtotal_ = place<T>(a.dtotal, a.rows), dx_ = place<T>(a.dx, a.rows);
     const float s = a.rstd[row];
     Source<T, KEPT> x;
     float2 g[4], xh[4], w[4], dot = both(0.0f);
-    auto take = [&](int64_t j) {
+    auto take = [&](int j) {
         x.template load<VEC>(a, x_, row, j, cols, vec);
         x.values(s, xh);
         widen8<T>(load8<T, VEC>(dy_, row, j, cols), g);
@@ -424,14 +426,14 @@ __global__ void __launch_bounds__(kLongThreads, 1) k_rms_dx_long(RmsNormBackward
 #pragma unroll
         for (int e = 0; e < 4; ++e) g[e] = mul2(g[e], w[e]);
     };
-    for (int64_t j = 8 * threadIdx.x; j < cols; j += 8 * kLongThreads) {
+    for (int j = 8 * (int)threadIdx.x; j < cols; j += 8 * kLongThreads) {
         take(j);
 #pragma unroll
         for (int e = 0; e < 4; ++e) dot = fma2(g[e], xh[e], dot);
     }
     const float mean = __fmul_rn(group_sum<kLongThreads>(dot.x + dot.y, slots, 0), __frcp_rn((float)cols));
-    for (int64_t base = 0; base < cols; base += 8 * kLongThreads) {
-        const int64_t j = base + 8 * threadIdx.x;
+    for (int base = 0; base < cols; base += 8 * kLongThreads) {
+        const int j = base + 8 * (int)threadIdx.x;
         take(j);
         if (a.dtotal.p) widen8<T>(load8<T, VEC>(dtotal_, row, j, cols), w);
 #pragma unroll
@@ -446,7 +448,8 @@ constexpr int kLongRows = 128;         // rows of a block of the next kernel, at
 template <typename T, bool VEC, bool KEPT>
 __global__ void __launch_bounds__(128) k_rms_dw_long(RmsNormBackward a)
 {
-    const int64_t per = a.rows / a.groups, cols = a.cols, j = 8 * ((int64_t)blockIdx.x * 128 + threadIdx.x);
+    const int64_t per = a.rows / a.groups;
+    const int cols = (int)a.cols, j = 8 * (int)(blockIdx.x * 128 + threadIdx.x);
     const int parts = gridDim.y, part = blockIdx.y;
     const int64_t first = blockIdx.z * per + per * part / parts, end = blockIdx.z * per + per * (part + 1) / parts;
     const bool vec = KEPT && on(a.kept.p, a.kept.stride, 8);
@@ -495,43 +498,64 @@ __global__ void __launch_bounds__(1024) k_rms_sums(RmsNormBackward a, int parts)
 // checkpoint's block is four neighbouring threads.
 // ---------------------------------------------------------------------------------------------
 constexpr int kFlat = 256, kAhead = 4;     // a thread asks for that many units before it works on the first
+constexpr int kWideUnits = 64;
 
-// Rows of `units` units each: the row of unit i is i / units, for i < 2^31 by a product (`magic` = ceil(2^(31 + s) / units),
-// 2^s >= units: the excess adds less than 1 / units).
+// Where a thread's four units are.  WIDE: a warp takes 128 units of one row, lane l the units l, l + 32, l + 64, l + 96
+// of them; rows of fewer units, one behind the other, 32 units a warp at a time.  Number i of a sequence of n to a row
+// is in row i / n, for i < 2^31 by a product (`magic` = ceil(2^(31 + s) / n), 2^s >= n: the excess adds less than 1 / n).
 struct Units {
-    unsigned units, magic, shift;
+    unsigned n, magic, shift;
     int64_t all;
 };
 static Units units_of(int64_t rows, int64_t units)
 {
+    const int64_t n = units >= kWideUnits ? (units + 127) / 128 : units;
     unsigned s = 0;
-    while (((int64_t)1 << s) < units) ++s;
-    return {(unsigned)units, (unsigned)((((uint64_t)1 << (31 + s)) + units - 1) / units), s, rows * units};
+    while (((int64_t)1 << s) < n) ++s;
+    return {(unsigned)n, (unsigned)((((uint64_t)1 << (31 + s)) + n - 1) / n), s, rows * n};
 }
-// Unit i; of those behind the last row: none (j = cols).
 struct UnitAt {
-    int64_t row, j;
+    int64_t row;
+    int j;          // cols: none
 };
-__device__ __forceinline__ UnitAt unit_at(int64_t i, const Units &n, int64_t cols)
+__device__ __forceinline__ int64_t row_of(int64_t i, const Units &u)
 {
-    if (i >= n.all) return {0, cols};
-    const int64_t row = n.all >> 31 ? i / n.units : n.shift ? __umulhi((unsigned)i, n.magic) >> (n.shift - 1) : i;
-    return {row, 8 * (i - row * n.units)};
+    return u.all >> 31 ? i / u.n : u.shift ? __umulhi((unsigned)i, u.magic) >> (u.shift - 1) : i;
 }
+template <bool WIDE>
+__device__ __forceinline__ void units_at(int64_t warp, const Units &u, int cols, UnitAt (&at)[kAhead])
+{
+    const int lane = threadIdx.x & 31;
+    if (WIDE) {
+        const int64_t row = row_of(warp, u);
+        const int j = ((int)(warp - row * u.n) * 128 + lane) * 8;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) at[k] = {row, min(j + k * 256, cols)};
+    } else {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t i = (warp * kAhead + k) * 32 + lane, row = row_of(i, u);
+            at[k] = {row, (int)(i - row * u.n) * 8};
+            if (i >= u.all) at[k] = {0, cols};
+        }
+    }
+}
+// Warps of a launch and what each of them takes in turn: WIDE one item, else 128.
+template <bool WIDE>
+__device__ __forceinline__ int64_t items(const Units &u) { return WIDE ? u.all : (u.all + 32 * kAhead - 1) / (32 * kAhead); }
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kFlat) k_checkpoint8(Matrix x, Kept8 kept, int64_t rows, int64_t cols, Units n)
+template <typename T, bool VEC, bool WIDE>
+__global__ void __launch_bounds__(kFlat) k_checkpoint8(Matrix x, Kept8 kept, int64_t rows, int cols, Units n)
 {
     const bool vec = on(kept.p, kept.stride, 8);
     const Place<T> x_ = place<T>(x, rows);
-    for (int64_t base = (int64_t)blockIdx.x * kFlat * kAhead; base < n.all; base += (int64_t)gridDim.x * kFlat * kAhead) {
+    const int64_t all = items<WIDE>(n), step = (int64_t)gridDim.x * (kFlat / 32);
+    for (int64_t i = (int64_t)blockIdx.x * (kFlat / 32) + threadIdx.x / 32; i < all; i += step) {
         UnitAt at[kAhead];
         Raw8<T> u[kAhead];
+        units_at<WIDE>(i, n, cols, at);
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            at[k] = unit_at(base + k * kFlat + threadIdx.x, n, cols);
-            u[k] = load8<T, VEC>(x_, at[k].row, at[k].j, cols);
-        }
+        for (int k = 0; k < kAhead; ++k) u[k] = load8<T, VEC>(x_, at[k].row, at[k].j, cols);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             float2 f[4];
@@ -541,20 +565,21 @@ __global__ void __launch_bounds__(kFlat) k_checkpoint8(Matrix x, Kept8 kept, int
     }
 }
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kFlat) k_restore8(Rows8 q, Kept8 kept, Matrix to, int64_t rows, int64_t cols, Units n)
+template <typename T, bool VEC, bool WIDE>
+__global__ void __launch_bounds__(kFlat) k_restore8(Rows8 q, Kept8 kept, Matrix to, int64_t rows, int cols, Units n)
 {
     const int8_t *p = kept.p ? kept.p : q.p;
     const int64_t stride = kept.p ? kept.stride : q.stride;
     const bool vec = on(p, stride, 8);
     const Place<T> to_ = place<T>(to, rows);
-    for (int64_t base = (int64_t)blockIdx.x * kFlat * kAhead; base < n.all; base += (int64_t)gridDim.x * kFlat * kAhead) {
+    const int64_t all = items<WIDE>(n), step = (int64_t)gridDim.x * (kFlat / 32);
+    for (int64_t i = (int64_t)blockIdx.x * (kFlat / 32) + threadIdx.x / 32; i < all; i += step) {
         UnitAt at[kAhead];
         uint2 b[kAhead];
         float s[kAhead];
+        units_at<WIDE>(i, n, cols, at);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            at[k] = unit_at(base + k * kFlat + threadIdx.x, n, cols);
             b[k] = load_bytes(p + at[k].row * stride, at[k].j, cols, vec);
             s[k] = 0.0f;
             if (at[k].j < cols)
@@ -689,17 +714,20 @@ void launch_rms_norm_backward(const RmsNormBackward &a, int type, cudaStream_t s
     else backward<f16>(a, st);
 }
 
-static dim3 flat_grid(const Units &n)
+static dim3 flat_grid(const Units &n, bool wide)
 {
-    const int64_t each = kFlat * kAhead, need = (n.all + each - 1) / each, most = kSms * 32;
+    const int64_t each = kFlat / 32 * (wide ? 1 : 32 * kAhead), need = (n.all + each - 1) / each, most = kSms * 32;
     return dim3((unsigned)(need < most ? need : most));
 }
 template <typename T>
 static void checkpoint(const Matrix &x, const Kept8 &kept, int64_t rows, int64_t cols, cudaStream_t st)
 {
-    auto kernel = starts_on_16(x, rows, sizeof(T)) ? k_checkpoint8<T, true> : k_checkpoint8<T, false>;
-    const Units n = units_of(rows, (cols + 31) / 32 * 4);
-    queue(kernel, flat_grid(n), kFlat, 0, st, x, kept, rows, cols, n);
+    const int64_t units = (cols + 31) / 32 * 4;
+    const bool vec = starts_on_16(x, rows, sizeof(T)), wide = units >= kWideUnits;
+    auto kernel = wide ? (vec ? k_checkpoint8<T, true, true> : k_checkpoint8<T, false, true>)
+                       : (vec ? k_checkpoint8<T, true, false> : k_checkpoint8<T, false, false>);
+    const Units n = units_of(rows, units);
+    queue(kernel, flat_grid(n, wide), kFlat, 0, st, x, kept, rows, (int)cols, n);
 }
 void launch_checkpoint8(const Matrix &x, const Kept8 &kept, int64_t rows, int64_t cols, int type, cudaStream_t st)
 {
@@ -710,9 +738,12 @@ void launch_checkpoint8(const Matrix &x, const Kept8 &kept, int64_t rows, int64_
 template <typename T>
 static void restore(const Rows8 &q, const Kept8 &kept, const Matrix &to, int64_t rows, int64_t cols, cudaStream_t st)
 {
-    auto kernel = starts_on_16(to, rows, sizeof(T)) ? k_restore8<T, true> : k_restore8<T, false>;
-    const Units n = units_of(rows, (cols + 7) / 8);
-    queue(kernel, flat_grid(n), kFlat, 0, st, q, kept, to, rows, cols, n);
+    const int64_t units = (cols + 7) / 8;
+    const bool vec = starts_on_16(to, rows, sizeof(T)), wide = units >= kWideUnits;
+    auto kernel = wide ? (vec ? k_restore8<T, true, true> : k_restore8<T, false, true>)
+                       : (vec ? k_restore8<T, true, false> : k_restore8<T, false, false>);
+    const Units n = units_of(rows, units);
+    queue(kernel, flat_grid(n, wide), kFlat, 0, st, q, kept, to, rows, (int)cols, n);
 }
 void launch_restore8(const Rows8 &q, const Kept8 &kept, const Matrix &to, int64_t rows, int64_t cols, int type, cudaStream_t st)
 {
