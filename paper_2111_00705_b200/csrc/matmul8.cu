@@ -71,7 +71,18 @@ __device__ __forceinline__ uint32_t at_rank(const void *p, int rank)
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(p)), "r"(rank));
     return at;
 }
-__device__ __forceinline__ void store_at(uint32_t at, int v) { asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
+__device__ __forceinline__ int load_at(uint32_t at)
+{
+    int v;
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ int4 load4_at(uint32_t at)
+{
+    int4 v;
+    asm volatile("ld.shared::cluster.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
 
 // What has become of a thread's waits: 0: all in time; 1: one ran out and the thread waited a second time, with the
 // default limit: the block's results are NaN; 2: that was in vain too: nothing more is waited for or started.
@@ -86,12 +97,30 @@ __device__ __forceinline__ int wait_for(uint64_t *bar, uint32_t parity, int limi
     return wait_again(bar, parity, limit < 0 ? kWaitLimit : limit, late);
 }
 
-template <typename T>
-__device__ __forceinline__ void store_product(const Matmul8 &a, int64_t token, int64_t channel, int sum, float x_scale, float w_scale, float bias,
-                                              bool late)
+// An output, in the documented steps (packed products and sums would be contracted by the assembler).
+__device__ __forceinline__ float output(int sum, float x_scale, float w_scale, float bias)
 {
-    const float v = __fadd_rn(__fmul_rn(__fmul_rn((float)sum, x_scale), w_scale), bias);
-    static_cast<T *>(a.y)[token * a.y_stride + channel] = narrow<T>(late ? __uint_as_float(0x7fc00000u) : v);
+    return __fadd_rn(__fmul_rn(__fmul_rn((float)sum, x_scale), w_scale), bias);
+}
+// Four tokens' outputs of a channel.
+__device__ __forceinline__ void outputs4(const int *sum, const float *x_scale, float w_scale, float bias, float2 &a, float2 &b)
+{
+    const float4 x = *reinterpret_cast<const float4 *>(x_scale);
+    a = make_float2(output(sum[0], x.x, w_scale, bias), output(sum[1], x.y, w_scale, bias));
+    b = make_float2(output(sum[2], x.z, w_scale, bias), output(sum[3], x.w, w_scale, bias));
+}
+// Four channels' outputs of a token; `vec`: every four of them start on a multiple of their size, n of them are there.
+template <typename T>
+__device__ __forceinline__ void store4(T *to, const float (&f)[4], bool vec, int n)
+{
+    if (vec && n >= 4) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(to) = make_float4(f[0], f[1], f[2], f[3]);
+        else *reinterpret_cast<uint2 *>(to) = make_uint2(Vec<T>::down(make_float2(f[0], f[1])), Vec<T>::down(make_float2(f[2], f[3])));
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < n) to[e] = narrow<T>(f[e]);
 }
 
 template <typename T, int BN>
@@ -103,12 +132,19 @@ __global__ void __launch_bounds__(128) k_matmul8(const __grid_constant__ CUtenso
     char *const stages = raw + (-smem_addr(raw) & 1023);
     __shared__ uint64_t full[kMaxRing], empty[kMaxRing], done;
     __shared__ uint32_t tmem;
-    __shared__ int lates[2];
+    __shared__ int lates[2], any_late;
     __shared__ float x_scale[BN];
-    const int warp = threadIdx.x >> 5, rank = blockIdx.x % splits;
+    __shared__ __align__(16) float w_scale[kRowsP], bias[kRowsP];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x % splits;
     const int64_t tile = blockIdx.x / splits, channel0 = tile / token_tiles * kRowsP, token0 = tile % token_tiles * BN;
     const int blocks = (int)((a.inner + kBytesK - 1) / kBytesK);
     const int first = (int)((int64_t)blocks * rank / splits), n = (int)((int64_t)blocks * (rank + 1) / splits) - first;
+    auto fill = [&](int i, int s) {
+        mbar_arrive_expect_tx(&full[s], STAGE);
+        char *to = stages + s * STAGE;
+        tma_2d(to, &wmap, (first + i) * kBytesK, (int)channel0, &full[s]);
+        tma_2d(to + kRowsP * kBytesK, &xmap, (first + i) * kBytesK, (int)token0, &full[s]);
+    };
     if (threadIdx.x == 0) {
         for (int i = 0; i < ring; ++i) {
             mbar_init(&full[i], 1);
@@ -116,34 +152,39 @@ __global__ void __launch_bounds__(128) k_matmul8(const __grid_constant__ CUtenso
         }
         mbar_init(&done, 1);
         mbar_fence_init();
+        for (int i = 0; i < min(n, ring); ++i) fill(i, i);
+        any_late = 0;
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem)), "r"(COLUMNS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     for (int i = threadIdx.x; i < BN; i += 128) x_scale[i] = token0 + i < a.tokens ? a.x.scale[token0 + i] : 0.0f;
+    {
+        const int64_t c = channel0 + threadIdx.x;
+        w_scale[threadIdx.x] = c < a.channels ? a.w.scale[c] : 0.0f;
+        bias[threadIdx.x] = c < a.channels && a.bias.p ? any_at(a.bias, c) : 0.0f;
+    }
     fence_before();
     __syncthreads();
     fence_after();
     const uint32_t sums = tmem;
     int late = 0;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < n; ++i) {
-            const int s = i % ring, phase = i / ring & 1;
-            if (i >= ring) late = wait_for(&empty[s], phase ^ 1, a.wait_limit, late);
+        int s = 0, phase = 0;
+        for (int i = ring; i < n; ++i) {
+            late = wait_for(&empty[s], phase, a.wait_limit, late);
             if (late == 2) {                            // what is under way lands before the block leaves
-                for (int k = max(0, i - ring); k < i; ++k) mbar_wait_bounded(&full[k % ring], k / ring & 1);
+                for (int k = i - ring; k < i; ++k) mbar_wait_bounded(&full[k % ring], k / ring & 1);
                 break;
             }
-            mbar_arrive_expect_tx(&full[s], STAGE);
-            char *to = stages + s * STAGE;
-            tma_2d(to, &wmap, (first + i) * kBytesK, (int)channel0, &full[s]);
-            tma_2d(to + kRowsP * kBytesK, &xmap, (first + i) * kBytesK, (int)token0, &full[s]);
+            fill(i, s);
+            if (++s == ring) { s = 0; phase ^= 1; }
         }
         lates[0] = late;
     } else if (threadIdx.x == 32) {
+        int s = 0, phase = 0;
         for (int i = 0; i < n; ++i) {
-            const int s = i % ring, phase = i / ring & 1;
             late = wait_for(&full[s], phase, a.wait_limit, late);
             if (late == 2) break;
             fence_after();
@@ -151,59 +192,59 @@ __global__ void __launch_bounds__(128) k_matmul8(const __grid_constant__ CUtenso
 #pragma unroll
             for (int k = 0; k < kBytesK / 32; ++k) mma8(sums, w + 2 * k, x + 2 * k, shape8(kRowsP, BN), i > 0 || k > 0);
             commit(&empty[s]);
+            if (++s == ring) { s = 0; phase ^= 1; }
         }
         commit(&done);
         lates[1] = late;
     }
     __syncwarp();
     late = wait_for(&done, 0, a.wait_limit, 0);
+    if (late) any_late = 1;
     __syncthreads();
     fence_after();
-    const int64_t channel = channel0 + threadIdx.x;
-    const bool mine = channel < a.channels;
-    const float w_scale = mine ? a.w.scale[channel] : 0.0f, bias = mine && a.bias.p ? any_at(a.bias, channel) : 0.0f;
-    const uint32_t lane_at = sums + ((uint32_t)warp << 21);
-    bool none = (late | lates[0] | lates[1]) != 0;
-    if (splits == 1) {
+    // The sums take the stages' place, a row of 128 channels for every token.  Every block of a cluster adds up a share of
+    // the tokens from all of them; a warp takes a token at a time, a lane four channels.
+    if (threadIdx.x == 0 && (lates[0] | lates[1])) any_late = 1;
+    int *const left = reinterpret_cast<int *>(stages);
+    const int n_tokens = (int)min((int64_t)BN, a.tokens - token0);
 #pragma unroll 1
-        for (int c = 0; c < BN; c += 16) {
-            if (token0 + c >= a.tokens) break;
-            int v[16];
-            __syncwarp();
-            read_sums(lane_at + c, v);
+    for (int c = 0; c < BN; c += 16) {
+        int v[16];
+        if (c >= n_tokens) break;
+        read_sums(sums + ((uint32_t)warp << 21) + c, v);
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (mine && token0 + c + e < a.tokens)
-                    store_product<T>(a, token0 + c + e, channel, v[e], x_scale[c + e], w_scale, bias, none);
-        }
-    } else {
-        // every block adds up a share of the tokens: the others send it their sums, in the place of its stages
-        const int share = BN / splits;
-        __shared__ int late_of[8];
-        __syncwarp();
-        cluster_barrier();                              // the stages of all are free
-        if ((int)threadIdx.x < splits) store_at(at_rank(&late_of[rank], threadIdx.x), none);
-#pragma unroll 1
-        for (int c = 0; c < BN; c += 16) {
-            int v[16];
-            __syncwarp();
-            read_sums(lane_at + c, v);
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                store_at(at_rank(stages, (c + e) / share) + (((rank * share + (c + e) % share) * kRowsP + threadIdx.x) << 2), v[e]);
-        }
-        __syncwarp();
-        cluster_barrier();
-        for (int r = 0; r < splits; ++r) none |= late_of[r] != 0;
-        const int *const sent = reinterpret_cast<const int *>(stages) + threadIdx.x;
-#pragma unroll 4
-        for (int c = 0; c < share; ++c) {
-            int v = 0;
-            for (int r = 0; r < splits; ++r) v += sent[(r * share + c) * kRowsP];
-            const int64_t token = token0 + rank * share + c;
-            if (mine && token < a.tokens) store_product<T>(a, token, channel, v, x_scale[rank * share + c], w_scale, bias, none);
-        }
+        for (int e = 0; e < 16; ++e) left[(c + e) * kRowsP + threadIdx.x] = v[e];
     }
+    __syncwarp();
+    if (splits > 1) cluster_barrier();
+    else __syncthreads();
+    const float4 ws = *reinterpret_cast<const float4 *>(&w_scale[4 * lane]), bs = *reinterpret_cast<const float4 *>(&bias[4 * lane]);
+    bool none = any_late != 0;
+    if (splits > 1)
+        for (int r = 0; r < splits; ++r) none |= load_at(at_rank(&any_late, r)) != 0;
+    const int share = BN / splits, channels = (int)min((int64_t)4, max((int64_t)0, a.channels - channel0 - 4 * lane));
+    const bool vec = (((uintptr_t)a.y | (uintptr_t)(a.y_stride * sizeof(T))) & (4 * sizeof(T) - 1)) == 0;
+    T *const to = static_cast<T *>(a.y) + token0 * a.y_stride + channel0 + 4 * lane;
+    const int last = min(n_tokens, (rank + 1) * share);
+#pragma unroll 2
+    for (int c = rank * share + warp; c < last; c += 4) {
+        int4 v;
+        if (splits == 1) {
+            v = *reinterpret_cast<const int4 *>(&left[c * kRowsP + 4 * lane]);
+        } else {
+            int4 u[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) u[r] = r < splits ? load4_at(at_rank(&left[c * kRowsP + 4 * lane], r)) : make_int4(0, 0, 0, 0);
+            v = u[0];
+#pragma unroll
+            for (int r = 1; r < 8; ++r) v = make_int4(v.x + u[r].x, v.y + u[r].y, v.z + u[r].z, v.w + u[r].w);
+        }
+        const float x = none ? __uint_as_float(0x7fc00000u) : x_scale[c];
+        const float f[4] = {output(v.x, x, ws.x, bs.x), output(v.y, x, ws.y, bs.y), output(v.z, x, ws.z, bs.z), output(v.w, x, ws.w, bs.w)};
+        store4<T>(to + c * a.y_stride, f, vec, channels);
+    }
+    __syncwarp();
+    if (splits > 1) cluster_barrier();                  // no block leaves while others read from it
     fence_before();
     __syncthreads();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sums), "r"(COLUMNS));
@@ -244,9 +285,8 @@ __device__ __forceinline__ void leave_tokens(T *to, const int (&v)[N], const flo
 {
 #pragma unroll
     for (int e = 0; e < N; e += 4) {
-        const float4 x = *reinterpret_cast<const float4 *>(x_scale + e);
-        const float2 a = add2(mul2(mul2(make_float2((float)v[e], (float)v[e + 1]), make_float2(x.x, x.y)), both(w_scale)), both(bias));
-        const float2 b = add2(mul2(mul2(make_float2((float)v[e + 2], (float)v[e + 3]), make_float2(x.z, x.w)), both(w_scale)), both(bias));
+        float2 a, b;
+        outputs4(v + e, x_scale + e, w_scale, bias, a, b);
         if constexpr (sizeof(T) == 4) {
             to[e * kRowsP] = a.x; to[(e + 1) * kRowsP] = a.y; to[(e + 2) * kRowsP] = b.x; to[(e + 3) * kRowsP] = b.y;
         } else {
@@ -293,31 +333,30 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     const uint32_t sums = tmem;
     int late = 0;
     if (threadIdx.x == 0) {
-        int i = 0;
+        int i = 0, s = 0, phase = 1;
         for (int tile = pair; tile < tiles && late < 2; tile += pairs) {
             const int channel = tile / token_tiles * kPairTile + rank * kRowsP, token = tile % token_tiles * kPairTile + rank * kRowsP;
             for (int b = 0; b < blocks; ++b, ++i) {
-                const int s = i % kPairRing, phase = i / kPairRing & 1;
-                if (i >= kPairRing) late = wait_for(&empty[s], phase ^ 1, a.wait_limit, late);
+                if (i >= kPairRing) late = wait_for(&empty[s], phase, a.wait_limit, late);
                 if (late == 2) break;
                 if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * kPairStage);
                 char *to = stages + s * kPairStage;
                 const uint32_t bar = at_rank(&full[s], 0);
                 tma_2d_pair(to, &wmap, b * kBytesK, channel, bar);
                 tma_2d_pair(to + kRowsP * kBytesK, &xmap, b * kBytesK, token, bar);
+                if (++s == kPairRing) { s = 0; phase ^= 1; }
             }
         }
         // what is under way lands before the pair leaves
         if (late == 2 && rank == 0)
             for (int k = max(0, i - kPairRing); k < i; ++k) mbar_wait_bounded(&full[k % kPairRing], k / kPairRing & 1);
     } else if (threadIdx.x == 32 && rank == 0) {
-        int i = 0, set = 0;
+        int set = 0, s = 0, phase = 0;
         for (int tile = pair; tile < tiles && late < 2; tile += pairs, ++set) {
             const int buffer = set & 1;
             if (set >= 2) late = wait_for(&drained[buffer], (set >> 1 & 1) ^ 1, a.wait_limit, late);
             fence_after();
-            for (int b = 0; b < blocks; ++b, ++i) {
-                const int s = i % kPairRing, phase = i / kPairRing & 1;
+            for (int b = 0; b < blocks; ++b) {
                 late = wait_for(&full[s], phase, a.wait_limit, late);
                 if (late == 2) break;
                 fence_after();
@@ -326,6 +365,7 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                 for (int k = 0; k < kBytesK / 32; ++k)
                     mma8_pair(sums + buffer * kPairTile, w + 2 * k, x + 2 * k, shape8(2 * kRowsP, kPairTile), b > 0 || k > 0);
                 commit_pair(&empty[s]);
+                if (++s == kPairRing) { s = 0; phase ^= 1; }
             }
             if (late < 2) commit_pair(&ready[buffer]);
         }
@@ -387,6 +427,80 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     __syncthreads();
     cluster_barrier();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(sums), "r"(2 * kPairTile));
+}
+
+// ---------------------------------------------------------------------------------------------
+// A few tokens: the weights are streamed once, 16 bytes a lane, and multiplied four at a time; what the kernel above
+// needs before its first byte arrives and after its last (tensor memory, barriers) costs more than its products are worth here.
+// A warp takes FEW_C channels and every `slices`-th stretch of 512 bytes of them; the slices' sums meet in shared memory.
+// ---------------------------------------------------------------------------------------------
+constexpr int kFewWarps = 8, kFewChannels = 4;
+
+// 16 bytes of a row, 0 beyond its end.
+template <bool KEEP>
+__device__ __forceinline__ int4 load16(const int8_t *row, int k, int inner)
+{
+    if (k + 16 <= inner) {
+        const int4 *p = reinterpret_cast<const int4 *>(row + k);
+        return KEEP ? __ldg(p) : __ldcs(p);
+    }
+    int w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (k + i < inner) w[i / 4] |= (int)(uint8_t)row[k + i] << (i % 4 * 8);
+    return make_int4(w[0], w[1], w[2], w[3]);
+}
+
+template <typename T, int TOKENS>
+__global__ void __launch_bounds__(kFewWarps * 32, 4) k_matmul8_few(Matmul8 a, int slices)
+{
+    constexpr int C = kFewChannels;
+    __shared__ int parts[kFewWarps][C * TOKENS];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, slice = warp % slices, inner = (int)a.inner;
+    const int64_t channel0 = ((int64_t)blockIdx.x * (kFewWarps / slices) + warp / slices) * C;
+    const int8_t *w[C], *x[TOKENS];
+#pragma unroll
+    for (int c = 0; c < C; ++c) w[c] = a.w.p + min(channel0 + c, a.channels - 1) * a.w.stride;
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t) x[t] = a.x.p + min((int64_t)t, a.tokens - 1) * a.x.stride;
+    int sums[C][TOKENS] = {};
+    if (channel0 < a.channels)
+#pragma unroll 2
+        for (int k = (slice * 32 + lane) * 16; k < inner; k += slices * 512) {
+            int4 v[C];
+#pragma unroll
+            for (int c = 0; c < C; ++c) v[c] = load16<false>(w[c], k, inner);
+#pragma unroll
+            for (int t = 0; t < TOKENS; ++t) {
+                const int4 u = load16<true>(x[t], k, inner);
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+                    sums[c][t] = __dp4a(v[c].w, u.w, __dp4a(v[c].z, u.z, __dp4a(v[c].y, u.y, __dp4a(v[c].x, u.x, sums[c][t]))));
+            }
+        }
+    int mine = 0;                                       // lane c TOKENS + t has channel c, token t
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int t = 0; t < TOKENS; ++t) {
+            const int v = __reduce_add_sync(0xffffffffu, sums[c][t]);
+            if (lane == c * TOKENS + t) mine = v;
+        }
+    if (slices > 1) {
+        if (lane < C * TOKENS) parts[warp][lane] = mine;
+        __syncthreads();
+        if (slice != 0) return;
+        mine = 0;
+        if (lane < C * TOKENS)
+            for (int i = 0; i < slices; ++i) mine += parts[warp + i][lane];
+    }
+    const int token = lane % TOKENS;
+    const int64_t channel = channel0 + lane / TOKENS;
+    if (lane < C * TOKENS && channel < a.channels && token < a.tokens) {
+        const float bias = a.bias.p ? any_at(a.bias, channel) : 0.0f;
+        static_cast<T *>(a.y)[token * a.y_stride + channel] =
+            narrow<T>(output(mine, a.x.scale[token], a.w.scale[channel], bias));
+    }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -480,9 +594,22 @@ static bool product_by_pairs(const Matmul8 &a, cudaStream_t st)
     queue(kernel, dim3((unsigned)(2 * (tiles < 74 ? tiles : 74))), kPairThreads, smem, st, wmap, xmap, ymap, a, (int)tiles, (int)token_tiles);
     return true;
 }
+template <typename T, int TOKENS>
+static bool product_of_few(const Matmul8 &a, cudaStream_t st)
+{
+    // warps for about 24 to an SM, as far as the rows' length allows
+    const int64_t channels = (a.channels + kFewChannels - 1) / kFewChannels;
+    int slices = 1;
+    while (slices < kFewWarps && channels * slices < 148 * 24 && a.inner > slices * 512) slices *= 2;
+    const int64_t blocks = (channels * slices + kFewWarps - 1) / kFewWarps;
+    queue(k_matmul8_few<T, TOKENS>, dim3((unsigned)blocks), kFewWarps * 32, 0, st, a, slices);
+    return true;
+}
 template <typename T>
 static bool product(const Matmul8 &a, cudaStream_t st)
 {
+    if (a.tokens == 1) return product_of_few<T, 1>(a, st);
+    if (a.tokens == 2) return product_of_few<T, 2>(a, st);
     if (a.tokens > 128 && (a.tokens + 255) / 256 * ((a.channels + 255) / 256) >= 74) return product_by_pairs<T>(a, st);
     if (a.tokens <= 16) return product_as<T, 16>(a, st);
     if (a.tokens <= 32) return product_as<T, 32>(a, st);

@@ -437,7 +437,7 @@ def test_product_every_length(inner):
 @pytest.mark.parametrize("bias", [None] + list(TYPES))
 def test_product_types_bias_and_strides(dtype, bias):
     g = gen(12, 83)
-    for tokens, channels, inner in ((1, 500, 768), (6, 333, 100), (20, 130, 512), (100, 1000, 260), (700, 515, 384)):
+    for tokens, channels, inner in ((1, 500, 768), (6, 333, 100), (20, 130, 512), (100, 1000, 260), (700, 515, 384), (300, 9500, 96)):
         check_product(tokens, channels, inner, g, TYPES[dtype], None if bias is None else TYPES[bias], pad=32, y_pad=3)
 
 
