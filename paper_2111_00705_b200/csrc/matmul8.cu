@@ -102,13 +102,6 @@ __device__ __forceinline__ float output(int sum, float x_scale, float w_scale, f
 {
     return __fadd_rn(__fmul_rn(__fmul_rn((float)sum, x_scale), w_scale), bias);
 }
-// Four tokens' outputs of a channel.
-__device__ __forceinline__ void outputs4(const int *sum, const float *x_scale, float w_scale, float bias, float2 &a, float2 &b)
-{
-    const float4 x = *reinterpret_cast<const float4 *>(x_scale);
-    a = make_float2(output(sum[0], x.x, w_scale, bias), output(sum[1], x.y, w_scale, bias));
-    b = make_float2(output(sum[2], x.z, w_scale, bias), output(sum[3], x.w, w_scale, bias));
-}
 // Four channels' outputs of a token; `vec`: every four of them start on a multiple of their size, n of them are there.
 template <typename T>
 __device__ __forceinline__ void store4(T *to, const float (&f)[4], bool vec, int n)
@@ -251,14 +244,16 @@ __global__ void __launch_bounds__(128) k_matmul8(const __grid_constant__ CUtenso
 }
 
 // ---------------------------------------------------------------------------------------------
-// Many tokens: pairs of blocks, one on each SM, that stay and take one tile of 256 channels and 256 tokens after
-// the other.  Each holds half of the channels' rows and half of the tokens', the tensor cores of the two read both
-// halves, and each ends up with the sums of its 128 channels and all 256 tokens.  Two sets of sums in tensor memory:
-// eight warps turn one into outputs while the other is being added up, four of them each half of the tokens, some tokens
-// at a time through shared memory, so that a token's 128 channels leave together.  The first block of a pair issues the products for both;
-// its `full` barriers count the copies of both, `empty` and `ready` are told to both, `drained` counts the warps of both.
+// Many tokens: pairs of blocks, one on each SM, that stay and take one tile of 256 tokens and 256 channels after
+// the other.  Here the tokens are the first operand: a thread then has a token's channels side by side, and they
+// are packed without passing through others.  Each block holds half of the tokens' rows and half of the channels', the
+// tensor cores of the two read both halves, and each ends up with the sums of its 128 tokens and all 256 channels.  Two
+// sets of sums in tensor memory: eight warps turn one into outputs while the other is being added up, each 32 tokens and
+// 128 channels, 128 bytes of a row at a time through shared memory.  The first block of a pair issues the products
+// for both; its `full` barriers count the copies of both, `empty` and `ready` are told to both, `drained` counts the
+// warps of both.
 // ---------------------------------------------------------------------------------------------
-constexpr int kPairTile = 256, kPairRing = 5, kPairStage = 2 * kRowsP * kBytesK, kPairThreads = 320, kLeaveBytes = 8192;
+constexpr int kPairTile = 256, kPairRing = 5, kPairStage = 2 * kRowsP * kBytesK, kPairThreads = 320, kLeaveBytes = 4096;
 
 __device__ __forceinline__ void tma_2d_pair(void *dst, const CUtensorMap *map, int x, int y, uint32_t bar)
 {
@@ -279,21 +274,65 @@ __device__ __forceinline__ void mma8_pair(uint32_t d, uint64_t a, uint64_t b, ui
 
 __device__ __forceinline__ void half_barrier(int half) { asm volatile("bar.sync %0, 128;" ::"r"(half + 1) : "memory"); }
 
-// N tokens' outputs of a thread's channel to the staging place: row i is token i's 128 channels.
-template <typename T, int N>
-__device__ __forceinline__ void leave_tokens(T *to, const int (&v)[N], const float *x_scale, float w_scale, float bias)
+// 32 channels' outputs of the thread's token to its warp's staging place: row `lane` of 128 bytes, its 16-byte vectors
+// swizzled as the copy engine wants them; the first goes to vector `at`.
+template <typename T>
+__device__ __forceinline__ void leave_channels(char *place, int lane, int at, const int (&v)[32], float x_scale, const float *w_scale, const float *bias)
 {
+    constexpr int N = 16 / sizeof(T);
 #pragma unroll
-    for (int e = 0; e < N; e += 4) {
-        float2 a, b;
-        outputs4(v + e, x_scale + e, w_scale, bias, a, b);
-        if constexpr (sizeof(T) == 4) {
-            to[e * kRowsP] = a.x; to[(e + 1) * kRowsP] = a.y; to[(e + 2) * kRowsP] = b.x; to[(e + 3) * kRowsP] = b.y;
-        } else {
-            const uint32_t p = Vec<T>::down(a), q = Vec<T>::down(b);
-            unsigned short *u = reinterpret_cast<unsigned short *>(to);
-            u[e * kRowsP] = (unsigned short)p; u[(e + 1) * kRowsP] = (unsigned short)(p >> 16);
-            u[(e + 2) * kRowsP] = (unsigned short)q; u[(e + 3) * kRowsP] = (unsigned short)(q >> 16);
+    for (int i = 0; i < 32 / N; ++i) {
+        float2 f[N / 2];
+#pragma unroll
+        for (int e = 0; e < N; e += 4) {
+            const int c = i * N + e;
+            const float4 w = *reinterpret_cast<const float4 *>(w_scale + c);
+            if (bias) {
+                const float4 b = *reinterpret_cast<const float4 *>(bias + c);
+                f[e / 2] = make_float2(output(v[c], x_scale, w.x, b.x), output(v[c + 1], x_scale, w.y, b.y));
+                f[e / 2 + 1] = make_float2(output(v[c + 2], x_scale, w.z, b.z), output(v[c + 3], x_scale, w.w, b.w));
+            } else {
+                f[e / 2] = mul2(mul2(make_float2((float)v[c], (float)v[c + 1]), both(x_scale)), make_float2(w.x, w.y));
+                f[e / 2 + 1] = mul2(mul2(make_float2((float)v[c + 2], (float)v[c + 3]), both(x_scale)), make_float2(w.z, w.w));
+            }
+        }
+        *reinterpret_cast<uint4 *>(place + lane * 128 + (((at + i) ^ (lane & 7)) << 4)) = Vec<T>::pack(f);
+    }
+}
+
+// The staged rows from shared memory to anywhere, `tokens` rows of `channels` outputs: 16-bit ones by words, those that begin
+// between two words shifted by one.
+template <typename T>
+__device__ __forceinline__ void leave_rows(const char *place, T *p, int64_t stride, int tokens, int channels, int lane)
+{
+    constexpr int ROWS = 8;                     // fetched together, before the first of them is stored
+#pragma unroll 1
+    for (int i = 0; i < tokens; i += ROWS) {
+        uint32_t w[ROWS], before[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+            w[r] = *reinterpret_cast<const uint32_t *>(place + (i + r) * 128 + (((lane >> 2) ^ r) << 4) + (lane & 3) * 4);
+        if constexpr (sizeof(T) == 2)
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) before[r] = __shfl_up_sync(0xffffffffu, w[r], 1);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r, p += stride) {
+            const bool there = i + r < tokens;
+            if constexpr (sizeof(T) == 4) {
+                if (there && lane < channels) p[lane] = __uint_as_float(w[r]);
+            } else {
+                unsigned short *u = reinterpret_cast<unsigned short *>(p);
+                const bool odd = (uintptr_t)p & 2;
+                const int e = 2 * lane - (odd ? 1 : 0);         // the word's first output
+                const bool whole = e >= 0 && e + 1 < channels;
+                if (there && whole) *reinterpret_cast<uint32_t *>(u + e) = odd ? __funnelshift_l(before[r], w[r], 16) : w[r];
+                // alone: the first of an odd row, the last of an even row of an odd number, or of an odd row of an even one
+                if (there && (odd || channels & 1)) {
+                    const int one = odd ? (lane == 0 ? 0 : lane == 31 && channels == 64 ? 63 : e + 1 == channels && e > 0 ? e : -1)
+                                        : (e + 1 == channels ? e : -1);
+                    if (one >= 0) u[one] = (unsigned short)(odd && one != 0 ? (one == 63 ? w[r] >> 16 : before[r] >> 16) : w[r]);
+                }
+            }
         }
     }
 }
@@ -308,7 +347,7 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     char *const stages = raw + (-smem_addr(raw) & 1023);
     __shared__ uint64_t full[kPairRing], empty[kPairRing], ready[2], drained[2];
     __shared__ uint32_t tmem;
-    __shared__ __align__(16) float x_scale[2][kPairTile];
+    __shared__ __align__(16) float w_scale[2][kPairTile], bias[2][kPairTile];
     const int warp = threadIdx.x >> 5, rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const int blocks = (int)((a.inner + kBytesK - 1) / kBytesK);
     if (threadIdx.x == 0) {
@@ -342,8 +381,8 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                 if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * kPairStage);
                 char *to = stages + s * kPairStage;
                 const uint32_t bar = at_rank(&full[s], 0);
-                tma_2d_pair(to, &wmap, b * kBytesK, channel, bar);
-                tma_2d_pair(to + kRowsP * kBytesK, &xmap, b * kBytesK, token, bar);
+                tma_2d_pair(to, &xmap, b * kBytesK, token, bar);
+                tma_2d_pair(to + kRowsP * kBytesK, &wmap, b * kBytesK, channel, bar);
                 if (++s == kPairRing) { s = 0; phase ^= 1; }
             }
         }
@@ -360,67 +399,71 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                 late = wait_for(&full[s], phase, a.wait_limit, late);
                 if (late == 2) break;
                 fence_after();
-                const uint64_t w = operand(stages + s * kPairStage), x = operand(stages + s * kPairStage + kRowsP * kBytesK);
+                const uint64_t x = operand(stages + s * kPairStage), w = operand(stages + s * kPairStage + kRowsP * kBytesK);
 #pragma unroll
                 for (int k = 0; k < kBytesK / 32; ++k)
-                    mma8_pair(sums + buffer * kPairTile, w + 2 * k, x + 2 * k, shape8(2 * kRowsP, kPairTile), b > 0 || k > 0);
+                    mma8_pair(sums + buffer * kPairTile, x + 2 * k, w + 2 * k, shape8(2 * kRowsP, kPairTile), b > 0 || k > 0);
                 commit_pair(&empty[s]);
                 if (++s == kPairRing) { s = 0; phase ^= 1; }
             }
             if (late < 2) commit_pair(&ready[buffer]);
         }
     } else if (warp >= 2) {
-        constexpr int CHUNK = kLeaveBytes / kRowsP / (int)sizeof(T), HALF = kPairTile / 2;  // tokens at a time: 16 or 32
-        const int lane = threadIdx.x & 31, quarter = warp & 3, half = (warp - 2) >> 2, row = quarter * 32 + lane;
-        const bool first = (threadIdx.x - 64) % 128 == 0;
-        char *const leave = stages + kPairRing * kPairStage + half * 2 * kLeaveBytes;
-        int set = 0, place = 0;
+        constexpr int CHUNK = 128 / (int)sizeof(T), HALF = kPairTile / 2;     // channels that leave together: 32 or 64
+        const int lane = threadIdx.x & 31, quarter = warp & 3, half = (warp - 2) >> 2, thread = quarter * 32 + lane;
+        char *const place = stages + kPairRing * kPairStage + (warp - 2) * kLeaveBytes;
+        int set = 0;
         for (int tile = pair; tile < tiles; tile += pairs, ++set) {
             const int buffer = set & 1;
-            const int64_t token0 = (int64_t)(tile % token_tiles) * kPairTile + half * HALF;
-            const int64_t channel0 = (int64_t)(tile / token_tiles) * kPairTile + rank * kRowsP;
-            const bool mine = channel0 + row < a.channels;
-            float w_scale = mine ? a.w.scale[channel0 + row] : 0.0f;
-            const float bias = mine && a.bias.p ? any_at(a.bias, channel0 + row) : 0.0f;
-            float *const xs = &x_scale[buffer][half * HALF];
-            xs[row] = token0 + row < a.tokens ? a.x.scale[token0 + row] : 0.0f;
+            const int64_t token0 = (int64_t)(tile % token_tiles) * kPairTile + rank * kRowsP + quarter * 32;
+            const int64_t channel0 = (int64_t)(tile / token_tiles) * kPairTile + half * HALF;
+            float x_scale = token0 + lane < a.tokens ? a.x.scale[token0 + lane] : 0.0f;
+            const bool real = channel0 + thread < a.channels;
+            w_scale[buffer][half * HALF + thread] = real ? a.w.scale[channel0 + thread] : 0.0f;
+            if (a.bias.p) bias[buffer][half * HALF + thread] = real ? any_at(a.bias, channel0 + thread) : 0.0f;
+            half_barrier(half);
             late = wait_for(&ready[buffer], set >> 1 & 1, a.wait_limit, late);
-            if (late) w_scale = __uint_as_float(0x7fc00000u);
+            if (late) x_scale = __uint_as_float(0x7fc00000u);
             __syncwarp();
             fence_after();
             const uint32_t at = sums + buffer * kPairTile + half * HALF + ((uint32_t)quarter << 21);
+            const int tokens = (int)min((int64_t)32, a.tokens - token0);
 #pragma unroll 1
-            for (int c = 0; c < HALF; c += CHUNK, place ^= 1) {
-                int v[CHUNK];
-                if constexpr (CHUNK == 32) read_sums32(at + c, v); else read_sums(at + c, v);
-                T *const to = reinterpret_cast<T *>(leave + place * kLeaveBytes);
-                if (TILED && first) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                half_barrier(half);                     // what was here before has left; the scales are there
-                leave_tokens<T, CHUNK>(to + row, v, xs + c, w_scale, bias);
-                if (TILED) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                half_barrier(half);
-                if (token0 + c >= a.tokens) continue;
+            for (int c = 0; c < HALF; c += CHUNK) {
+                if (tokens <= 0 || channel0 + c >= a.channels) break;
+#pragma unroll
+                for (int d = 0; d < CHUNK; d += 32) {
+                    int v[32];
+                    read_sums32(at + c + d, v);
+                    if (d == 0) {                       // what was here before has left
+                        if (TILED && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                        __syncwarp();
+                    }
+                    const int first = half * HALF + c + d;
+                    leave_channels<T>(place, lane, d * (int)sizeof(T) / 16, v, x_scale, &w_scale[buffer][first],
+                                      a.bias.p ? &bias[buffer][first] : nullptr);
+                }
                 if (TILED) {
-                    if (first) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
                         asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
-                                     ::"l"(&ymap), "r"((int)channel0), "r"((int)(token0 + c)), "r"(smem_addr(to)) : "memory");
+                                     ::"l"(&ymap), "r"((int)channel0 + c), "r"((int)token0), "r"(smem_addr(place)) : "memory");
                         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     }
                 } else {
-#pragma unroll 4
-                    for (int i = quarter; i < CHUNK; i += 4)
-#pragma unroll
-                        for (int k = 0; k < kRowsP; k += 32)
-                            if (channel0 + k + lane < a.channels && token0 + c + i < a.tokens)
-                                static_cast<T *>(a.y)[(token0 + c + i) * a.y_stride + channel0 + k + lane] = to[i * kRowsP + k + lane];
+                    __syncwarp();
+                    leave_rows<T>(place, static_cast<T *>(a.y) + token0 * a.y_stride + channel0 + c, a.y_stride, tokens,
+                                  (int)min((int64_t)CHUNK, a.channels - channel0 - c), lane);
+                    __syncwarp();
                 }
             }
             fence_before();
             __syncwarp();
             if (lane == 0)
-                asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(at_rank(&drained[buffer], 0)) : "memory");
+                asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(at_rank(&drained[buffer], 0)) : "memory");
         }
-        if (TILED && first) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if (TILED && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
     fence_before();
@@ -538,27 +581,38 @@ template <typename T> static CUtensorMapDataType type_of()
     return std::is_same<T, float>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
            : std::is_same<T, bf16>::value ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
 }
-// Boxes of 128 channels of some tokens.
-static bool describe_outputs(CUtensorMap *map, const Matmul8 &a, CUtensorMapDataType type, int size, int box_rows)
+// Boxes of 128 bytes of 32 tokens.
+static bool describe_outputs(CUtensorMap *map, const Matmul8 &a, CUtensorMapDataType type, int size)
 {
     const EncodeTiled fn = encode_tiled();
     if (!fn) return false;
     const cuuint64_t dims[2] = {(cuuint64_t)a.channels, (cuuint64_t)a.tokens};
     const cuuint64_t strides[1] = {(cuuint64_t)(a.tokens > 1 ? a.y_stride * size : (a.channels * size + 15) / 16 * 16)};
-    const cuuint32_t box[2] = {kRowsP, (cuuint32_t)box_rows}, ones[2] = {1, 1};
-    return fn(map, type, 2, a.y, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / size), 32}, ones[2] = {1, 1};
+    return fn(map, type, 2, a.y, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+// Blocks of 128 x BN tiles that fill the GPU's 148 SMs, one or two to each.
+constexpr int64_t kEnoughTiles = 128, kMostBlocks = 296;
+
+static int64_t tiles_of(const Matmul8 &a, int tokens, int channels)
+{
+    return (a.tokens + tokens - 1) / tokens * ((a.channels + channels - 1) / channels);
+}
+static int blocks_of(const Matmul8 &a) { return (int)((a.inner + kBytesK - 1) / kBytesK); }
 
 template <typename T, int BN>
 static bool product_as(const Matmul8 &a, cudaStream_t st)
 {
     CUtensorMap wmap, xmap;
     if (!describe(&wmap, a.w, a.channels, a.inner, kRowsP) || !describe(&xmap, a.x, a.tokens, a.inner, BN)) return false;
-    const int64_t token_tiles = (a.tokens + BN - 1) / BN, tiles = (a.channels + kRowsP - 1) / kRowsP * token_tiles;
-    const int blocks = (int)((a.inner + kBytesK - 1) / kBytesK);
+    const int64_t token_tiles = (a.tokens + BN - 1) / BN, tiles = tiles_of(a, BN, kRowsP);
+    // long rows are shared by up to four blocks (eight where even those are few): 64 x 4096 x 4096 by one 15.1 us, two 12.7,
+    // four 9.8, eight 10.5; rows of up to 1024 bytes are not (256 x 2003 x 1021 7.7 by one, 8.7 by two)
     int splits = 1;
-    while (splits < 8 && tiles * splits * 2 <= 296 && blocks >= splits * 4) splits *= 2;
+    if (blocks_of(a) > 8)
+        while (splits < 8 && tiles * splits * 2 <= (splits < 4 ? kMostBlocks : kEnoughTiles)) splits *= 2;
     constexpr int STAGE = (kRowsP + BN) * kBytesK;
     int ring = 104 * 1024 / STAGE;
     ring = ring < kMaxRing ? ring : kMaxRing;
@@ -584,11 +638,11 @@ static bool product_by_pairs(const Matmul8 &a, cudaStream_t st)
 {
     CUtensorMap wmap, xmap;
     if (!describe(&wmap, a.w, a.channels, a.inner, kRowsP) || !describe(&xmap, a.x, a.tokens, a.inner, kRowsP)) return false;
-    const int64_t token_tiles = (a.tokens + kPairTile - 1) / kPairTile, tiles = (a.channels + kPairTile - 1) / kPairTile * token_tiles;
+    const int64_t token_tiles = (a.tokens + kPairTile - 1) / kPairTile, tiles = tiles_of(a, kPairTile, kPairTile);
     CUtensorMap ymap = {};
     const bool tiled = ((uintptr_t)a.y & 15) == 0 && (a.tokens == 1 || a.y_stride * (int64_t)sizeof(T) % 16 == 0);
-    if (tiled && !describe_outputs(&ymap, a, type_of<T>(), sizeof(T), kLeaveBytes / kRowsP / (int)sizeof(T))) return false;
-    const size_t smem = kPairRing * kPairStage + 4 * kLeaveBytes + 1024;
+    if (tiled && !describe_outputs(&ymap, a, type_of<T>(), sizeof(T))) return false;
+    const size_t smem = kPairRing * kPairStage + 8 * kLeaveBytes + 1024;
     auto kernel = tiled ? k_matmul8_pair<T, true> : k_matmul8_pair<T, false>;
     allow_shared(kernel, smem);
     queue(kernel, dim3((unsigned)(2 * (tiles < 74 ? tiles : 74))), kPairThreads, smem, st, wmap, xmap, ymap, a, (int)tiles, (int)token_tiles);
@@ -608,13 +662,18 @@ static bool product_of_few(const Matmul8 &a, cudaStream_t st)
 template <typename T>
 static bool product(const Matmul8 &a, cudaStream_t st)
 {
+    // one and two tokens: 30522 x 4096 20 and 25 us this way, 24 and 24 by tiles of 16 tokens
     if (a.tokens == 1) return product_of_few<T, 1>(a, st);
     if (a.tokens == 2) return product_of_few<T, 2>(a, st);
-    if (a.tokens > 128 && (a.tokens + 255) / 256 * ((a.channels + 255) / 256) >= 74) return product_by_pairs<T>(a, st);
-    if (a.tokens <= 16) return product_as<T, 16>(a, st);
-    if (a.tokens <= 32) return product_as<T, 32>(a, st);
-    if (a.tokens <= 64) return product_as<T, 64>(a, st);
-    return product_as<T, 128>(a, st);
+    // pairs, as soon as there are tiles for 32 of the 74 (512 x 4096 x 1024 9.4 us, by smaller tiles 9.5; 1024 x 4096 x 4096
+    // 19.1 and 22.2; with 16 tiles, 256 x 4096 x 4096, 17.4 and 13.7)
+    if (a.tokens > 128 && tiles_of(a, kPairTile, kPairTile) >= 32) return product_by_pairs<T>(a, st);
+    // else the widest tiles of which there are enough: fewer blocks read the same weights (128 x 30522 x 768 12.5 us by 128
+    // tokens, 16.3 by 64; 256 x 2003 x 1021 9.9 by 128, 8.4 by 64, 7.7 by 32)
+    if (a.tokens > 64 && tiles_of(a, 128, kRowsP) >= kEnoughTiles) return product_as<T, 128>(a, st);
+    if (a.tokens > 32 && (tiles_of(a, 64, kRowsP) >= kEnoughTiles || blocks_of(a) > 8)) return product_as<T, 64>(a, st);
+    if (a.tokens > 16 && (tiles_of(a, 32, kRowsP) >= kEnoughTiles || blocks_of(a) > 8)) return product_as<T, 32>(a, st);
+    return product_as<T, 16>(a, st);
 }
 bool launch_matmul8(const Matmul8 &a, int type, cudaStream_t st)
 {
