@@ -300,39 +300,68 @@ __device__ __forceinline__ void leave_channels(char *place, int lane, int at, co
     }
 }
 
-// The staged rows from shared memory to anywhere, `tokens` rows of `channels` outputs: 16-bit ones by words, those that begin
-// between two words shifted by one.
-template <typename T>
-__device__ __forceinline__ void leave_rows(const char *place, T *p, int64_t stride, int tokens, int channels, int lane)
+// Staged rows of 128 bytes from shared memory to rows that are no whole vectors: rows `first`, first + step, ..,
+// by words; ODD: they begin between two words, and so each word is put together from two.  No branch in between: rows
+// overlap.
+__device__ __forceinline__ uint32_t staged_word(const char *place, int row, int lane)
 {
-    constexpr int ROWS = 8;                     // fetched together, before the first of them is stored
+    return *reinterpret_cast<const uint32_t *>(place + row * 128 + ((((lane >> 2) ^ row) & 7) << 4) + (lane & 3) * 4);
+}
+template <bool ODD>
+__device__ __forceinline__ void leave_words(const char *place, unsigned short *p, int64_t stride, int first, int step, int tokens, int lane)
+{
+    constexpr int ROWS = 8;
+    p += first * stride;
 #pragma unroll 1
-    for (int i = 0; i < tokens; i += ROWS) {
+    for (int i = first; i < tokens; i += ROWS * step) {
         uint32_t w[ROWS], before[ROWS];
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r)
-            w[r] = *reinterpret_cast<const uint32_t *>(place + (i + r) * 128 + (((lane >> 2) ^ r) << 4) + (lane & 3) * 4);
-        if constexpr (sizeof(T) == 2)
+        for (int r = 0; r < ROWS; ++r) w[r] = staged_word(place, (i + r * step) & 31, lane);
+        if (ODD)
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) before[r] = __shfl_up_sync(0xffffffffu, w[r], 1);
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r, p += stride) {
-            const bool there = i + r < tokens;
-            if constexpr (sizeof(T) == 4) {
-                if (there && lane < channels) p[lane] = __uint_as_float(w[r]);
+        for (int r = 0; r < ROWS; ++r, p += step * stride) {
+            if (i + r * step >= tokens) break;
+            if (!ODD) {
+                reinterpret_cast<uint32_t *>(p)[lane] = w[r];
             } else {
-                unsigned short *u = reinterpret_cast<unsigned short *>(p);
-                const bool odd = (uintptr_t)p & 2;
-                const int e = 2 * lane - (odd ? 1 : 0);         // the word's first output
-                const bool whole = e >= 0 && e + 1 < channels;
-                if (there && whole) *reinterpret_cast<uint32_t *>(u + e) = odd ? __funnelshift_l(before[r], w[r], 16) : w[r];
-                // alone: the first of an odd row, the last of an even row of an odd number, or of an odd row of an even one
-                if (there && (odd || channels & 1)) {
-                    const int one = odd ? (lane == 0 ? 0 : lane == 31 && channels == 64 ? 63 : e + 1 == channels && e > 0 ? e : -1)
-                                        : (e + 1 == channels ? e : -1);
-                    if (one >= 0) u[one] = (unsigned short)(odd && one != 0 ? (one == 63 ? w[r] >> 16 : before[r] >> 16) : w[r]);
-                }
+                if (lane > 0) reinterpret_cast<uint32_t *>(p - 1)[lane] = __funnelshift_l(before[r], w[r], 16);
+                if ((lane + 1 & 31) < 2) p[lane ? 63 : 0] = (unsigned short)(lane ? w[r] >> 16 : w[r]);
             }
+        }
+    }
+}
+// `tokens` staged rows of `channels` outputs to anywhere.
+template <typename T>
+__device__ __forceinline__ void leave_rows(const char *place, T *p, int64_t stride, int tokens, int channels, int lane)
+{
+    if (sizeof(T) == 2 && channels == 64) {
+        unsigned short *u = reinterpret_cast<unsigned short *>(p);
+        const int odd = (int)((uintptr_t)p >> 1 & 1);
+        if (stride & 1) {
+            leave_words<false>(place, u, stride, odd, 2, tokens, lane);
+            leave_words<true>(place, u, stride, 1 - odd, 2, tokens, lane);
+        } else if (odd) {
+            leave_words<true>(place, u, stride, 0, 1, tokens, lane);
+        } else {
+            leave_words<false>(place, u, stride, 0, 1, tokens, lane);
+        }
+        return;
+    }
+    if (sizeof(T) == 4 && channels == 32) {
+        leave_words<false>(place, reinterpret_cast<unsigned short *>(p), 2 * stride, 0, 1, tokens, lane);
+        return;
+    }
+#pragma unroll 1
+    for (int i = 0; i < tokens; ++i, p += stride) {
+        const uint32_t w = staged_word(place, i, lane);
+        if constexpr (sizeof(T) == 4) {
+            if (lane < channels) p[lane] = __uint_as_float(w);
+        } else {
+            unsigned short *u = reinterpret_cast<unsigned short *>(p) + 2 * lane;
+            if (2 * lane < channels) u[0] = (unsigned short)w;
+            if (2 * lane + 1 < channels) u[1] = (unsigned short)(w >> 16);
         }
     }
 }
