@@ -8,6 +8,15 @@ namespace cdadam {
 // A unit as it stands in memory.
 template <typename T> struct Raw8 { uint32_t w[2 * sizeof(T)]; };
 
+// Makes the compiler take the unit apart anew, instead of keeping what it is made of.
+__device__ __forceinline__ void anew(uint32_t &w) { asm volatile("" : "+r"(w)); }
+template <typename T>
+__device__ __forceinline__ void anew(Raw8<T> &u)
+{
+#pragma unroll
+    for (int i = 0; i < 2 * (int)sizeof(T); ++i) anew(u.w[i]);
+}
+
 template <typename T>
 __device__ __forceinline__ void widen8(const Raw8<T> &u, float2 (&f)[4])
 {
@@ -37,7 +46,8 @@ __device__ __forceinline__ uint32_t element_bits(const float *p) { return __floa
 __device__ __forceinline__ uint32_t element_bits(const bf16 *p) { return __ldcs(reinterpret_cast<const unsigned short *>(p)); }
 __device__ __forceinline__ uint32_t element_bits(const f16 *p) { return __ldcs(reinterpret_cast<const unsigned short *>(p)); }
 
-// A matrix as units are taken from it.  VEC: every row starts on 16 bytes, a unit is one or two vectors.  Otherwise a
+// A matrix as units are taken from it.  VEC: every row starts on 16 bytes and is whole units (8-bit rows start on 8
+// bytes), a unit is one or two vectors.  Otherwise a
 // unit is cut out of the aligned vectors around it (and put into those that it shares with its
 // neighbours, which are the neighbouring threads' units): a third of the time of eight elements one by one.  A
 // vector may hold bytes of the rows before and after; of the first and last rows, where those would lie
@@ -55,14 +65,16 @@ __device__ __forceinline__ Place<T> place(const Matrix &m, int64_t rows)
     return {static_cast<T *>(m.p), m.stride, rows, m.stride > 0 ? 47 / (m.stride * (int64_t)sizeof(T)) + 1 : rows};
 }
 
-// w[i + k] for i = 0 .. N - 1, 0 <= k < 4.
-template <int N>
-__device__ __forceinline__ void skip_words(uint32_t (&w)[N + 4], unsigned k)
+// f with the constant k in the place of the number, 0 <= k < 4 (mostly the same for a whole warp): cheaper than
+// selecting among registers.
+template <int K> struct Words { static constexpr int n = K; };
+template <typename F>
+__device__ __forceinline__ void by_words(unsigned k, F f)
 {
-#pragma unroll
-    for (int i = 0; i < N + 2; ++i) w[i] = k & 2 ? w[i + 2] : w[i];
-#pragma unroll
-    for (int i = 0; i < N + 1; ++i) w[i] = k & 1 ? w[i + 1] : w[i];
+    if (k == 0) f(Words<0>());
+    else if (k == 1) f(Words<1>());
+    else if (k == 2) f(Words<2>());
+    else f(Words<3>());
 }
 
 template <typename T>
@@ -85,7 +97,9 @@ __device__ __forceinline__ Raw8<T> load8(const Place<T> &m, int64_t r, int j, in
     const T *const row = m.row(r);
     Raw8<T> u;
     if (VEC) {
-        if (j + 8 > cols) return load_elements(row, j, cols);
+#pragma unroll
+        for (int i = 0; i < W; ++i) u.w[i] = 0;
+        if (j >= cols) return u;
         const uint4 *p = reinterpret_cast<const uint4 *>(row + j);
 #pragma unroll
         for (int i = 0; i < W / 4; ++i) {
@@ -104,10 +118,12 @@ __device__ __forceinline__ Raw8<T> load8(const Place<T> &m, int64_t r, int j, in
         const uint4 v = p[i];               // the neighbours' next one: in the first-level cache
         w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
     }
-    skip_words<W>(w, (unsigned)(at >> 2) & 3);
     const unsigned bits = sizeof(T) == 4 ? 0 : (unsigned)(at & 3) * 8;
+    by_words((unsigned)(at >> 2) & 3, [&](auto words) {
+                constexpr int k = decltype(words)::n;
 #pragma unroll
-    for (int i = 0; i < W; ++i) u.w[i] = sizeof(T) == 4 ? w[i] : __funnelshift_r(w[i], w[i + 1], bits);
+        for (int i = 0; i < W; ++i) u.w[i] = sizeof(T) == 4 ? w[i + k] : __funnelshift_r(w[i + k], w[(i + k + 1) % (W + 4)], bits);
+    });
     if (j + 8 > cols)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -129,14 +145,10 @@ __device__ __forceinline__ void store8(const Place<T> &m, int64_t r, int j, int 
     constexpr int W = 2 * sizeof(T);
     T *const row = m.row(r);
     if (VEC) {
-        if (j + 8 <= cols) {
+        if (j < cols) {
             uint4 *p = reinterpret_cast<uint4 *>(row + j);
 #pragma unroll
             for (int i = 0; i < W / 4; ++i) __stcs(p + i, make_uint4(u.w[4 * i], u.w[4 * i + 1], u.w[4 * i + 2], u.w[4 * i + 3]));
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (j + e < cols) store_element(row, j, u, e);
         }
         return;
     }
@@ -152,19 +164,21 @@ __device__ __forceinline__ void store8(const Place<T> &m, int64_t r, int j, int 
     const int j_before = __shfl_up_sync(0xffffffffu, j, 1);
     const bool whole = j + 8 - (int)over <= cols && (over == 0 || (lane > 0 && j > 0 && j_before == j - 8));
     if (whole) {
-        const unsigned from = 16 - (unsigned)(at & 15);         // byte of w where the vectors begin
-        skip_words<W>(w, from >> 2 & 3);
-        if (from < 16 || over) {
-            const unsigned bits = (from & 3) * 8;
-            if (sizeof(T) != 4)
-#pragma unroll
-                for (int i = 0; i < W; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
-        }
         uint4 *p = reinterpret_cast<uint4 *>(at & ~(uintptr_t)15);
+        const unsigned from = 16 - (unsigned)(at & 15), bits = (from & 3) * 8;      // byte of w where the vectors begin
+        if (over == 0) {
 #pragma unroll
-        for (int i = 0; i < W / 4; ++i)
-            __stcs(p + i, over ? make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3])
-                               : make_uint4(u.w[4 * i], u.w[4 * i + 1], u.w[4 * i + 2], u.w[4 * i + 3]));
+            for (int i = 0; i < W / 4; ++i) __stcs(p + i, make_uint4(u.w[4 * i], u.w[4 * i + 1], u.w[4 * i + 2], u.w[4 * i + 3]));
+        } else {
+            by_words(from >> 2, [&](auto words) {
+                constexpr int k = decltype(words)::n;
+                uint32_t v[W];
+#pragma unroll
+                for (int i = 0; i < W; ++i) v[i] = sizeof(T) == 4 ? w[i + k] : __funnelshift_r(w[i + k], w[(i + k + 1) % (W + 4)], bits);
+#pragma unroll
+                for (int i = 0; i < W / 4; ++i) __stcs(p + i, make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+            });
+        }
     }
     // what no vector takes: the first elements where there is none, the last where the next lane has none
     const bool next = __shfl_down_sync(0xffffffffu, whole && over > 0, 1) && lane < 31;
@@ -176,9 +190,11 @@ __device__ __forceinline__ void store8(const Place<T> &m, int64_t r, int j, int 
             if (e >= first && e < last && j + e < cols) store_element(row, j, u, e);
 }
 
-// Eight bytes; `vec`: rows start on 8 bytes.
+// Eight bytes; `vec`: rows start on 8 bytes (known with VEC).
+template <bool VEC>
 __device__ __forceinline__ uint2 load_bytes(const int8_t *row, int j, int cols, bool vec)
 {
+    if (VEC) return j < cols ? __ldcs(reinterpret_cast<const uint2 *>(row + j)) : make_uint2(0, 0);
     if (vec && j + 8 <= cols) return __ldcs(reinterpret_cast<const uint2 *>(row + j));
     uint32_t w[2] = {0, 0};
 #pragma unroll
@@ -186,8 +202,13 @@ __device__ __forceinline__ uint2 load_bytes(const int8_t *row, int j, int cols, 
         if (j + e < cols) w[e / 4] |= (uint32_t)(uint8_t)row[j + e] << (e % 4 * 8);
     return make_uint2(w[0], w[1]);
 }
+template <bool VEC>
 __device__ __forceinline__ void store_bytes(int8_t *row, int j, int cols, bool vec, uint2 v)
 {
+    if (VEC) {
+        if (j < cols) *reinterpret_cast<uint2 *>(row + j) = v;
+        return;
+    }
     if (vec && j + 8 <= cols) {
         *reinterpret_cast<uint2 *>(row + j) = v;
         return;

@@ -221,6 +221,30 @@ template <> struct Vec<f16> {
     }
 };
 
+// 1 / sqrt(v): the approximation and one Newton step, within 1 ulp or so and a third of the
+// instructions of the correctly rounded quotient and root.  0 and infinity have no step to take (0
+// times infinity): v = 0 gives infinity, a sum of squares that overflowed gives 0.
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const float r = rsqrtf(v);
+    return r > 0.0f && r < 3e38f ? r * fmaf(-0.5f * r * v, r, 1.5f) : r;
+}
+
+// Element i of a gradient whose type is known at run time only; accumulate: added to what is there.
+__device__ __forceinline__ void store_grad(void *p, int64_t i, int type, int accumulate, float v)
+{
+    if (type == 0) {
+        float *q = static_cast<float *>(p) + i;
+        *q = accumulate ? *q + v : v;
+    } else if (type == 1) {
+        bf16 *q = static_cast<bf16 *>(p) + i;
+        *q = narrow<bf16>(accumulate ? widen(*q) + v : v);
+    } else {
+        f16 *q = static_cast<f16 *>(p) + i;
+        *q = narrow<f16>(accumulate ? widen(*q) + v : v);
+    }
+}
+
 template <typename T> __device__ __forceinline__ T minus_inf() { return narrow<T>(kNegInf); }
 
 }  // namespace cdadam

@@ -266,15 +266,6 @@ __device__ __forceinline__ int wait_chunk(uint64_t *bars, const Ring &ring, int 
     return wait_slowly(bars, ring.stages, ring.wait_limit, late, s, phase, row0, step, end);
 }
 
-// 1 / sqrt(v): the approximation and one Newton step, within 1 ulp or so and a third of the
-// instructions of the correctly rounded quotient and root.  0 and infinity have no step to take (0
-// times infinity): v = 0 gives infinity, a sum of squares that overflowed gives 0.
-__device__ __forceinline__ float inverse_root(float v)
-{
-    const float r = rsqrtf(v);
-    return r > 0.0f && r < 3e38f ? r * fmaf(-0.5f * r * v, r, 1.5f) : r;
-}
-
 // ---------------------------------------------------------------------------------------------
 // Forward.  A group works on two rows at a time: their sums go through the same shuffles and
 // barriers, and parameters are taken from shared memory once for both (20000 x 4096 bf16: 71 us a
@@ -496,20 +487,6 @@ __global__ void __launch_bounds__(kLongBlock) k_norm_long(NormForward a)
 // 1024 columns 6.3 TB/s and 16 us beside that, 500 columns 6.0 TB/s and 15 us, 128 columns 3.4 TB/s (the
 // sums over a row) and 12 us: 32768 rows take 48, 31 and 19.5 us.
 // ---------------------------------------------------------------------------------------------
-__device__ __forceinline__ void store_grad(void *p, int64_t i, int type, int accumulate, float v)
-{
-    if (type == 0) {
-        float *q = static_cast<float *>(p) + i;
-        *q = accumulate ? *q + v : v;
-    } else if (type == 1) {
-        bf16 *q = static_cast<bf16 *>(p) + i;
-        *q = narrow<bf16>(accumulate ? widen(*q) + v : v);
-    } else {
-        f16 *q = static_cast<f16 *>(p) + i;
-        *q = narrow<f16>(accumulate ? widen(*q) + v : v);
-    }
-}
-
 // The sums w, b of column j of group g from this block.
 __device__ __forceinline__ void leave_sums(const NormBackward &a, int64_t g, int blocks, int64_t j, float w, float b)
 {

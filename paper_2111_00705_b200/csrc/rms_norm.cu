@@ -52,13 +52,6 @@ __device__ __forceinline__ float group_sum(float sum, float *slot, int group)
     return sum;
 }
 
-// 1 / sqrt(v): the approximation and one Newton step, within 1 ulp or so; 0 gives infinity, infinity 0.
-__device__ __forceinline__ float inverse_root(float v)
-{
-    const float r = rsqrtf(v);
-    return r > 0.0f && r < 3e38f ? __fmul_rn(r, fmaf(__fmul_rn(__fmul_rn(-0.5f, r), v), r, 1.5f)) : r;
-}
-
 // The weight, widened, in shared memory, 0 beyond the row: columns 0 .. 3 of the units in one plane, 4 .. 7
 // in another, so that a warp's 16-byte reads are adjacent.
 __device__ __forceinline__ void fill_weight(float *w, const AnyVec &v, int cols, int units)
@@ -88,13 +81,14 @@ __device__ __forceinline__ Raw8<T> sum8(const Raw8<T> &x, const Raw8<T> &residua
 }
 
 // A block of 32 columns of a checkpoint: four neighbouring threads' units.
+template <bool VEC>
 __device__ __forceinline__ void keep8(const Kept8 &k, int64_t row, int j, int cols, const float2 (&f)[4], bool vec)
 {
     uint32_t m = __float_as_uint(largest8(0.0f, f));
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
     const uint32_t e = kept_exponent(m);
-    store_bytes(k.p + row * k.stride, j, cols, vec, to_kept8(f, m, e));
+    store_bytes<VEC>(k.p + row * k.stride, j, cols, vec, to_kept8(f, m, e));
     if ((threadIdx.x & 3) == 0 && j < cols) k.exponents[row * k.exponents_stride + (j >> 5)] = (uint8_t)e;
 }
 
@@ -125,19 +119,22 @@ __device__ __forceinline__ void finish8(const RmsNorm &a, const Place<T> &y, con
         for (int e = 0; e < 4; ++e) f[e] = mul2(p[e], both(st.s));
         store8<T, VEC>(y, row, j, (int)a.cols, narrow8<T>(f));
     }
-    if (a.q.p) store_bytes(a.q.p + row * a.q.stride, j, (int)a.cols, q_vec, st.finite ? to_rows8(p, st.step) : make_uint2(0, 0));
+    if (a.q.p) store_bytes<VEC>(a.q.p + row * a.q.stride, j, (int)a.cols, q_vec, st.finite ? to_rows8(p, st.step) : make_uint2(0, 0));
 }
 
 // ---------------------------------------------------------------------------------------------
 // Forward.
 // ---------------------------------------------------------------------------------------------
-// Blocks an SM holds: as many as the registers of a thread's units allow.
-constexpr int forward_blocks(int size, int steps, int threads)
+// Blocks an SM holds.  A thread's units of 16 bits fit into 80 registers, 768 threads (16384 x 4096 bf16 in 8 bits 112 us; with
+// 64 registers, 1024 threads, some of them in memory, 120); rows that are cut out of vectors wait longer for memory and gain by
+// more threads all the same (3001 x 1021 f32 16.9 us, with fewer 19.2; 20000 x 1022 bf16 in 8 bits 76 and 86).
+constexpr int forward_blocks(int size, int steps, int threads, bool vec)
 {
-    return (size * steps <= 4 ? 1024 : size * steps <= 8 ? 768 : 512) / threads > 0 ? (size * steps <= 4 ? 1024 : size * steps <= 8 ? 768 : 512) / threads : 1;
+    return threads > 512 ? 1 : (vec ? (size * steps <= 4 ? 768 : 512) : size * steps <= 4 ? 1024 : size * steps <= 8 ? 768 : 512) / threads;
 }
+
 template <typename T, int THREADS, int STEPS, int BT, bool VEC>
-__global__ void __launch_bounds__(BT, forward_blocks(sizeof(T), STEPS, BT)) k_rms_norm(RmsNorm a)
+__global__ void __launch_bounds__(BT, forward_blocks(sizeof(T), STEPS, BT, VEC)) k_rms_norm(RmsNorm a)
 {
     constexpr int GROUPS = BT / THREADS, UNITS = THREADS * STEPS;
     constexpr bool AHEAD = BT < 1024 || sizeof(T) == 2;       // the next row's units fit into the registers
@@ -176,7 +173,7 @@ __global__ void __launch_bounds__(BT, forward_blocks(sizeof(T), STEPS, BT)) k_rm
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
             const int u = t + k * THREADS;
-            if (a.kept.p) keep8(a.kept, row, 8 * u, cols, p[k], kept_vec);
+            if (a.kept.p) keep8<VEC>(a.kept, row, 8 * u, cols, p[k], kept_vec);
             float2 f[4];
             weight8(w, u, UNITS, f);
 #pragma unroll
@@ -222,7 +219,7 @@ __global__ void __launch_bounds__(kLongThreads, 1) k_rms_norm_long(RmsNorm a)
         if (a.residual.p) h = sum8<T>(h, load8<T, VEC>(residual_, row, j, cols));
         if (a.total.p) store8<T, VEC>(total_, row, j, cols, h);
         widen8<T>(h, f);
-        if (a.kept.p) keep8(a.kept, row, j, cols, f, kept_vec);
+        if (a.kept.p) keep8<VEC>(a.kept, row, j, cols, f, kept_vec);
         weight8_long(a.weight, j, cols, w);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -261,20 +258,6 @@ __global__ void __launch_bounds__(kLongThreads, 1) k_rms_norm_long(RmsNorm a)
 // its own columns in registers, so everything is read once.  `parts` blocks share a group; with more than one each
 // leaves its sums in the workspace and k_rms_sums adds them in order: the same bits every time.
 // ---------------------------------------------------------------------------------------------
-__device__ __forceinline__ void store_gradient(void *p, int64_t i, int type, int accumulate, float v)
-{
-    if (type == 0) {
-        float *q = static_cast<float *>(p) + i;
-        *q = accumulate ? *q + v : v;
-    } else if (type == 1) {
-        bf16 *q = static_cast<bf16 *>(p) + i;
-        *q = narrow<bf16>(accumulate ? widen(*q) + v : v);
-    } else {
-        f16 *q = static_cast<f16 *>(p) + i;
-        *q = narrow<f16>(accumulate ? widen(*q) + v : v);
-    }
-}
-
 // A unit of the activations, as they were or as a checkpoint.
 template <typename T, bool KEPT> struct Source {
     Raw8<T> u;
@@ -289,6 +272,7 @@ template <typename T, bool KEPT> struct Source {
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = mul2(f[e], both(s));
     }
+    __device__ __forceinline__ void forget() { anew(u); }
 };
 template <typename T> struct Source<T, true> {
     uint2 u;
@@ -296,7 +280,7 @@ template <typename T> struct Source<T, true> {
     template <bool VEC>
     __device__ __forceinline__ void load(const RmsNormBackward &a, const Place<T> &, int64_t row, int j, int cols, bool vec)
     {
-        u = load_bytes(a.kept.p + row * a.kept.stride, j, cols, vec);
+        u = load_bytes<VEC>(a.kept.p + row * a.kept.stride, j, cols, vec);
         exponent = j < cols ? __ldg(a.kept.exponents + row * a.kept.exponents_stride + (j >> 5)) : 1;
     }
     __device__ __forceinline__ void values(float s, float2 (&f)[4]) const
@@ -306,10 +290,15 @@ template <typename T> struct Source<T, true> {
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = mul2(mul2(f[e], both(step)), both(s));
     }
+    __device__ __forceinline__ void forget()
+    {
+        anew(u.x);
+        anew(u.y);
+    }
 };
 
 template <typename T, int THREADS, int STEPS, int BT, bool VEC, bool KEPT>
-__global__ void __launch_bounds__(BT, BT == 256 ? 2 : 1) k_rms_norm_backward(RmsNormBackward a)
+__global__ void __launch_bounds__(BT, 512 / BT) k_rms_norm_backward(RmsNormBackward a)
 {
     constexpr int GROUPS = BT / THREADS, UNITS = THREADS * STEPS;
     extern __shared__ __align__(16) float w[];          // the weight; at the end the groups' sums
@@ -332,6 +321,7 @@ __global__ void __launch_bounds__(BT, BT == 256 ? 2 : 1) k_rms_norm_backward(Rms
             x[k].template load<VEC>(a, x_, n, j, cols, vec);
         }
     };
+    if (a.dweight && gridDim.x > 1) grid_dep_launch();  // of k_rms_sums, which waits for all of this
     if (row < end) fetch(row);
     fill_weight(w, a.weight, cols, UNITS);
     __syncthreads();
@@ -371,6 +361,8 @@ __global__ void __launch_bounds__(BT, BT == 256 ? 2 : 1) k_rms_norm_backward(Rms
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
             float2 g[4], xh[4], f[4];
+            x_now[k].forget();
+            anew(dy_now[k]);
             x_now[k].values(s, xh);
             widen8<T>(dy_now[k], g);
             weight8(w, t + k * THREADS, UNITS, f);
@@ -402,7 +394,7 @@ __global__ void __launch_bounds__(BT, BT == 256 ? 2 : 1) k_rms_norm_backward(Rms
     for (int j = threadIdx.x; j < cols; j += BT) {
         const float v = w[(j & 4 ? 4 * UNITS : 0) + (j >> 3) * 4 + (j & 3)];
         if (gridDim.x > 1) a.parts[((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * cols + j] = v;
-        else store_gradient(a.dweight, blockIdx.y * a.dweight_stride + j, a.grad_type, a.accumulate, v);
+        else store_grad(a.dweight, blockIdx.y * a.dweight_stride + j, a.grad_type, a.accumulate, v);
     }
 }
 
@@ -471,7 +463,7 @@ __global__ void __launch_bounds__(128) k_rms_dw_long(RmsNormBackward a)
         if (j + e >= cols) break;
         const float v = e & 1 ? sums[e / 2].y : sums[e / 2].x;
         if (parts > 1) a.parts[((int64_t)blockIdx.z * parts + part) * cols + j + e] = v;
-        else store_gradient(a.dweight, blockIdx.z * a.dweight_stride + j + e, a.grad_type, a.accumulate, v);
+        else store_grad(a.dweight, blockIdx.z * a.dweight_stride + j + e, a.grad_type, a.accumulate, v);
     }
 }
 
@@ -490,7 +482,7 @@ __global__ void __launch_bounds__(1024) k_rms_sums(RmsNormBackward a, int parts)
     __syncthreads();
     v = warp_sum(sh[lane][warp]);                       // column `warp` of the block
     if (lane == 0 && (int64_t)blockIdx.x * 32 + warp < a.cols)
-        store_gradient(a.dweight, blockIdx.y * a.dweight_stride + (int64_t)blockIdx.x * 32 + warp, a.grad_type, a.accumulate, v);
+        store_grad(a.dweight, blockIdx.y * a.dweight_stride + (int64_t)blockIdx.x * 32 + warp, a.grad_type, a.accumulate, v);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -560,7 +552,7 @@ __global__ void __launch_bounds__(kFlat) k_checkpoint8(Matrix x, Kept8 kept, int
         for (int k = 0; k < kAhead; ++k) {
             float2 f[4];
             widen8<T>(u[k], f);
-            keep8(kept, at[k].row, at[k].j, cols, f, vec);
+            keep8<VEC>(kept, at[k].row, at[k].j, cols, f, vec);
         }
     }
 }
@@ -580,7 +572,7 @@ __global__ void __launch_bounds__(kFlat) k_restore8(Rows8 q, Kept8 kept, Matrix 
         units_at<WIDE>(i, n, cols, at);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            b[k] = load_bytes(p + at[k].row * stride, at[k].j, cols, vec);
+            b[k] = load_bytes<VEC>(p + at[k].row * stride, at[k].j, cols, vec);
             s[k] = 0.0f;
             if (at[k].j < cols)
                 s[k] = kept.p ? kept_step(__ldg(kept.exponents + at[k].row * kept.exponents_stride + (at[k].j >> 5))) : __ldg(q.scale + at[k].row);
@@ -599,16 +591,17 @@ __global__ void __launch_bounds__(kFlat) k_restore8(Rows8 q, Kept8 kept, Matrix 
 // ---------------------------------------------------------------------------------------------
 // Launches
 // ---------------------------------------------------------------------------------------------
-static bool starts_on_16(const Matrix &m, int64_t rows, int size)
+static bool starts_on(int bytes, const void *p, int64_t rows, int64_t row_bytes)
 {
-    return !m.p || (((uintptr_t)m.p & 15) == 0 && (rows <= 1 || (m.stride * size & 15) == 0));
+    return !p || (((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0 && (rows <= 1 || (row_bytes & (bytes - 1)) == 0));
 }
+static bool starts_on_16(const Matrix &m, int64_t rows, int size) { return starts_on(16, m.p, rows, m.stride * size); }
 
 template <typename T, int THREADS, int STEPS, int BT>
 static void forward_as(const RmsNorm &a, bool vec, cudaStream_t st)
 {
     auto kernel = vec ? k_rms_norm<T, THREADS, STEPS, BT, true> : k_rms_norm<T, THREADS, STEPS, BT, false>;
-    const int64_t groups = BT / THREADS, need = (a.rows + groups - 1) / groups, most = kSms * forward_blocks(sizeof(T), STEPS, BT);
+    const int64_t groups = BT / THREADS, need = (a.rows + groups - 1) / groups, most = kSms * forward_blocks(sizeof(T), STEPS, BT, vec);
     const size_t smem = (size_t)THREADS * STEPS * 32;
     allow_shared(kernel, smem);
     queue(kernel, dim3((unsigned)(need < most ? need : most)), BT, smem, st, a);
@@ -618,7 +611,8 @@ static void forward(const RmsNorm &a, cudaStream_t st)
 {
     const int size = sizeof(T);
     const bool vec = starts_on_16(a.x, a.rows, size) && starts_on_16(a.residual, a.rows, size) && starts_on_16(a.total, a.rows, size) &&
-                     starts_on_16(a.y, a.rows, size);
+                     starts_on_16(a.y, a.rows, size) && starts_on(8, a.q.p, a.rows, a.q.stride) &&
+                     starts_on(8, a.kept.p, a.rows, a.kept.stride) && a.cols % 8 == 0;
     const int64_t units = (a.cols + 7) / 8;
     if (units <= 32) forward_as<T, 32, 1, 256>(a, vec, st);
     else if (units <= 64) forward_as<T, 32, 2, 256>(a, vec, st);
@@ -692,7 +686,7 @@ static void backward(const RmsNormBackward &a, cudaStream_t st)
 {
     const int size = sizeof(T);
     const bool vec = starts_on_16(a.dy, a.rows, size) && starts_on_16(a.x, a.rows, size) && starts_on_16(a.dtotal, a.rows, size) &&
-                     starts_on_16(a.dx, a.rows, size);
+                     starts_on_16(a.dx, a.rows, size) && starts_on(8, a.kept.p, a.rows, a.kept.stride) && a.cols % 8 == 0;
     const int64_t units = (a.cols + 7) / 8;
     const int parts = (int)backward_parts(a.rows, a.cols, a.groups);
     bool queued;
@@ -723,7 +717,7 @@ template <typename T>
 static void checkpoint(const Matrix &x, const Kept8 &kept, int64_t rows, int64_t cols, cudaStream_t st)
 {
     const int64_t units = (cols + 31) / 32 * 4;
-    const bool vec = starts_on_16(x, rows, sizeof(T)), wide = units >= kWideUnits;
+    const bool vec = starts_on_16(x, rows, sizeof(T)) && starts_on(8, kept.p, rows, kept.stride) && cols % 8 == 0, wide = units >= kWideUnits;
     auto kernel = wide ? (vec ? k_checkpoint8<T, true, true> : k_checkpoint8<T, false, true>)
                        : (vec ? k_checkpoint8<T, true, false> : k_checkpoint8<T, false, false>);
     const Units n = units_of(rows, units);
@@ -739,7 +733,8 @@ template <typename T>
 static void restore(const Rows8 &q, const Kept8 &kept, const Matrix &to, int64_t rows, int64_t cols, cudaStream_t st)
 {
     const int64_t units = (cols + 7) / 8;
-    const bool vec = starts_on_16(to, rows, sizeof(T)), wide = units >= kWideUnits;
+    const bool vec = starts_on_16(to, rows, sizeof(T)) && starts_on(8, q.p, rows, q.stride) && starts_on(8, kept.p, rows, kept.stride) && cols % 8 == 0;
+    const bool wide = units >= kWideUnits;
     auto kernel = wide ? (vec ? k_restore8<T, true, true> : k_restore8<T, false, true>)
                        : (vec ? k_restore8<T, true, false> : k_restore8<T, false, false>);
     const Units n = units_of(rows, units);
