@@ -751,10 +751,11 @@ def _rows8(rows, cols, device):
 
 def _bytes(t, what, device, shape, dtype=torch.int8):
     """(pointer, row stride) of a matrix of bytes."""
-    if t.get_device() != device or t.shape != shape or t.dtype != dtype or (shape[1] > 1 and t.stride(1) != 1):
+    stride = t.stride()
+    if t.shape != shape or t.dtype != dtype or t.get_device() != device or (stride[1] != 1 and shape[1] > 1):
         raise ValueError("%s must be %s %s on device %d with adjacent row elements, not %s %s on %s"
                          % (what, tuple(shape), dtype, device, tuple(t.shape), t.dtype, t.device))
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), stride[0]
 
 
 def _checkpoint(pair, device, shape):
@@ -770,9 +771,8 @@ def checkpoint8_like(x):
     return _rows8(rows, cols, x.device), torch.empty(rows, -(-cols // CHECKPOINT_BLOCK), dtype=torch.uint8, device=x.device)
 
 
-def _rms_norm(x, weight, residual, eps, y, q, scale, total, rstd, checkpoint):
-    device, shape, dtype = x.get_device(), x.shape, x.dtype
-    px, sx = _matrix(x, "x")
+def _rms_norm(x, at, device, shape, dtype, weight, residual, eps, y, q, scale, total, rstd, checkpoint):
+    px, sx = at
     rows, cols = shape
     pr, sr = (None, 0) if residual is None else _matrix(residual, "residual", device, shape, dtype)
     pt, st = (None, 0) if total is None else _matrix(total, "total", device, shape, dtype)
@@ -793,39 +793,37 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, out=None, checkpoint=None,
     any of the three types.  out: (y, total, rstd) to write into, each may be None: y is then allocated, total and
     rstd are not computed.  checkpoint: (kept, exponents) to write the sum's checkpoint into
     (checkpoint8_like).  No automatic differentiation: rms_norm_backward is the gradient."""
-    _matrix(x, "x")
-    device = x.get_device()
+    at, device, shape, dtype = _matrix(x, "x"), x.get_device(), x.shape, x.dtype
     if device < 0 or stream is not None or device != _current():
         with _elsewhere(x, stream):
             return rms_norm(x, weight, residual, eps, out, checkpoint)
     if out is None:
-        y, rstd = torch.empty(x.shape, dtype=x.dtype, device=x.device), torch.empty(x.shape[0], device=x.device)
+        y, rstd = torch.empty(shape, dtype=dtype, device=x.device), torch.empty(shape[0], device=x.device)
         total = None if residual is None else torch.empty_like(y)
     else:
         y, total, rstd = out
         if y is None:
-            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _rms_norm(x, weight, residual, eps, y, None, None, total, rstd, checkpoint)
+            y = torch.empty(shape, dtype=dtype, device=x.device)
+    _rms_norm(x, at, device, shape, dtype, weight, residual, eps, y, None, None, total, rstd, checkpoint)
     return y, total, rstd
 
 
 def rms_norm8(x, weight=None, residual=None, eps=1e-6, out=None, checkpoint=None, stream=None):
     """rms_norm with its output in 8 bits: (q, scale, total, rstd), as matmul8 takes it.  out: the four to write
     into; total and rstd may be None: not computed."""
-    _matrix(x, "x")
-    device = x.get_device()
+    at, device, shape, dtype = _matrix(x, "x"), x.get_device(), x.shape, x.dtype
     if device < 0 or stream is not None or device != _current():
         with _elsewhere(x, stream):
             return rms_norm8(x, weight, residual, eps, out, checkpoint)
     if out is None:
-        q = _rows8(*x.shape, x.device)
-        scale, rstd = torch.empty(2, x.shape[0], device=x.device).unbind(0)
-        total = None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        q = _rows8(*shape, x.device)
+        scale, rstd = torch.empty(2, shape[0], device=x.device).unbind(0)
+        total = None if residual is None else torch.empty(shape, dtype=dtype, device=x.device)
     else:
         q, scale, total, rstd = out
         if q is None or scale is None:
             raise ValueError("out needs q and scale")
-    _rms_norm(x, weight, residual, eps, None, q, scale, total, rstd, checkpoint)
+    _rms_norm(x, at, device, shape, dtype, weight, residual, eps, None, q, scale, total, rstd, checkpoint)
     return q, scale, total, rstd
 
 
@@ -957,10 +955,11 @@ def matmul8(x, x_scale, w, w_scale, bias=None, dtype=torch.bfloat16, out=None, s
     if device < 0 or stream is not None or device != _current():
         with _elsewhere(x, stream):
             return matmul8(x, x_scale, w, w_scale, bias, dtype, out)
-    if x.dim() != 2 or w.dim() != 2:
+    shape, w_shape = x.shape, w.shape
+    if len(shape) != 2 or len(w_shape) != 2:
         raise ValueError("x and w must be matrices")
-    (tokens, inner), channels = x.shape, w.shape[0]
-    px, sx = _bytes(x, "x", device, (tokens, inner))
+    (tokens, inner), channels = shape, w_shape[0]
+    px, sx = _bytes(x, "x", device, shape)
     pw, sw = _bytes(w, "w", device, (channels, inner))
     pb = _vector(bias, "bias", device, (channels,), _TYPES)
     if out is None:

@@ -89,46 +89,61 @@ __device__ __forceinline__ Raw8<T> load_elements(const T *row, int j, int cols)
     return u;
 }
 
-// Columns j .. j + 7 of row r, 0 beyond its end.
-template <typename T, bool VEC>
-__device__ __forceinline__ Raw8<T> load8(const Place<T> &m, int64_t r, int j, int cols)
-{
-    constexpr int W = 2 * sizeof(T);
-    const T *const row = m.row(r);
-    Raw8<T> u;
-    if (VEC) {
+// Columns j .. j + 7 of row r on their way: the aligned vectors around them, or the elements where a vector would reach
+// beyond the matrix.  Asking for them and taking them are two steps with branches in the second alone, so that a thread
+// can have several on their way at once.
+template <typename T, bool VEC> struct Unit {
+    static constexpr int W = 2 * (int)sizeof(T);
+    uint32_t w[VEC ? W : W + 4];
+
+    // not `edge`: row r is none of those at the matrix's ends
+    __device__ __forceinline__ void ask(const Place<T> &m, int64_t r, int j, int cols, bool edge)
+    {
+        const T *const row = m.row(r);
+        const uint4 *p = reinterpret_cast<const uint4 *>((uintptr_t)(row + j) & ~(uintptr_t)15);
+        const bool some = j < cols;
+        if (VEC || !edge) {
 #pragma unroll
-        for (int i = 0; i < W; ++i) u.w[i] = 0;
-        if (j >= cols) return u;
-        const uint4 *p = reinterpret_cast<const uint4 *>(row + j);
+            for (int i = 0; i < (VEC ? W / 4 : W / 4 + 1); ++i) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (some) v = VEC ? __ldcs(p + i) : p[i];   // else also the neighbour's next one: in the first-level cache
+                w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+            }
+        } else {
+            const Raw8<T> u = load_elements(row, j, cols);
 #pragma unroll
-        for (int i = 0; i < W / 4; ++i) {
-            const uint4 v = __ldcs(p + i);
-            u.w[4 * i] = v.x; u.w[4 * i + 1] = v.y; u.w[4 * i + 2] = v.z; u.w[4 * i + 3] = v.w;
+            for (int i = 0; i < W; ++i) w[i] = u.w[i];
+        }
+    }
+    // 0 beyond the row's end
+    __device__ __forceinline__ Raw8<T> take(const Place<T> &m, int64_t r, int j, int cols, bool edge) const
+    {
+        Raw8<T> u;
+        if constexpr (VEC) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) u.w[i] = w[i];
+        } else {
+            const unsigned at = edge ? 0 : (unsigned)(uintptr_t)m.row(r), bits = sizeof(T) == 4 ? 0 : (at & 3) * 8;
+            by_words(at >> 2 & 3, [&](auto words) {
+                constexpr int k = decltype(words)::n;
+#pragma unroll
+                for (int i = 0; i < W; ++i) u.w[i] = sizeof(T) == 4 ? w[i + k] : __funnelshift_r(w[i + k], w[(i + k + 1) % (W + 4)], bits);
+            });
+            if (j + 8 > cols)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (j + e >= cols) u.w[e * sizeof(T) / 4] &= sizeof(T) == 4 ? 0u : e & 1 ? 0x0000ffffu : 0xffff0000u;
         }
         return u;
     }
-    if (j >= cols || (m.edge(r) && (j * (int)sizeof(T) < 16 || (j + 8) * (int)sizeof(T) + 16 > cols * (int)sizeof(T))))
-        return load_elements(row, j, cols);
-    const uintptr_t at = (uintptr_t)(row + j);
-    const uint4 *p = reinterpret_cast<const uint4 *>(at & ~(uintptr_t)15);
-    uint32_t w[W + 4];
-#pragma unroll
-    for (int i = 0; i < W / 4 + 1; ++i) {
-        const uint4 v = p[i];               // the neighbours' next one: in the first-level cache
-        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
-    }
-    const unsigned bits = sizeof(T) == 4 ? 0 : (unsigned)(at & 3) * 8;
-    by_words((unsigned)(at >> 2) & 3, [&](auto words) {
-                constexpr int k = decltype(words)::n;
-#pragma unroll
-        for (int i = 0; i < W; ++i) u.w[i] = sizeof(T) == 4 ? w[i + k] : __funnelshift_r(w[i + k], w[(i + k + 1) % (W + 4)], bits);
-    });
-    if (j + 8 > cols)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (j + e >= cols) u.w[e * sizeof(T) / 4] &= sizeof(T) == 4 ? 0u : e & 1 ? 0x0000ffffu : 0xffff0000u;
-    return u;
+};
+template <typename T, bool VEC>
+__device__ __forceinline__ Raw8<T> load8(const Place<T> &m, int64_t r, int j, int cols)
+{
+    const bool edge = !VEC && m.edge(r);
+    Unit<T, VEC> u;
+    u.ask(m, r, j, cols, edge);
+    return u.take(m, r, j, cols, edge);
 }
 
 template <typename T>

@@ -1,6 +1,6 @@
 // Root-mean-square norm with the residual's addition, its gradient, and the 8-bit formats of rows.
 //
-// All are bound by memory: every matrix is read once and written once.  A group of 32 to 512 threads
+// All are bound by memory: every matrix is read once and written once.  A group of 32 to 1024 threads
 // takes a row at a time, every thread up to four units of eight columns, and asks for its next row's units
 // before it works on the present ones.
 #include "eight_bits.cuh"
@@ -128,9 +128,9 @@ __device__ __forceinline__ void finish8(const RmsNorm &a, const Place<T> &y, con
 // Blocks an SM holds.  A thread's units of 16 bits fit into 80 registers, 768 threads (16384 x 4096 bf16 in 8 bits 112 us; with
 // 64 registers, 1024 threads, some of them in memory, 120); rows that are cut out of vectors wait longer for memory and gain by
 // more threads all the same (3001 x 1021 f32 16.9 us, with fewer 19.2; 20000 x 1022 bf16 in 8 bits 76 and 86).
-constexpr int forward_blocks(int size, int steps, int threads, bool vec)
+constexpr int forward_blocks(int size, int steps, int threads, bool)
 {
-    return threads > 512 ? 1 : (vec ? (size * steps <= 4 ? 768 : 512) : size * steps <= 4 ? 1024 : size * steps <= 8 ? 768 : 512) / threads;
+    return threads > 512 ? 1 : (size * steps <= 4 ? 768 : 512) / threads;
 }
 
 template <typename T, int THREADS, int STEPS, int BT, bool VEC>
@@ -145,13 +145,14 @@ __global__ void __launch_bounds__(BT, forward_blocks(sizeof(T), STEPS, BT, VEC))
     const bool q_vec = on(a.q.p, a.q.stride, 8), kept_vec = on(a.kept.p, a.kept.stride, 8);
     const Place<T> x_ = place<T>(a.x, a.rows), residual_ = place<T>(a.residual, a.rows), total_ = place<T>(a.total, a.rows), y_ = place<T>(a.y, a.rows);
     int64_t row = (int64_t)blockIdx.x * GROUPS + group;
-    Raw8<T> x[STEPS], r[STEPS];
+    Unit<T, VEC> x[STEPS], r[STEPS];
     auto fetch = [&](int64_t n) {
+        const bool edge = !VEC && x_.edge(n), r_edge = !VEC && residual_.edge(n);
 #pragma unroll
-        for (int k = 0; k < STEPS; ++k) x[k] = load8<T, VEC>(x_, n, 8 * (t + k * THREADS), cols);
+        for (int k = 0; k < STEPS; ++k) x[k].ask(x_, n, 8 * (t + k * THREADS), cols, edge);
         if (a.residual.p)
 #pragma unroll
-            for (int k = 0; k < STEPS; ++k) r[k] = load8<T, VEC>(residual_, n, 8 * (t + k * THREADS), cols);
+            for (int k = 0; k < STEPS; ++k) r[k].ask(residual_, n, 8 * (t + k * THREADS), cols, r_edge);
     };
     if (AHEAD && row < a.rows) fetch(row);
     fill_weight(w, a.weight, cols, UNITS);
@@ -160,14 +161,14 @@ __global__ void __launch_bounds__(BT, forward_blocks(sizeof(T), STEPS, BT, VEC))
         float2 p[STEPS][4], squares = both(0.0f);
         float top = 0.0f;
         if (!AHEAD) fetch(row);
-        if (a.residual.p)
-#pragma unroll
-            for (int k = 0; k < STEPS; ++k) x[k] = sum8<T>(x[k], r[k]);
+        const bool edge = !VEC && x_.edge(row), r_edge = !VEC && residual_.edge(row);
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
-            const int u = t + k * THREADS;
-            if (a.total.p) store8<T, VEC>(total_, row, 8 * u, cols, x[k]);
-            widen8<T>(x[k], p[k]);
+            const int j = 8 * (t + k * THREADS);
+            Raw8<T> h = x[k].take(x_, row, j, cols, edge);
+            if (a.residual.p) h = sum8<T>(h, r[k].take(residual_, row, j, cols, r_edge));
+            if (a.total.p) store8<T, VEC>(total_, row, j, cols, h);
+            widen8<T>(h, p[k]);
         }
         if (AHEAD && row + step < a.rows) fetch(row + step);
 #pragma unroll
@@ -258,49 +259,57 @@ __global__ void __launch_bounds__(kLongThreads, 1) k_rms_norm_long(RmsNorm a)
 // its own columns in registers, so everything is read once.  `parts` blocks share a group; with more than one each
 // leaves its sums in the workspace and k_rms_sums adds them in order: the same bits every time.
 // ---------------------------------------------------------------------------------------------
-// A unit of the activations, as they were or as a checkpoint.
-template <typename T, bool KEPT> struct Source {
-    Raw8<T> u;
-    template <bool VEC>
-    __device__ __forceinline__ void load(const RmsNormBackward &, const Place<T> &x, int64_t row, int j, int cols, bool)
+// A unit of the activations times s, as they were or as a checkpoint.
+template <typename T, bool VEC, bool KEPT> struct Source {
+    Unit<T, VEC> u;
+    __device__ __forceinline__ void ask(const RmsNormBackward &, const Place<T> &x, int64_t row, int j, int cols, bool)
     {
-        u = load8<T, VEC>(x, row, j, cols);
+        u.ask(x, row, j, cols, !VEC && x.edge(row));
     }
-    __device__ __forceinline__ void values(float s, float2 (&f)[4]) const
+    __device__ __forceinline__ void take(const RmsNormBackward &, const Place<T> &x, int64_t row, int j, int cols, Raw8<T> &now) const
     {
-        widen8<T>(u, f);
+        now = u.take(x, row, j, cols, !VEC && x.edge(row));
+    }
+    typedef Raw8<T> Now;
+    static __device__ __forceinline__ void values(const Now &now, float s, float2 (&f)[4])
+    {
+        widen8<T>(now, f);
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = mul2(f[e], both(s));
     }
-    __device__ __forceinline__ void forget() { anew(u); }
 };
-template <typename T> struct Source<T, true> {
+struct Kept {
     uint2 u;
     uint32_t exponent;
-    template <bool VEC>
-    __device__ __forceinline__ void load(const RmsNormBackward &a, const Place<T> &, int64_t row, int j, int cols, bool vec)
+};
+__device__ __forceinline__ void anew(Kept &k)
+{
+    anew(k.u.x);
+    anew(k.u.y);
+}
+template <typename T, bool VEC> struct Source<T, VEC, true> {
+    Kept u;
+    __device__ __forceinline__ void ask(const RmsNormBackward &a, const Place<T> &, int64_t row, int j, int cols, bool vec)
     {
-        u = load_bytes<VEC>(a.kept.p + row * a.kept.stride, j, cols, vec);
-        exponent = j < cols ? __ldg(a.kept.exponents + row * a.kept.exponents_stride + (j >> 5)) : 1;
+        u.u = load_bytes<VEC>(a.kept.p + row * a.kept.stride, j, cols, vec);
+        u.exponent = j < cols ? __ldg(a.kept.exponents + row * a.kept.exponents_stride + (j >> 5)) : 1;
     }
-    __device__ __forceinline__ void values(float s, float2 (&f)[4]) const
+    typedef Kept Now;
+    __device__ __forceinline__ void take(const RmsNormBackward &, const Place<T> &, int64_t, int, int, Kept &now) const { now = u; }
+    static __device__ __forceinline__ void values(const Kept &now, float s, float2 (&f)[4])
     {
-        const float step = kept_step(exponent);
-        unpack_bytes(u, f);
+        const float step = kept_step(now.exponent);
+        unpack_bytes(now.u, f);
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = mul2(mul2(f[e], both(step)), both(s));
-    }
-    __device__ __forceinline__ void forget()
-    {
-        anew(u.x);
-        anew(u.y);
     }
 };
 
 template <typename T, int THREADS, int STEPS, int BT, bool VEC, bool KEPT>
-__global__ void __launch_bounds__(BT, 512 / BT) k_rms_norm_backward(RmsNormBackward a)
+__global__ void __launch_bounds__(BT, BT > 512 ? 1 : 512 / BT) k_rms_norm_backward(RmsNormBackward a)
 {
     constexpr int GROUPS = BT / THREADS, UNITS = THREADS * STEPS;
+    constexpr bool AHEAD = STEPS * BT <= 1024 && (VEC || sizeof(T) == 2);    // the next row's units fit into the registers
     extern __shared__ __align__(16) float w[];          // the weight; at the end the groups' sums
     __shared__ float slots[GROUPS][2][THREADS / 32];
     const int t = threadIdx.x % THREADS, group = threadIdx.x / THREADS, cols = (int)a.cols;
@@ -309,20 +318,22 @@ __global__ void __launch_bounds__(BT, 512 / BT) k_rms_norm_backward(RmsNormBackw
     const float over = __frcp_rn((float)cols);
     const Place<T> dy_ = place<T>(a.dy, a.rows), x_ = place<T>(a.x, a.rows), dtotal_ = place<T>(a.dtotal, a.rows), dx_ = place<T>(a.dx, a.rows);
     int64_t row = blockIdx.y * per + (int64_t)blockIdx.x * GROUPS + group;
-    Raw8<T> dy[STEPS];
-    Source<T, KEPT> x[STEPS];
+    Unit<T, VEC> dy[STEPS], more[STEPS];
+    Source<T, VEC, KEPT> x[STEPS];
     float rstd = 0.0f;
     auto fetch = [&](int64_t n) {
         rstd = __ldg(a.rstd + n);
+        const bool edge = !VEC && dy_.edge(n), more_edge = !VEC && dtotal_.edge(n);
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
             const int j = 8 * (t + k * THREADS);
-            dy[k] = load8<T, VEC>(dy_, n, j, cols);
-            x[k].template load<VEC>(a, x_, n, j, cols, vec);
+            dy[k].ask(dy_, n, j, cols, edge);
+            x[k].ask(a, x_, n, j, cols, vec);
+            if (AHEAD && a.dtotal.p) more[k].ask(dtotal_, n, j, cols, more_edge);
         }
     };
     if (a.dweight && gridDim.x > 1) grid_dep_launch();  // of k_rms_sums, which waits for all of this
-    if (row < end) fetch(row);
+    if (AHEAD && row < end) fetch(row);
     fill_weight(w, a.weight, cols, UNITS);
     __syncthreads();
     float2 sums[STEPS][4];
@@ -331,23 +342,24 @@ __global__ void __launch_bounds__(BT, 512 / BT) k_rms_norm_backward(RmsNormBackw
 #pragma unroll
         for (int e = 0; e < 4; ++e) sums[k][e] = both(0.0f);
     for (int slot = 0; row < end; row += step, slot ^= 1) {
+        if (!AHEAD) fetch(row);
         float2 dot = both(0.0f);
         const float s = rstd;
-        Raw8<T> dy_now[STEPS], more[STEPS];
-        Source<T, KEPT> x_now[STEPS];
+        Raw8<T> dy_now[STEPS], more_now[STEPS];
+        typename Source<T, VEC, KEPT>::Now x_now[STEPS];
+        const bool edge = !VEC && dy_.edge(row), more_edge = !VEC && dtotal_.edge(row);
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
-            dy_now[k] = dy[k];
-            x_now[k] = x[k];
+            const int j = 8 * (t + k * THREADS);
+            dy_now[k] = dy[k].take(dy_, row, j, cols, edge);
+            x[k].take(a, x_, row, j, cols, x_now[k]);
+            if (AHEAD && a.dtotal.p) more_now[k] = more[k].take(dtotal_, row, j, cols, more_edge);
         }
-        if (a.dtotal.p)
-#pragma unroll
-            for (int k = 0; k < STEPS; ++k) more[k] = load8<T, VEC>(dtotal_, row, 8 * (t + k * THREADS), cols);
-        if (row + step < end) fetch(row + step);
+        if (AHEAD && row + step < end) fetch(row + step);
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
             float2 g[4], xh[4], f[4];
-            x_now[k].values(s, xh);
+            Source<T, VEC, KEPT>::values(x_now[k], s, xh);
             widen8<T>(dy_now[k], g);
             weight8(w, t + k * THREADS, UNITS, f);
 #pragma unroll
@@ -357,18 +369,22 @@ __global__ void __launch_bounds__(BT, 512 / BT) k_rms_norm_backward(RmsNormBackw
             }
         }
         if (!a.dx.p) continue;
+        if (!AHEAD && a.dtotal.p)
+#pragma unroll
+            for (int k = 0; k < STEPS; ++k) more[k].ask(dtotal_, row, 8 * (t + k * THREADS), cols, more_edge);
         const float mean = __fmul_rn(group_sum<THREADS>(dot.x + dot.y, slots[group][slot], group), over);
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
             float2 g[4], xh[4], f[4];
-            x_now[k].forget();
+            anew(x_now[k]);
             anew(dy_now[k]);
-            x_now[k].values(s, xh);
+            Source<T, VEC, KEPT>::values(x_now[k], s, xh);
             widen8<T>(dy_now[k], g);
             weight8(w, t + k * THREADS, UNITS, f);
 #pragma unroll
             for (int e = 0; e < 4; ++e) g[e] = fma2(xh[e], both(-mean), mul2(g[e], f[e]));
-            if (a.dtotal.p) widen8<T>(more[k], f);
+            if (!AHEAD && a.dtotal.p) more_now[k] = more[k].take(dtotal_, row, 8 * (t + k * THREADS), cols, more_edge);
+            if (a.dtotal.p) widen8<T>(more_now[k], f);
 #pragma unroll
             for (int e = 0; e < 4; ++e) g[e] = a.dtotal.p ? fma2(g[e], both(s), f[e]) : mul2(g[e], both(s));
             store8<T, VEC>(dx_, row, 8 * (t + k * THREADS), cols, narrow8<T>(g));
@@ -408,11 +424,13 @@ __global__ void __launch_bounds__(kLongThreads, 1) k_rms_dx_long(RmsNormBackward
     const bool vec = KEPT && on(a.kept.p, a.kept.stride, 8);
     const Place<T> dy_ = place<T>(a.dy, a.rows), x_ = place<T>(a.x, a.rows), dtotal_ = place<T>(a.dtotal, a.rows), dx_ = place<T>(a.dx, a.rows);
     const float s = a.rstd[row];
-    Source<T, KEPT> x;
     float2 g[4], xh[4], w[4], dot = both(0.0f);
     auto take = [&](int j) {
-        x.template load<VEC>(a, x_, row, j, cols, vec);
-        x.values(s, xh);
+        Source<T, VEC, KEPT> x;
+        typename Source<T, VEC, KEPT>::Now now;
+        x.ask(a, x_, row, j, cols, vec);
+        x.take(a, x_, row, j, cols, now);
+        x.values(now, s, xh);
         widen8<T>(load8<T, VEC>(dy_, row, j, cols), g);
         weight8_long(a.weight, j, cols, w);
 #pragma unroll
@@ -450,11 +468,13 @@ __global__ void __launch_bounds__(128) k_rms_dw_long(RmsNormBackward a)
     if (j >= cols) return;
 #pragma unroll 4
     for (int64_t row = first; row < end; ++row) {
-        Source<T, KEPT> x;
+        Source<T, VEC, KEPT> x;
+        typename Source<T, VEC, KEPT>::Now now;
         float2 g[4], xh[4];
-        x.template load<VEC>(a, x_, row, j, cols, vec);
+        x.ask(a, x_, row, j, cols, vec);
         widen8<T>(load8<T, VEC>(dy_, row, j, cols), g);
-        x.values(__ldg(a.rstd + row), xh);
+        x.take(a, x_, row, j, cols, now);
+        x.values(now, __ldg(a.rstd + row), xh);
 #pragma unroll
         for (int e = 0; e < 4; ++e) sums[e] = fma2(g[e], xh[e], sums[e]);
     }
@@ -476,8 +496,14 @@ __global__ void __launch_bounds__(1024) k_rms_sums(RmsNormBackward a, int parts)
     float v = 0.0f;
     grid_dep_wait();
     if (j < a.cols)
-#pragma unroll 4
-        for (int i = warp; i < parts; i += 32) v += __ldcg(a.parts + ((int64_t)blockIdx.y * parts + i) * a.cols + j);
+        for (int i = warp; i < parts; i += 32 * 10) {   // 296 parts at once
+            float f[10];
+#pragma unroll
+            for (int k = 0; k < 10; ++k)
+                f[k] = i + 32 * k < parts ? __ldcg(a.parts + ((int64_t)blockIdx.y * parts + i + 32 * k) * a.cols + j) : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 10; ++k) v += f[k];
+        }
     sh[warp][lane] = v;
     __syncthreads();
     v = warp_sum(sh[lane][warp]);                       // column `warp` of the block
@@ -544,14 +570,14 @@ __global__ void __launch_bounds__(kFlat) k_checkpoint8(Matrix x, Kept8 kept, int
     const int64_t all = items<WIDE>(n), step = (int64_t)gridDim.x * (kFlat / 32);
     for (int64_t i = (int64_t)blockIdx.x * (kFlat / 32) + threadIdx.x / 32; i < all; i += step) {
         UnitAt at[kAhead];
-        Raw8<T> u[kAhead];
+        Unit<T, VEC> u[kAhead];
         units_at<WIDE>(i, n, cols, at);
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) u[k] = load8<T, VEC>(x_, at[k].row, at[k].j, cols);
+        for (int k = 0; k < kAhead; ++k) u[k].ask(x_, at[k].row, at[k].j, cols, !VEC && x_.edge(at[k].row));
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             float2 f[4];
-            widen8<T>(u[k], f);
+            widen8<T>(u[k].take(x_, at[k].row, at[k].j, cols, !VEC && x_.edge(at[k].row)), f);
             keep8<VEC>(kept, at[k].row, at[k].j, cols, f, vec);
         }
     }
@@ -639,7 +665,7 @@ void launch_rms_norm(const RmsNorm &a, int type, cudaStream_t st)
 static int backward_threads(int64_t cols)
 {
     const int64_t units = (cols + 7) / 8;
-    return units <= 64 ? 32 : units <= 128 ? 64 : units <= 256 ? 128 : units <= 512 ? 256 : units <= 1024 ? 512 : 0;
+    return units <= 64 ? 32 : units <= 128 ? 64 : units <= 256 ? 128 : units <= 512 ? 256 : units <= 2048 ? 512 : 0;
 }
 static int backward_block(int threads) { return threads > 256 ? threads : 256; }
 static int64_t backward_parts(int64_t rows, int64_t cols, int64_t groups)
@@ -696,6 +722,7 @@ static void backward(const RmsNormBackward &a, cudaStream_t st)
     else if (units <= 256) queued = backward_as<T, 128, 2, 256>(a, parts, vec, st);
     else if (units <= 512) queued = backward_as<T, 256, 2, 256>(a, parts, vec, st);
     else if (units <= 1024) queued = backward_as<T, 512, 2, 512>(a, parts, vec, st);
+    else if (units <= 2048) queued = sizeof(T) == 2 ? backward_as<T, 512, 4, 512>(a, parts, vec, st) : backward_as<T, 1024, 2, 1024>(a, parts, vec, st);
     else if (a.kept.p) queued = vec ? backward_long<T, true, true>(a, parts, st) : backward_long<T, false, true>(a, parts, st);
     else queued = vec ? backward_long<T, true, false>(a, parts, st) : backward_long<T, false, false>(a, parts, st);
     if (queued && a.dweight && parts > 1)
