@@ -152,12 +152,12 @@ __device__ __forceinline__ void store_element(T *row, int j, const Raw8<T> &u, i
     if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t *>(row)[j + e] = u.w[e];
     else reinterpret_cast<unsigned short *>(row)[j + e] = (unsigned short)(u.w[e / 2] >> (e % 2 * 16));
 }
-// All lanes of the warp call it (with j >= cols: nothing is stored); lane l + 1 has the unit behind lane l's, or
-// one of another row.
-template <typename T, bool VEC>
+// All lanes of the warp call it (with j >= cols: nothing is stored).  SEQ: they have one row's units one behind the other;
+// else lane l + 1 has the unit behind lane l's or one of another row.
+template <typename T, bool VEC, bool SEQ>
 __device__ __forceinline__ void store8(const Place<T> &m, int64_t r, int j, int cols, const Raw8<T> &u)
 {
-    constexpr int W = 2 * sizeof(T);
+    constexpr int W = 2 * sizeof(T), EACH = 16 / sizeof(T);     // elements of a vector
     T *const row = m.row(r);
     if (VEC) {
         if (j < cols) {
@@ -167,42 +167,63 @@ __device__ __forceinline__ void store8(const Place<T> &m, int64_t r, int j, int 
         }
         return;
     }
-    // the aligned vectors whose last bytes are the unit's first ones begin with the last `over` elements of the
-    // unit before
+    // the aligned vectors that end in the unit: the first begins with the last `over` elements of the unit before, whose
+    // lane leaves them to this one
     const uintptr_t at = (uintptr_t)(row + j);
-    const unsigned over = (unsigned)(at & 15) / (unsigned)sizeof(T), lane = threadIdx.x & 31;
+    const int over = (int)((unsigned)(at & 15) / (unsigned)sizeof(T)), lane = threadIdx.x & 31;
     uint32_t w[W + 4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = __shfl_up_sync(0xffffffffu, u.w[W - 4 + i], 1);
 #pragma unroll
     for (int i = 0; i < W; ++i) w[4 + i] = u.w[i];
-    const int j_before = __shfl_up_sync(0xffffffffu, j, 1);
-    const bool whole = j + 8 - (int)over <= cols && (over == 0 || (lane > 0 && j > 0 && j_before == j - 8));
-    if (whole) {
-        uint4 *p = reinterpret_cast<uint4 *>(at & ~(uintptr_t)15);
-        const unsigned from = 16 - (unsigned)(at & 15), bits = (from & 3) * 8;      // byte of w where the vectors begin
-        if (over == 0) {
+    bool before = lane > 0 && j > 0;
+    if (!SEQ) before &= __shfl_up_sync(0xffffffffu, j, 1) == j - 8;
+    const bool v0 = (before || over == 0) && j + EACH - over <= cols, v1 = j + 8 - over <= cols;  // vectors that it can store
+    uint4 *const p = reinterpret_cast<uint4 *>(at & ~(uintptr_t)15);
+    const unsigned from = 16 - (unsigned)(at & 15), bits = (from & 3) * 8;      // byte of w where the vectors begin
+    auto put = [&](const uint32_t (&v)[W]) {
+        if (v0) __stcs(p, make_uint4(v[0], v[1], v[2], v[3]));
+        if constexpr (W == 8)
+            if (v1) __stcs(p + 1, make_uint4(v[4], v[5], v[6], v[7]));
+    };
+    if (over == 0) {
+        put(u.w);
+    } else {
+        by_words(from >> 2, [&](auto words) {
+            constexpr int k = decltype(words)::n;
+            uint32_t v[W];
 #pragma unroll
-            for (int i = 0; i < W / 4; ++i) __stcs(p + i, make_uint4(u.w[4 * i], u.w[4 * i + 1], u.w[4 * i + 2], u.w[4 * i + 3]));
-        } else {
-            by_words(from >> 2, [&](auto words) {
-                constexpr int k = decltype(words)::n;
-                uint32_t v[W];
-#pragma unroll
-                for (int i = 0; i < W; ++i) v[i] = sizeof(T) == 4 ? w[i + k] : __funnelshift_r(w[i + k], w[(i + k + 1) % (W + 4)], bits);
-#pragma unroll
-                for (int i = 0; i < W / 4; ++i) __stcs(p + i, make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
-            });
-        }
+            for (int i = 0; i < W; ++i) v[i] = sizeof(T) == 4 ? w[i + k] : __funnelshift_r(w[i + k], w[(i + k + 1) % (W + 4)], bits);
+            put(v);
+        });
     }
-    // what no vector takes: the first elements where there is none, the last where the next lane has none
-    const bool next = __shfl_down_sync(0xffffffffu, whole && over > 0, 1) && lane < 31;
-    const int j_next = __shfl_down_sync(0xffffffffu, j, 1);
-    const int first = whole ? 8 - (int)over : 0, last = over > 0 && next && j_next == j + 8 ? 8 - (int)over : 8;
-    if (first < last)
+    // elements in no vector: lane 0's first ones and lane 31's last ones, and what is around the ends of a row
+    const unsigned stored = __ballot_sync(0xffffffffu, v0);
+    bool next = lane < 31 && (stored >> (lane + 1 & 31) & 1);
+    if (!SEQ) next &= __shfl_down_sync(0xffffffffu, j, 1) == j + 8;
+    const unsigned open = __ballot_sync(0xffffffffu, j < cols && (!v0 || (W == 8 && !v1) || (over > 0 && !next)));
+    if (open == 0) return;
+    const int j31 = j + 8 * (31 - lane);
+    if (SEQ && open == 0x80000001u && j31 + 8 <= cols) {
+        // as many as a vector has: a lane for each
+        const bool head = lane < EACH - over;
+        uint32_t v[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e >= first && e < last && j + e < cols) store_element(row, j, u, e);
+        for (int i = 0; i < 4; ++i) v[i] = __shfl_sync(0xffffffffu, W == 8 && lane == 31 ? u.w[W - 4 + i] : u.w[i], head ? 0 : 31);
+        const int i = sizeof(T) == 4 ? lane : lane >> 1;
+        const uint32_t one = i & 2 ? (i & 1 ? v[3] : v[2]) : (i & 1 ? v[1] : v[0]);
+        if (lane < EACH) {
+            T *const to = row + (head ? j31 - 248 : j31 + 8 - EACH) + lane;
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t *>(to) = one;
+            else *reinterpret_cast<unsigned short *>(to) = (unsigned short)(lane & 1 ? one >> 16 : one);
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const bool done = e < EACH - over ? v0 : e < 8 - over ? v1 : next;
+        if (!done && j + e < cols) store_element(row, j, u, e);
+    }
 }
 
 // Eight bytes; `vec`: rows start on 8 bytes (known with VEC).

@@ -117,7 +117,7 @@ __device__ __forceinline__ void finish8(const RmsNorm &a, const Place<T> &y, con
         float2 f[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = mul2(p[e], both(st.s));
-        store8<T, VEC>(y, row, j, (int)a.cols, narrow8<T>(f));
+        store8<T, VEC, true>(y, row, j, (int)a.cols, narrow8<T>(f));
     }
     if (a.q.p) store_bytes<VEC>(a.q.p + row * a.q.stride, j, (int)a.cols, q_vec, st.finite ? to_rows8(p, st.step) : make_uint2(0, 0));
 }
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(BT, forward_blocks(sizeof(T), STEPS, BT, VEC))
             const int j = 8 * (t + k * THREADS);
             Raw8<T> h = x[k].take(x_, row, j, cols, edge);
             if (a.residual.p) h = sum8<T>(h, r[k].take(residual_, row, j, cols, r_edge));
-            if (a.total.p) store8<T, VEC>(total_, row, j, cols, h);
+            if (a.total.p) store8<T, VEC, true>(total_, row, j, cols, h);
             widen8<T>(h, p[k]);
         }
         if (AHEAD && row + step < a.rows) fetch(row + step);
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(kLongThreads, 1) k_rms_norm_long(RmsNorm a)
         const int j = base + 8 * (int)threadIdx.x;
         Raw8<T> h = load8<T, VEC>(x_, row, j, cols);
         if (a.residual.p) h = sum8<T>(h, load8<T, VEC>(residual_, row, j, cols));
-        if (a.total.p) store8<T, VEC>(total_, row, j, cols, h);
+        if (a.total.p) store8<T, VEC, true>(total_, row, j, cols, h);
         widen8<T>(h, f);
         if (a.kept.p) keep8<VEC>(a.kept, row, j, cols, f, kept_vec);
         weight8_long(a.weight, j, cols, w);
@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(BT, BT > 512 ? 1 : 512 / BT) k_rms_norm_backwa
             if (a.dtotal.p) widen8<T>(more_now[k], f);
 #pragma unroll
             for (int e = 0; e < 4; ++e) g[e] = a.dtotal.p ? fma2(g[e], both(s), f[e]) : mul2(g[e], both(s));
-            store8<T, VEC>(dx_, row, 8 * (t + k * THREADS), cols, narrow8<T>(g));
+            store8<T, VEC, true>(dx_, row, 8 * (t + k * THREADS), cols, narrow8<T>(g));
         }
     }
     if (!a.dweight) return;
@@ -451,7 +451,7 @@ __global__ void __launch_bounds__(kLongThreads, 1) k_rms_dx_long(RmsNormBackward
             const float2 d = fma2(xh[e], both(-mean), g[e]);
             g[e] = a.dtotal.p ? fma2(d, both(s), w[e]) : mul2(d, both(s));
         }
-        store8<T, VEC>(dx_, row, j, cols, narrow8<T>(g));
+        store8<T, VEC, true>(dx_, row, j, cols, narrow8<T>(g));
     }
 }
 constexpr int kLongRows = 128;         // rows of a block of the next kernel, at least
@@ -609,7 +609,7 @@ __global__ void __launch_bounds__(kFlat) k_restore8(Rows8 q, Kept8 kept, Matrix 
             unpack_bytes(b[k], f);
 #pragma unroll
             for (int e = 0; e < 4; ++e) f[e] = mul2(f[e], both(s[k]));
-            store8<T, VEC>(to_, at[k].row, at[k].j, cols, narrow8<T>(f));
+            store8<T, VEC, WIDE>(to_, at[k].row, at[k].j, cols, narrow8<T>(f));
         }
     }
 }
