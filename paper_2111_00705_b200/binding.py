@@ -779,8 +779,8 @@ def _rms_norm(x, at, device, shape, dtype, weight, residual, eps, y, q, scale, t
     py, sy = (None, 0) if y is None else _matrix(y, "y", device, shape, dtype)
     pq, sq = (None, 0) if q is None else _bytes(q, "q", device, shape)
     pk, sk, pe, se = (None, 0, None, 0) if checkpoint is None else _checkpoint(checkpoint, device, shape)
-    w, _, wt = _parameters(weight, None, cols, device)
-    code = lib().cdadam_rms_norm(px, sx, pr, sr, w, rows, cols, eps, _TYPES[dtype], wt, pt, st, py, sy, pq, sq,
+    w = _vector(weight, "weight", device, (cols,), _TYPES)
+    code = lib().cdadam_rms_norm(px, sx, pr, sr, w, rows, cols, eps, _TYPES[dtype], F32 if w is None else _TYPES[weight.dtype], pt, st, py, sy, pq, sq,
                                  _vector(scale, "scale", device, (rows,), _FLOAT), pk, sk, pe, se,
                                  _vector(rstd, "rstd", device, (rows,), _FLOAT), _raw_stream(device))
     if code:
@@ -844,7 +844,8 @@ def rms_norm_backward(dy, x, weight, rstd, dtotal=None, groups=1, accumulate=Fal
         px, sx, pe, se = _checkpoint(x, device, shape)
     else:
         (px, sx), pe, se = _matrix(x, "x", device, shape, dtype), None, 0
-    w, _, wt = _parameters(weight, None, cols, device)
+    w = _vector(weight, "weight", device, (cols,), _TYPES)
+    wt = F32 if w is None else _TYPES[weight.dtype]
     pdt, sdt = (None, 0) if dtotal is None else _matrix(dtotal, "dtotal", device, shape, dtype)
     sums = (groups, cols)
     if out is None:

@@ -9,6 +9,7 @@
 
 #include <type_traits>
 
+#include "cluster.cuh"
 #include "elements.cuh"
 
 namespace cdadam {
@@ -61,29 +62,6 @@ __device__ __forceinline__ void read_sums32(uint32_t addr, int (&v)[32])
                    "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
                  : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void cluster_barrier()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t at_rank(const void *p, int rank)
-{
-    uint32_t at;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(p)), "r"(rank));
-    return at;
-}
-__device__ __forceinline__ int load_at(uint32_t at)
-{
-    int v;
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-    return v;
-}
-__device__ __forceinline__ int4 load4_at(uint32_t at)
-{
-    int4 v;
-    asm volatile("ld.shared::cluster.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-    return v;
-}
-
 // What has become of a thread's waits: 0: all in time; 1: one ran out and the thread waited a second time, with the
 // default limit: the block's results are NaN; 2: that was in vain too: nothing more is waited for or started.
 __device__ __noinline__ int wait_again(uint64_t *bar, uint32_t parity, int limit, int late)

@@ -3,6 +3,7 @@
 // All are bound by memory: every matrix is read once and written once.  A group of 32 to 1024 threads
 // takes a row at a time, every thread up to four units of eight columns, and asks for its next row's units
 // before it works on the present ones.
+#include "cluster.cuh"
 #include "eight_bits.cuh"
 
 namespace cdadam {
@@ -256,8 +257,9 @@ __global__ void __launch_bounds__(kLongThreads, 1) k_rms_norm_long(RmsNorm a)
 
 // ---------------------------------------------------------------------------------------------
 // Backward.  A block works on rows of one group of rows, and every thread keeps the sums over rows of
-// its own columns in registers, so everything is read once.  `parts` blocks share a group; with more than one each
-// leaves its sums in the workspace and k_rms_sums adds them in order: the same bits every time.
+// its own columns in registers, so everything is read once.  `parts` blocks share a group.  Up to eight are a cluster
+// and add their sums up through shared memory (a second launch costs the host 5 us); of more, each leaves its sums in the
+// workspace and k_rms_sums adds them.  All in order: the same bits every time.
 // ---------------------------------------------------------------------------------------------
 // A unit of the activations times s, as they were or as a checkpoint.
 template <typename T, bool VEC, bool KEPT> struct Source {
@@ -305,6 +307,8 @@ template <typename T, bool VEC> struct Source<T, VEC, true> {
     }
 };
 
+constexpr int kClusterParts = 8;
+
 template <typename T, int THREADS, int STEPS, int BT, bool VEC, bool KEPT>
 __global__ void __launch_bounds__(BT, BT > 512 ? 1 : 512 / BT) k_rms_norm_backward(RmsNormBackward a)
 {
@@ -332,7 +336,7 @@ __global__ void __launch_bounds__(BT, BT > 512 ? 1 : 512 / BT) k_rms_norm_backwa
             if (AHEAD && a.dtotal.p) more[k].ask(dtotal_, n, j, cols, more_edge);
         }
     };
-    if (a.dweight && gridDim.x > 1) grid_dep_launch();  // of k_rms_sums, which waits for all of this
+    if (a.dweight && gridDim.x > kClusterParts) grid_dep_launch();  // of k_rms_sums, which waits for all of this
     if (AHEAD && row < end) fetch(row);
     fill_weight(w, a.weight, cols, UNITS);
     __syncthreads();
@@ -407,9 +411,25 @@ __global__ void __launch_bounds__(BT, BT > 512 ? 1 : 512 / BT) k_rms_norm_backwa
                 }
     }
     __syncthreads();
+    const int parts = (int)gridDim.x;
+    if (parts > 1 && parts <= kClusterParts) {
+        cluster_barrier();
+        for (int j = (int)blockIdx.x * BT + threadIdx.x; j < cols; j += parts * BT) {
+            const float *const at = &w[(j & 4 ? 4 * UNITS : 0) + (j >> 3) * 4 + (j & 3)];
+            float f[kClusterParts], v = 0.0f;
+#pragma unroll
+            for (int r = 0; r < kClusterParts; ++r) f[r] = r < parts ? __int_as_float(load_at(at_rank(at, r))) : 0.0f;
+#pragma unroll
+            for (int r = 0; r < kClusterParts; ++r) v += f[r];
+            store_grad(a.dweight, blockIdx.y * a.dweight_stride + j, a.grad_type, a.accumulate, v);
+        }
+        __syncwarp();
+        cluster_barrier();                              // no block leaves while others read from it
+        return;
+    }
     for (int j = threadIdx.x; j < cols; j += BT) {
         const float v = w[(j & 4 ? 4 * UNITS : 0) + (j >> 3) * 4 + (j & 3)];
-        if (gridDim.x > 1) a.parts[((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * cols + j] = v;
+        if (parts > 1) a.parts[((int64_t)blockIdx.y * parts + blockIdx.x) * cols + j] = v;
         else store_grad(a.dweight, blockIdx.y * a.dweight_stride + j, a.grad_type, a.accumulate, v);
     }
 }
@@ -679,15 +699,19 @@ static int64_t backward_parts(int64_t rows, int64_t cols, int64_t groups)
     } else {
         const int block = backward_block(threads), at_once = block == 256 ? 2 : 1;
         most = kSms * at_once / groups;
-        parts = (per + block / threads - 1) / (block / threads);
+        parts = (per + 3 * (block / threads) - 1) / (3 * (block / threads));  // three rows a group, or more
     }
     parts = parts < most ? parts : most;
-    return parts < 1 ? 1 : parts > 65535 ? 65535 : parts;
+    parts = parts < 1 ? 1 : parts > 65535 ? 65535 : parts;
+    // a cluster, up to three times its rows: 64 x 4096 from two launches 9.5 us, but 16 of the host's
+    if (threads && parts <= 3 * kClusterParts) parts = parts > 4 ? 8 : parts > 2 ? 4 : parts;
+    return parts;
 }
+static bool in_a_cluster(int64_t cols, int64_t parts) { return backward_threads(cols) && parts <= kClusterParts; }
 int64_t rms_norm_workspace(int64_t rows, int64_t cols, int64_t groups)
 {
     const int64_t parts = backward_parts(rows, cols, groups);
-    return parts > 1 ? parts * groups * cols * 4 : 0;
+    return parts > 1 && !in_a_cluster(cols, parts) ? parts * groups * cols * 4 : 0;
 }
 
 template <typename T, int THREADS, int STEPS, int BT>
@@ -697,7 +721,18 @@ static bool backward_as(const RmsNormBackward &a, int parts, bool vec, cudaStrea
                            : (vec ? k_rms_norm_backward<T, THREADS, STEPS, BT, true, false> : k_rms_norm_backward<T, THREADS, STEPS, BT, false, false>);
     const size_t smem = (size_t)THREADS * STEPS * 32;
     allow_shared(kernel, smem);
-    return queue(kernel, dim3((unsigned)parts, (unsigned)a.groups), BT, smem, st, a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)parts, (unsigned)a.groups);
+    cfg.blockDim = dim3(BT);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)parts;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = parts > 1 && parts <= kClusterParts;
+    return cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess;
 }
 template <typename T, bool VEC, bool KEPT>
 static bool backward_long(const RmsNormBackward &a, int parts, cudaStream_t st)
@@ -725,7 +760,7 @@ static void backward(const RmsNormBackward &a, cudaStream_t st)
     else if (units <= 2048) queued = sizeof(T) == 2 ? backward_as<T, 512, 4, 512>(a, parts, vec, st) : backward_as<T, 1024, 2, 1024>(a, parts, vec, st);
     else if (a.kept.p) queued = vec ? backward_long<T, true, true>(a, parts, st) : backward_long<T, false, true>(a, parts, st);
     else queued = vec ? backward_long<T, true, false>(a, parts, st) : backward_long<T, false, false>(a, parts, st);
-    if (queued && a.dweight && parts > 1)
+    if (queued && a.dweight && parts > 1 && !in_a_cluster(a.cols, parts))
         launch_after(k_rms_sums, dim3((unsigned)((a.cols + 31) / 32), (unsigned)a.groups), dim3(1024), 0, st, a, parts);
 }
 void launch_rms_norm_backward(const RmsNormBackward &a, int type, cudaStream_t st)
