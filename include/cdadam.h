@@ -658,12 +658,12 @@ int cdadam_distill(const void *logits, int64_t logits_stride,
 /*
  * A worker's operators in 8 bits.
  *
- * Four more parts of the same computation: the root-mean-square norm with the residual's addition
- * in front of it, activations kept in 8 bits until the backward pass needs them (a checkpoint),
- * products of 8-bit matrices, and what turns rows into 8 bits and back.  Matrices, types, streams and
- * errors are as above; no wait inside these kernels has a limit that the caller sets
- * unless said otherwise.  8-bit matrices are signed, row-major, elements of a row adjacent, rows any
- * stride >= the row's length apart; rows that start on 16 bytes are fastest (a product takes no others).
+ * Four more parts of the same computation: the root-mean-square norm with the residual's addition in front
+ * of it, activations kept in 8 bits until the backward pass needs them (a checkpoint), products of 8-bit
+ * matrices, and what turns rows into 8 bits and back.  Matrices, types, streams and errors are as above; no
+ * output may overlap an input or another output but as said.  8-bit matrices are signed, row-major, elements of
+ * a row adjacent, rows any stride >= the row's length apart (>= 0 for inputs but a product's); rows that start on
+ * 16 bytes are fastest (a product takes no others).
  *
  * Two formats of 8 bits:
  *   rows     q_j and one binary32 step per row: the value is q_j * scale.  With m = max |p_j| over the row,
@@ -693,7 +693,8 @@ int cdadam_distill(const void *logits, int64_t logits_stride,
  *   total may be x or residual, y may be x or residual (same address and stride), not the same one;
  *   eps >= 0, 1 <= cols <= CDADAM_MAX_NORM_COLS, rows < 2^31.  At least one output must be given.
  * A row with a NaN is NaN; with an infinity, or finite with a sum of squares beyond binary32, s = 0 (y is
- * NaN at the infinities and 0 elsewhere).
+ * NaN at the infinities and 0 elsewhere); with eps = 0 a row whose squares are all below binary32's range (a row of zeros)
+ * has s infinite (y is NaN where h is 0, infinite elsewhere).
  */
 int cdadam_rms_norm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride,
                     const void *weight, int64_t rows, int64_t cols, float eps, int type, int weight_type,
@@ -743,12 +744,13 @@ int cdadam_checkpoint8_restore(const int8_t *kept, int64_t kept_stride,
  *     y_tc = (sum_k x_tk w_ck) x_scale_t w_scale_c + bias_c,
  * the sum exact (32-bit integers), the rest in binary32 in this order, rounded once to `type`.
  *   x        tokens x inner bytes, w channels x inner bytes; rows start on 16 bytes (address and strides are
- *            multiples of 16); 1 <= inner <= CDADAM_MAX_INNER, tokens, channels < 2^31
+ *            multiples of 16); 1 <= inner <= CDADAM_MAX_INNER, tokens, channels <= 2^30 and
+ *            (tokens / 128 + 1) (channels / 128 + 1) < 2^27
  *   x_scale, w_scale   tokens and channels floats;   bias   channels elements of `bias_type`, or NULL: 0
  *   y        tokens x channels of `type`
  * There is no gradient: it is for passes that need none (a teacher's, an evaluation, decoding).
- * More than 8 tokens: the kernel waits for its own copies with the limit of cdadam_set_operator_wait_limit;
- * what depends on one that did not arrive is NaN.
+ * More than two tokens: the kernels wait for their own copies with the limit of cdadam_set_operator_wait_limit; what depends
+ * on one that did not arrive is NaN.
  */
 int cdadam_matmul8(const int8_t *x, int64_t x_stride, const float *x_scale,
                    const int8_t *w, int64_t w_stride, const float *w_scale, const void *bias,

@@ -1,10 +1,9 @@
-// Product of 8-bit matrices with a scale for every token and channel.
+// Product of 8-bit matrices with a scale for every token and channel: sums of 8-bit products in 32-bit integers, exact in
+// any order, so that tiles, splits and schedules are free; then three roundings in binary32 and one to the type.
 //
-// A block takes 128 channels and BN tokens: the weights are the first operand of the tensor core's product (its 128
-// rows), the tokens the second, so that few tokens cost a narrow product and every weight is read once per BN
-// tokens.  One thread fills a ring of stages (128 bytes of every row) by tiled bulk copies, one issues the products,
-// the sums stay in tensor memory as 32-bit integers, exact in any order.  Where there are few tiles, a
-// cluster of blocks shares the row's length and adds its sums up through shared memory.
+// Three kernels.  One and two tokens are bound by reading the weights once and need nothing but loads and integer dot products
+// (k_matmul8_few).  Up to a few hundred tokens, the weights still are most of what is read: blocks of 128 channels
+// and up to 128 tokens (k_matmul8).  Beyond, the tensor cores are the bound: pairs of SMs on tiles of 256 x 256 (k_matmul8_pair).
 #include <cuda.h>
 
 #include <type_traits>
@@ -94,6 +93,16 @@ __device__ __forceinline__ void store4(T *to, const float (&f)[4], bool vec, int
         if (e < n) to[e] = narrow<T>(f[e]);
 }
 
+// ---------------------------------------------------------------------------------------------
+// A block takes 128 channels and BN tokens: the weights are the first operand of the tensor core's product (its 128
+// rows), the tokens the second, so that few tokens cost a narrow product and every weight is read once per BN
+// tokens.  One thread fills a ring of stages (128 bytes of every row) by tiled bulk copies, one issues the products,
+// the sums stay in tensor memory.  Where there are few tiles, a cluster of blocks shares the rows' length; its blocks fetch
+// each other's sums from shared memory, 16 bytes at a time.
+// Measured: 64 tokens x 131072 channels x 4096 97 us (5.7 TB/s), 64 x 30522 x 4096 26 to 28 us (4.8 TB/s; what is beside
+// the weights' 19 us is the launch, the first copy's way and the last tile's outputs), 64 x 4096 x 4096 10 us,
+// 509 x 2003 x 1021 8.4 us.
+// ---------------------------------------------------------------------------------------------
 template <typename T, int BN>
 __global__ void __launch_bounds__(128) k_matmul8(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, Matmul8 a,
                                                  int ring, int splits, int token_tiles)
@@ -230,6 +239,9 @@ __global__ void __launch_bounds__(128) k_matmul8(const __grid_constant__ CUtenso
 // 128 channels, 128 bytes of a row at a time through shared memory.  The first block of a pair issues the products
 // for both; its `full` barriers count the copies of both, `empty` and `ready` are told to both, `drained` counts the
 // warps of both.
+// Measured: 4096 tokens x 131072 channels x 4096 bf16 1.42 to 1.49 ms (2.96 POP/s; back to back under the power limit 1.6 to 1.7),
+// 4096 x 30528 x 768 90 us, 4096 x 30522 x 768 (rows that are no whole vectors) 115; a library's 8-bit product
+// with 32-bit integer output and no scales 1.38 ms for the first.
 // ---------------------------------------------------------------------------------------------
 constexpr int kPairTile = 256, kPairRing = 5, kPairStage = 2 * kRowsP * kBytesK, kPairThreads = 320, kLeaveBytes = 4096;
 
@@ -344,7 +356,7 @@ __device__ __forceinline__ void leave_rows(const char *place, T *p, int64_t stri
     }
 }
 
-// TILED: the outputs' rows start on 16 bytes and leave by tiled bulk copies.
+// TILED: the outputs' rows are whole 16-byte vectors and leave by tiled bulk copies.
 template <typename T, bool TILED>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap, Matmul8 a,
@@ -465,6 +477,8 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                     __syncwarp();
                 }
             }
+            // relaxed: all that the next products may overwrite has been read into registers (a release would wait for
+            // the outputs' stores as well: 4096 x 30528 x 768 117 us instead of 90)
             fence_before();
             __syncwarp();
             if (lane == 0)
@@ -480,9 +494,11 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
 }
 
 // ---------------------------------------------------------------------------------------------
-// A few tokens: the weights are streamed once, 16 bytes a lane, and multiplied four at a time; what the kernel above
-// needs before its first byte arrives and after its last (tensor memory, barriers) costs more than its products are worth here.
-// A warp takes FEW_C channels and every `slices`-th stretch of 512 bytes of them; the slices' sums meet in shared memory.
+// One and two tokens: the weights are streamed once, 16 bytes a lane, and multiplied four at a time; what the kernels above
+// need before their first byte arrives and after their last (tensor memory, barriers) costs more than their products are worth
+// here.  From three tokens on the dot products would be the bound (16 a clock and SM: 4 x 30522 x 4096 31 us, by k_matmul8 24).
+// A warp takes kFewChannels channels and every `slices`-th stretch of 512 bytes of them; the slices' sums meet in shared memory.
+// Measured, one token: 131072 x 4096 82 us (6.5 TB/s), 30522 x 768 8 us, 4096 x 4096 4.7 us, 1000 x 768 2.5 us.
 // ---------------------------------------------------------------------------------------------
 constexpr int kFewWarps = 8, kFewChannels = 4;
 
@@ -647,7 +663,9 @@ static bool product_by_pairs(const Matmul8 &a, cudaStream_t st)
     if (!describe(&wmap, a.w, a.channels, a.inner, kRowsP) || !describe(&xmap, a.x, a.tokens, a.inner, kRowsP)) return false;
     const int64_t token_tiles = (a.tokens + kPairTile - 1) / kPairTile, tiles = tiles_of(a, kPairTile, kPairTile);
     CUtensorMap ymap = {};
-    const bool tiled = ((uintptr_t)a.y & 15) == 0 && (a.tokens == 1 || a.y_stride * (int64_t)sizeof(T) % 16 == 0);
+    // (a tiled copy writes whole 16-byte vectors: of a row that ends inside one it would overwrite what lies behind)
+    const bool tiled = ((uintptr_t)a.y & 15) == 0 && a.channels * (int64_t)sizeof(T) % 16 == 0 &&
+                       (a.tokens == 1 || a.y_stride * (int64_t)sizeof(T) % 16 == 0);
     if (tiled && !describe_outputs(&ymap, a, type_of<T>(), sizeof(T))) return false;
     const size_t smem = kPairRing * kPairStage + 8 * kLeaveBytes + 1024;
     auto kernel = tiled ? k_matmul8_pair<T, true> : k_matmul8_pair<T, false>;
@@ -669,7 +687,7 @@ static bool product_of_few(const Matmul8 &a, cudaStream_t st)
 template <typename T>
 static bool product(const Matmul8 &a, cudaStream_t st)
 {
-    // one and two tokens: 30522 x 4096 20 and 25 us this way, 24 and 24 by tiles of 16 tokens
+    // 30522 x 768: one token 8.0 us this way and 8.9 by tiles of 16 tokens, two 9.6 and 9.1; 1000 x 768 2.5 and 8.5; 131072 x 4096 82 and 89
     if (a.tokens == 1) return product_of_few<T, 1>(a, st);
     if (a.tokens == 2) return product_of_few<T, 2>(a, st);
     // pairs, as soon as there are tiles for 32 of the 74 (512 x 4096 x 1024 9.4 us, by smaller tiles 9.5; 1024 x 4096 x 4096

@@ -412,8 +412,9 @@ int cdadam_matmul8(const int8_t *x, int64_t x_stride, const float *x_scale, cons
 {
     static const char fn[] = "cdadam_matmul8";
     if (!known(type) || !known(bias_type)) return refuse(fn, "unknown element type %d, %d", type, bias_type);
-    if (tokens < 0 || tokens > kMaxRows || channels < 0 || channels > kMaxRows)
-        return refuse(fn, "tokens = %lld or channels = %lld is outside [0, 2^31)", (long long)tokens, (long long)channels);
+    constexpr int64_t most = (int64_t)1 << 30;
+    if (tokens < 0 || tokens > most || channels < 0 || channels > most)
+        return refuse(fn, "tokens = %lld or channels = %lld is outside [0, 2^30]", (long long)tokens, (long long)channels);
     if (inner < 1 || inner > CDADAM_MAX_INNER)
         return refuse(fn, "inner = %lld is outside [1, %d]", (long long)inner, (int)CDADAM_MAX_INNER);
     if ((tokens / 128 + 1) * (channels / 128 + 1) >= (int64_t)1 << 27)

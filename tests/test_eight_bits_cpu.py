@@ -64,7 +64,7 @@ REFUSED = [
     (checkpoint, dict(ks=39)), (checkpoint, dict(es=1)), (checkpoint, dict(xs=-1)),
     (restore, dict(t=4)), (restore, dict(x=None)), (restore, dict(k=None)), (restore, dict(e=None)), (restore, dict(xs=39)),
     (restore, dict(ks=-1)), (restore, dict(es=-1)),
-    (product, dict(t=3)), (product, dict(bt=3)), (product, dict(tokens=-1)), (product, dict(channels=1 << 31)), (product, dict(inner=0)),
+    (product, dict(t=3)), (product, dict(bt=3)), (product, dict(tokens=-1)), (product, dict(channels=(1 << 30) + 1)), (product, dict(tokens=1 << 31)), (product, dict(inner=0)),
     (product, dict(inner=cd.MAX_INNER + 1, xs=1 << 18, ws=1 << 18)), (product, dict(x=None)), (product, dict(w=None)),
     (product, dict(y=None)), (product, dict(xsc=None)), (product, dict(wsc=None)), (product, dict(x=P + 8)), (product, dict(w=P + 1)),
     (product, dict(xs=40)), (product, dict(ws=56)), (product, dict(xs=32)), (product, dict(ws=32)), (product, dict(ys=5)),

@@ -448,6 +448,22 @@ def test_product_of_many_tiles():
         check_product(tokens, channels, inner, g, torch.bfloat16)
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("shift,pad", [(0, 0), (0, 1), (1, 0), (1, 1), (2, 2), (0, 2), (3, 2), (8, 8), (5, 11)])
+def test_product_of_many_tokens_to_rows_that_start_anywhere(shift, pad, dtype):
+    g = gen(shift * 16 + pad, 91)
+    for tokens, channels in ((300, 4100), (513, 3000 + pad), (1000, 2049)):
+        x, w = eight(tokens, 150, g), eight(channels, 150, g)
+        xs, ws = torch.rand(tokens, generator=g, device="cuda") + 0.01, torch.randn(channels, generator=g, device="cuda") * 0.01
+        b = torch.randn(channels, generator=g, device="cuda")
+        buf = torch.full((shift + tokens * (channels + pad) + 64,), math.nan, device="cuda").to(TYPES[dtype])
+        out = torch.as_strided(buf, (tokens, channels), (channels + pad, 1), shift)
+        for bias in (None, b):
+            cd.matmul8(x, xs, w, ws, bias, out=out)
+            assert torch.equal(out, product64(x, xs, w, ws, bias, TYPES[dtype]))
+        assert buf.isfinite().sum() == tokens * channels      # and nothing around the rows
+
+
 def test_product_of_the_largest_sums():
     for tokens in (1, 8, 9, 300):
         x = torch.full((tokens, 131072), -128, dtype=torch.int8, device="cuda")[:, :131071]
@@ -585,6 +601,34 @@ def test_product_waits_that_run_out(tokens):
         cd.set_operator_wait_limit(-1)
     assert got.isnan().all()
     assert torch.equal(cd.matmul8(x, xs, w, ws), want)
+
+
+def test_calls_of_several_threads():
+    """Sizes that differ in the shared memory their kernels take, from host threads with streams of their own."""
+    import threading
+    g = gen(21, 127)
+    x, w = eight(400, 500, g), eight(9000, 500, g)
+    xs, ws = torch.ones(400, device="cuda"), torch.ones(9000, device="cuda")
+    a = [torch.randn(64, cols, generator=g, device="cuda") for cols in (100, 9000, 16000)]
+    jobs = [lambda t=t: cd.matmul8(x[:t], xs[:t], w, ws) for t in (1, 20, 100, 400)]
+    jobs += [lambda m=m: cd.rms_norm_backward(m, m, None, xs[:64])[1] for m in a]
+    want = [j().clone() for j in jobs]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def run(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(40):
+                got = jobs[i]()
+                torch.cuda.current_stream().synchronize()
+                if not torch.equal(got, want[i]):
+                    wrong.append(i)
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(len(jobs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
 
 
 def test_rows_far_apart():
