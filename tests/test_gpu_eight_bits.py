@@ -389,6 +389,36 @@ def test_backward_against_differences():
     assert abs(slope - want) <= size * 2.0 ** -10, (slope, want, size)
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("cols", [1, 5, 40, 260, 1000, 1021, 4099, 9001, 17003])
+def test_nothing_around_the_rows_is_written(cols, dtype):
+    """Every output of the activations' type into rows that start anywhere, on buffers of NaN; inputs likewise, so that a
+    value from outside a row would show."""
+    g = gen(cols, 131)
+    dt = TYPES[dtype]
+    for shift, pad in ((0, 0), (1, 0), (0, 1), (3, 2), (8, 8), (5, 7), (4, 4)):
+        for rows in (1, 2, 37):
+            x, r, dy = (matrix(rows, cols, dt, g, 1.0, pad, shift) for _ in range(3))
+            w = torch.randn(cols, generator=g, device="cuda")
+
+            def out():
+                buf = torch.full((shift + rows * (cols + pad) + 40,), math.nan, device="cuda").to(dt)
+                return buf, torch.as_strided(buf, (rows, cols), (cols + pad, 1), shift)
+            want = cd.rms_norm(x.contiguous(), w, r.contiguous())
+            kept = cd.checkpoint8(x)
+            q, scale = cd.quantize_rows(x)
+            dwant = cd.rms_norm_backward(dy.contiguous(), x.contiguous(), w, want[2], r.contiguous())
+            for buf, view, expected, call in (
+                    (*out(), want[0], lambda v: cd.rms_norm(x, w, r, out=(v, None, None))),
+                    (*out(), want[1], lambda v: cd.rms_norm(x, w, r, out=(None, v, None))),
+                    (*out(), dwant[0], lambda v: cd.rms_norm_backward(dy, x, w, want[2], r, out=(v, None))),
+                    (*out(), cd.checkpoint8_restore(*kept, dtype=dt), lambda v: cd.checkpoint8_restore(*kept, out=v)),
+                    (*out(), cd.dequantize_rows(q, scale, dt), lambda v: cd.dequantize_rows(q, scale, out=v))):
+                call(view)
+                close(view, expected.double(), expected.double().abs() * 2.0 ** -6 + 1e-3)
+                assert (~buf.isnan()).sum() == rows * cols     # a gradient may be beyond binary16: infinite, not NaN
+
+
 # ---------------------------------------------------------------------------------------------
 # products
 # ---------------------------------------------------------------------------------------------
