@@ -543,19 +543,20 @@ __global__ void __launch_bounds__(1024) k_rms_sums(RmsNormBackward a, int parts)
 // checkpoint's block is four neighbouring threads.  Measured: 32768 x 4096 bf16 into a checkpoint and back 128 us (6.35 TB/s, the
 // copy rate less 3 %), 1023 x 5001 f32 21 us (two launches, rows that start anywhere).
 // ---------------------------------------------------------------------------------------------
-constexpr int kFlat = 256, kAhead = 4;     // a thread asks for that many units before it works on the first
+constexpr int kFlat = 256;
+// Units that a thread asks for before it works on the first: what fits into 64 registers.
+template <typename T, bool VEC> constexpr int kAhead = sizeof(T) == 4 && !VEC ? 2 : 4;
 constexpr int kWideUnits = 64;             // of a row: from there on a warp's 128 units in one row are half used at least
 
-// Where a thread's four units are.  WIDE: a warp takes 128 units of one row, lane l the units l, l + 32, l + 64, l + 96
-// of them; rows of fewer units, one behind the other, 32 units a warp at a time.  Number i of a sequence of n to a row
+// Where a thread's A units are.  WIDE: a warp takes 32 A units of one row, lane l the units l, l + 32, .. of them; rows of fewer units, one behind the other, 32 units a warp at a time.  Number i of a sequence of n to a row
 // is in row i / n, for i < 2^31 by a product (`magic` = ceil(2^(31 + s) / n), 2^s >= n: the excess adds less than 1 / n).
 struct Units {
     unsigned n, magic, shift;
     int64_t all;
 };
-static Units units_of(int64_t rows, int64_t units)
+static Units units_of(int64_t rows, int64_t units, int each)
 {
-    const int64_t n = units >= kWideUnits ? (units + 127) / 128 : units;
+    const int64_t n = units >= kWideUnits ? (units + 32 * each - 1) / (32 * each) : units;
     unsigned s = 0;
     while (((int64_t)1 << s) < n) ++s;
     return {(unsigned)n, (unsigned)((((uint64_t)1 << (31 + s)) + n - 1) / n), s, rows * n};
@@ -568,42 +569,43 @@ __device__ __forceinline__ int64_t row_of(int64_t i, const Units &u)
 {
     return u.all >> 31 ? i / u.n : u.shift ? __umulhi((unsigned)i, u.magic) >> (u.shift - 1) : i;
 }
-template <bool WIDE>
-__device__ __forceinline__ void units_at(int64_t warp, const Units &u, int cols, UnitAt (&at)[kAhead])
+template <bool WIDE, int A>
+__device__ __forceinline__ void units_at(int64_t warp, const Units &u, int cols, UnitAt (&at)[A])
 {
     const int lane = threadIdx.x & 31;
     if (WIDE) {
         const int64_t row = row_of(warp, u);
-        const int j = ((int)(warp - row * u.n) * 128 + lane) * 8;
+        const int j = ((int)(warp - row * u.n) * 32 * A + lane) * 8;
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) at[k] = {row, min(j + k * 256, cols)};
+        for (int k = 0; k < A; ++k) at[k] = {row, min(j + k * 256, cols)};
     } else {
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int64_t i = (warp * kAhead + k) * 32 + lane, row = row_of(i, u);
+        for (int k = 0; k < A; ++k) {
+            const int64_t i = (warp * A + k) * 32 + lane, row = row_of(i, u);
             at[k] = {row, (int)(i - row * u.n) * 8};
             if (i >= u.all) at[k] = {0, cols};
         }
     }
 }
-// Warps of a launch and what each of them takes in turn: WIDE one item, else 128.
-template <bool WIDE>
-__device__ __forceinline__ int64_t items(const Units &u) { return WIDE ? u.all : (u.all + 32 * kAhead - 1) / (32 * kAhead); }
+// What the warps of a launch take in turn.
+template <bool WIDE, int A>
+__device__ __forceinline__ int64_t items(const Units &u) { return WIDE ? u.all : (u.all + 32 * A - 1) / (32 * A); }
 
 template <typename T, bool VEC, bool WIDE>
 __global__ void __launch_bounds__(kFlat) k_checkpoint8(Matrix x, Kept8 kept, int64_t rows, int cols, Units n)
 {
+    constexpr int A = kAhead<T, VEC>;
     const bool vec = on(kept.p, kept.stride, 8);
     const Place<T> x_ = place<T>(x, rows);
-    const int64_t all = items<WIDE>(n), step = (int64_t)gridDim.x * (kFlat / 32);
+    const int64_t all = items<WIDE, A>(n), step = (int64_t)gridDim.x * (kFlat / 32);
     for (int64_t i = (int64_t)blockIdx.x * (kFlat / 32) + threadIdx.x / 32; i < all; i += step) {
-        UnitAt at[kAhead];
-        Unit<T, VEC> u[kAhead];
-        units_at<WIDE>(i, n, cols, at);
+        UnitAt at[A];
+        Unit<T, VEC> u[A];
+        units_at<WIDE, A>(i, n, cols, at);
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) u[k].ask(x_, at[k].row, at[k].j, cols, !VEC && x_.edge(at[k].row));
+        for (int k = 0; k < A; ++k) u[k].ask(x_, at[k].row, at[k].j, cols, !VEC && x_.edge(at[k].row));
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
+        for (int k = 0; k < A; ++k) {
             float2 f[4];
             widen8<T>(u[k].take(x_, at[k].row, at[k].j, cols, !VEC && x_.edge(at[k].row)), f);
             keep8<VEC>(kept, at[k].row, at[k].j, cols, f, vec);
@@ -614,25 +616,26 @@ __global__ void __launch_bounds__(kFlat) k_checkpoint8(Matrix x, Kept8 kept, int
 template <typename T, bool VEC, bool WIDE>
 __global__ void __launch_bounds__(kFlat) k_restore8(Rows8 q, Kept8 kept, Matrix to, int64_t rows, int cols, Units n)
 {
+    constexpr int A = kAhead<T, VEC>;
     const int8_t *p = kept.p ? kept.p : q.p;
     const int64_t stride = kept.p ? kept.stride : q.stride;
     const bool vec = on(p, stride, 8);
     const Place<T> to_ = place<T>(to, rows);
-    const int64_t all = items<WIDE>(n), step = (int64_t)gridDim.x * (kFlat / 32);
+    const int64_t all = items<WIDE, A>(n), step = (int64_t)gridDim.x * (kFlat / 32);
     for (int64_t i = (int64_t)blockIdx.x * (kFlat / 32) + threadIdx.x / 32; i < all; i += step) {
-        UnitAt at[kAhead];
-        uint2 b[kAhead];
-        float s[kAhead];
-        units_at<WIDE>(i, n, cols, at);
+        UnitAt at[A];
+        uint2 b[A];
+        float s[A];
+        units_at<WIDE, A>(i, n, cols, at);
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
+        for (int k = 0; k < A; ++k) {
             b[k] = load_bytes<VEC>(p + at[k].row * stride, at[k].j, cols, vec);
             s[k] = 0.0f;
             if (at[k].j < cols)
                 s[k] = kept.p ? kept_step(__ldg(kept.exponents + at[k].row * kept.exponents_stride + (at[k].j >> 5))) : __ldg(q.scale + at[k].row);
         }
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
+        for (int k = 0; k < A; ++k) {
             float2 f[4];
             unpack_bytes(b[k], f);
 #pragma unroll
@@ -778,9 +781,9 @@ void launch_rms_norm_backward(const RmsNormBackward &a, int type, cudaStream_t s
     else backward<f16>(a, st);
 }
 
-static dim3 flat_grid(const Units &n, bool wide)
+static dim3 flat_grid(const Units &n, bool wide, int ahead)
 {
-    const int64_t each = kFlat / 32 * (wide ? 1 : 32 * kAhead), need = (n.all + each - 1) / each, most = kSms * 32;
+    const int64_t each = kFlat / 32 * (wide ? 1 : 32 * ahead), need = (n.all + each - 1) / each, most = kSms * 32;
     return dim3((unsigned)(need < most ? need : most));
 }
 template <typename T>
@@ -790,8 +793,9 @@ static void checkpoint(const Matrix &x, const Kept8 &kept, int64_t rows, int64_t
     const bool vec = starts_on_16(x, rows, sizeof(T)) && starts_on(8, kept.p, rows, kept.stride) && cols % 8 == 0, wide = units >= kWideUnits;
     auto kernel = wide ? (vec ? k_checkpoint8<T, true, true> : k_checkpoint8<T, false, true>)
                        : (vec ? k_checkpoint8<T, true, false> : k_checkpoint8<T, false, false>);
-    const Units n = units_of(rows, units);
-    queue(kernel, flat_grid(n, wide), kFlat, 0, st, x, kept, rows, (int)cols, n);
+    const int each = vec ? kAhead<T, true> : kAhead<T, false>;
+    const Units n = units_of(rows, units, each);
+    queue(kernel, flat_grid(n, wide, each), kFlat, 0, st, x, kept, rows, (int)cols, n);
 }
 void launch_checkpoint8(const Matrix &x, const Kept8 &kept, int64_t rows, int64_t cols, int type, cudaStream_t st)
 {
@@ -807,8 +811,9 @@ static void restore(const Rows8 &q, const Kept8 &kept, const Matrix &to, int64_t
     const bool wide = units >= kWideUnits;
     auto kernel = wide ? (vec ? k_restore8<T, true, true> : k_restore8<T, false, true>)
                        : (vec ? k_restore8<T, true, false> : k_restore8<T, false, false>);
-    const Units n = units_of(rows, units);
-    queue(kernel, flat_grid(n, wide), kFlat, 0, st, q, kept, to, rows, (int)cols, n);
+    const int each = vec ? kAhead<T, true> : kAhead<T, false>;
+    const Units n = units_of(rows, units, each);
+    queue(kernel, flat_grid(n, wide, each), kFlat, 0, st, q, kept, to, rows, (int)cols, n);
 }
 void launch_restore8(const Rows8 &q, const Kept8 &kept, const Matrix &to, int64_t rows, int64_t cols, int type, cudaStream_t st)
 {
