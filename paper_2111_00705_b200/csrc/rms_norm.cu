@@ -541,11 +541,12 @@ __global__ void __launch_bounds__(1024) k_rms_sums(RmsNormBackward a, int parts)
 // ---------------------------------------------------------------------------------------------
 // The formats by themselves, unit by unit.  Rows are padded to whole blocks of four units, so that a
 // checkpoint's block is four neighbouring threads.  Measured: 32768 x 4096 bf16 into a checkpoint and back 128 us (6.35 TB/s, the
-// copy rate less 3 %), 1023 x 5001 f32 21 us (two launches, rows that start anywhere).
+// copy rate less 3 %), 1023 x 5001 f32 19 us (two launches, rows that start anywhere).
 // ---------------------------------------------------------------------------------------------
 constexpr int kFlat = 256;
-// Units that a thread asks for before it works on the first: what fits into 64 registers.
-template <typename T, bool VEC> constexpr int kAhead = sizeof(T) == 4 && !VEC ? 2 : 4;
+// Units that a thread asks for before it works on the first: what fits into 64 registers (8000 x 5001 f32 109 us by four, 98 by
+// two; 100000 x 100 bf16 41 and 36).
+template <typename T, bool VEC> constexpr int kAhead = VEC ? 4 : 2;
 constexpr int kWideUnits = 64;             // of a row: from there on a warp's 128 units in one row are half used at least
 
 // Where a thread's A units are.  WIDE: a warp takes 32 A units of one row, lane l the units l, l + 32, .. of them; rows of fewer units, one behind the other, 32 units a warp at a time.  Number i of a sequence of n to a row
