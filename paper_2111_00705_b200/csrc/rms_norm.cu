@@ -128,7 +128,7 @@ __device__ __forceinline__ void finish8(const RmsNorm &a, const Place<T> &y, con
 // it does not wait for the sum: the sum of squares and the largest |p| go through the same exchange, and the rounding of s
 // cannot move a value across a half.
 // Measured: 16384 x 4096 bf16 with residual and sum in 8 bits 72 us of the 113 with reading back (6.1 TB/s); 30000 x 768 bf16
-// 32 us (5.7 TB/s), 8000 x 4096 f32 104 (5.0); 3001 x 1021 f32 16 us, 20000 x 1022 bf16 54 (3.0 TB/s; rows that start anywhere
+// 32 us (5.7 TB/s), 8000 x 4096 f32 105 (5.0); 3001 x 1021 f32 14 us, 20000 x 1022 bf16 54 (3.0 TB/s; rows that start anywhere
 // cost 460 instructions a unit and warp instead of 190).
 // ---------------------------------------------------------------------------------------------
 // Blocks an SM holds.  A thread's units of 16 bits fit into 80 registers, 768 threads (16384 x 4096 bf16 in 8 bits 112 us; with
@@ -664,6 +664,18 @@ static void forward_as(const RmsNorm &a, bool vec, cudaStream_t st)
     allow_shared(kernel, smem);
     queue(kernel, dim3((unsigned)(need < most ? need : most)), BT, smem, st, a);
 }
+// Rows of more than 384 units.
+template <typename T>
+static void forward_wide(const RmsNorm &a, bool vec, cudaStream_t st)
+{
+    const int64_t units = (a.cols + 7) / 8;
+    if (units <= 512) forward_as<T, 256, 2, 256>(a, vec, st);
+    else if (units <= 768) forward_as<T, 256, 3, 256>(a, vec, st);
+    else if (units <= 1024) forward_as<T, 512, 2, 512>(a, vec, st);
+    else if (units <= 1536) forward_as<T, 512, 3, 512>(a, vec, st);
+    else if (units <= 2048) forward_as<T, 1024, 2, 1024>(a, vec, st);
+    else queue(vec ? k_rms_norm_long<T, true> : k_rms_norm_long<T, false>, dim3((unsigned)a.rows), kLongThreads, 0, st, a);
+}
 template <typename T>
 static void forward(const RmsNorm &a, cudaStream_t st)
 {
@@ -672,19 +684,27 @@ static void forward(const RmsNorm &a, cudaStream_t st)
                      starts_on_16(a.y, a.rows, size) && starts_on(8, a.q.p, a.rows, a.q.stride) &&
                      starts_on(8, a.kept.p, a.rows, a.kept.stride) && a.cols % 8 == 0;
     const int64_t units = (a.cols + 7) / 8;
+    // Binary32: one unit a thread up to 384 units (20000 x 1021 61 us, two units 72; 8000 x 3000 66 and 80; 30000 x 500 45 and 49; of
+    // more two, 8000 x 4096 in 8 bits 115 us, by one 126).  16 bits: two or three (16384 x 4096 in 8 bits 113 us, by one 162;
+    // 16000 x 2048 45 and 50; 30000 x 768 32 and 36).  By the width alone: the order of the sums, so their bits, go by the sizes.
     if (units <= 32) forward_as<T, 32, 1, 256>(a, vec, st);
-    else if (units <= 64) forward_as<T, 32, 2, 256>(a, vec, st);
-    else if (units <= 96) forward_as<T, 32, 3, 256>(a, vec, st);
-    else if (units <= 128) forward_as<T, 64, 2, 256>(a, vec, st);
-    else if (units <= 192) forward_as<T, 64, 3, 256>(a, vec, st);
-    else if (units <= 256) forward_as<T, 128, 2, 256>(a, vec, st);
-    else if (units <= 384) forward_as<T, 128, 3, 256>(a, vec, st);
-    else if (units <= 512) forward_as<T, 256, 2, 256>(a, vec, st);
-    else if (units <= 768) forward_as<T, 256, 3, 256>(a, vec, st);
-    else if (units <= 1024) forward_as<T, 512, 2, 512>(a, vec, st);
-    else if (units <= 1536) forward_as<T, 512, 3, 512>(a, vec, st);
-    else if (units <= 2048) forward_as<T, 1024, 2, 1024>(a, vec, st);
-    else queue(vec ? k_rms_norm_long<T, true> : k_rms_norm_long<T, false>, dim3((unsigned)a.rows), kLongThreads, 0, st, a);
+    else if constexpr (sizeof(T) == 4) {
+        if (units <= 64) forward_as<T, 64, 1, 256>(a, vec, st);
+        else if (units <= 96) forward_as<T, 96, 1, 192>(a, vec, st);
+        else if (units <= 128) forward_as<T, 128, 1, 256>(a, vec, st);
+        else if (units <= 192) forward_as<T, 192, 1, 192>(a, vec, st);
+        else if (units <= 256) forward_as<T, 256, 1, 256>(a, vec, st);
+        else if (units <= 384) forward_as<T, 384, 1, 384>(a, vec, st);
+        else forward_wide<T>(a, vec, st);
+    } else {
+        if (units <= 64) forward_as<T, 32, 2, 256>(a, vec, st);
+        else if (units <= 96) forward_as<T, 32, 3, 256>(a, vec, st);
+        else if (units <= 128) forward_as<T, 64, 2, 256>(a, vec, st);
+        else if (units <= 192) forward_as<T, 64, 3, 256>(a, vec, st);
+        else if (units <= 256) forward_as<T, 128, 2, 256>(a, vec, st);
+        else if (units <= 384) forward_as<T, 128, 3, 256>(a, vec, st);
+        else forward_wide<T>(a, vec, st);
+    }
 }
 void launch_rms_norm(const RmsNorm &a, int type, cudaStream_t st)
 {
@@ -763,13 +783,18 @@ static void backward(const RmsNormBackward &a, cudaStream_t st)
     const int64_t units = (a.cols + 7) / 8;
     const int parts = (int)backward_parts(a.rows, a.cols, a.groups);
     bool queued;
+    // two units a thread (32768 x 4096 bf16 161 us, by one and 512 threads 208; 20000 x 2048 from a checkpoint 56 and 61; 16384 x 1536
+    // 43 and 44; 16384 x 768 for 8 workers 24.7 and, with 96 threads, 23.9)
     if (units <= 32) queued = backward_as<T, 32, 1, 256>(a, parts, vec, st);
     else if (units <= 64) queued = backward_as<T, 32, 2, 256>(a, parts, vec, st);
     else if (units <= 128) queued = backward_as<T, 64, 2, 256>(a, parts, vec, st);
     else if (units <= 256) queued = backward_as<T, 128, 2, 256>(a, parts, vec, st);
     else if (units <= 512) queued = backward_as<T, 256, 2, 256>(a, parts, vec, st);
     else if (units <= 1024) queued = backward_as<T, 512, 2, 512>(a, parts, vec, st);
-    else if (units <= 2048) queued = sizeof(T) == 2 ? backward_as<T, 512, 4, 512>(a, parts, vec, st) : backward_as<T, 1024, 2, 1024>(a, parts, vec, st);
+    else if (units <= 2048) {
+        if constexpr (sizeof(T) == 2) queued = backward_as<T, 512, 4, 512>(a, parts, vec, st);
+        else queued = backward_as<T, 1024, 2, 1024>(a, parts, vec, st);
+    }
     else if (a.kept.p) queued = vec ? backward_long<T, true, true>(a, parts, st) : backward_long<T, false, true>(a, parts, st);
     else queued = vec ? backward_long<T, true, false>(a, parts, st) : backward_long<T, false, false>(a, parts, st);
     if (queued && a.dweight && parts > 1 && !in_a_cluster(a.cols, parts))

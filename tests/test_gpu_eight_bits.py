@@ -361,6 +361,51 @@ def test_backward_in_place_and_selected_outputs(dtype, cols):
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+@pytest.mark.parametrize("cols", [40, 1000, 1021, 9000, 17000])
+def test_backward_from_a_checkpoint_that_starts_anywhere(cols):
+    g = gen(cols, 137)
+    x, dy = matrix(50, cols, torch.bfloat16, g), matrix(50, cols, torch.bfloat16, g)
+    given, rstd, dx, dw = check_backward(dy, x, None, 5, None, True)
+    for pad, shift in ((3, 1), (8, 4), (16, 0)):
+        kept, exps = byte_matrix(50, cols, pad, shift)[0], byte_matrix(50, -(-cols // 32), pad, shift, torch.uint8)[0]
+        kept.copy_(given[0])
+        exps.copy_(given[1])
+        got = cd.rms_norm_backward(dy, (kept, exps), None, rstd, groups=5)
+        assert torch.equal(got[0], dx) and torch.equal(got[1], dw)
+
+
+def test_backward_of_the_most_groups():
+    g = gen(22, 139)
+    x, dy = matrix(2 * 65535, 8, torch.float32, g), matrix(2 * 65535, 8, torch.float32, g)
+    check_backward(dy, x, None, 65535)
+    check_backward(dy, x, None, 65535, checkpoint=True)
+    x, dy = matrix(65535, 16400, torch.bfloat16, g), matrix(65535, 16400, torch.bfloat16, g)
+    rstd = torch.ones(65535, device="cuda")
+    dw = torch.empty(65535, 16400, dtype=torch.bfloat16, device="cuda")
+    cd.rms_norm_backward(dy, x, None, rstd, groups=65535, out=(None, dw))
+    for a in range(0, 65535, 8192):
+        want = dy[a:a + 8192].float() * x[a:a + 8192].float()
+        assert torch.equal(dw[a:a + 8192], want.bfloat16())
+
+
+def test_single_outputs_of_the_norm():
+    """Through the C entry point, each output alone and all of them."""
+    g = gen(23, 149)
+    x, r = (torch.randn(33, 520, generator=g, device="cuda").bfloat16() for _ in range(2))
+    w = torch.randn(520, generator=g, device="cuda")
+    kept = cd.checkpoint8_like(x)
+    y, total, rstd = cd.rms_norm(x, w, r, checkpoint=kept)
+    q, scale, _, _ = cd.rms_norm8(x, w, r)
+    want = {"total": total, "y": y, "q": q, "scale": scale, "kept": kept[0], "exponents": kept[1], "rstd": rstd}
+    for names in (("total",), ("y",), ("q", "scale"), ("kept", "exponents"), ("rstd",), tuple(want)):
+        got = {n: torch.zeros_like(want[n], memory_format=torch.contiguous_format) for n in names}
+        p = {n: got[n].data_ptr() if n in got else None for n in want}
+        code = cd.lib().cdadam_rms_norm(x.data_ptr(), 520, r.data_ptr(), 520, w.data_ptr(), 33, 520, 1e-6, cd.BF16, cd.F32, p["total"], 520,
+                                        p["y"], 520, p["q"], 520, p["scale"], p["kept"], 520, p["exponents"], 17, p["rstd"],
+                                        torch.cuda.current_stream().cuda_stream)
+        assert code == cd.OK and all(torch.equal(got[n], want[n]) for n in names), names
+
+
 def test_backward_without_rows():
     e = torch.empty(0, 70, device="cuda")
     dw = torch.full((2, 70), 5.0, device="cuda")
@@ -562,7 +607,7 @@ def test_teacher_and_student_together():
     close(dw, each.sum(1), each.abs().sum(1) * SUM + 1e-30, "dweight")
 
 
-@pytest.mark.parametrize("tokens", [1, 30, 300])
+@pytest.mark.parametrize("tokens", [1, 2, 30, 300, 2100])
 def test_captured_and_replayed(tokens):
     """One graph of the whole chain, replayed on other inputs in the same buffers."""
     g = gen(17, tokens)
