@@ -68,6 +68,12 @@ __device__ __noinline__ int wait_again(uint64_t *bar, uint32_t parity, int limit
     if (late == 2 || (limit > 0 && mbar_wait_bounded(bar, parity, limit))) return late;
     return mbar_wait_bounded(bar, parity) ? 1 : 2;
 }
+// After a wait in vain, whichever thread's it was: the copies that may still be under way (of the last stages of a ring, of
+// `started` in all) land before the block leaves its shared memory.
+__device__ __noinline__ void land(uint64_t *full, int started, int ring)
+{
+    for (int k = max(0, started - ring); k < started; ++k) mbar_wait_bounded(&full[k % ring], k / ring & 1);
+}
 __device__ __forceinline__ int wait_for(uint64_t *bar, uint32_t parity, int limit, int late)
 {
     if (limit != 0 && mbar_try_wait(bar, parity)) return late;
@@ -149,16 +155,13 @@ __global__ void __launch_bounds__(128) k_matmul8(const __grid_constant__ CUtenso
     __syncthreads();
     fence_after();
     const uint32_t sums = tmem;
-    int late = 0;
+    int late = 0, started = 0;
     if (threadIdx.x == 0) {
         int s = 0, phase = 0;
-        for (int i = ring; i < n; ++i) {
+        for (started = min(n, ring); started < n; ++started) {
             late = wait_for(&empty[s], phase, a.wait_limit, late);
-            if (late == 2) {                            // what is under way lands before the block leaves
-                for (int k = i - ring; k < i; ++k) mbar_wait_bounded(&full[k % ring], k / ring & 1);
-                break;
-            }
-            fill(i, s);
+            if (late == 2) break;
+            fill(started, s);
             if (++s == ring) { s = 0; phase ^= 1; }
         }
         lates[0] = late;
@@ -184,7 +187,11 @@ __global__ void __launch_bounds__(128) k_matmul8(const __grid_constant__ CUtenso
     fence_after();
     // The sums take the stages' place, a row of 128 channels for every token.  Every block of a cluster adds up a share of
     // the tokens from all of them; a warp takes a token at a time, a lane four channels.
-    if (threadIdx.x == 0 && (lates[0] | lates[1])) any_late = 1;
+    if (threadIdx.x == 0 && (lates[0] | lates[1])) {
+        any_late = 1;
+        if (max(lates[0], lates[1]) == 2) land(full, started, ring);
+    }
+    __syncwarp();
     int *const left = reinterpret_cast<int *>(stages);
     const int n_tokens = (int)min((int64_t)BN, a.tokens - token0);
 #pragma unroll 1
@@ -366,6 +373,7 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     char *const stages = raw + (-smem_addr(raw) & 1023);
     __shared__ uint64_t full[kPairRing], empty[kPairRing], ready[2], drained[2];
     __shared__ uint32_t tmem;
+    __shared__ int lates[2];
     __shared__ __align__(16) float w_scale[2][kPairTile], bias[2][kPairTile];
     const int warp = threadIdx.x >> 5, rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const int blocks = (int)((a.inner + kBytesK - 1) / kBytesK);
@@ -377,6 +385,7 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         for (int i = 0; i < 2; ++i) {
             mbar_init(&ready[i], 1);
             mbar_init(&drained[i], 16);
+            lates[i] = 0;
         }
         mbar_fence_init();
     }
@@ -389,13 +398,13 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     cluster_barrier();
     fence_after();
     const uint32_t sums = tmem;
-    int late = 0;
+    int late = 0, started = 0;
     if (threadIdx.x == 0) {
-        int i = 0, s = 0, phase = 1;
+        int s = 0, phase = 1;
         for (int tile = pair; tile < tiles && late < 2; tile += pairs) {
             const int channel = tile / token_tiles * kPairTile + rank * kRowsP, token = tile % token_tiles * kPairTile + rank * kRowsP;
-            for (int b = 0; b < blocks; ++b, ++i) {
-                if (i >= kPairRing) late = wait_for(&empty[s], phase, a.wait_limit, late);
+            for (int b = 0; b < blocks; ++b, ++started) {
+                if (started >= kPairRing) late = wait_for(&empty[s], phase, a.wait_limit, late);
                 if (late == 2) break;
                 if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * kPairStage);
                 char *to = stages + s * kPairStage;
@@ -405,9 +414,7 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                 if (++s == kPairRing) { s = 0; phase ^= 1; }
             }
         }
-        // what is under way lands before the pair leaves
-        if (late == 2 && rank == 0)
-            for (int k = max(0, i - kPairRing); k < i; ++k) mbar_wait_bounded(&full[k % kPairRing], k / kPairRing & 1);
+        lates[0] = late;
     } else if (threadIdx.x == 32 && rank == 0) {
         int set = 0, s = 0, phase = 0;
         for (int tile = pair; tile < tiles && late < 2; tile += pairs, ++set) {
@@ -427,6 +434,7 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
             }
             if (late < 2) commit_pair(&ready[buffer]);
         }
+        lates[1] = late;
     } else if (warp >= 2) {
         constexpr int CHUNK = 128 / (int)sizeof(T), HALF = kPairTile / 2;     // channels that leave together: 32 or 64
         const int lane = threadIdx.x & 31, quarter = warp & 3, half = (warp - 2) >> 2, thread = quarter * 32 + lane;
@@ -489,6 +497,9 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     __syncwarp();
     fence_before();
     __syncthreads();
+    // (the barriers of the first block count the copies of both)
+    if (threadIdx.x == 0 && rank == 0 && max(lates[0], lates[1]) == 2) land(full, started, kPairRing);
+    __syncwarp();
     cluster_barrier();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(sums), "r"(2 * kPairTile));
 }
