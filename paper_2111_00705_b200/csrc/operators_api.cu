@@ -104,7 +104,8 @@ int check_shape(const char *fn, int64_t rows, int64_t cols, int type)
     return CDADAM_OK;
 }
 
-cdadam::Matrix matrix(const void *p, int64_t stride) { return {const_cast<void *>(p), stride}; }
+// The stride of a single row says nothing and was not checked: kernels get 0.
+cdadam::Matrix matrix(const void *p, int64_t stride, int64_t rows) { return {const_cast<void *>(p), rows > 1 ? stride : 0}; }
 cdadam::Rows8 rows8(const int8_t *p, int64_t stride, const float *scale) { return {const_cast<int8_t *>(p), stride, const_cast<float *>(scale)}; }
 cdadam::Kept8 kept8(const int8_t *p, int64_t stride, const uint8_t *exponents, int64_t exponents_stride)
 {
@@ -293,8 +294,8 @@ int cdadam_rms_norm(const void *x, int64_t x_stride, const void *residual, int64
     if (misaligned(weight, size_of(weight_type)) || misaligned(scale, 4) || misaligned(rstd, 4))
         return refuse(fn, "weight, scale or rstd is not aligned to its elements");
     if (rows == 0) return CDADAM_OK;
-    cdadam::RmsNorm a = {matrix(x, x_stride), matrix(residual, residual_stride), {weight, weight_type}, rows, cols, eps, 1,
-                         matrix(total, total_stride), matrix(y, y_stride), rows8(q, q_stride, scale),
+    cdadam::RmsNorm a = {matrix(x, x_stride, rows), matrix(residual, residual_stride, rows), {weight, weight_type}, rows, cols, eps, 1,
+                         matrix(total, total_stride, rows), matrix(y, y_stride, rows), rows8(q, q_stride, scale),
                          kept8(kept, kept_stride, exponents, exponents_stride), rstd};
     cdadam::launch_rms_norm(a, type, (cudaStream_t)stream);
     return launched(fn);
@@ -337,9 +338,9 @@ int cdadam_rms_norm_backward(const void *dy, int64_t dy_stride, const void *x, i
     if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 16)))
         return refuse(fn, "workspace: %lld bytes, 16-byte aligned, are needed, %lld given", (long long)need,
                       (long long)(workspace ? workspace_bytes : 0));
-    cdadam::RmsNormBackward a = {matrix(dy, dy_stride), matrix(exponents ? nullptr : x, x_stride),
+    cdadam::RmsNormBackward a = {matrix(dy, dy_stride, rows), matrix(exponents ? nullptr : x, x_stride, rows),
                                  kept8(exponents ? (const int8_t *)x : nullptr, x_stride, exponents, exponents_stride), {weight, weight_type}, rstd,
-                                 matrix(dtotal, dtotal_stride), rows, cols, groups, matrix(dx, dx_stride), dweight, dweight_stride,
+                                 matrix(dtotal, dtotal_stride, rows), rows, cols, groups, matrix(dx, dx_stride, rows), dweight, dweight_stride,
                                  grad_type, accumulate != 0, (float *)workspace};
     if (rows == 0 && !dweight) return CDADAM_OK;
     cdadam::launch_rms_norm_backward(a, type, (cudaStream_t)stream);
@@ -357,7 +358,7 @@ int cdadam_quantize_rows(const void *x, int64_t x_stride, int64_t rows, int64_t 
     if (misaligned(scale, 4)) return refuse(fn, "scale is not aligned to its elements");
     if (rows == 0) return CDADAM_OK;
     cdadam::RmsNorm a = {};
-    a.x = matrix(x, x_stride);
+    a.x = matrix(x, x_stride, rows);
     a.rows = rows;
     a.cols = cols;
     a.q = rows8(q, q_stride, scale);
@@ -375,7 +376,7 @@ int cdadam_dequantize_rows(const int8_t *q, int64_t q_stride, const float *scale
     if (rows > 0 && !scale) return refuse(fn, "scale is NULL");
     if (misaligned(scale, 4)) return refuse(fn, "scale is not aligned to its elements");
     if (rows == 0) return CDADAM_OK;
-    cdadam::launch_restore8(rows8(q, q_stride, scale), kept8(nullptr, 0, nullptr, 0), matrix(y, y_stride), rows, cols, type,
+    cdadam::launch_restore8(rows8(q, q_stride, scale), kept8(nullptr, 0, nullptr, 0), matrix(y, y_stride, rows), rows, cols, type,
                             (cudaStream_t)stream);
     return launched(fn);
 }
@@ -388,7 +389,7 @@ int cdadam_checkpoint8(const void *x, int64_t x_stride, int64_t rows, int64_t co
     if (int rc = check_matrix(fn, "x", x, x_stride, rows, cols, type, false)) return rc;
     if (int rc = check_kept(fn, kept, kept_stride, exponents, exponents_stride, rows, cols, true)) return rc;
     if (rows == 0) return CDADAM_OK;
-    cdadam::launch_checkpoint8(matrix(x, x_stride), kept8(kept, kept_stride, exponents, exponents_stride), rows, cols, type,
+    cdadam::launch_checkpoint8(matrix(x, x_stride, rows), kept8(kept, kept_stride, exponents, exponents_stride), rows, cols, type,
                                (cudaStream_t)stream);
     return launched(fn);
 }
@@ -401,7 +402,7 @@ int cdadam_checkpoint8_restore(const int8_t *kept, int64_t kept_stride, const ui
     if (int rc = check_kept(fn, kept, kept_stride, exponents, exponents_stride, rows, cols, false)) return rc;
     if (int rc = check_matrix(fn, "x", x, x_stride, rows, cols, type, true)) return rc;
     if (rows == 0) return CDADAM_OK;
-    cdadam::launch_restore8(rows8(nullptr, 0, nullptr), kept8(kept, kept_stride, exponents, exponents_stride), matrix(x, x_stride), rows,
+    cdadam::launch_restore8(rows8(nullptr, 0, nullptr), kept8(kept, kept_stride, exponents, exponents_stride), matrix(x, x_stride, rows), rows,
                             cols, type, (cudaStream_t)stream);
     return launched(fn);
 }
