@@ -742,11 +742,12 @@ int cdadam_checkpoint8_restore(const int8_t *kept, int64_t kept_stride,
 /*
  * Product of 8-bit matrices in the rows format: for every token t and channel c
  *     y_tc = (sum_k x_tk w_ck) x_scale_t w_scale_c + bias_c,
- * the sum exact (32-bit integers), the rest in binary32 in this order, rounded once to `type`.
+ * the sum exact (32-bit integers), the rest in binary32 in this order, rounded once to `type`; without bias nothing is
+ * added (a zero keeps its sign).
  *   x        tokens x inner bytes, w channels x inner bytes; rows start on 16 bytes (address and strides are
  *            multiples of 16); 1 <= inner <= CDADAM_MAX_INNER, tokens, channels <= 2^30 and
  *            (tokens / 128 + 1) (channels / 128 + 1) < 2^27
- *   x_scale, w_scale   tokens and channels floats;   bias   channels elements of `bias_type`, or NULL: 0
+ *   x_scale, w_scale   tokens and channels floats;   bias   channels elements of `bias_type`, or NULL
  *   y        tokens x channels of `type`
  * There is no gradient: it is for passes that need none (a teacher's, an evaluation, decoding).
  * More than two tokens: the kernels wait for their own copies with the limit of cdadam_set_operator_wait_limit; what depends

@@ -80,7 +80,9 @@ __device__ __forceinline__ int wait_for(uint64_t *bar, uint32_t parity, int limi
     return wait_again(bar, parity, limit < 0 ? kWaitLimit : limit, late);
 }
 
-// An output, in the documented steps (packed products and sums would be contracted by the assembler).
+// An output, in the documented steps (packed products and sums would be contracted by the assembler).  Without a bias, -0: that
+// sum is the other term, whichever zero it may be.
+constexpr float kNoBias = -0.0f;
 __device__ __forceinline__ float output(int sum, float x_scale, float w_scale, float bias)
 {
     return __fadd_rn(__fmul_rn(__fmul_rn((float)sum, x_scale), w_scale), bias);
@@ -149,7 +151,7 @@ __global__ void __launch_bounds__(128) k_matmul8(const __grid_constant__ CUtenso
     {
         const int64_t c = channel0 + threadIdx.x;
         w_scale[threadIdx.x] = c < a.channels ? a.w.scale[c] : 0.0f;
-        bias[threadIdx.x] = c < a.channels && a.bias.p ? any_at(a.bias, c) : 0.0f;
+        bias[threadIdx.x] = c < a.channels && a.bias.p ? any_at(a.bias, c) : kNoBias;
     }
     fence_before();
     __syncthreads();
@@ -574,7 +576,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 4) k_matmul8_few(Matmul8 a, in
     const int token = lane % TOKENS;
     const int64_t channel = channel0 + lane / TOKENS;
     if (lane < C * TOKENS && channel < a.channels && token < a.tokens) {
-        const float bias = a.bias.p ? any_at(a.bias, channel) : 0.0f;
+        const float bias = a.bias.p ? any_at(a.bias, channel) : kNoBias;
         static_cast<T *>(a.y)[token * a.y_stride + channel] =
             narrow<T>(output(mine, a.x.scale[token], a.w.scale[channel], bias));
     }
