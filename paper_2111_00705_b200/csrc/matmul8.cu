@@ -6,6 +6,7 @@
 // and up to 128 tokens (k_matmul8).  Beyond, the tensor cores are the bound: pairs of SMs on tiles of 256 x 256 (k_matmul8_pair).
 #include <cuda.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "cluster.cuh"
@@ -588,16 +589,20 @@ __global__ void __launch_bounds__(kFewWarps * 32, 4) k_matmul8_few(Matmul8 a, in
 typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
+// Kept for the process once it is found; NULL: not this time (where the look-up failed, the reason stays for the caller's
+// cudaGetLastError()), and the next call looks again.
 static EncodeTiled encode_tiled()
 {
-    static EncodeTiled fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess)
-            p = nullptr;
-        return reinterpret_cast<EncodeTiled>(p);
-    }();
+    static std::atomic<EncodeTiled> kept{nullptr};
+    EncodeTiled fn = kept.load(std::memory_order_acquire);
+    if (fn) return fn;
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+        return nullptr;
+    fn = reinterpret_cast<EncodeTiled>(p);
+    kept.store(fn, std::memory_order_release);
     return fn;
 }
 // Boxes of 128 bytes of `rows` rows; what lies beyond a row's end or the last row reads as 0.

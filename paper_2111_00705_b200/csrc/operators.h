@@ -161,7 +161,7 @@ int64_t rms_norm_workspace(int64_t rows, int64_t cols, int64_t groups);
 void launch_checkpoint8(const Matrix &x, const Kept8 &kept, int64_t rows, int64_t cols, int type, cudaStream_t st);
 // values of the rows format (kept.p NULL) or of a checkpoint
 void launch_restore8(const Rows8 &q, const Kept8 &kept, const Matrix &to, int64_t rows, int64_t cols, int type, cudaStream_t st);
-// false: the matrices could not be described to the copy engine (the driver refused)
+// false: the matrices could not be described to the copy engine (the driver refused; the runtime may hold the reason)
 bool launch_matmul8(const Matmul8 &a, int type, cudaStream_t st);
 
 }  // namespace cdadam

@@ -436,7 +436,11 @@ int cdadam_matmul8(const int8_t *x, int64_t x_stride, const float *x_scale, cons
     cdadam::Matmul8 a = {rows8(x, x_stride, x_scale), rows8(w, w_stride, w_scale), {bias, bias_type}, tokens, channels, inner, y, y_stride,
                          wait_limit};
     if (!cdadam::launch_matmul8(a, type, (cudaStream_t)stream)) {
-        cdadam::set_last_error("cdadam_matmul8: the driver did not describe the matrices to the copy engine");
+        const cudaError_t e = cudaGetLastError();       // taken here: it is not the next call's
+        char msg[256];
+        snprintf(msg, sizeof msg, "%s: the driver did not describe the matrices to the copy engine%s%s", fn, e == cudaSuccess ? "" : ": ",
+                 e == cudaSuccess ? "" : cudaGetErrorString(e));
+        cdadam::set_last_error(msg);
         return CDADAM_ERR_CUDA;
     }
     return launched(fn);
