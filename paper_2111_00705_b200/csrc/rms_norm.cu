@@ -720,23 +720,35 @@ static int backward_threads(int64_t cols)
     return units <= 64 ? 32 : units <= 128 ? 64 : units <= 256 ? 128 : units <= 512 ? 256 : units <= 2048 ? 512 : 0;
 }
 static int backward_block(int threads) { return threads > 256 ? threads : 256; }
+static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Whether nine to 24 blocks a group are a cluster of eight instead.  Each then has more rows, but nothing goes through the
+// workspace and k_rms_sums, whose time grows with the columns and the groups (device time by eight and by all, bf16; n: groups).
+// Few rows: the second launch is 2 us of the host's (64 x 4096 of one 10.5 and 9.0 us, with the host 10.5 and 11.6).
+// More: by what the others would save (n = 16: 2048 x 4096 21 and 28 us, 4096 x 4096 35 and 34, 16384 x 4096 122 and 90, 8192 x 768
+// 16.6 and 13.5; n = 24: 6144 x 4096 36 and 45, 12288 x 4096 71 and 76, 24000 x 768 29 and 24).
+// Blocks that have an SM to themselves: the GPU holds 15 clusters of them (8192 columns, 1024 rows a group: n = 15 152 and 163 us,
+// n = 16 286 and 170).
+static bool eight_of(int64_t per, int64_t cols, int64_t groups, int64_t parts, int together, int at_once)
+{
+    if (parts > 3 * kClusterParts) return false;
+    const int64_t rows = ceil_div(per, kClusterParts * together), saved = rows - ceil_div(per, parts * together);
+    if (rows <= 9) return true;
+    if (at_once == 1 && groups > 15) return false;
+    const int64_t worth = cols * (groups > 16 ? groups : 16) / 3200;
+    return saved <= (worth > 4 ? worth : 4);
+}
 static int64_t backward_parts(int64_t rows, int64_t cols, int64_t groups)
 {
     const int64_t per = rows / groups;
     const int threads = backward_threads(cols);
-    int64_t most, parts;
-    if (threads == 0) {
-        most = (kSms * 16 * 1024 + cols * groups - 1) / (cols * groups);
-        parts = per / kLongRows;
-    } else {
-        const int block = backward_block(threads), at_once = block == 256 ? 2 : 1;
-        most = kSms * at_once / groups;
-        parts = (per + 3 * (block / threads) - 1) / (3 * (block / threads));  // three rows a group, or more
-    }
+    const int together = threads ? backward_block(threads) / threads : 0, at_once = backward_block(threads) == 256 ? 2 : 1;
+    // three rows a group of threads, or more
+    const int64_t most = threads ? kSms * at_once / groups : ceil_div(kSms * 16 * 1024, cols * groups);
+    int64_t parts = threads ? ceil_div(per, 3 * together) : per / kLongRows;
     parts = parts < most ? parts : most;
     parts = parts < 1 ? 1 : parts > 65535 ? 65535 : parts;
-    // a cluster, up to three times its rows: 64 x 4096 from two launches 9.5 us, but 16 of the host's
-    if (threads && parts <= 3 * kClusterParts) parts = parts > 4 ? 8 : parts > 2 ? 4 : parts;
+    if (threads && (parts <= kClusterParts || eight_of(per, cols, groups, parts, together, at_once)))
+        parts = parts > 4 ? 8 : parts > 2 ? 4 : parts;
     return parts;
 }
 static bool in_a_cluster(int64_t cols, int64_t parts) { return backward_threads(cols) && parts <= kClusterParts; }
