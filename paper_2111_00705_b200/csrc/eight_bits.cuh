@@ -296,7 +296,8 @@ constexpr uint32_t kInfBits = 0x7f800000u;
 // Rows format.  127 p / m in binary32 is off by less than 127 (2^-23 + 2^-47) < 2^-15.9 (a quotient and a product, each
 // rounded once): only where it is that near to a half can its nearest integer be another than the exact quotient's.
 // There 254 |p| against (2 k + 1) m decides, both exact in binary64 (9 and 24 bits); so it does for all of a row
-// whose m is so small that 127 / m is beyond binary32.
+// whose m is so small that 127 / m is beyond binary32.  Products h w are that near to a half once in 25000, but 16-bit p by
+// themselves (rows of activations, a weight of ones) often lie on one: 16384 x 4096 bf16 155 us, f16 93, f32 80.
 struct Step {
     float m, inverse;
     bool tiny;

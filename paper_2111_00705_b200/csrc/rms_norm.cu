@@ -127,9 +127,9 @@ __device__ __forceinline__ void finish8(const RmsNorm &a, const Place<T> &y, con
 // Forward: one read of x and residual, one write of each output.  What is quantised is p = h w and not p s, so that
 // it does not wait for the sum: the sum of squares and the largest |p| go through the same exchange, and the rounding of s
 // cannot move a value across a half.
-// Measured: 16384 x 4096 bf16 with residual and sum in 8 bits 72 us of the 113 with reading back (6.1 TB/s); 30000 x 768 bf16
-// 32 us (5.7 TB/s), 8000 x 4096 f32 105 (5.0); 3001 x 1021 f32 14 us, 20000 x 1022 bf16 54 (3.0 TB/s; rows that start anywhere
-// cost 460 instructions a unit and warp instead of 190).
+// Measured: 16384 x 4096 bf16 with residual and sum in 8 bits 90 us (5.2 TB/s; 113 with reading back, which alone takes 32);
+// 30000 x 768 bf16 32 us (5.7 TB/s), 8000 x 4096 f32 105 (5.0); 3001 x 1021 f32 15 us, 20000 x 1022 bf16 54 (3.0 TB/s; rows that start
+// anywhere cost 460 instructions a unit and warp instead of 190).
 // ---------------------------------------------------------------------------------------------
 // Blocks an SM holds.  A thread's units of 16 bits fit into 80 registers, 768 threads (16384 x 4096 bf16 in 8 bits 112 us; with
 // 64 registers and 1024 threads, some of them in memory, 120).
@@ -200,7 +200,8 @@ __global__ void __launch_bounds__(BT, forward_blocks(sizeof(T), STEPS, BT)) k_rm
     }
 }
 
-// Rows too long for the registers of a block: read twice, the second time from the caches.
+// Rows too long for the registers of a block: read twice, the second time from the caches.  4000 x 20000 bf16 with residual and
+// sum 272 us (2.4 TB/s), 4000 x 20001 405; 64 x 200000 f32 104.
 constexpr int kLongThreads = 1024;
 
 __device__ __forceinline__ void weight8_long(const AnyVec &v, int j, int cols, float2 (&f)[4])
@@ -261,10 +262,11 @@ __global__ void __launch_bounds__(kLongThreads, 1) k_rms_norm_long(RmsNorm a)
 
 // ---------------------------------------------------------------------------------------------
 // Backward.  A block works on rows of one group of rows, and every thread keeps the sums over rows of
-// its own columns in registers, so everything is read once.  `parts` blocks share a group.  Up to eight are a cluster
-// and add their sums up through shared memory (a second launch costs the host 5 us); of more, each leaves its sums in the
-// workspace and k_rms_sums adds them.  All in order: the same bits every time.
-// Measured: 32768 x 4096 bf16 from a checkpoint, with dtotal, 161 us (5.9 TB/s); 16384 x 768 bf16 for 8 workers 24.7 us, of which
+// its own columns, so everything is read once.  (In registers up to 8192 columns, but for up to 132 bytes, most in binary32; beyond, up to
+// 144 bytes of a thread's 16-bit whole vectors are in memory, 828 of rows that start anywhere, 240 to 740 in binary32.)  `parts`
+// blocks share a group.  Up to eight are a cluster and add their sums up through shared memory; of more (eight_of), each leaves its
+// sums in the workspace and k_rms_sums adds them.  All in order: the same bits every time.
+// Measured: 32768 x 4096 bf16 from a checkpoint, with dtotal, 161 us (5.9 TB/s); 16384 x 768 bf16 for 8 workers 25 us, of which
 // k_rms_sums 4; 16384 x 1536 bf16 43 us (4.6 TB/s), 8000 x 4096 f32 96 (5.5); 20000 x 1022 bf16 57, 3001 x 1021 f16 from a checkpoint
 // 16.6 us (two launches, three rows a group).
 // ---------------------------------------------------------------------------------------------
@@ -441,7 +443,8 @@ __global__ void __launch_bounds__(BT, BT > 512 ? 1 : 512 / BT) k_rms_norm_backwa
     }
 }
 
-// Rows too long for a block's registers: dx a row at a time, read twice; the weight's gradient column by column.
+// Rows too long for a block's registers: dx a row at a time, read twice; the weight's gradient column by column.  4000 x 20000 bf16
+// with dtotal 376 us (of which k_rms_dx_long 200, k_rms_dw_long 85 by themselves), from a checkpoint 377; 4000 x 20001 530 and 510.
 template <typename T, bool VEC, bool KEPT>
 __global__ void __launch_bounds__(kLongThreads, 1) k_rms_dx_long(RmsNormBackward a)
 {
@@ -540,8 +543,8 @@ __global__ void __launch_bounds__(1024) k_rms_sums(RmsNormBackward a, int parts)
 
 // ---------------------------------------------------------------------------------------------
 // The formats by themselves, unit by unit.  Rows are padded to whole blocks of four units, so that a
-// checkpoint's block is four neighbouring threads.  Measured: 32768 x 4096 bf16 into a checkpoint and back 128 us (6.35 TB/s, the
-// copy rate less 3 %), 1023 x 5001 f32 19 us (two launches, rows that start anywhere).
+// checkpoint's block is four neighbouring threads.  Measured: 32768 x 4096 bf16 into a checkpoint and back 128 to 130 us (6.3 TB/s, the
+// copy rate less 4 %), 1023 x 5001 f32 20 us (two launches, rows that start anywhere).
 // ---------------------------------------------------------------------------------------------
 constexpr int kFlat = 256;
 // Units that a thread asks for before it works on the first: what fits into 64 registers (8000 x 5001 f32 109 us by four, 98 by
@@ -796,7 +799,7 @@ static void backward(const RmsNormBackward &a, cudaStream_t st)
     const int parts = (int)backward_parts(a.rows, a.cols, a.groups);
     bool queued;
     // two units a thread (32768 x 4096 bf16 161 us, by one and 512 threads 208; 20000 x 2048 from a checkpoint 56 and 61; 16384 x 1536
-    // 43 and 44; 16384 x 768 for 8 workers 24.7 and, with 96 threads, 23.9)
+    // 43 and 44; 16384 x 768 for 8 workers 24.7 and, with 96 threads, 23.9, not enough for variants of its own)
     if (units <= 32) queued = backward_as<T, 32, 1, 256>(a, parts, vec, st);
     else if (units <= 64) queued = backward_as<T, 32, 2, 256>(a, parts, vec, st);
     else if (units <= 128) queued = backward_as<T, 64, 2, 256>(a, parts, vec, st);
