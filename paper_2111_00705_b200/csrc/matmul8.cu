@@ -503,8 +503,12 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     __syncwarp();
     fence_before();
     __syncthreads();
-    // (the barriers of the first block count the copies of both)
-    if (threadIdx.x == 0 && rank == 0 && max(lates[0], lates[1]) == 2) land(full, started, kPairRing);
+    // (the barriers of the first block count the copies of both; of a stage that it gave up, the second may have started its
+    // half all the same: that barrier stays open, but the limit lasts longer than any copy)
+    if (threadIdx.x == 0 && rank == 0 && max(lates[0], lates[1]) == 2) {
+        land(full, started, kPairRing);
+        if (lates[0] == 2) mbar_wait_bounded(&full[started % kPairRing], started / kPairRing & 1);
+    }
     __syncwarp();
     cluster_barrier();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(sums), "r"(2 * kPairTile));
