@@ -250,8 +250,8 @@ __global__ void __launch_bounds__(128) k_matmul8(const __grid_constant__ CUtenso
 // for both; its `full` barriers count the copies of both, `empty` and `ready` are told to both, `drained` counts the
 // warps of both.
 // Measured: 4096 tokens x 131072 channels x 4096 bf16 1.42 to 1.49 ms (2.96 POP/s; back to back under the power limit 1.6 to 1.7),
-// 4096 x 30528 x 768 90 to 104 us, 4096 x 30522 x 768 (rows that are no whole vectors) 115 to 145 (the slower ones with bytes of every
-// value, back to back); a library's 8-bit product with 32-bit integer output and no scales 1.38 ms for the first.
+// 4096 x 30528 x 768 90 to 104 us, 4096 x 30522 x 768 (rows that are no whole vectors) 115 to 145 (from GPU to
+// GPU); a library's 8-bit product with 32-bit integer output and no scales 1.38 ms for the first.
 // ---------------------------------------------------------------------------------------------
 constexpr int kPairTile = 256, kPairRing = 5, kPairStage = 2 * kRowsP * kBytesK, kPairThreads = 320, kLeaveBytes = 4096;
 
@@ -491,8 +491,8 @@ k_matmul8_pair(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
             // The products may overwrite the set: all of it is in registers.  Nothing but those reads is handed over, and their
             // order is that of tensor memory: the reads' wait, the fence, an arrival; on the other side a wait, the fence, the
             // product.  So the arrival is relaxed.  A release, even right behind the last read, also waits for the outputs
-            // stored so far (4096 x 30528 x 768 133 us instead of 102, 4096 x 30522 x 768 174 instead of 145); a relaxed one there
-            // gains nothing (104 and 144).
+            // stored so far (on one GPU: 4096 x 30528 x 768 133 us instead of 102, 4096 x 30522 x 768 174 instead of 145); a
+            // relaxed one there gains nothing (104 and 144).
             fence_before();
             __syncwarp();
             if (lane == 0)
